@@ -34,6 +34,7 @@
  * Conventions shared by every call
  *   - Tensor pointers are DEVICE pointers (except the *_host entry points),
  *     owned by the caller, contiguous, row-major, 16-byte aligned.
+ *     (topk_qk_norm_rope_fwd takes strided q, k and v.)
  *   - Shapes: q, out [B, H, Lq, d]; k, v [B, H, Lk, d];
  *             x [N, d_model]; W1, W2 [d_ff, d_model]; ffn out [N, d_model].
  *   - dtype: TOPK_F32 (fp32 in/out, fp32 FMA scores, never TF32) or
@@ -85,8 +86,10 @@ enum {
                                 lists are compacted exactly rather than overflow);
                                 outputs invalid */
   TOPK_ERR_NO_DEVICE = -6,   /* no usable sm_103 device */
-  TOPK_ERR_SCRATCH_LIMIT = -7 /* the problem needs more scratch than the fixed buffer of
+  TOPK_ERR_SCRATCH_LIMIT = -7, /* the problem needs more scratch than the fixed buffer of
                                  topk_ffn_fwd_noalloc holds */
+  TOPK_ERR_RANGE = -8        /* a position outside the rotation tables (its nearest row was used) or
+                                a row outside the cache (not written); reported by topk_check() */
 };
 
 /*
@@ -242,6 +245,69 @@ int topk_attn_bwd(const void* q, const void* k, const void* v, const void* dout,
 int topk_ffn_bwd(const void* x, const void* W1, const void* W2, const float* dout, const int32_t* idx,
                  const float* score, float* dx, float* dW1, float* dW2, int N, int d_model, int d_ff, int topk,
                  void* stream);
+
+/*
+ * Query/key norm with the position rotation: what stands between a layer's
+ * q/k/v projection and its attention, in one pass.  For every token (b, t) and
+ * head, with x the head's row of d elements:
+ *   n = x (mean(x^2) + eps)^-1/2 w      if normalize (w = 1 where NULL), else n = x
+ *   a' = a cos[p, i] - b sin[p, i], b' = b cos[p, i] + a sin[p, i]
+ *                                       for pair i < rot / 2 of q and k, where
+ *     (a, b) = (n[i], n[i + rot/2]), or (n[2i], n[2i+1]) if interleaved, and
+ *     p = positions[axis(i)][b, t];  elements from rot on are not rotated
+ *   q' is multiplied by q_scale (the temperature, footnote to Eq. 1); v is copied.
+ * Pair i belongs to the first axis x with i < sections[0] + .. + sections[x]
+ * (one axis for text; time, height and width for video).
+ *   q, k, v  : q [B, L, Hq, d], k and v [B, L, Hkv, d], `dtype`, 16-byte aligned, with
+ *              element strides {batch, token, head}, each a multiple of 4, and contiguous
+ *              rows: views of one packed projection output, for instance.  Hkv need not
+ *              equal Hq.  v may be NULL.
+ *   q_weight, k_weight: [d], `dtype`, 16-byte aligned, or NULL.
+ *   cos, sin : [table_rows, rot / 2] fp32 (NULL if rot is 0).  positions: [axes, B, L] int32, or NULL for
+ *              p = t on every axis.  A position outside the tables takes the nearest row
+ *              and is reported as TOPK_ERR_RANGE by topk_check().
+ *   d        : a multiple of 8, at most 256.  rot: a multiple of 8, at most d (0: none).
+ *   axes     : 1 to 4; their sections are >= 0 and sum to rot / 2.
+ * Sums are taken in fp32 and each result is rounded once, to nearest.
+ */
+typedef struct {
+  const void *q, *k, *v;
+  long long q_stride[3], k_stride[3], v_stride[3];
+  const void *q_weight, *k_weight;
+  const float *cos, *sin;
+  const int32_t* positions;
+  int table_rows, B, L, Hq, Hkv, d, rot, axes;
+  int sections[4];
+  int interleaved, normalize, dtype;
+  float eps, q_scale;
+} topk_qk_args;
+
+/*
+ * Forward.  q_out [B, Hq, L, d], k_out and v_out [B, Hkv, cap, d], contiguous.
+ * Without cache_start (NULL) cap must equal L; with it ([B] int32, device) token t of
+ * batch b is written to row cache_start[b] + t of k_out and v_out, whose other rows are
+ * left alone (a key/value cache with room for cap rows); a row outside [0, cap) is not
+ * written and is reported as TOPK_ERR_RANGE by topk_check().  v_out is NULL iff v is.
+ */
+int topk_qk_norm_rope_fwd(const topk_qk_args* args, void* q_out, void* k_out, void* v_out, int cap,
+                          const int32_t* cache_start, void* stream);
+
+/*
+ * Backward, from the gradients of the forward pass's outputs (cap = L).  With R the
+ * rotation: g = R^T dout (times q_scale for q), dw = sum over tokens and heads of g x r,
+ * u = g w, dx = r u - x r^3 mean(u x), where r = (mean(x^2) + eps)^-1/2.
+ *   args       : the forward pass's q, k, weights, tables and positions (args->v is not read).
+ *   dq, dk, dv : contiguous [B, Hq, L, d], [B, Hkv, L, d] (x 2); grad_dtype TOPK_F32, or
+ *                TOPK_BF16 where `dtype` is TOPK_BF16.  dv may be NULL.
+ *   dqkv       : [B, L, Hq + 2 Hkv (Hq + Hkv without dv), d] of `dtype`: q's heads, k's, v's.
+ *   dq_weight, dk_weight: [d] fp32 or NULL; written only if normalize.  Blocks add up in a
+ *                fixed order: two runs give the same bits.
+ *   Scratch: topk_qk_norm_rope_bwd_workspace_bytes(), at most 2 d floats for each of two
+ *   blocks per SM, from the library's pool.
+ */
+int topk_qk_norm_rope_bwd(const topk_qk_args* args, const void* dq, const void* dk, const void* dv, int grad_dtype,
+                          void* dqkv, float* dq_weight, float* dk_weight, void* stream);
+size_t topk_qk_norm_rope_bwd_workspace_bytes(int B, int L, int d);
 
 /* Scratch bytes of the two backward calls for these arguments; 0 if invalid or unsupported. */
 size_t topk_attn_bwd_workspace_bytes(int B, int H, int Lq, int Lk, int d, int topk, int dtype);

@@ -457,6 +457,102 @@ size_t topk_ffn_workspace_bytes(int N, int d_model, int d_ff, int topk) {
 }
 
 namespace {
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Checks the public description and fills the kernels' form of it.
+int make_qk(const topk_qk_args* a, bool with_v, QkArgs* p) {
+  if (!a || !a->q || !a->k || (with_v && !a->v)) return TOPK_ERR_INVALID_ARG;
+  if (a->rot > 0 && (!a->cos || !a->sin)) return TOPK_ERR_INVALID_ARG;
+  if (a->B <= 0 || a->L <= 0 || a->Hq <= 0 || a->Hkv <= 0 || a->d <= 0 || a->table_rows <= 0) return TOPK_ERR_INVALID_ARG;
+  if (a->rot < 0 || a->rot > a->d || a->axes < 1 || a->axes > 4) return TOPK_ERR_INVALID_ARG;
+  if (a->dtype != TOPK_F32 && a->dtype != TOPK_BF16) return TOPK_ERR_INVALID_ARG;
+  if (!a->normalize && (a->q_weight || a->k_weight)) return TOPK_ERR_INVALID_ARG;
+  if (!(a->eps >= 0.f)) return TOPK_ERR_INVALID_ARG;
+  if (a->rot > 0 && !a->positions && a->L > a->table_rows) return TOPK_ERR_INVALID_ARG;
+  int sum = 0;
+  for (int x = 0; x < a->axes; ++x) {
+    if (a->sections[x] < 0 || a->sections[x] > a->rot) return TOPK_ERR_INVALID_ARG;
+    sum += a->sections[x];
+    p->bound[x] = sum;
+  }
+  if (2 * sum != a->rot) return TOPK_ERR_INVALID_ARG;
+  if (a->d % 8 != 0 || a->d > 256 || a->rot % 8 != 0) return TOPK_ERR_UNSUPPORTED;
+  if (a->Hq > 65536 || a->Hkv > 65536 || static_cast<long long>(a->B) * a->L > (1ll << 33)) return TOPK_ERR_UNSUPPORTED;
+  for (int x = 0; x < 3; ++x) {
+    if (a->q_stride[x] < 0 || a->k_stride[x] < 0 || (with_v && a->v_stride[x] < 0)) return TOPK_ERR_INVALID_ARG;
+    if (a->q_stride[x] % 4 || a->k_stride[x] % 4 || (with_v && a->v_stride[x] % 4)) return TOPK_ERR_UNSUPPORTED;
+    p->q_stride[x] = a->q_stride[x], p->k_stride[x] = a->k_stride[x], p->v_stride[x] = with_v ? a->v_stride[x] : 0;
+  }
+  for (const void* x : {a->q, a->k, with_v ? a->v : a->q, a->q_weight, a->k_weight, static_cast<const void*>(a->cos),
+                        static_cast<const void*>(a->sin)})
+    if (!aligned16(x)) return TOPK_ERR_UNSUPPORTED;
+  if (!aligned4(a->positions)) return TOPK_ERR_UNSUPPORTED;
+  p->q = a->q, p->k = a->k, p->v = with_v ? a->v : nullptr;
+  p->q_weight = a->q_weight, p->k_weight = a->k_weight, p->cos = a->cos, p->sin = a->sin, p->positions = a->positions;
+  p->table_rows = a->table_rows, p->B = a->B, p->L = a->L, p->Hq = a->Hq, p->Hkv = a->Hkv, p->d = a->d, p->rot = a->rot;
+  p->axes = a->axes, p->interleaved = a->interleaved != 0, p->normalize = a->normalize != 0, p->bf16 = a->dtype == TOPK_BF16;
+  p->eps = a->eps, p->q_scale = a->q_scale;
+  return TOPK_OK;
+}
+
+// The device the call runs on, or null where it is not a GB300.
+DeviceState* gb300() {
+  DeviceState* dev = device_state();
+  return dev && dev->cc_major == 10 && dev->cc_minor == 3 ? dev : nullptr;
+}
+
+int launched(int n) {
+  if (n == 0) return TOPK_ERR_UNSUPPORTED;
+  if (n < 0) return TOPK_ERR_CUDA;
+  t_last_launches = n;
+  return TOPK_OK;
+}
+}  // namespace
+
+int topk_qk_norm_rope_fwd(const topk_qk_args* args, void* q_out, void* k_out, void* v_out, int cap,
+                          const int32_t* cache_start, void* stream) {
+  QkArgs p;
+  const int rc = make_qk(args, args && args->v, &p);
+  if (rc) return rc;
+  if (!q_out || !k_out || (v_out != nullptr) != (p.v != nullptr)) return TOPK_ERR_INVALID_ARG;
+  if (cap <= 0 || (!cache_start && cap != p.L)) return TOPK_ERR_INVALID_ARG;
+  if (!aligned16(q_out) || !aligned16(k_out) || !aligned16(v_out) || !aligned4(cache_start)) return TOPK_ERR_UNSUPPORTED;
+  DeviceState* dev = gb300();
+  if (!dev) return TOPK_ERR_NO_DEVICE;
+  return launched(qk_norm_rope_fwd(p, q_out, k_out, v_out, cap, cache_start, dev->num_sms, make_ctl(dev),
+                                   static_cast<cudaStream_t>(stream)));
+}
+
+int topk_qk_norm_rope_bwd(const topk_qk_args* args, const void* dq, const void* dk, const void* dv, int grad_dtype,
+                          void* dqkv, float* dq_weight, float* dk_weight, void* stream) {
+  QkArgs p;
+  const int rc = make_qk(args, false, &p);
+  if (rc) return rc;
+  if (!dq || !dk || !dqkv) return TOPK_ERR_INVALID_ARG;
+  if (grad_dtype != TOPK_F32 && grad_dtype != TOPK_BF16) return TOPK_ERR_INVALID_ARG;
+  if (grad_dtype == TOPK_BF16 && !p.bf16) return TOPK_ERR_UNSUPPORTED;
+  if (!aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(dqkv) || !aligned4(dq_weight) || !aligned4(dk_weight))
+    return TOPK_ERR_UNSUPPORTED;
+  DeviceState* dev = gb300();
+  if (!dev) return TOPK_ERR_NO_DEVICE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  void* buf = nullptr;
+  if (p.normalize && (dq_weight || dk_weight) &&
+      !pool_alloc(&buf, static_cast<size_t>(qk_bwd_blocks(p.B, p.L, dev->num_sms)) * 2 * p.d * sizeof(float), st))
+    return TOPK_ERR_CUDA;
+  const int n = qk_norm_rope_bwd(p, dq, dk, dv, grad_dtype == TOPK_BF16, dqkv, dq_weight, dk_weight, static_cast<float*>(buf),
+                                 dev->num_sms, make_ctl(dev), st);
+  if (buf) cudaFreeAsync(buf, st);
+  return launched(n);
+}
+
+size_t topk_qk_norm_rope_bwd_workspace_bytes(int B, int L, int d) {
+  if (B <= 0 || L <= 0 || d <= 0 || d % 8 != 0 || d > 256) return 0;
+  const DeviceState* dev = device_state();
+  return static_cast<size_t>(qk_bwd_blocks(B, L, dev ? dev->num_sms : kAssumedSms)) * 2 * d * sizeof(float);
+}
+
+namespace {
 // After a synchronising host-buffer call: report any device-side error flag.
 int host_call_status(int rc) {
   if (rc != TOPK_OK) return rc;
@@ -467,7 +563,8 @@ int host_call_status(int rc) {
   if (!word) return TOPK_OK;
   const unsigned zero = 0;
   cudaMemcpy(dev->error_word, &zero, sizeof zero, cudaMemcpyHostToDevice);
-  return (word & kDevErrTimeout) ? TOPK_ERR_TIMEOUT : TOPK_ERR_WORKSPACE;
+  if (word & kDevErrTimeout) return TOPK_ERR_TIMEOUT;
+  return (word & kDevErrWorkspace) ? TOPK_ERR_WORKSPACE : TOPK_ERR_RANGE;
 }
 }  // namespace
 
@@ -697,7 +794,7 @@ int topk_check(void* stream) {
   }
   if (word & kDevErrTimeout) return TOPK_ERR_TIMEOUT;
   if (word & kDevErrWorkspace) return TOPK_ERR_WORKSPACE;
-  return TOPK_OK;
+  return (word & kDevErrRange) ? TOPK_ERR_RANGE : TOPK_OK;
 }
 
 const char* topk_error_string(int code) {
@@ -710,6 +807,7 @@ const char* topk_error_string(int code) {
     case TOPK_ERR_WORKSPACE: return "per-row candidate list overflowed; outputs invalid";
     case TOPK_ERR_NO_DEVICE: return "no usable sm_103 device";
     case TOPK_ERR_SCRATCH_LIMIT: return "problem needs more scratch than the fixed no-allocation buffer holds";
+    case TOPK_ERR_RANGE: return "a position outside the rotation tables or a row outside the cache";
     default: return "unknown error code";
   }
 }

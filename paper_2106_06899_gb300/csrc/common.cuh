@@ -17,6 +17,7 @@ namespace topk {
 // device error word values (bit flags, OR-ed together)
 constexpr unsigned kDevErrTimeout = 1u;
 constexpr unsigned kDevErrWorkspace = 2u;
+constexpr unsigned kDevErrRange = 4u;  // a position or cache row outside its table
 
 struct DevCtl {
   unsigned* error;          // device word, OR-ed with kDevErr* flags

@@ -129,6 +129,30 @@ struct FfnPlainArgs {
 size_t ffn_plain_workspace_bytes(int N, int d_ff, int chunk);
 int ffn_plain(const FfnPlainArgs& a, int num_sms, cudaStream_t st);
 
+// Query/key norm with the position rotation (norm_rope.cu).  Strides are in
+// elements: batch, token, head; a head's row is contiguous.  bound[x] is the
+// first pair of axis x + 1.
+struct QkArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  long long q_stride[3], k_stride[3], v_stride[3];
+  const void* q_weight;
+  const void* k_weight;
+  const float* cos;
+  const float* sin;
+  const int32_t* positions;
+  int table_rows, B, L, Hq, Hkv, d, rot, axes;
+  int bound[4];
+  int interleaved, normalize, bf16;
+  float eps, q_scale;
+};
+int qk_bwd_blocks(int B, int L, int num_sms);  // the backward grid: one partial row of weight gradients each
+int qk_norm_rope_fwd(const QkArgs& p, void* qo, void* ko, void* vo, int cap, const int32_t* start, int num_sms, const DevCtl& ctl,
+                     cudaStream_t st);
+int qk_norm_rope_bwd(const QkArgs& p, const void* dq, const void* dk, const void* dv, bool grad_bf16, void* dqkv, float* dqw,
+                     float* dkw, float* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st);
+
 // Driver entry point for cuTensorMapEncodeTiled (resolved once, no libcuda link).
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                    const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,

@@ -22,6 +22,17 @@ _lock = threading.Lock()
 _lib = None
 
 
+class _QkArgs(ctypes.Structure):
+    """topk_qk_args"""
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "k", "v")]
+                + [(n, ctypes.c_longlong * 3) for n in ("q_stride", "k_stride", "v_stride")]
+                + [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "cos", "sin", "positions")]
+                + [(n, ctypes.c_int) for n in ("table_rows", "B", "L", "Hq", "Hkv", "d", "rot", "axes")]
+                + [("sections", ctypes.c_int * 4)]
+                + [(n, ctypes.c_int) for n in ("interleaved", "normalize", "dtype")]
+                + [(n, ctypes.c_float) for n in ("eps", "q_scale")])
+
+
 class TopkError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -63,6 +74,10 @@ def lib() -> ctypes.CDLL:
             L.topk_attn_bwd_workspace_bytes.restype = sz
             L.topk_ffn_bwd_workspace_bytes.argtypes = [i32] * 4
             L.topk_ffn_bwd_workspace_bytes.restype = sz
+            L.topk_qk_norm_rope_fwd.argtypes = [ctypes.POINTER(_QkArgs), vp, vp, vp, i32, vp, vp]
+            L.topk_qk_norm_rope_bwd.argtypes = [ctypes.POINTER(_QkArgs), vp, vp, vp, i32, vp, vp, vp, vp]
+            L.topk_qk_norm_rope_bwd_workspace_bytes.argtypes = [i32] * 3
+            L.topk_qk_norm_rope_bwd_workspace_bytes.restype = sz
             L.topk_check.argtypes = [vp]
             L.topk_error_string.argtypes = [i32]
             L.topk_error_string.restype = ctypes.c_char_p
@@ -76,7 +91,8 @@ def lib() -> ctypes.CDLL:
                       "topk_attn_fwd_host", "topk_ffn_fwd_host", "topk_ffn_fwd_noalloc", "topk_check",
                       "topk_last_launch_count",
                       "topk_debug_skip_arrive", "topk_pool_usage", "topk_pool_trim", "topk_attn_bwd",
-                      "topk_ffn_bwd", "topk_attn_fwd_masked", "topk_vanilla_attn_fwd", "topk_vanilla_ffn_fwd"):
+                      "topk_ffn_bwd", "topk_attn_fwd_masked", "topk_vanilla_attn_fwd", "topk_vanilla_ffn_fwd",
+                      "topk_qk_norm_rope_fwd", "topk_qk_norm_rope_bwd"):
                 getattr(L, f).restype = i32
             _lib = L
     return _lib
@@ -313,6 +329,88 @@ def topk_ffn_bwd(x, W1, W2, dout, idx, score, dx, dW1, dW2, stream=None) -> None
     _check(rc, "topk_ffn_bwd")
 
 
+def rope_tables(positions: int, rot: int, base: float = 10000.0, device="cuda"):
+    """(cos, sin), fp32 [positions, rot / 2], of the angles p * base^(-2 i / rot), formed in fp64."""
+    angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * float(base) ** (
+        -torch.arange(rot // 2, dtype=torch.float64, device=device) * 2 / max(rot, 1))
+    return angle.cos().float(), angle.sin().float()
+
+
+def _qk_args(q, k, v, cos, sin, positions, q_weight, k_weight, eps, q_scale, sections, interleaved, normalize):
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if t is not None and (t.dim() != 4 or t.stride(3) != 1):
+            raise ValueError(f"{name} must be a [B, L, H, d] tensor with contiguous rows")
+    B, L, Hq, d = q.shape
+    Hkv = k.shape[2]
+    if tuple(k.shape) != (B, L, Hkv, d) or (v is not None and v.shape != k.shape):
+        raise ValueError("shape mismatch between q, k, v")
+    if k.dtype != q.dtype or (v is not None and v.dtype != q.dtype):
+        raise TypeError("q, k, v must share a dtype")
+    half = cos.shape[-1]
+    for name, t in (("cos", cos), ("sin", sin)):
+        if t.dtype != torch.float32 or t.dim() != 2 or t.shape != cos.shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous [positions, rot / 2] float32 tensor")
+    sections = (half,) if sections is None else tuple(int(n) for n in sections)
+    if not 1 <= len(sections) <= 4:
+        raise ValueError("sections must name 1 to 4 axes")
+    if positions is not None and (positions.dtype != torch.int32 or tuple(positions.shape) != (len(sections), B, L)
+                                  or not positions.is_contiguous()):
+        raise ValueError("positions must be a contiguous [axes, B, L] int32 tensor")
+    for name, t in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if t is not None and (t.dtype != q.dtype or tuple(t.shape) != (d,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous [d] tensor of q's dtype")
+    a = _QkArgs(_ptr(q), _ptr(k), _ptr(v), q.stride()[:3], k.stride()[:3], (0, 0, 0) if v is None else v.stride()[:3],
+                _ptr(q_weight), _ptr(k_weight), _ptr(cos), _ptr(sin), _ptr(positions), cos.shape[0], B, L, Hq, Hkv, d,
+                2 * half, len(sections), sections, int(bool(interleaved)), int(bool(normalize)), _dtype_code(q), eps, q_scale)
+    return a, (B, L, Hq, Hkv, d)
+
+
+def topk_qk_norm_rope_fwd(q, k, v, cos, sin, q_out, k_out, v_out, *, cache_start=None, positions=None, q_weight=None,
+                          k_weight=None, eps: float = 1e-6, q_scale: float = 1.0, sections=None, interleaved: bool = False,
+                          normalize: bool = True, stream=None) -> None:
+    """RMS norm of each query and key head, rotation by position and q_scale: q [B,L,Hq,d], k/v
+    [B,L,Hkv,d] (strided views allowed) into q_out [B,Hq,L,d] and k_out/v_out [B,Hkv,cap,d]; with
+    cache_start ([B] int32) token t of batch b goes to row cache_start[b] + t of k_out/v_out."""
+    a, (B, L, Hq, Hkv, d) = _qk_args(q, k, v, cos, sin, positions, q_weight, k_weight, eps, q_scale, sections, interleaved,
+                                     normalize)
+    cap = k_out.shape[2]
+    for name, t, shape in (("q_out", q_out, (B, Hq, L, d)), ("k_out", k_out, (B, Hkv, cap, d)),
+                           ("v_out", v_out, (B, Hkv, cap, d))):
+        if t is not None and (t.dtype != q.dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {list(shape)} {q.dtype} tensor")
+    if cache_start is not None and (cache_start.dtype != torch.int32 or tuple(cache_start.shape) != (B,)
+                                    or not cache_start.is_contiguous()):
+        raise ValueError("cache_start must be a [B] int32 tensor")
+    rc = lib().topk_qk_norm_rope_fwd(ctypes.byref(a), _ptr(q_out), _ptr(k_out), _ptr(v_out), cap, _ptr(cache_start),
+                                     _stream(stream))
+    _check(rc, "topk_qk_norm_rope_fwd")
+
+
+def topk_qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, dqkv, dq_weight, dk_weight, *, positions=None, q_weight=None,
+                          k_weight=None, eps: float = 1e-6, q_scale: float = 1.0, sections=None, interleaved: bool = False,
+                          normalize: bool = True, stream=None) -> None:
+    """Backward: dq [B,Hq,L,d], dk/dv [B,Hkv,L,d] (fp32 or bf16) into dqkv [B,L,Hq+2Hkv,d] (q's dtype; Hq+Hkv
+    heads without dv) and the norms' weight gradients [d] fp32 (or None)."""
+    a, (B, L, Hq, Hkv, d) = _qk_args(q, k, None, cos, sin, positions, q_weight, k_weight, eps, q_scale, sections, interleaved,
+                                     normalize)
+    for name, t, h in (("dq", dq, Hq), ("dk", dk, Hkv), ("dv", dv, Hkv)):
+        if t is not None and (t.dtype != dq.dtype or tuple(t.shape) != (B, h, L, d) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {[B, h, L, d]} {dq.dtype} tensor")
+    want = (B, L, Hq + (Hkv if dv is None else 2 * Hkv), d)
+    if dqkv.dtype != q.dtype or tuple(dqkv.shape) != want or not dqkv.is_contiguous():
+        raise ValueError(f"dqkv must be a contiguous {list(want)} {q.dtype} tensor")
+    for name, t in (("dq_weight", dq_weight), ("dk_weight", dk_weight)):
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (d,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous [d] float32 tensor")
+    rc = lib().topk_qk_norm_rope_bwd(ctypes.byref(a), _ptr(dq), _ptr(dk), _ptr(dv), _dtype_code(dq), _ptr(dqkv), _ptr(dq_weight),
+                                     _ptr(dk_weight), _stream(stream))
+    _check(rc, "topk_qk_norm_rope_bwd")
+
+
+def topk_qk_norm_rope_bwd_workspace_bytes(B, L, d) -> int:
+    return int(lib().topk_qk_norm_rope_bwd_workspace_bytes(B, L, d))
+
+
 def topk_attn_bwd_workspace_bytes(B, H, Lq, Lk, d, topk, dtype) -> int:
     return int(lib().topk_attn_bwd_workspace_bytes(B, H, Lq, Lk, d, topk, dtype))
 
@@ -409,3 +507,36 @@ def ffn_bwd(x, W1, W2, dout, idx, score, stream=None):
     dW2 = torch.empty(W2.shape, dtype=torch.float32, device=W2.device)
     topk_ffn_bwd(x, W1, W2, dout, idx, score, dx, dW1, dW2, stream)
     return dx, dW1, dW2
+
+
+def qk_norm_rope(q, k, v, cos, sin, cache=None, cache_start=None, **options):
+    """Norm, rotation and scale of a projection's q [B,L,Hq,d] and k, v [B,L,Hkv,d] for the attention:
+    (q [B,Hq,L,d], k, v [B,Hkv,L,d]).  With cache = (keys, values), each [B,Hkv,cap,d], k and v are written
+    into it from row cache_start[b] on ([B] int32) and the caches are returned.  v may be None (without a
+    cache).  Options as topk_qk_norm_rope_fwd."""
+    B, L, Hq, d = q.shape
+    qo = torch.empty(B, Hq, L, d, dtype=q.dtype, device=q.device)
+    if cache is not None:
+        if cache_start is None or v is None:
+            raise ValueError("a cache needs cache_start and v")
+        ko, vo = cache
+    else:
+        if cache_start is not None:
+            raise ValueError("cache_start needs a cache")
+        ko = torch.empty(B, k.shape[2], L, d, dtype=q.dtype, device=q.device)
+        vo = None if v is None else torch.empty_like(ko)
+    topk_qk_norm_rope_fwd(q, k, v, cos, sin, qo, ko, vo, cache_start=cache_start, **options)
+    return qo, ko, vo
+
+
+def qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, **options):
+    """Gradients (dqkv [B,L,Hq+2Hkv,d] packed in q's dtype, dq_weight, dk_weight fp32 [d]) of qk_norm_rope; the weight
+    gradients are None with normalize=False.  dv may be None."""
+    B, L, Hq, d = q.shape
+    Hkv = k.shape[2]
+    dqkv = torch.empty(B, L, Hq + (Hkv if dv is None else 2 * Hkv), d, dtype=q.dtype, device=q.device)
+    gq = gk = None
+    if options.get("normalize", True):
+        gq, gk = (torch.empty(d, dtype=torch.float32, device=q.device) for _ in range(2))
+    topk_qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, dqkv, gq, gk, **options)
+    return dqkv, gq, gk

@@ -1,0 +1,81 @@
+"""The operators around the attention refuse bad arguments before anything is launched (no GPU needed)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2106_06899_gb300 import build
+from paper_2106_06899_gb300 import topk as T
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build_library()
+    return T.lib()
+
+
+def _qk(**kw):
+    a = dict(q=16, k=16, v=16, q_stride=(64, 64, 64), k_stride=(64, 64, 64), v_stride=(64, 64, 64), q_weight=None, k_weight=None,
+             cos=16, sin=16, positions=None, table_rows=8, B=1, L=8, Hq=2, Hkv=1, d=64, rot=64, axes=1, sections=(32, 0, 0, 0),
+             interleaved=0, normalize=1, dtype=1, eps=1e-6, q_scale=1.0)
+    a.update(kw)
+    return T._QkArgs(*[a[n] for n, _ in T._QkArgs._fields_])
+
+
+BAD = [
+    (dict(q=None), -1), (dict(k=None), -1), (dict(cos=None), -1), (dict(B=0), -1), (dict(L=-1), -1), (dict(Hq=0), -1), (dict(Hkv=0), -1),
+    (dict(rot=72), -1), (dict(axes=0), -1), (dict(axes=5), -1), (dict(sections=(31, 0, 0, 0)), -1), (dict(axes=2, sections=(33, -1, 0, 0)), -1),
+    (dict(dtype=2), -1), (dict(normalize=0, q_weight=16), -1), (dict(eps=-1.0), -1), (dict(eps=float("nan")), -1),
+    (dict(table_rows=7), -1), (dict(q_stride=(-64, 64, 64)), -1), (dict(q_stride=(64, 66, 64)), -2),
+    (dict(d=60, rot=56, sections=(28, 0, 0, 0)), -2), (dict(d=264), -2), (dict(rot=60, sections=(30, 0, 0, 0)), -2), (dict(q=24), -2), (dict(q_weight=8), -2), (dict(positions=18), -2),
+]
+
+
+@pytest.mark.parametrize("kw,code", BAD, ids=str)
+def test_qk_arguments(lib, kw, code):
+    a = _qk(**kw)
+    assert lib.topk_qk_norm_rope_fwd(ctypes.byref(a), 16, 16, 16, 8, None, None) == code
+    assert lib.topk_qk_norm_rope_bwd(ctypes.byref(a), 16, 16, 16, 0, 16, 16, 16, None) == code
+
+
+def test_qk_outputs(lib):
+    f, a = lib.topk_qk_norm_rope_fwd, _qk()
+    ref = ctypes.byref(a)
+    assert f(None, 16, 16, 16, 8, None, None) == -1
+    assert f(ref, None, 16, 16, 8, None, None) == -1
+    assert f(ref, 16, 16, None, 8, None, None) == -1   # v without v_out
+    assert f(ref, 16, 16, 16, 9, None, None) == -1     # a cache without its start rows
+    assert f(ref, 16, 16, 16, 0, 16, None) == -1
+    assert f(ref, 24, 16, 16, 8, None, None) == -2
+    assert f(ref, 16, 16, 16, 9, 18, None) == -2
+    b = lib.topk_qk_norm_rope_bwd
+    assert b(ref, None, 16, 16, 0, 16, 16, 16, None) == -1
+    assert b(ref, 16, 16, 16, 3, 16, 16, 16, None) == -1
+    assert b(ctypes.byref(_qk(dtype=0)), 16, 16, 16, 1, 16, 16, 16, None) == -2
+    assert b(ref, 16, 16, 24, 0, 16, 16, 16, None) == -2
+    assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 100, 64) == 13 * 2 * 64 * 4
+    assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 1 << 20, 64) <= 2 * 160 * 2 * 64 * 4
+    assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 100, 60) == 0
+
+
+def test_qk_binding_shapes():
+    q = torch.zeros(1, 8, 2, 64, dtype=torch.bfloat16)
+    cos, sin = T.rope_tables(8, 64, device="cpu")
+    with pytest.raises(ValueError):
+        T.qk_norm_rope(q, q[:, :7], None, cos, sin)
+    with pytest.raises(ValueError):
+        T.qk_norm_rope(q, q, q[..., ::2], cos, sin)
+    with pytest.raises(TypeError):
+        T.qk_norm_rope(q, q.float(), None, cos, sin)
+    with pytest.raises(ValueError):
+        T.qk_norm_rope(q, q, q, cos.double(), sin)
+    with pytest.raises(ValueError):
+        T.qk_norm_rope(q, q, q, cos, sin, q_weight=torch.ones(64))
+    with pytest.raises(ValueError):
+        T.qk_norm_rope(q, q, q, cos, sin, positions=torch.zeros(2, 1, 8, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        T.qk_norm_rope(q, q, q, cos, sin, sections=(8, 8, 8, 4, 4))
+    with pytest.raises(ValueError):
+        T.qk_norm_rope(q, q, q, cos, sin, cache_start=torch.zeros(1, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        T.qk_norm_rope(q, q, q, cos, sin, cache=(q, q))
