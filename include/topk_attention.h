@@ -309,6 +309,46 @@ int topk_qk_norm_rope_bwd(const topk_qk_args* args, const void* dq, const void* 
                           void* dqkv, float* dq_weight, float* dk_weight, void* stream);
 size_t topk_qk_norm_rope_bwd_workspace_bytes(int B, int L, int d);
 
+/*
+ * One AdamW step over many tensors, in place:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2  (g: the gradient x *grad_scale)
+ *   p = p (1 - lr wd) - lr / (1 - beta1^step)  m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in fp32, each operation rounded by itself in the order written (lr / (..) last).
+ *   tensors    : `count` descriptions in HOST memory, read before the call returns.  Tensors may
+ *                be of any length (0 is skipped) and alignment; 16-byte aligned ones (8-byte
+ *                for 8-bit states) take vector accesses.  No two may overlap.
+ *   param_dtype, grad_dtype: TOPK_F32 or TOPK_BF16, of all tensors.
+ *   state_bits : 32: m and v fp32 [n].  8: m and v hold e4m3 floats [n], with one fp32 scale for
+ *                every 256 elements in m_scale, v_scale [ceil(n / 256)] (value = float x scale,
+ *                scale = largest magnitude / 448; a block whose scale is below 2^-100 is zero); v
+ *                holds the ROOT of the second moment.  They are rounded stochastically; the
+ *                update uses the values before rounding.
+ *   master     : NULL, or (TOPK_BF16 parameters, all tensors or none) fp32 [n] that the step
+ *                reads and updates; param is then its copy, rounded to nearest.  bf16
+ *                parameters without a master are rounded stochastically.
+ *   seed       : of the random bits, which are a hash of (seed, step, index + element): a
+ *                repeated step gives the same bits.  `index` numbers the tensor's first element
+ *                among all of the optimizer's.
+ *   step       : 1 for the first step.  0 <= beta < 1, eps >= 0; lr, wd finite.
+ *   grad_scale : NULL, or a device float that multiplies the gradients (loss unscaling,
+ *                clipping); if it is not finite the step changes nothing.
+ * A non-finite gradient spoils its element, and with 8-bit states its block's moments.
+ * One launch for every 352 tensors; no scratch.  Errors as topk_attn_fwd.
+ */
+typedef struct {
+  void* param;
+  const void* grad;
+  float* master;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  long long n, index;
+  double lr, weight_decay;
+} topk_adamw_tensor;
+
+int topk_adamw_step(const topk_adamw_tensor* tensors, int count, int param_dtype, int grad_dtype, int state_bits,
+                    double beta1, double beta2, double eps, long long step, const float* grad_scale, uint32_t seed,
+                    void* stream);
+
 /* Scratch bytes of the two backward calls for these arguments; 0 if invalid or unsupported. */
 size_t topk_attn_bwd_workspace_bytes(int B, int H, int Lq, int Lk, int d, int topk, int dtype);
 size_t topk_ffn_bwd_workspace_bytes(int N, int d_model, int d_ff, int topk);

@@ -5,6 +5,7 @@
 // the caller's; the only state kept here is per-device: the device error
 // word (OR-ed by kernels whose bounded waits ran out) and the SM count.
 #include <atomic>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <mutex>
@@ -544,6 +545,39 @@ int topk_qk_norm_rope_bwd(const topk_qk_args* args, const void* dq, const void* 
                                  dev->num_sms, make_ctl(dev), st);
   if (buf) cudaFreeAsync(buf, st);
   return launched(n);
+}
+
+int topk_adamw_step(const topk_adamw_tensor* tensors, int count, int param_dtype, int grad_dtype, int state_bits,
+                    double beta1, double beta2, double eps, long long step, const float* grad_scale, uint32_t seed,
+                    void* stream) {
+  if (count < 0 || (count > 0 && !tensors) || step < 1) return TOPK_ERR_INVALID_ARG;
+  for (int dt : {param_dtype, grad_dtype})
+    if (dt != TOPK_F32 && dt != TOPK_BF16) return TOPK_ERR_INVALID_ARG;
+  if (state_bits != 32 && state_bits != 8) return TOPK_ERR_INVALID_ARG;
+  if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0)) return TOPK_ERR_INVALID_ARG;
+  if (!aligned4(grad_scale)) return TOPK_ERR_UNSUPPORTED;
+  const uintptr_t pa = param_dtype == TOPK_F32 ? 3 : 1, ga = grad_dtype == TOPK_F32 ? 3 : 1;
+  for (int k = 0; k < count; ++k) {
+    const topk_adamw_tensor& t = tensors[k];
+    if (t.n < 0 || !std::isfinite(t.lr) || !std::isfinite(t.weight_decay)) return TOPK_ERR_INVALID_ARG;
+    if (t.n == 0) continue;
+    if (!t.param || !t.grad || !t.m || !t.v) return TOPK_ERR_INVALID_ARG;
+    if (state_bits == 8 && (!t.m_scale || !t.v_scale)) return TOPK_ERR_INVALID_ARG;
+    if (t.master && param_dtype != TOPK_BF16) return TOPK_ERR_INVALID_ARG;
+    if ((t.master != nullptr) != (tensors[0].master != nullptr) && tensors[0].n) return TOPK_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(t.param) & pa) || (reinterpret_cast<uintptr_t>(t.grad) & ga) || !aligned4(t.master) ||
+        !aligned4(t.m_scale) || !aligned4(t.v_scale) || (state_bits == 32 && (!aligned4(t.m) || !aligned4(t.v))))
+      return TOPK_ERR_UNSUPPORTED;
+    if (t.n > (1ll << 40)) return TOPK_ERR_UNSUPPORTED;
+  }
+  DeviceState* dev = gb300();
+  if (!dev) return TOPK_ERR_NO_DEVICE;
+  const AdamwArgs a{tensors, count, param_dtype == TOPK_BF16, grad_dtype == TOPK_BF16, state_bits == 8, beta1, beta2, eps,
+                    step, grad_scale, seed};
+  const int n = adamw_step(a, dev->num_sms, static_cast<cudaStream_t>(stream));
+  if (n < 0) return TOPK_ERR_CUDA;
+  t_last_launches = n;  // 0 where every tensor is empty
+  return TOPK_OK;
 }
 
 size_t topk_qk_norm_rope_bwd_workspace_bytes(int B, int L, int d) {

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "common.cuh"
+#include "topk_attention.h"
 
 namespace topk {
 
@@ -152,6 +153,18 @@ int qk_norm_rope_fwd(const QkArgs& p, void* qo, void* ko, void* vo, int cap, con
                      cudaStream_t st);
 int qk_norm_rope_bwd(const QkArgs& p, const void* dq, const void* dk, const void* dv, bool grad_bf16, void* dqkv, float* dqw,
                      float* dkw, float* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st);
+
+// AdamW over many tensors (adamw.cu); the arguments are checked.
+struct AdamwArgs {
+  const topk_adamw_tensor* tensors;
+  int count;
+  bool param_bf16, grad_bf16, bits8;
+  double beta1, beta2, eps;
+  long long step;
+  const float* grad_scale;
+  uint32_t seed;
+};
+int adamw_step(const AdamwArgs& a, int num_sms, cudaStream_t st);
 
 // Driver entry point for cuTensorMapEncodeTiled (resolved once, no libcuda link).
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,

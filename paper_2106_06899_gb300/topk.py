@@ -78,6 +78,8 @@ def lib() -> ctypes.CDLL:
             L.topk_qk_norm_rope_bwd.argtypes = [ctypes.POINTER(_QkArgs), vp, vp, vp, i32, vp, vp, vp, vp]
             L.topk_qk_norm_rope_bwd_workspace_bytes.argtypes = [i32] * 3
             L.topk_qk_norm_rope_bwd_workspace_bytes.restype = sz
+            L.topk_adamw_step.argtypes = [vp, i32, i32, i32, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                                          ctypes.c_longlong, vp, ctypes.c_uint32, vp]
             L.topk_check.argtypes = [vp]
             L.topk_error_string.argtypes = [i32]
             L.topk_error_string.restype = ctypes.c_char_p
@@ -92,7 +94,7 @@ def lib() -> ctypes.CDLL:
                       "topk_last_launch_count",
                       "topk_debug_skip_arrive", "topk_pool_usage", "topk_pool_trim", "topk_attn_bwd",
                       "topk_ffn_bwd", "topk_attn_fwd_masked", "topk_vanilla_attn_fwd", "topk_vanilla_ffn_fwd",
-                      "topk_qk_norm_rope_fwd", "topk_qk_norm_rope_bwd"):
+                      "topk_qk_norm_rope_fwd", "topk_qk_norm_rope_bwd", "topk_adamw_step"):
                 getattr(L, f).restype = i32
             _lib = L
     return _lib

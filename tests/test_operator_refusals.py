@@ -79,3 +79,55 @@ def test_qk_binding_shapes():
         T.qk_norm_rope(q, q, q, cos, sin, cache_start=torch.zeros(1, dtype=torch.int32))
     with pytest.raises(ValueError):
         T.qk_norm_rope(q, q, q, cos, sin, cache=(q, q))
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("param", "grad", "master", "m", "v", "m_scale", "v_scale")]
+                + [("n", ctypes.c_longlong), ("index", ctypes.c_longlong), ("lr", ctypes.c_double), ("weight_decay", ctypes.c_double)])
+
+
+def _adamw(lib, count=1, pdt=0, gdt=0, bits=32, b1=0.9, b2=0.999, eps=1e-8, step=1, gs=None, **kw):
+    a = dict(param=16, grad=16, master=None, m=16, v=16, m_scale=16, v_scale=16, n=8, index=0, lr=1e-3, weight_decay=0.0)
+    a.update(kw)
+    t = _Tensor(*[a[n] for n, _ in _Tensor._fields_])
+    return lib.topk_adamw_step(ctypes.addressof(t), count, pdt, gdt, bits, b1, b2, eps, step, gs, 0, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(count=-1), -1), (dict(step=0), -1), (dict(pdt=2), -1), (dict(gdt=5), -1), (dict(bits=16), -1), (dict(b1=1.0), -1), (dict(b2=-0.1), -1),
+    (dict(eps=-1.0), -1), (dict(eps=float("nan")), -1), (dict(n=-1), -1), (dict(lr=float("inf")), -1), (dict(weight_decay=float("nan")), -1),
+    (dict(param=None), -1), (dict(grad=None), -1), (dict(m=None), -1), (dict(v=None), -1), (dict(bits=8, m_scale=None), -1),
+    (dict(master=16), -1), (dict(param=18), -2), (dict(pdt=1, param=17), -2), (dict(grad=18), -2), (dict(m=18), -2), (dict(gs=18), -2),
+    (dict(bits=8, v_scale=18), -2),
+], ids=str)
+def test_adamw_arguments(lib, kw, code):
+    assert _adamw(lib, **kw) == code
+
+
+def test_adamw_record_matches_the_header(lib):
+    from paper_2106_06899_gb300 import optim
+
+    assert optim._TENSOR.itemsize == ctypes.sizeof(_Tensor)
+    assert [(n, optim._TENSOR.fields[n][1]) for n in optim._TENSOR.names] == [(n, getattr(_Tensor, n).offset) for n, _ in _Tensor._fields_]
+
+
+def test_adamw_binding():
+    from paper_2106_06899_gb300 import optim
+
+    p = torch.zeros(8, 4)
+    for bad in (dict(params=[]), dict(params=[p], state_bits=4), dict(params=[p, p.bfloat16()]), dict(params=[p.t()]),
+                dict(params=[p], masters=True), dict(params=[p.bfloat16()], masters=[p.bfloat16()]), dict(params=[p], state={"exp_avg": p})):
+        with pytest.raises(ValueError):
+            optim.AdamW(**bad)
+    opt = optim.AdamW([p])
+    with pytest.raises(ValueError):
+        opt.step([])
+    with pytest.raises(ValueError):
+        opt.step([torch.zeros(31)])
+    with pytest.raises(TypeError):
+        opt.step([torch.zeros(8, 4, dtype=torch.float16)])
+    with pytest.raises(ValueError):
+        opt.step([p], grad_scale=torch.zeros(2))
+    with pytest.raises(ValueError):
+        opt.load_state_dict(optim.AdamW([p], state_bits=8).state_dict())
+    assert optim.AdamW([p], state_bits=8).moments(0)[0].shape == p.shape
