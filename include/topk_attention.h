@@ -310,6 +310,38 @@ int topk_qk_norm_rope_bwd(const topk_qk_args* args, const void* dq, const void* 
 size_t topk_qk_norm_rope_bwd_workspace_bytes(int B, int L, int d);
 
 /*
+ * The linear layer with its epilogue: z = x w^T + bias, y = act(z) + residual.
+ *   x        : [M, K].  w: [N, K] (row n: the weights of output n).  bias: [N] or NULL.
+ *   residual : [M, N] or NULL.  y: [M, N].  preact: NULL, or [M, N], which receives z for
+ *              the backward pass.  All bf16, contiguous, 16-byte aligned; y and preact overlap no
+ *              input, but y may be the residual itself.
+ *   act      : TOPK_ACT_*; GELU is z Phi(z) (the exact form), SILU z / (1 + e^-z).
+ *   M >= 1; N and K multiples of 8.  Sums in fp32, every result rounded once, to nearest.
+ *   Scratch: topk_linear_workspace_bytes(): 0, or fp32 partial sums (parts x M x N) where the
+ *   outputs are too few tiles for the SMs and the sum is split; parts are added in order, so
+ *   two runs give the same bits.  Errors as topk_attn_fwd.
+ */
+enum { TOPK_ACT_NONE = 0, TOPK_ACT_RELU = 1, TOPK_ACT_GELU = 2, TOPK_ACT_SILU = 3 };
+
+int topk_linear_fwd(const void* x, const void* w, const void* bias, const void* residual, void* y, void* preact, int M,
+                    int N, int K, int act, void* stream);
+size_t topk_linear_workspace_bytes(int M, int N, int K);
+
+/*
+ * Backward: dz = dy act'(z) (ReLU's slope at 0 is 0), dx = dz w, dw = dz^T x, db = the column sums
+ * of dz.  The residual's gradient is dy itself.
+ *   dy, preact : [M, N] bf16; preact is z (NULL iff act is TOPK_ACT_NONE).
+ *   dx         : [M, K] bf16 or NULL.  dw: [N, K], db: [N], of grad_dtype (TOPK_F32 or TOPK_BF16), or
+ *                NULL; at least one of the three is asked for.
+ *   Sums are fp32; with an activation dz is rounded to bf16 before the two products (the
+ *   tensor cores' operand), not before db.
+ *   Scratch: topk_linear_bwd_workspace_bytes(): dz, the partial sums of db and of split products.
+ */
+int topk_linear_bwd(const void* dy, const void* x, const void* w, const void* preact, void* dx, void* dw, void* db, int M,
+                    int N, int K, int act, int grad_dtype, void* stream);
+size_t topk_linear_bwd_workspace_bytes(int M, int N, int K, int act);
+
+/*
  * One AdamW step over many tensors, in place:
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2  (g: the gradient x *grad_scale)
  *   p = p (1 - lr wd) - lr / (1 - beta1^step)  m / (sqrt(v) / sqrt(1 - beta2^step) + eps)

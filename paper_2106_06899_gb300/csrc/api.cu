@@ -547,6 +547,69 @@ int topk_qk_norm_rope_bwd(const topk_qk_args* args, const void* dq, const void* 
   return launched(n);
 }
 
+namespace {
+int validate_linear(int M, int N, int K, int act) {
+  if (M <= 0 || N <= 0 || K <= 0 || act < TOPK_ACT_NONE || act > TOPK_ACT_SILU) return TOPK_ERR_INVALID_ARG;
+  if (N % 8 != 0 || K % 8 != 0) return TOPK_ERR_UNSUPPORTED;
+  // tile and block counts stay far below 2^31
+  if (M > (1 << 28) || N > (1 << 24) || static_cast<long long>(M) * N > (1ll << 38) || static_cast<long long>(N) * K > (1ll << 38) ||
+      static_cast<long long>(M) * K > (1ll << 38))
+    return TOPK_ERR_UNSUPPORTED;
+  return TOPK_OK;
+}
+}  // namespace
+
+int topk_linear_fwd(const void* x, const void* w, const void* bias, const void* residual, void* y, void* preact, int M,
+                    int N, int K, int act, void* stream) {
+  if (!x || !w || !y) return TOPK_ERR_INVALID_ARG;
+  const int rc = validate_linear(M, N, K, act);
+  if (rc) return rc;
+  for (const void* p : {x, w, bias, residual, static_cast<const void*>(y), static_cast<const void*>(preact)})
+    if (!aligned16(p)) return TOPK_ERR_UNSUPPORTED;
+  DeviceState* dev = gb300();
+  if (!dev) return TOPK_ERR_NO_DEVICE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const size_t ws = linear_fwd_workspace_bytes(M, N, K, dev->num_sms);
+  void* buf = nullptr;
+  if (ws && !pool_alloc(&buf, ws, st)) return TOPK_ERR_CUDA;
+  const LinearArgs a{x, w, bias, residual, y, preact, M, N, K, act};
+  const int n = linear_fwd(a, buf, dev->num_sms, make_ctl(dev), st);
+  if (buf) cudaFreeAsync(buf, st);
+  return launched(n);
+}
+
+size_t topk_linear_workspace_bytes(int M, int N, int K) {
+  if (validate_linear(M, N, K, TOPK_ACT_NONE) != TOPK_OK) return 0;
+  const DeviceState* dev = device_state();
+  return linear_fwd_workspace_bytes(M, N, K, dev ? dev->num_sms : kAssumedSms);
+}
+
+int topk_linear_bwd(const void* dy, const void* x, const void* w, const void* preact, void* dx, void* dw, void* db, int M,
+                    int N, int K, int act, int grad_dtype, void* stream) {
+  if (!dy || !x || !w || (!dx && !dw && !db)) return TOPK_ERR_INVALID_ARG;
+  const int rc = validate_linear(M, N, K, act);
+  if (rc) return rc;
+  if ((preact != nullptr) != (act != TOPK_ACT_NONE)) return TOPK_ERR_INVALID_ARG;
+  if (grad_dtype != TOPK_F32 && grad_dtype != TOPK_BF16) return TOPK_ERR_INVALID_ARG;
+  for (const void* p : {dy, x, w, preact, static_cast<const void*>(dx), static_cast<const void*>(dw), static_cast<const void*>(db)})
+    if (!aligned16(p)) return TOPK_ERR_UNSUPPORTED;
+  DeviceState* dev = gb300();
+  if (!dev) return TOPK_ERR_NO_DEVICE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  void* buf = nullptr;
+  if (!pool_alloc(&buf, linear_bwd_workspace_bytes(M, N, K, act, dev->num_sms), st)) return TOPK_ERR_CUDA;
+  const LinearBwdArgs a{dy, x, w, preact, dx, dw, db, M, N, K, act, grad_dtype == TOPK_F32};
+  const int n = linear_bwd(a, buf, dev->num_sms, make_ctl(dev), st);
+  cudaFreeAsync(buf, st);
+  return launched(n);
+}
+
+size_t topk_linear_bwd_workspace_bytes(int M, int N, int K, int act) {
+  if (validate_linear(M, N, K, act) != TOPK_OK) return 0;
+  const DeviceState* dev = device_state();
+  return linear_bwd_workspace_bytes(M, N, K, act, dev ? dev->num_sms : kAssumedSms);
+}
+
 int topk_adamw_step(const topk_adamw_tensor* tensors, int count, int param_dtype, int grad_dtype, int state_bits,
                     double beta1, double beta2, double eps, long long step, const float* grad_scale, uint32_t seed,
                     void* stream) {

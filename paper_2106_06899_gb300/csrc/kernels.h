@@ -166,6 +166,34 @@ struct AdamwArgs {
 };
 int adamw_step(const AdamwArgs& a, int num_sms, cudaStream_t st);
 
+// The linear layer (linear.cu): y [M][N] = act(x [M][K] w[N][K]^T + bias) + residual, all bf16;
+// z: the pre-activations, or null.
+constexpr int kActNone = TOPK_ACT_NONE, kActRelu = TOPK_ACT_RELU, kActGelu = TOPK_ACT_GELU, kActSilu = TOPK_ACT_SILU;
+struct LinearArgs {
+  const void* x;
+  const void* w;
+  const void* bias;
+  const void* residual;
+  void* y;
+  void* z;
+  int M, N, K, act;
+};
+struct LinearBwdArgs {
+  const void* dy;
+  const void* x;
+  const void* w;
+  const void* z;
+  void* dx;  // bf16, or null
+  void* dw;  // bf16 or fp32 (grad_f32), or null
+  void* db;
+  int M, N, K, act;
+  bool grad_f32;
+};
+size_t linear_fwd_workspace_bytes(int M, int N, int K, int num_sms);
+size_t linear_bwd_workspace_bytes(int M, int N, int K, int act, int num_sms);
+int linear_fwd(const LinearArgs& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st);
+int linear_bwd(const LinearBwdArgs& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st);
+
 // Driver entry point for cuTensorMapEncodeTiled (resolved once, no libcuda link).
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                    const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,

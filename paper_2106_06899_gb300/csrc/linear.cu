@@ -1,0 +1,668 @@
+// linear.cu -- the linear layer y = act(x W^T + b) + r and its backward pass, on
+// the tensor cores.
+//
+// Three products of one form, D[m, n] = sum_k A(m, k) B(n, k), bf16 operands and fp32
+// sums in TMEM:
+//   forward  D = y  [M, N]: A = x (k contiguous),           B = W (k contiguous)
+//   dx = dz W       [M, K]: A = dz (n, the sum, contiguous), B = W read across its rows
+//   dW = dz^T x     [N, K]: A = dz and B = x read across their rows
+// An operand whose sum index is contiguous is staged K-major, the other kind MN-major
+// (64 x 64 boxes, 128-byte swizzle; the instruction transposes), so no transposed copy
+// is ever made.  dz = dy act'(z) is formed once, as bf16 (its one rounding: the tensor
+// cores take bf16), by a kernel that also adds up db.
+//
+// linear_mma_kernel is persistent, one CTA per SM: a TMA warp, an MMA warp that feeds
+// 128 x BN tiles into one of two TMEM accumulators, and eight epilogue warps that read
+// the other one: bias, activation and residual are applied to the fp32 sums, rounded
+// once, staged in shared memory and stored by TMA, which clips ragged edges.  Few tiles
+// and a long sum (dW, a few hundred tokens) are split along the sum: each part writes
+// fp32 partial tiles, and linear_join_kernel adds them in a fixed order with the same
+// epilogue.  Up to kFewRows tokens (decoding) go to linear_few_kernel, which is
+// bound by reading W once.
+#include <cuda_bf16.h>
+
+#include "kernels.h"
+
+namespace topk {
+
+namespace {
+
+constexpr int BM = 128, BK = 64;
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpiWarps;
+
+template <int BN>
+struct Layout {
+  static constexpr uint32_t A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2;
+  static constexpr uint32_t STAGE = A_BYTES + B_BYTES;
+  static constexpr uint32_t EPI = 4096;  // a warp's 32 rows of 128 bytes
+  static constexpr int S = (232448 - 2048 - kEpiWarps * EPI) / STAGE > 6 ? 6 : (232448 - 2048 - kEpiWarps * EPI) / STAGE;
+  static constexpr size_t OFF_EPI = static_cast<size_t>(S) * STAGE;
+  static constexpr size_t OFF_BAR = OFF_EPI + kEpiWarps * EPI;
+  static constexpr int NBARS = 2 * S + 5;  // full/empty per stage, accumulator full/empty x 2, drain
+  static constexpr size_t BYTES = 1024 + OFF_BAR + NBARS * 8 + 16;
+  static_assert(BYTES <= 232448 && S >= 3, "shared memory");
+};
+
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const DevCtl& ctl, volatile int* abort_flag) {
+  int ok = 0;
+  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity, ctl, abort_flag) ? 1 : 0;
+  return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
+
+__device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity, const DevCtl& ctl) {
+  const unsigned long long t0 = global_ns();
+  while (!mbar_try_wait(bar, parity)) {
+    if (global_ns() - t0 > ctl.wait_limit_ns) {
+      atomicOr(ctl.error, kDevErrTimeout);
+      return;
+    }
+  }
+}
+
+// MN-major tile of 64 x 64 boxes (128-byte rows of 64 MN elements, one row per k): 64-element
+// blocks of MN are 8192 bytes apart, groups of eight k 1024.
+__device__ __forceinline__ uint64_t sdesc_mn128(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(8192 >> 4) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+
+__device__ __forceinline__ void tma_store_3d(const void* map, const void* smem, int c0, int c1, int c2) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(smem_u32(smem)), "r"(c0), "r"(c1), "r"(c2)
+               : "memory");
+}
+
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+__device__ __forceinline__ void unpack8(uint4 u, float (&v)[8]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[2 * e] = __uint_as_float(w[e] << 16), v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+}
+
+__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+
+__device__ __forceinline__ float act_of(float z, int act) {
+  if (act == kActRelu) return z < 0.f ? 0.f : z;  // a NaN stays
+  if (act == kActGelu) return 0.5f * z * (1.f + erff(z * 0.70710678f));
+  if (act == kActSilu) return z * sigmoid(z);
+  return z;
+}
+
+__device__ __forceinline__ float act_slope(float z, int act) {
+  if (act == kActRelu) return z > 0.f ? 1.f : 0.f;
+  if (act == kActGelu) return 0.5f * (1.f + erff(z * 0.70710678f)) + z * 0.39894228f * __expf(-0.5f * z * z);
+  if (act == kActSilu) {
+    const float s = sigmoid(z);
+    return s * (1.f + z * (1.f - s));
+  }
+  return 1.f;
+}
+
+struct Epi {
+  const __nv_bfloat16* bias;      // [N] or null
+  const __nv_bfloat16* residual;  // [M][N] or null
+  int act, keep;                  // keep: also store the pre-activations
+};
+
+// Work units: output tiles in bands of eight row tiles (neighbouring CTAs share rows of A and
+// columns of B in L2), for each part of the sum.
+struct Grid {
+  int m_tiles, n_tiles, parts, k_blocks;
+};
+
+__device__ __forceinline__ void unit_of(const Grid& g, int u, int& mt, int& nt, int& part) {
+  constexpr int kBand = 8;
+  const int tiles = g.m_tiles * g.n_tiles;
+  part = u / tiles;
+  int t = u - part * tiles;
+  const int band = t / (kBand * g.n_tiles);
+  t -= band * kBand * g.n_tiles;
+  const int rows = min(kBand, g.m_tiles - band * kBand);
+  nt = t / rows;
+  mt = band * kBand + t - nt * rows;
+}
+
+// Out: __nv_bfloat16 or float (the result, or a part's partial sums).
+template <int BN, bool A_MN, bool B_MN, typename Out>
+__global__ void __launch_bounds__(kThreads, 1)
+    linear_mma_kernel(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUtensorMap tmb,
+                      const __grid_constant__ CUtensorMap tmo, const __grid_constant__ CUtensorMap tmz, Epi epi, Grid grid, int M,
+                      int N, DevCtl ctl) {
+  using L = Layout<BN>;
+  constexpr int S = L::S;
+  constexpr uint32_t IDESC = idesc_bf16_f32(BM, BN) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
+  constexpr uint32_t TMEM_COLS = 2 * BN <= 128 ? 128 : (2 * BN <= 256 ? 256 : 512);
+
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
+  uint64_t* full = bars;
+  uint64_t* empty = bars + S;
+  uint64_t* acc_full = bars + 2 * S;       // [2]
+  uint64_t* acc_empty = bars + 2 * S + 2;  // [2]
+  uint64_t* drain = bars + 2 * S + 4;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::NBARS);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&acc_full[b], 1);
+      mbar_init(&acc_empty[b], kEpiWarps);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, TMEM_COLS);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int units = grid.m_tiles * grid.n_tiles * grid.parts;
+  auto k_first = [&](int part) { return static_cast<int>(static_cast<long long>(grid.k_blocks) * part / grid.parts); };
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ loads
+    if (lane == 0) {
+      tma_prefetch_desc(&tma);
+      tma_prefetch_desc(&tmb);
+      uint32_t it = 0;
+      bool ok = true;
+      for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
+        int mt, nt, part;
+        unit_of(grid, u, mt, nt, part);
+        for (int kb = k_first(part), end = k_first(part + 1); kb < end; ++kb, ++it) {
+          const int s = it % S;
+          if (!mbar_wait(&empty[s], ((it / S) & 1u) ^ 1u, ctl, abort_flag)) {
+            ok = false;
+            break;
+          }
+          uint8_t* a = smem + static_cast<size_t>(s) * L::STAGE;
+          uint8_t* b = a + L::A_BYTES;
+          mbar_arrive_expect_tx(&full[s], L::STAGE);
+          if constexpr (A_MN) {
+            for (int r = 0; r < BM / 64; ++r) tma_load_3d(a + r * 8192, &tma, &full[s], mt * BM + r * 64, kb * BK, 0);
+          } else {
+            tma_load_3d(a, &tma, &full[s], kb * BK, mt * BM, 0);
+          }
+          if constexpr (B_MN) {
+            for (int r = 0; r < BN / 64; ++r) tma_load_3d(b + r * 8192, &tmb, &full[s], nt * BN + r * 64, kb * BK, 0);
+          } else {
+            tma_load_3d(b, &tmb, &full[s], kb * BK, nt * BN, 0);
+          }
+        }
+      }
+      // every issued copy must land before the CTA exits
+      for (uint32_t back = 1; back <= static_cast<uint32_t>(S) && back <= it; ++back) {
+        const uint32_t t = it - back;
+        drain_wait(&full[t % S], (t / S) & 1u, ctl);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ products
+    if (lane == 0) {
+      uint32_t it = 0, tile = 0;
+      bool ok = true;
+      for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++tile) {
+        int mt, nt, part;
+        unit_of(grid, u, mt, nt, part);
+        const uint32_t buf = tile & 1u;
+        if (!mbar_wait(&acc_empty[buf], ((tile >> 1) & 1u) ^ 1u, ctl, abort_flag)) break;
+        tc_fence_after();
+        const uint32_t acc = tmem_base + buf * BN;
+        const int first = k_first(part), end = k_first(part + 1);
+        for (int kb = first; kb < end; ++kb, ++it) {
+          const int s = it % S;
+          if (!mbar_wait(&full[s], (it / S) & 1u, ctl, abort_flag)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t a = smem_u32(smem + static_cast<size_t>(s) * L::STAGE), b = a + L::A_BYTES;
+#pragma unroll
+          for (int k = 0; k < BK / 16; ++k)
+            mma_bf16_ss(acc, A_MN ? sdesc_mn128(a + k * 2048) : sdesc_k128(a + k * 32),
+                        B_MN ? sdesc_mn128(b + k * 2048) : sdesc_k128(b + k * 32), IDESC, kb > first || k > 0 ? 1u : 0u);
+          mma_commit(&empty[s]);
+        }
+        if (ok) mma_commit(&acc_full[buf]);
+      }
+      // all issued MMAs must complete before TMEM is freed
+      mma_commit(drain);
+      drain_wait(drain, 0, ctl);
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------ epilogue
+    const int quad = warp & 3, half = (warp - 2) >> 2;
+    uint8_t* stage = smem + L::OFF_EPI + static_cast<size_t>(warp - 2) * L::EPI;
+    uint8_t* row_s = stage + lane * 128;
+    constexpr int COLS = sizeof(Out) == 2 ? 64 : 32;  // columns of a staged 128-byte row
+    // Stages 128 bytes a row (sixteen-byte chunk c at c ^ (row & 7)) and stores the 32 rows.
+    auto put = [&](const CUtensorMap& map, const uint32_t (&w)[32], int col, int row0, int part) {
+      if (lane == 0) bulk_wait_read();  // the buffer's previous store has been read
+      __syncwarp();
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        *reinterpret_cast<uint4*>(row_s + ((c ^ (lane & 7)) << 4)) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        tma_store_3d(&map, stage, col, row0, part);
+        bulk_commit();
+      }
+    };
+    uint32_t tile = 0;
+    for (int u = blockIdx.x; u < units; u += gridDim.x, ++tile) {
+      int mt, nt, part;
+      unit_of(grid, u, mt, nt, part);
+      const uint32_t buf = tile & 1u;
+      if (!warp_wait(&acc_full[buf], (tile >> 1) & 1u, ctl, abort_flag)) break;
+      tc_fence_after();
+      const int row0 = mt * BM + quad * 32, row = row0 + lane;
+      const uint32_t taddr = tmem_base + buf * BN + (static_cast<uint32_t>(quad * 32) << 16);
+#pragma unroll 1
+      for (int c = half; c < BN / COLS; c += 2) {
+        const int col = nt * BN + c * COLS;
+        uint32_t w[32];
+        if constexpr (sizeof(Out) == 4) {
+          float v[32];
+          tmem_ld32(taddr + c * COLS, v);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(v[e]);
+          if (row0 < M && col < N) put(tmo, w, col, row0, part);
+        } else {
+          float v[64];
+          tmem_ld64(taddr + c * COLS, v);
+          tmem_wait_ld();
+          if (row0 >= M || col >= N) continue;
+          if (epi.bias) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              if (col + 8 * e < N) {
+                float b[8];
+                unpack8(__ldg(reinterpret_cast<const uint4*>(epi.bias + col) + e), b);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[8 * e + i] += b[i];
+              }
+            }
+          }
+          if (epi.keep) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) w[e] = pack2(v[2 * e], v[2 * e + 1]);
+            put(tmz, w, col, row0, 0);
+          }
+          if (epi.act == kActRelu) {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) v[e] = act_of(v[e], kActRelu);
+          } else if (epi.act == kActGelu) {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) v[e] = act_of(v[e], kActGelu);
+          } else if (epi.act == kActSilu) {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) v[e] = act_of(v[e], kActSilu);
+          }
+          if (epi.residual && row < M) {
+            const uint4* r = reinterpret_cast<const uint4*>(epi.residual + static_cast<size_t>(row) * N + col);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              if (col + 8 * e < N) {
+                float b[8];
+                unpack8(__ldg(r + e), b);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[8 * e + i] += b[i];
+              }
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e) w[e] = pack2(v[2 * e], v[2 * e + 1]);
+          put(tmo, w, col, row0, 0);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&acc_empty[buf]);
+    }
+    if (lane == 0) bulk_wait_all();
+    __syncwarp();
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, TMEM_COLS);
+  }
+}
+
+// Eight neighbouring outputs from their fp32 sums.
+template <typename Out>
+__device__ __forceinline__ void finish8(float (&v)[8], const Epi& epi, Out* out, __nv_bfloat16* z, size_t at, int col) {
+  if (epi.bias) {
+    float b[8];
+    unpack8(__ldg(reinterpret_cast<const uint4*>(epi.bias + col)), b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += b[e];
+  }
+  if (epi.keep)
+    *reinterpret_cast<uint4*>(z + at) = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = act_of(v[e], epi.act);
+  if (epi.residual) {
+    float b[8];
+    unpack8(__ldg(reinterpret_cast<const uint4*>(epi.residual + at)), b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += b[e];
+  }
+  if constexpr (sizeof(Out) == 2) {
+    *reinterpret_cast<uint4*>(out + at) = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+  } else {
+    reinterpret_cast<float4*>(out + at)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(out + at)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+}
+
+// Adds the parts' partial sums [parts][M][N] in order and finishes the outputs.
+template <typename Out>
+__global__ void linear_join_kernel(const float* __restrict__ partial, int parts, long long MN, int N, Epi epi, Out* __restrict__ out,
+                                   __nv_bfloat16* __restrict__ z) {
+  const long long i = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) * 8;
+  if (i >= MN) return;
+  float v[8] = {};
+  for (int p = 0; p < parts; ++p) {
+    const float4* s = reinterpret_cast<const float4*>(partial + static_cast<size_t>(p) * MN + i);
+    const float4 a = s[0], b = s[1];
+    v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w, v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
+  }
+  finish8(v, epi, out, z, static_cast<size_t>(i), static_cast<int>(i % N));
+}
+
+// ------------------------------------------------------------ few rows
+constexpr int kFewRows = 16;
+
+// y for up to MR tokens: a warp takes eight rows of W (one 16-byte output a token), reads each
+// once, 512 bytes at a time, and holds 8 x MR sums a lane; x comes from L1.  The kWarps
+// warps of a block share the sum and are added up in shared memory.
+template <int MR, typename Out>
+__global__ void __launch_bounds__(256) linear_few_kernel(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ w, int M, int N,
+                                                         int K, Epi epi, Out* __restrict__ out, __nv_bfloat16* __restrict__ z) {
+  constexpr int kRows = 8 / (MR > 4 ? 2 : 1);  // rows of W a warp walks at a time
+  constexpr int kWarps = 8;
+  __shared__ float sums[kWarps][MR][8];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n0 = blockIdx.x * 8;
+#pragma unroll
+  for (int pass = 0; pass < 8 / kRows; ++pass) {
+    float acc[kRows][MR] = {};
+    for (int k = (warp * 32 + lane) * 8; k < K; k += kWarps * 256) {
+      uint4 wv[kRows];
+#pragma unroll
+      for (int r = 0; r < kRows; ++r)
+        wv[r] = __ldg(reinterpret_cast<const uint4*>(w + static_cast<size_t>(n0 + pass * kRows + r) * K + k));
+#pragma unroll
+      for (int m = 0; m < MR; ++m) {
+        if (m >= M) break;
+        float xv[8];
+        unpack8(__ldg(reinterpret_cast<const uint4*>(x + static_cast<size_t>(m) * K + k)), xv);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          float wf[8];
+          unpack8(wv[r], wf);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[r][m] = fmaf(xv[e], wf[e], acc[r][m]);
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int m = 0; m < MR; ++m) {
+        float a = acc[r][m];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+        if (lane == 0) sums[warp][m][pass * kRows + r] = a;
+      }
+  }
+  __syncthreads();
+  const int m = threadIdx.x;
+  if (m < M) {
+    float v[8] = {};
+    for (int i = 0; i < kWarps; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += sums[i][m][e];
+    finish8(v, epi, out, z, static_cast<size_t>(m) * N + n0, n0);
+  }
+}
+
+// ------------------------------------------------------------ dz and db
+constexpr int kDzRows = 32;  // rows of a block
+
+// dz = dy act'(z) as bf16 (nothing is written for act none: dz is dy), and the block's sums of its
+// unrounded columns.  A thread takes eight columns of every fourth row.
+__global__ void __launch_bounds__(256) linear_dz_kernel(const __nv_bfloat16* __restrict__ dy, const __nv_bfloat16* __restrict__ z, int M, int N,
+                                                        int act, __nv_bfloat16* __restrict__ dz, float* __restrict__ partial) {
+  __shared__ float sums[4][64 * 8];
+  const int cx = threadIdx.x & 63, ry = threadIdx.x >> 6;
+  const int col = (blockIdx.y * 64 + cx) * 8;
+  const long long m0 = static_cast<long long>(blockIdx.x) * kDzRows;
+  float a[8] = {};
+  if (col < N) {
+    for (int r = ry; r < kDzRows && m0 + r < M; r += 4) {
+      const size_t at = static_cast<size_t>(m0 + r) * N + col;
+      float g[8];
+      unpack8(__ldg(reinterpret_cast<const uint4*>(dy + at)), g);
+      if (act != kActNone) {
+        float zv[8];
+        unpack8(__ldg(reinterpret_cast<const uint4*>(z + at)), zv);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[e] *= act_slope(zv[e], act);
+        *reinterpret_cast<uint4*>(dz + at) = make_uint4(pack2(g[0], g[1]), pack2(g[2], g[3]), pack2(g[4], g[5]), pack2(g[6], g[7]));
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) a[e] += g[e];
+    }
+  }
+  if (!partial) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[ry][cx * 8 + e] = a[e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 512; i += 256)
+    if (blockIdx.y * 512 + i < N)
+      partial[static_cast<size_t>(blockIdx.x) * N + blockIdx.y * 512 + i] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+}
+
+// db[n] = the row blocks' partial sums, in order: 32 columns a block, eight threads each.
+template <typename Out>
+__global__ void linear_db_kernel(const float* __restrict__ partial, int rows, int N, Out* __restrict__ db) {
+  __shared__ float sums[8][33];
+  const int n = blockIdx.x * 32 + threadIdx.x;
+  float a = 0.f;
+  if (n < N)
+    for (int r = threadIdx.y; r < rows; r += 8) a += partial[static_cast<size_t>(r) * N + n];
+  sums[threadIdx.y][threadIdx.x] = a;
+  __syncthreads();
+  if (threadIdx.y == 0 && n < N) {
+    for (int y = 1; y < 8; ++y) a += sums[y][threadIdx.x];
+    if constexpr (sizeof(Out) == 2)
+      db[n] = __float2bfloat16_rn(a);
+    else
+      db[n] = a;
+  }
+}
+
+// ------------------------------------------------------------ host
+bool make_out_map(CUtensorMap* map, const void* base, bool f32, uint64_t cols, uint64_t rows, uint64_t parts) {
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return false;
+  const uint64_t e = f32 ? 4 : 2;
+  cuuint64_t dims[3] = {cols, rows, parts};
+  cuuint64_t strides[2] = {cols * e, cols * rows * e};
+  cuuint32_t box[3] = {f32 ? 32u : 64u, 32, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return enc(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box,
+             estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// How a product is cut: tile width and parts of the sum.  `out_rows` x `out_cols`, summed over `sum`.
+struct Cut {
+  int bn, parts;
+};
+
+Cut cut_of(int out_rows, int out_cols, int sum, int num_sms) {
+  const int mt = (out_rows + BM - 1) / BM, kb = (sum + BK - 1) / BK;
+  Cut best{128, 1};
+  // the time of a wave is that of its tiles; 256-wide tiles read less of A per product
+  double least = 1e30;
+  for (int bn : {256, 128}) {
+    const long long tiles = static_cast<long long>(mt) * ((out_cols + bn - 1) / bn);
+    const double waves = static_cast<double>((tiles + num_sms - 1) / num_sms) * bn * (bn == 128 ? 1.15 : 1.0);
+    if (waves < least) least = waves, best.bn = bn;
+  }
+  const long long tiles = static_cast<long long>(mt) * ((out_cols + best.bn - 1) / best.bn);
+  // a part has at least eight blocks of the sum, so that its loads outlast its partial tile's store
+  if (tiles * 2 <= num_sms) {
+    long long p = num_sms / tiles;
+    if (p > kb / 8) p = kb / 8;
+    best.parts = p < 1 ? 1 : static_cast<int>(p);
+  }
+  return best;
+}
+
+template <int BN, bool A_MN, bool B_MN, typename Out>
+int launch_mma(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to, const CUtensorMap& tz, const Epi& epi, const Grid& g, int rows,
+               int cols, int num_sms, const DevCtl& ctl, cudaStream_t st) {
+  auto kern = linear_mma_kernel<BN, A_MN, B_MN, Out>;
+  constexpr int bytes = static_cast<int>(Layout<BN>::BYTES);
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return -1;
+  const long long units = static_cast<long long>(g.m_tiles) * g.n_tiles * g.parts;
+  kern<<<static_cast<int>(units < num_sms ? units : num_sms), kThreads, bytes, st>>>(ta, tb, to, tz, epi, g, rows, cols, ctl);
+  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+}
+
+// D [rows][cols] = sum over `sum`; a is [rows][sum] or, A_MN, [sum][rows]; b likewise.
+template <bool A_MN, bool B_MN>
+int product(const void* a, const void* b, int rows, int cols, int sum, const Epi& epi, void* out, bool out_f32, void* z, float* partial,
+            int num_sms, const DevCtl& ctl, cudaStream_t st) {
+  const Cut cut = cut_of(rows, cols, sum, num_sms);
+  CUtensorMap ta, tb, to, tz;
+  if (!(A_MN ? make_tmap_bf16_3d(&ta, a, rows, sum, 1, 64) : make_tmap_bf16_3d(&ta, a, sum, rows, 1, BM))) return -1;
+  if (!(B_MN ? make_tmap_bf16_3d(&tb, b, cols, sum, 1, 64) : make_tmap_bf16_3d(&tb, b, sum, cols, 1, cut.bn))) return -1;
+  const bool f32 = out_f32 || cut.parts > 1;
+  if (!make_out_map(&to, cut.parts > 1 ? partial : out, f32, cols, rows, cut.parts)) return -1;
+  tz = to;
+  if (epi.keep && cut.parts == 1 && !make_out_map(&tz, z, false, cols, rows, 1)) return -1;
+  const Grid g{(rows + BM - 1) / BM, (cols + cut.bn - 1) / cut.bn, cut.parts, (sum + BK - 1) / BK};
+  int n;
+  if (cut.bn == 256)
+    n = f32 ? launch_mma<256, A_MN, B_MN, float>(ta, tb, to, tz, epi, g, rows, cols, num_sms, ctl, st)
+            : launch_mma<256, A_MN, B_MN, __nv_bfloat16>(ta, tb, to, tz, epi, g, rows, cols, num_sms, ctl, st);
+  else
+    n = f32 ? launch_mma<128, A_MN, B_MN, float>(ta, tb, to, tz, epi, g, rows, cols, num_sms, ctl, st)
+            : launch_mma<128, A_MN, B_MN, __nv_bfloat16>(ta, tb, to, tz, epi, g, rows, cols, num_sms, ctl, st);
+  if (n < 0 || cut.parts == 1) return n;
+  const long long MN = static_cast<long long>(rows) * cols;
+  const int blocks = static_cast<int>((MN / 8 + 255) / 256);
+  if (out_f32)
+    linear_join_kernel<float><<<blocks, 256, 0, st>>>(partial, cut.parts, MN, cols, epi, static_cast<float*>(out), static_cast<__nv_bfloat16*>(z));
+  else
+    linear_join_kernel<__nv_bfloat16><<<blocks, 256, 0, st>>>(partial, cut.parts, MN, cols, epi, static_cast<__nv_bfloat16*>(out),
+                                                              static_cast<__nv_bfloat16*>(z));
+  return cudaGetLastError() == cudaSuccess ? n + 1 : -1;
+}
+
+size_t partial_bytes(int rows, int cols, int sum, int num_sms) {
+  const Cut c = cut_of(rows, cols, sum, num_sms);
+  return c.parts > 1 ? static_cast<size_t>(c.parts) * rows * cols * sizeof(float) : 0;
+}
+
+size_t round256(size_t b) { return (b + 255) / 256 * 256; }
+
+template <int MR>
+int launch_few(const LinearArgs& a, const Epi& epi, cudaStream_t st) {
+  linear_few_kernel<MR, __nv_bfloat16><<<a.N / 8, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(a.x), static_cast<const __nv_bfloat16*>(a.w), a.M,
+                                                                a.N, a.K, epi, static_cast<__nv_bfloat16*>(a.y), static_cast<__nv_bfloat16*>(a.z));
+  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+}
+
+}  // namespace
+
+size_t linear_fwd_workspace_bytes(int M, int N, int K, int num_sms) { return M <= kFewRows ? 0 : partial_bytes(M, N, K, num_sms); }
+
+int linear_fwd(const LinearArgs& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
+  const Epi epi{static_cast<const __nv_bfloat16*>(a.bias), static_cast<const __nv_bfloat16*>(a.residual), a.act, a.z != nullptr};
+  if (a.M <= 1) return launch_few<1>(a, epi, st);
+  if (a.M <= 2) return launch_few<2>(a, epi, st);
+  if (a.M <= 4) return launch_few<4>(a, epi, st);
+  if (a.M <= 8) return launch_few<8>(a, epi, st);
+  if (a.M <= kFewRows) return launch_few<kFewRows>(a, epi, st);
+  return product<false, false>(a.x, a.w, a.M, a.N, a.K, epi, a.y, false, a.z, static_cast<float*>(workspace), num_sms, ctl, st);
+}
+
+// dz (unless act is none), the row blocks' sums for db, and the larger of the two products' partial sums.
+size_t linear_bwd_workspace_bytes(int M, int N, int K, int act, int num_sms) {
+  const size_t dz = act == kActNone ? 0 : round256(static_cast<size_t>(M) * N * 2);
+  const size_t db = round256(static_cast<size_t>((M + kDzRows - 1) / kDzRows) * N * sizeof(float));
+  const size_t p1 = partial_bytes(M, K, N, num_sms), p2 = partial_bytes(N, K, M, num_sms);
+  return dz + db + (p1 > p2 ? p1 : p2);
+}
+
+int linear_bwd(const LinearBwdArgs& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const size_t dz_bytes = a.act == kActNone ? 0 : round256(static_cast<size_t>(a.M) * a.N * 2);
+  const int row_blocks = (a.M + kDzRows - 1) / kDzRows;
+  float* sums = reinterpret_cast<float*>(ws + dz_bytes);
+  float* partial = reinterpret_cast<float*>(ws + dz_bytes + round256(static_cast<size_t>(row_blocks) * a.N * sizeof(float)));
+  const void* dz = a.act == kActNone ? a.dy : ws;
+  const Epi none{nullptr, nullptr, kActNone, 0};
+  int launches = 0;
+  if (a.act != kActNone || a.db) {
+    linear_dz_kernel<<<dim3(row_blocks, (a.N + 511) / 512), 256, 0, st>>>(static_cast<const __nv_bfloat16*>(a.dy), static_cast<const __nv_bfloat16*>(a.z),
+                                                                          a.M, a.N, a.act, reinterpret_cast<__nv_bfloat16*>(ws), a.db ? sums : nullptr);
+    if (cudaGetLastError() != cudaSuccess) return -1;
+    ++launches;
+  }
+  if (a.db) {
+    if (a.grad_f32)
+      linear_db_kernel<float><<<(a.N + 31) / 32, dim3(32, 8), 0, st>>>(sums, row_blocks, a.N, static_cast<float*>(a.db));
+    else
+      linear_db_kernel<__nv_bfloat16><<<(a.N + 31) / 32, dim3(32, 8), 0, st>>>(sums, row_blocks, a.N, static_cast<__nv_bfloat16*>(a.db));
+    if (cudaGetLastError() != cudaSuccess) return -1;
+    ++launches;
+  }
+  if (a.dx) {
+    const int n = product<false, true>(dz, a.w, a.M, a.K, a.N, none, a.dx, false, nullptr, partial, num_sms, ctl, st);
+    if (n < 0) return -1;
+    launches += n;
+  }
+  if (a.dw) {
+    const int n = product<true, true>(dz, a.x, a.N, a.K, a.M, none, a.dw, a.grad_f32, nullptr, partial, num_sms, ctl, st);
+    if (n < 0) return -1;
+    launches += n;
+  }
+  return launches;
+}
+
+}  // namespace topk

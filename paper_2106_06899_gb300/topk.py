@@ -18,6 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libtopk.so")
 
 TOPK_F32, TOPK_BF16 = 0, 1
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}  # TOPK_ACT_*
 _lock = threading.Lock()
 _lib = None
 
@@ -78,6 +79,12 @@ def lib() -> ctypes.CDLL:
             L.topk_qk_norm_rope_bwd.argtypes = [ctypes.POINTER(_QkArgs), vp, vp, vp, i32, vp, vp, vp, vp]
             L.topk_qk_norm_rope_bwd_workspace_bytes.argtypes = [i32] * 3
             L.topk_qk_norm_rope_bwd_workspace_bytes.restype = sz
+            L.topk_linear_fwd.argtypes = [vp] * 6 + [i32] * 4 + [vp]
+            L.topk_linear_bwd.argtypes = [vp] * 7 + [i32] * 5 + [vp]
+            L.topk_linear_workspace_bytes.argtypes = [i32] * 3
+            L.topk_linear_workspace_bytes.restype = sz
+            L.topk_linear_bwd_workspace_bytes.argtypes = [i32] * 4
+            L.topk_linear_bwd_workspace_bytes.restype = sz
             L.topk_adamw_step.argtypes = [vp, i32, i32, i32, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                           ctypes.c_longlong, vp, ctypes.c_uint32, vp]
             L.topk_check.argtypes = [vp]
@@ -94,7 +101,7 @@ def lib() -> ctypes.CDLL:
                       "topk_last_launch_count",
                       "topk_debug_skip_arrive", "topk_pool_usage", "topk_pool_trim", "topk_attn_bwd",
                       "topk_ffn_bwd", "topk_attn_fwd_masked", "topk_vanilla_attn_fwd", "topk_vanilla_ffn_fwd",
-                      "topk_qk_norm_rope_fwd", "topk_qk_norm_rope_bwd", "topk_adamw_step"):
+                      "topk_qk_norm_rope_fwd", "topk_qk_norm_rope_bwd", "topk_adamw_step", "topk_linear_fwd", "topk_linear_bwd"):
                 getattr(L, f).restype = i32
             _lib = L
     return _lib
@@ -413,6 +420,49 @@ def topk_qk_norm_rope_bwd_workspace_bytes(B, L, d) -> int:
     return int(lib().topk_qk_norm_rope_bwd_workspace_bytes(B, L, d))
 
 
+def _act_code(act: str) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}")
+    return ACTIVATIONS[act]
+
+
+def _linear_check(tensors) -> None:
+    for name, t, shape, dtypes in tensors:
+        if t is not None and (t.dtype not in dtypes or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {list(shape)} tensor of {' or '.join(map(str, dtypes))}")
+
+
+def topk_linear_fwd(x, w, y, bias=None, residual=None, preact=None, act: str = "none", stream=None) -> None:
+    """y = act(x w^T + bias) + residual: x [M,K], w [N,K], bias [N], residual, y and preact (z, written) [M,N], bf16."""
+    (M, K), N, bf = x.shape, w.shape[0], (torch.bfloat16,)
+    _linear_check((("x", x, (M, K), bf), ("w", w, (N, K), bf), ("bias", bias, (N,), bf), ("residual", residual, (M, N), bf),
+                   ("y", y, (M, N), bf), ("preact", preact, (M, N), bf)))
+    rc = lib().topk_linear_fwd(_ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(y), _ptr(preact), M, N, K, _act_code(act),
+                               _stream(stream))
+    _check(rc, "topk_linear_fwd")
+
+
+def topk_linear_bwd(dy, x, w, dx, dw, db, preact=None, act: str = "none", stream=None) -> None:
+    """Gradients of topk_linear_fwd: dx [M,K] bf16, dw [N,K] and db [N] bf16 or fp32 (one dtype); None where not wanted."""
+    (M, K), N, bf = x.shape, w.shape[0], (torch.bfloat16,)
+    grads = [t for t in (dw, db) if t is not None]
+    either = (grads[0].dtype,) if grads and grads[0].dtype in (torch.float32, torch.bfloat16) else (torch.float32, torch.bfloat16)
+    _linear_check((("dy", dy, (M, N), bf), ("x", x, (M, K), bf), ("w", w, (N, K), bf), ("preact", preact, (M, N), bf),
+                   ("dx", dx, (M, K), bf), ("dw", dw, (N, K), either), ("db", db, (N,), either)))
+    code = _dtype_code(grads[0]) if grads else TOPK_BF16
+    rc = lib().topk_linear_bwd(_ptr(dy), _ptr(x), _ptr(w), _ptr(preact), _ptr(dx), _ptr(dw), _ptr(db), M, N, K, _act_code(act), code,
+                               _stream(stream))
+    _check(rc, "topk_linear_bwd")
+
+
+def topk_linear_workspace_bytes(M, N, K) -> int:
+    return int(lib().topk_linear_workspace_bytes(M, N, K))
+
+
+def topk_linear_bwd_workspace_bytes(M, N, K, act: str = "none") -> int:
+    return int(lib().topk_linear_bwd_workspace_bytes(M, N, K, _act_code(act)))
+
+
 def topk_attn_bwd_workspace_bytes(B, H, Lq, Lk, d, topk, dtype) -> int:
     return int(lib().topk_attn_bwd_workspace_bytes(B, H, Lq, Lk, d, topk, dtype))
 
@@ -542,3 +592,22 @@ def qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, **options):
         gq, gk = (torch.empty(d, dtype=torch.float32, device=q.device) for _ in range(2))
     topk_qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, dqkv, gq, gk, **options)
     return dqkv, gq, gk
+
+
+def linear(x, w, bias=None, act: str = "none", residual=None, return_preact: bool = False, stream=None):
+    """act(x w^T + bias) + residual for x [M,K] and w [N,K] (bf16); with return_preact also x w^T + bias, which
+    linear_bwd takes for an activation."""
+    y = torch.empty(x.shape[0], w.shape[0], dtype=x.dtype, device=x.device)
+    z = torch.empty_like(y) if return_preact else None
+    topk_linear_fwd(x, w, y, bias, residual, z, act, stream)
+    return (y, z) if return_preact else y
+
+
+def linear_bwd(dy, x, w, preact=None, act: str = "none", bias: bool = False, need_dx: bool = True, need_dw: bool = True,
+               grad_dtype=torch.bfloat16, stream=None):
+    """Gradients (dx, dw, db) of linear; the residual's is dy.  dw and db are of grad_dtype; None where not wanted."""
+    dx = torch.empty_like(x) if need_dx else None
+    dw = torch.empty(w.shape, dtype=grad_dtype, device=w.device) if need_dw else None
+    db = torch.empty(w.shape[0], dtype=grad_dtype, device=w.device) if bias else None
+    topk_linear_bwd(dy, x, w, dx, dw, db, preact, act, stream)
+    return dx, dw, db

@@ -131,3 +131,44 @@ def test_adamw_binding():
     with pytest.raises(ValueError):
         opt.load_state_dict(optim.AdamW([p], state_bits=8).state_dict())
     assert optim.AdamW([p], state_bits=8).moments(0)[0].shape == p.shape
+
+
+def test_linear_arguments(lib):
+    f, b = lib.topk_linear_fwd, lib.topk_linear_bwd
+
+    def fwd(x=16, w=16, bias=None, res=None, y=16, z=None, M=4, N=16, K=16, act=0):
+        return f(x, w, bias, res, y, z, M, N, K, act, None)
+
+    def bwd(dy=16, x=16, w=16, z=None, dx=16, dw=16, db=16, M=4, N=16, K=16, act=0, dt=1):
+        return b(dy, x, w, z, dx, dw, db, M, N, K, act, dt, None)
+
+    for kw, code in ((dict(x=None), -1), (dict(w=None), -1), (dict(M=0), -1), (dict(N=-8), -1), (dict(K=0), -1), (dict(act=4), -1), (dict(act=-1), -1),
+                     (dict(N=20), -2), (dict(K=12), -2), (dict(x=24), -2), (dict(M=1 << 29), -2)):
+        assert fwd(**kw) == code, kw
+        assert bwd(**kw) == code, kw
+    for kw, code in ((dict(y=None), -1), (dict(bias=24), -2), (dict(res=8), -2), (dict(z=8), -2)):
+        assert fwd(**kw) == code, kw
+    for kw, code in ((dict(dy=None), -1), (dict(dx=None, dw=None, db=None), -1), (dict(z=16), -1), (dict(act=1), -1), (dict(dt=2), -1), (dict(db=8), -2)):
+        assert bwd(**kw) == code, kw
+
+
+def test_linear_scratch():
+    # one wave of tiles or more, or few rows: none; a split sum: parts x outputs in fp32
+    assert T.topk_linear_workspace_bytes(32768, 768, 768) == 0
+    assert T.topk_linear_workspace_bytes(4, 4096, 1024) == 0
+    ws = T.topk_linear_workspace_bytes(64, 512, 4096)
+    assert ws > 0 and ws % (64 * 512 * 4) == 0 and ws <= 160 * 64 * 512 * 4
+    assert T.topk_linear_workspace_bytes(64, 510, 4096) == 0
+    assert T.topk_linear_bwd_workspace_bytes(8192, 4096, 1024, "relu") >= 8192 * 4096 * 2
+    assert T.topk_linear_bwd_workspace_bytes(8192, 4096, 1024, "relu") <= 2 * 8192 * 4096 * 2
+
+
+def test_linear_binding():
+    x, w = torch.zeros(4, 16, dtype=torch.bfloat16), torch.zeros(8, 16, dtype=torch.bfloat16)
+    for bad in (dict(act="tanh"), dict(bias=torch.zeros(8)), dict(residual=torch.zeros(4, 7, dtype=torch.bfloat16))):
+        with pytest.raises(ValueError):
+            T.linear(x, w, **bad)
+    with pytest.raises(ValueError):
+        T.linear(x.float(), w)
+    with pytest.raises(ValueError):
+        T.linear_bwd(x, x, w)
