@@ -539,7 +539,7 @@ int topk_qk_norm_rope_bwd(const topk_qk_args* args, const void* dq, const void* 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   void* buf = nullptr;
   if (p.normalize && (dq_weight || dk_weight) &&
-      !pool_alloc(&buf, static_cast<size_t>(qk_bwd_blocks(p.B, p.L, dev->num_sms)) * 2 * p.d * sizeof(float), st))
+      !pool_alloc(&buf, static_cast<size_t>(qk_bwd_partial_rows(p.B, p.L, p.Hq, p.Hkv, dev->num_sms)) * p.d * sizeof(float), st))
     return TOPK_ERR_CUDA;
   const int n = qk_norm_rope_bwd(p, dq, dk, dv, grad_dtype == TOPK_BF16, dqkv, dq_weight, dk_weight, static_cast<float*>(buf),
                                  dev->num_sms, make_ctl(dev), st);
@@ -643,10 +643,10 @@ int topk_adamw_step(const topk_adamw_tensor* tensors, int count, int param_dtype
   return TOPK_OK;
 }
 
-size_t topk_qk_norm_rope_bwd_workspace_bytes(int B, int L, int d) {
-  if (B <= 0 || L <= 0 || d <= 0 || d % 8 != 0 || d > 256) return 0;
+size_t topk_qk_norm_rope_bwd_workspace_bytes(int B, int L, int Hq, int Hkv, int d) {
+  if (B <= 0 || L <= 0 || Hq <= 0 || Hkv <= 0 || Hq > 65536 || Hkv > 65536 || d <= 0 || d % 8 != 0 || d > 256) return 0;
   const DeviceState* dev = device_state();
-  return static_cast<size_t>(qk_bwd_blocks(B, L, dev ? dev->num_sms : kAssumedSms)) * 2 * d * sizeof(float);
+  return static_cast<size_t>(qk_bwd_partial_rows(B, L, Hq, Hkv, dev ? dev->num_sms : kAssumedSms)) * d * sizeof(float);
 }
 
 namespace {

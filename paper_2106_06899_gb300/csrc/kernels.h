@@ -148,7 +148,7 @@ struct QkArgs {
   int interleaved, normalize, bf16;
   float eps, q_scale;
 };
-int qk_bwd_blocks(int B, int L, int num_sms);  // the backward grid: one partial row of weight gradients each
+int qk_bwd_partial_rows(int B, int L, int Hq, int Hkv, int num_sms);  // rows of d floats in the backward pass's scratch
 int qk_norm_rope_fwd(const QkArgs& p, void* qo, void* ko, void* vo, int cap, const int32_t* start, int num_sms, const DevCtl& ctl,
                      cudaStream_t st);
 int qk_norm_rope_bwd(const QkArgs& p, const void* dq, const void* dk, const void* dv, bool grad_bf16, void* dqkv, float* dqw,

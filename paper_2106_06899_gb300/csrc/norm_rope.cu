@@ -29,6 +29,7 @@ namespace {
 
 constexpr int kWarps = 8;        // tokens per block
 constexpr unsigned kFull = 0xffffffffu;
+constexpr int kBwdBlocksPerSm = 3;
 
 __device__ __forceinline__ void load4(const float* p, float (&v)[4]) {
   const float4 f = *reinterpret_cast<const float4*>(p);
@@ -133,271 +134,324 @@ __device__ __forceinline__ void rotate(float (&a)[4], float (&b)[4], const float
 }
 
 template <typename T>
-__device__ __forceinline__ void load_weight(const void* w, const Lane& l, float (&a)[4], float (&b)[4]) {
+__device__ __forceinline__ void load_weight(const T* w, const Lane& l, float (&a)[4], float (&b)[4]) {
   if (w && l.on) {
-    load4(static_cast<const T*>(w) + l.a, a);
-    load4(static_cast<const T*>(w) + l.b, b);
+    load4(w + l.a, a);
+    load4(w + l.b, b);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) a[e] = b[e] = 1.f;
   }
 }
 
+// A warp's share of a token: `rows` heads of one kind (q, k or v), U x R at most.
+// The groups of a token are q's, then k's, then v's.
+enum Kind { kQ, kK, kV };
+
+struct Group {
+  int kind, h0, rows;
+};
+
+__device__ __forceinline__ Group group_of(const QkArgs& p, int g, int size) {
+  const int nq = (p.Hq + size - 1) / size, nk = (p.Hkv + size - 1) / size;
+  Group o;
+  o.kind = g < nq ? kQ : (g < nq + nk ? kK : kV);
+  const int i = g - (o.kind == kQ ? 0 : (o.kind == kK ? nq : nq + nk));
+  const int heads = o.kind == kQ ? p.Hq : p.Hkv;
+  o.h0 = i * size;
+  o.rows = min(size, heads - o.h0);
+  return o;
+}
+
+// Loads as they lie in memory: a lane holds a row in four registers (bf16), and the loads of
+// all its rows go out before the first is used.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<float> {
+  float4 u;
+  __device__ __forceinline__ void load(const float* p) { u = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void zero() { u = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w; }
+};
+template <>
+struct Raw<__nv_bfloat16> {
+  uint2 u;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void zero() { u = make_uint2(0u, 0u); }
+  __device__ __forceinline__ void get(float (&v)[4]) const {
+    v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xffff0000u);
+    v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xffff0000u);
+  }
+};
+
 template <typename T, int G, int U>
-__global__ void __launch_bounds__(kWarps * 32) qk_fwd_kernel(const __grid_constant__ QkArgs p, T* __restrict__ qo, T* __restrict__ ko,
-                                                            T* __restrict__ vo, int cap, const int32_t* __restrict__ start,
-                                                            int heads_per_item, DevCtl ctl) {
+__global__ void __launch_bounds__(kWarps * 32, 4) qk_fwd_kernel(const __grid_constant__ QkArgs p, T* __restrict__ qo, T* __restrict__ ko,
+                                                               T* __restrict__ vo, int cap, const int32_t* __restrict__ start, DevCtl ctl) {
   constexpr int R = 32 / G;  // rows (heads) of a warp at a time
   const int lane = threadIdx.x & 31, j = lane % G, sub = lane / G;
   const long long token = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
   if (token >= static_cast<long long>(p.B) * p.L) return;
   const int b = static_cast<int>(token / p.L), t = static_cast<int>(token % p.L);
-  const int heads = p.Hq + p.Hkv + (p.v ? p.Hkv : 0);
-  const int h0 = blockIdx.y * heads_per_item, h1 = min(h0 + heads_per_item, heads);
+  const Group g = group_of(p, blockIdx.y, R * U);
   const Lane l = lane_of(p, j);
-  float c[4], s[4], wqa[4], wqb[4], wka[4], wkb[4];
-  load_angles(p, l, j, b, t, ctl, c, s);
-  load_weight<T>(p.q_weight, l, wqa, wqb);
-  load_weight<T>(p.k_weight, l, wka, wkb);
-  // the token's row of the key and value caches
+  const void* in = g.kind == kQ ? p.q : (g.kind == kK ? p.k : p.v);
+  const long long* stride = g.kind == kQ ? p.q_stride : (g.kind == kK ? p.k_stride : p.v_stride);
+  const T* src = static_cast<const T*>(in) + b * stride[0] + t * stride[1] + (g.h0 + sub) * stride[2];
+  const long long step = R * stride[2];
+  Raw<T> ra[U], rb[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (u * R + sub < g.rows && l.on) {
+      ra[u].load(src + u * step + l.a);
+      rb[u].load(src + u * step + l.b);
+    } else {
+      ra[u].zero();
+      rb[u].zero();
+    }
+  }
+  // the output row of the group's first head
+  const int heads = g.kind == kQ ? p.Hq : p.Hkv, rows = g.kind == kQ ? p.L : cap;
   long long row = t;
-  if (start) {
+  if (start && g.kind != kQ) {
     row += __ldg(start + b);
     if (row < 0 || row >= cap) {
       if (lane == 0) atomicOr(ctl.error, kDevErrRange);
-      row = -1;
+      return;
     }
   }
-  const float inv_d = 1.f / p.d;
-  for (int hb = h0; hb < h1; hb += R * U) {
-    float xa[U][4], xb[U][4];
+  T* dst = (g.kind == kQ ? qo : (g.kind == kK ? ko : vo)) + ((static_cast<long long>(b) * heads + g.h0 + sub) * rows + row) * p.d;
+  const long long out_step = static_cast<long long>(R) * rows * p.d;
+  if (g.kind == kV) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int h = hb + u * R + sub;
-      const T* src;
-      if (h < p.Hq)
-        src = static_cast<const T*>(p.q) + b * p.q_stride[0] + t * p.q_stride[1] + h * p.q_stride[2];
-      else if (h < p.Hq + p.Hkv)
-        src = static_cast<const T*>(p.k) + b * p.k_stride[0] + t * p.k_stride[1] + (h - p.Hq) * p.k_stride[2];
-      else
-        src = static_cast<const T*>(p.v) + b * p.v_stride[0] + t * p.v_stride[1] + (h - p.Hq - p.Hkv) * p.v_stride[2];
-      if (h < h1 && l.on) {
-        load4(src + l.a, xa[u]);
-        load4(src + l.b, xb[u]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) xa[u][e] = xb[u][e] = 0.f;
-      }
+      if (u * R + sub >= g.rows || !l.on) continue;
+      *reinterpret_cast<Raw<T>*>(dst + u * out_step + l.a) = ra[u];
+      *reinterpret_cast<Raw<T>*>(dst + u * out_step + l.b) = rb[u];
     }
+    return;
+  }
+  float c[4], s[4], wa[4], wb[4];
+  load_angles(p, l, j, b, t, ctl, c, s);
+  load_weight(static_cast<const T*>(g.kind == kQ ? p.q_weight : p.k_weight), l, wa, wb);
+  const float scale = g.kind == kQ ? p.q_scale : 1.f, inv_d = 1.f / p.d;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = hb + u * R + sub;
-      const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
+  for (int u = 0; u < U; ++u) {
+    float xa[4], xb[4];
+    ra[u].get(xa);
+    rb[u].get(xb);
+    if (p.normalize) {
       float ss = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) ss += xa[u][e] * xa[u][e] + xb[u][e] * xb[u][e];
-      ss = group_sum<G>(ss);
-      if (!is_v) {
-        const float r = p.normalize ? rsqrtf(ss * inv_d + p.eps) : 1.f;
+      for (int e = 0; e < 4; ++e) ss += xa[e] * xa[e] + xb[e] * xb[e];
+      const float r = rsqrtf(group_sum<G>(ss) * inv_d + p.eps);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          xa[u][e] = xa[u][e] * r * (is_q ? wqa[e] : wka[e]);
-          xb[u][e] = xb[u][e] * r * (is_q ? wqb[e] : wkb[e]);
-        }
-        rotate(xa[u], xb[u], c, s, p.interleaved);
-        if (is_q) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) xa[u][e] *= p.q_scale, xb[u][e] *= p.q_scale;
-        }
-      }
-      if (h >= h1 || !l.on) continue;
-      T* dst;
-      if (is_q)
-        dst = qo + ((static_cast<size_t>(b) * p.Hq + h) * p.L + t) * p.d;
-      else if (row < 0)
-        continue;
-      else if (!is_v)
-        dst = ko + ((static_cast<size_t>(b) * p.Hkv + (h - p.Hq)) * cap + row) * p.d;
-      else
-        dst = vo + ((static_cast<size_t>(b) * p.Hkv + (h - p.Hq - p.Hkv)) * cap + row) * p.d;
-      store4(dst + l.a, xa[u]);
-      store4(dst + l.b, xb[u]);
+      for (int e = 0; e < 4; ++e) xa[e] = xa[e] * r * wa[e], xb[e] = xb[e] * r * wb[e];
     }
+    rotate(xa, xb, c, s, p.interleaved);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) xa[e] *= scale, xb[e] *= scale;
+    if (u * R + sub >= g.rows || !l.on) continue;
+    store4(dst + u * out_step + l.a, xa);
+    store4(dst + u * out_step + l.b, xb);
   }
 }
 
-// Backward.  Blocks take tokens in strides of the grid and keep the sums of
-// both weight gradients in registers (eight elements of q's and of k's per
-// lane); each block adds its lanes up in a fixed order and writes one partial
-// row, and qk_bwd_weights_kernel adds the partial rows, so that the result does
-// not depend on the order in which blocks run.
+// Backward.  A block keeps one group of heads and walks over tokens in strides of the grid, so
+// that its lanes sum their eight elements' weight gradient in registers; at the end the
+// block adds its lanes up in a fixed order and writes one partial row.
+// qk_bwd_weights_kernel adds the partial rows: the result does not depend on the order in
+// which blocks run.
 template <typename T, typename GT, int G, int U>
-__global__ void __launch_bounds__(kWarps * 32) qk_bwd_kernel(const __grid_constant__ QkArgs p, const GT* __restrict__ dq,
-                                                            const GT* __restrict__ dk, const GT* __restrict__ dv,
-                                                            T* __restrict__ dqkv, float* __restrict__ partial, DevCtl ctl) {
+__global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm)
+    qk_bwd_kernel(const __grid_constant__ QkArgs p, const GT* __restrict__ dq, const GT* __restrict__ dk, const GT* __restrict__ dv,
+                  T* __restrict__ dqkv, float* __restrict__ partial, DevCtl ctl) {
   constexpr int R = 32 / G;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane % G, sub = lane / G;
-  const int heads = p.Hq + p.Hkv + (dv ? p.Hkv : 0);
+  const int all = p.Hq + (dv ? 2 : 1) * p.Hkv;
   const long long tokens = static_cast<long long>(p.B) * p.L;
   const Lane l = lane_of(p, j);
-  float wqa[4], wqb[4], wka[4], wkb[4];
-  load_weight<T>(p.q_weight, l, wqa, wqb);
-  load_weight<T>(p.k_weight, l, wka, wkb);
-  float gqa[4] = {}, gqb[4] = {}, gka[4] = {}, gkb[4] = {};
-  const float inv_d = 1.f / p.d;
+  const Group g = group_of(p, blockIdx.y, R * U);
+  const int heads = g.kind == kQ ? p.Hq : p.Hkv;
+  const GT* grad = g.kind == kQ ? dq : (g.kind == kK ? dk : dv);
+  const T* in = static_cast<const T*>(g.kind == kQ ? p.q : p.k);
+  const long long* stride = g.kind == kQ ? p.q_stride : p.k_stride;
+  const bool norm = p.normalize && g.kind != kV;
+  float wa[4], wb[4], ga[4] = {}, gb[4] = {};
+  load_weight(static_cast<const T*>(g.kind == kQ ? p.q_weight : p.k_weight), l, wa, wb);
+  const float scale = g.kind == kQ ? p.q_scale : 1.f, inv_d = 1.f / p.d;
   for (long long token = static_cast<long long>(blockIdx.x) * kWarps + warp; token < tokens;
        token += static_cast<long long>(gridDim.x) * kWarps) {
     const int b = static_cast<int>(token / p.L), t = static_cast<int>(token % p.L);
-    float c[4], s[4];
-    load_angles(p, l, j, b, t, ctl, c, s);
+    const GT* gs = grad + ((static_cast<long long>(b) * heads + g.h0 + sub) * p.L + t) * p.d;
+    const long long gstep = static_cast<long long>(R) * p.L * p.d;
+    const T* xs = in + b * stride[0] + t * stride[1] + (g.h0 + sub) * stride[2];
+    Raw<GT> qa[U], qb[U];
+    Raw<T> ra[U], rb[U];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] = -s[e];  // the transpose turns the other way
-    for (int hb = 0; hb < heads; hb += R * U) {
-      float ga[U][4], gb[U][4], xa[U][4], xb[U][4];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = hb + u * R + sub;
-        const GT* gs;
-        const T* xs = nullptr;
-        if (h < p.Hq) {
-          gs = dq + ((static_cast<size_t>(b) * p.Hq + h) * p.L + t) * p.d;
-          xs = static_cast<const T*>(p.q) + b * p.q_stride[0] + t * p.q_stride[1] + h * p.q_stride[2];
-        } else if (h < p.Hq + p.Hkv) {
-          gs = dk + ((static_cast<size_t>(b) * p.Hkv + (h - p.Hq)) * p.L + t) * p.d;
-          xs = static_cast<const T*>(p.k) + b * p.k_stride[0] + t * p.k_stride[1] + (h - p.Hq) * p.k_stride[2];
-        } else {
-          gs = dv + ((static_cast<size_t>(b) * p.Hkv + (h - p.Hq - p.Hkv)) * p.L + t) * p.d;
-        }
-        const bool on = h < heads && l.on;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) ga[u][e] = gb[u][e] = xa[u][e] = xb[u][e] = 0.f;
-        if (on) {
-          load4(gs + l.a, ga[u]);
-          load4(gs + l.b, gb[u]);
-        }
-        if (on && xs && p.normalize) {
-          load4(xs + l.a, xa[u]);
-          load4(xs + l.b, xb[u]);
-        }
+    for (int u = 0; u < U; ++u) {
+      const bool on = u * R + sub < g.rows && l.on;
+      if (on) {
+        qa[u].load(gs + u * gstep + l.a);
+        qb[u].load(gs + u * gstep + l.b);
+      } else {
+        qa[u].zero();
+        qb[u].zero();
       }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = hb + u * R + sub;
-        const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
-        if (!is_v) {
-          rotate(ga[u], gb[u], c, s, p.interleaved);
-          if (is_q) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) ga[u][e] *= p.q_scale, gb[u][e] *= p.q_scale;
-          }
-        }
-        if (p.normalize) {  // values have xa = xb = 0 here and keep their gradients
-          float ss = 0.f, dot = 0.f, ua[4], ub[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            ua[e] = ga[u][e] * (is_q ? wqa[e] : wka[e]);
-            ub[e] = gb[u][e] * (is_q ? wqb[e] : wkb[e]);
-            ss += xa[u][e] * xa[u][e] + xb[u][e] * xb[u][e];
-            dot += ua[e] * xa[u][e] + ub[e] * xb[u][e];
-          }
-          ss = group_sum<G>(ss);
-          dot = group_sum<G>(dot);
-          const float r = rsqrtf(ss * inv_d + p.eps), k3 = r * r * r * dot * inv_d;
-          if (!is_v) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float da = ga[u][e] * xa[u][e] * r, db = gb[u][e] * xb[u][e] * r;
-              gqa[e] += is_q ? da : 0.f, gqb[e] += is_q ? db : 0.f;
-              gka[e] += is_q ? 0.f : da, gkb[e] += is_q ? 0.f : db;
-              ga[u][e] = r * ua[e] - xa[u][e] * k3;
-              gb[u][e] = r * ub[e] - xb[u][e] * k3;
-            }
-          }
-        }
-        if (h >= heads || !l.on) continue;
-        T* dst = dqkv + (token * heads + h) * p.d;
-        store4(dst + l.a, ga[u]);
-        store4(dst + l.b, gb[u]);
+      if (on && norm) {
+        ra[u].load(xs + u * R * stride[2] + l.a);
+        rb[u].load(xs + u * R * stride[2] + l.b);
+      } else {
+        ra[u].zero();
+        rb[u].zero();
       }
     }
+    T* dst = dqkv + (token * all + (g.kind == kQ ? 0 : (g.kind == kK ? p.Hq : p.Hq + p.Hkv)) + g.h0 + sub) * p.d;
+    float c[4], s[4];
+    if (g.kind != kV) load_angles(p, l, j, b, t, ctl, c, s);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float ya[4], yb[4];
+      qa[u].get(ya);
+      qb[u].get(yb);
+      if (g.kind != kV) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ya[e] *= scale, yb[e] *= scale;
+        const float back[4] = {-s[0], -s[1], -s[2], -s[3]};  // the transpose turns the other way
+        rotate(ya, yb, c, back, p.interleaved);
+      }
+      if (norm) {
+        float xa[4], xb[4], ss = 0.f, dot = 0.f;
+        ra[u].get(xa);
+        rb[u].get(xb);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          ss += xa[e] * xa[e] + xb[e] * xb[e];
+          dot += ya[e] * wa[e] * xa[e] + yb[e] * wb[e] * xb[e];
+        }
+        const float r = rsqrtf(group_sum<G>(ss) * inv_d + p.eps), k3 = r * r * r * group_sum<G>(dot) * inv_d;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          ga[e] += ya[e] * xa[e] * r;
+          gb[e] += yb[e] * xb[e] * r;
+          ya[e] = r * (ya[e] * wa[e]) - xa[e] * k3;
+          yb[e] = r * (yb[e] * wb[e]) - xb[e] * k3;
+        }
+      }
+      if (u * R + sub >= g.rows || !l.on) continue;
+      store4(dst + u * R * p.d + l.a, ya);
+      store4(dst + u * R * p.d + l.b, yb);
+    }
   }
-  if (!partial) return;
+  if (!partial || g.kind == kV) return;
   // lanes of one j, then warps, in a fixed order
-  __shared__ float sums[kWarps][2][G][8];
+  __shared__ float sums[kWarps][G][8];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
 #pragma unroll
     for (int o = G; o < 32; o <<= 1) {
-      gqa[e] += __shfl_xor_sync(kFull, gqa[e], o);
-      gqb[e] += __shfl_xor_sync(kFull, gqb[e], o);
-      gka[e] += __shfl_xor_sync(kFull, gka[e], o);
-      gkb[e] += __shfl_xor_sync(kFull, gkb[e], o);
+      ga[e] += __shfl_xor_sync(kFull, ga[e], o);
+      gb[e] += __shfl_xor_sync(kFull, gb[e], o);
     }
-    if (sub == 0) {
-      sums[warp][0][j][e] = gqa[e], sums[warp][0][j][e + 4] = gqb[e];
-      sums[warp][1][j][e] = gka[e], sums[warp][1][j][e + 4] = gkb[e];
-    }
+    if (sub == 0) sums[warp][j][e] = ga[e], sums[warp][j][e + 4] = gb[e];
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * G * 8; i += kWarps * 32) {
-    const int which = i / (G * 8), jj = (i / 8) % G, e = i % 8;
+  for (int i = threadIdx.x; i < G * 8; i += kWarps * 32) {
+    const int jj = i / 8, e = i % 8;
     const Lane o = lane_of(p, jj);
     if (!o.on) continue;
     float a = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) a += sums[w][which][jj][e];
-    partial[(static_cast<size_t>(blockIdx.x) * 2 + which) * p.d + (e < 4 ? o.a + e : o.b + e - 4)] = a;
+    for (int w = 0; w < kWarps; ++w) a += sums[w][jj][e];
+    partial[(static_cast<size_t>(blockIdx.y) * gridDim.x + blockIdx.x) * p.d + (e < 4 ? o.a + e : o.b + e - 4)] = a;
   }
 }
 
-// dw[c] = sum of the blocks' partial rows; one block of 32 x 8 threads takes 32 columns.
-__global__ void qk_bwd_weights_kernel(const float* __restrict__ partial, int blocks, int d, float* __restrict__ dqw,
-                                      float* __restrict__ dkw) {
-  __shared__ float sums[8][33];
-  const int i = blockIdx.x * 32 + threadIdx.x;
+// dw[c] = sum of the partial rows of q's groups (blockIdx.y 0) or k's, in order: 32 columns a block,
+// 32 threads each.
+__global__ void __launch_bounds__(1024) qk_bwd_weights_kernel(const float* __restrict__ partial, int q_rows, int k_rows, int d,
+                                                              float* __restrict__ dqw, float* __restrict__ dkw) {
+  __shared__ float sums[32][33];
+  const int c = blockIdx.x * 32 + threadIdx.x;
+  const int first = blockIdx.y ? q_rows : 0, end = blockIdx.y ? q_rows + k_rows : q_rows;
   float a = 0.f;
-  if (i < 2 * d)
-    for (int b = threadIdx.y; b < blocks; b += 8) a += partial[static_cast<size_t>(b) * 2 * d + i];
+  if (c < d) {
+#pragma unroll 4
+    for (int r = first + threadIdx.y; r < end; r += 32) a += partial[static_cast<size_t>(r) * d + c];
+  }
   sums[threadIdx.y][threadIdx.x] = a;
   __syncthreads();
-  if (threadIdx.y == 0 && i < 2 * d) {
-    for (int y = 1; y < 8; ++y) a += sums[y][threadIdx.x];
-    float* out = i < d ? dqw : dkw;
-    if (out) out[i < d ? i : i - d] = a;
+  if (threadIdx.y == 0 && c < d) {
+    for (int y = 1; y < 32; ++y) a += sums[y][threadIdx.x];
+    float* out = blockIdx.y ? dkw : dqw;
+    if (out) out[c] = a;
   }
 }
 
-constexpr int kBwdBlocksPerSm = 2;
+int groups_of(int heads, int size) { return (heads + size - 1) / size; }
+
+// Rows a lane holds at once: the fewest padded rows over q, k and v, and of those the most (more
+// loads in flight, the token's angles loaded less often).
+int rows_per_lane(const QkArgs& p, int R, int most) {
+  int best = 1, least = 1 << 30;
+  for (int u = 1; u <= most; ++u) {
+    const int rows = (groups_of(p.Hq, R * u) + 2 * groups_of(p.Hkv, R * u)) * u;
+    if (rows <= least) least = rows, best = u;
+  }
+  return best;
+}
+
+template <typename F>
+int by_rows(int u, F f) {
+  switch (u) {
+    case 1: return f(std::integral_constant<int, 1>());
+    case 2: return f(std::integral_constant<int, 2>());
+    case 3: return f(std::integral_constant<int, 3>());
+    default: return f(std::integral_constant<int, 4>());
+  }
+}
 
 template <typename T, int G>
 int launch_fwd(const QkArgs& p, void* qo, void* ko, void* vo, int cap, const int32_t* start, int num_sms, const DevCtl& ctl,
                cudaStream_t st) {
   const long long tokens = static_cast<long long>(p.B) * p.L;
-  const int heads = p.Hq + p.Hkv + (p.v ? p.Hkv : 0);
   constexpr int R = 32 / G;
   const long long blocks = (tokens + kWarps - 1) / kWarps;
-  // few tokens: their heads are shared out until every SM has some
-  int per = heads;
-  while (per > R && blocks * ((heads + per - 1) / per) < 2LL * num_sms) per = (per + 1) / 2;
-  per = (per + R - 1) / R * R;
-  const dim3 grid(static_cast<unsigned>(blocks), (heads + per - 1) / per);
-  qk_fwd_kernel<T, G, 2><<<grid, kWarps * 32, 0, st>>>(p, static_cast<T*>(qo), static_cast<T*>(ko), static_cast<T*>(vo), cap,
-                                                       start, per, ctl);
-  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+  // few tokens: one row a lane, for more warps
+  const int u = blocks < num_sms ? 1 : rows_per_lane(p, R, 4);
+  return by_rows(u, [&](auto n) {
+    constexpr int U = decltype(n)::value;
+    const dim3 grid(static_cast<unsigned>(blocks), groups_of(p.Hq, R * U) + (p.v ? 2 : 1) * groups_of(p.Hkv, R * U));
+    qk_fwd_kernel<T, G, U><<<grid, kWarps * 32, 0, st>>>(p, static_cast<T*>(qo), static_cast<T*>(ko), static_cast<T*>(vo), cap, start, ctl);
+    return cudaGetLastError() == cudaSuccess ? 1 : -1;
+  });
+}
+
+// Blocks that walk over the tokens, for each group.
+int bwd_blocks(int B, int L, int groups, int num_sms) {
+  const long long want = (static_cast<long long>(B) * L + kWarps - 1) / kWarps;
+  const long long most = (static_cast<long long>(num_sms) * kBwdBlocksPerSm + groups - 1) / groups;
+  return static_cast<int>(want < most ? want : most);
 }
 
 template <typename T, typename GT, int G>
 int launch_bwd(const QkArgs& p, const void* dq, const void* dk, const void* dv, void* dqkv, float* dqw, float* dkw,
                float* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
-  const int blocks = qk_bwd_blocks(p.B, p.L, num_sms);
+  constexpr int R = 32 / G;
   const bool weights = p.normalize && (dqw || dkw);
-  qk_bwd_kernel<T, GT, G, 2><<<blocks, kWarps * 32, 0, st>>>(p, static_cast<const GT*>(dq), static_cast<const GT*>(dk),
-                                                             static_cast<const GT*>(dv), static_cast<T*>(dqkv),
-                                                             weights ? workspace : nullptr, ctl);
-  if (cudaGetLastError() != cudaSuccess) return -1;
-  if (!weights) return 1;
-  qk_bwd_weights_kernel<<<(2 * p.d + 31) / 32, dim3(32, 8), 0, st>>>(workspace, blocks, p.d, dqw, dkw);
-  return cudaGetLastError() == cudaSuccess ? 2 : -1;
+  constexpr int kRows = sizeof(T) == 2 ? 2 : 1;  // what 80 registers hold of a row and its gradient
+  return by_rows(rows_per_lane(p, R, kRows), [&](auto n) {
+    constexpr int U = decltype(n)::value < kRows ? decltype(n)::value : kRows;
+    const int nq = groups_of(p.Hq, R * U), nk = groups_of(p.Hkv, R * U), groups = nq + (dv ? 2 : 1) * nk;
+    const int blocks = bwd_blocks(p.B, p.L, groups, num_sms);
+    qk_bwd_kernel<T, GT, G, U><<<dim3(blocks, groups), kWarps * 32, 0, st>>>(p, static_cast<const GT*>(dq), static_cast<const GT*>(dk),
+                                                                            static_cast<const GT*>(dv), static_cast<T*>(dqkv),
+                                                                            weights ? workspace : nullptr, ctl);
+    if (cudaGetLastError() != cudaSuccess) return -1;
+    if (!weights) return 1;
+    qk_bwd_weights_kernel<<<dim3((p.d + 31) / 32, 2), dim3(32, 32), 0, st>>>(workspace, nq * blocks, nk * blocks, p.d, dqw, dkw);
+    return cudaGetLastError() == cudaSuccess ? 2 : -1;
+  });
 }
 
 template <typename F>
@@ -412,9 +466,12 @@ int by_lanes(int d, F f) {
 
 }  // namespace
 
-int qk_bwd_blocks(int B, int L, int num_sms) {
-  const long long want = (static_cast<long long>(B) * L + kWarps - 1) / kWarps, most = static_cast<long long>(num_sms) * kBwdBlocksPerSm;
-  return static_cast<int>(want < most ? want : most);
+// Partial rows of weight gradients: at most one for each block of a full grid and one more for each
+// group, or one for each eight tokens and head.
+int qk_bwd_partial_rows(int B, int L, int Hq, int Hkv, int num_sms) {
+  const long long heads = static_cast<long long>(Hq) + Hkv, full = static_cast<long long>(num_sms) * kBwdBlocksPerSm + heads;
+  const long long few = (static_cast<long long>(B) * L + kWarps - 1) / kWarps * heads;
+  return static_cast<int>(few < full ? few : full);
 }
 
 int qk_norm_rope_fwd(const QkArgs& p, void* qo, void* ko, void* vo, int cap, const int32_t* start, int num_sms, const DevCtl& ctl,

@@ -77,7 +77,7 @@ def lib() -> ctypes.CDLL:
             L.topk_ffn_bwd_workspace_bytes.restype = sz
             L.topk_qk_norm_rope_fwd.argtypes = [ctypes.POINTER(_QkArgs), vp, vp, vp, i32, vp, vp]
             L.topk_qk_norm_rope_bwd.argtypes = [ctypes.POINTER(_QkArgs), vp, vp, vp, i32, vp, vp, vp, vp]
-            L.topk_qk_norm_rope_bwd_workspace_bytes.argtypes = [i32] * 3
+            L.topk_qk_norm_rope_bwd_workspace_bytes.argtypes = [i32] * 5
             L.topk_qk_norm_rope_bwd_workspace_bytes.restype = sz
             L.topk_linear_fwd.argtypes = [vp] * 6 + [i32] * 4 + [vp]
             L.topk_linear_bwd.argtypes = [vp] * 7 + [i32] * 5 + [vp]
@@ -416,8 +416,8 @@ def topk_qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, dqkv, dq_weight, dk_weight
     _check(rc, "topk_qk_norm_rope_bwd")
 
 
-def topk_qk_norm_rope_bwd_workspace_bytes(B, L, d) -> int:
-    return int(lib().topk_qk_norm_rope_bwd_workspace_bytes(B, L, d))
+def topk_qk_norm_rope_bwd_workspace_bytes(B, L, Hq, Hkv, d) -> int:
+    return int(lib().topk_qk_norm_rope_bwd_workspace_bytes(B, L, Hq, Hkv, d))
 
 
 def _act_code(act: str) -> int:

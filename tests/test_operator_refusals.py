@@ -53,9 +53,9 @@ def test_qk_outputs(lib):
     assert b(ref, 16, 16, 16, 3, 16, 16, 16, None) == -1
     assert b(ctypes.byref(_qk(dtype=0)), 16, 16, 16, 1, 16, 16, 16, None) == -2
     assert b(ref, 16, 16, 24, 0, 16, 16, 16, None) == -2
-    assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 100, 64) == 13 * 2 * 64 * 4
-    assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 1 << 20, 64) <= 2 * 160 * 2 * 64 * 4
-    assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 100, 60) == 0
+    assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 100, 2, 1, 64) == 13 * 3 * 64 * 4
+    assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 1 << 20, 32, 8, 64) <= (4 * 160 + 40) * 64 * 4
+    assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 100, 2, 1, 60) == 0
 
 
 def test_qk_binding_shapes():
