@@ -302,7 +302,7 @@ int topk_qk_norm_rope_fwd(const topk_qk_args* args, void* q_out, void* k_out, vo
  *   dqkv       : [B, L, Hq + 2 Hkv (Hq + Hkv without dv), d] of `dtype`: q's heads, k's, v's.
  *   dq_weight, dk_weight: [d] fp32 or NULL; written only if normalize.  Blocks add up in a
  *                fixed order: two runs give the same bits.
- *   Scratch: topk_qk_norm_rope_bwd_workspace_bytes(), at most d floats for each of three blocks per
+ *   Scratch: topk_qk_norm_rope_bwd_workspace_bytes(), at most d floats for each of eight blocks per
  *   SM and for each head, from the library's pool.
  */
 int topk_qk_norm_rope_bwd(const topk_qk_args* args, const void* dq, const void* dk, const void* dv, int grad_dtype,

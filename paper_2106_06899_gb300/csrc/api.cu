@@ -478,7 +478,8 @@ int make_qk(const topk_qk_args* a, bool with_v, QkArgs* p) {
   }
   if (2 * sum != a->rot) return TOPK_ERR_INVALID_ARG;
   if (a->d % 8 != 0 || a->d > 256 || a->rot % 8 != 0) return TOPK_ERR_UNSUPPORTED;
-  if (a->Hq > 65536 || a->Hkv > 65536 || static_cast<long long>(a->B) * a->L > (1ll << 33)) return TOPK_ERR_UNSUPPORTED;
+  if (a->Hq > 65536 || a->Hkv > 65536 || static_cast<long long>(a->B) * a->L > (1ll << 30))
+    return TOPK_ERR_UNSUPPORTED;
   for (int x = 0; x < 3; ++x) {
     if (a->q_stride[x] < 0 || a->k_stride[x] < 0 || (with_v && a->v_stride[x] < 0)) return TOPK_ERR_INVALID_ARG;
     if (a->q_stride[x] % 4 || a->k_stride[x] % 4 || (with_v && a->v_stride[x] % 4)) return TOPK_ERR_UNSUPPORTED;

@@ -9,16 +9,17 @@
 // with cos/sin from row pos[axis(i)][b, t] of fp32 tables; pair i is
 // (n_i, n_{i + rot/2}), or (n_2i, n_2i+1) when interleaved.  Backward, from the
 // gradient of the outputs (R orthogonal, so its transpose undoes it):
-//   g = R^T dout,  dw += g x r,  u = g w,  dx = r u - x r^3 mean(u x).
+//   g = R^T dout,  dw += g x r,  u = g w,  dx = r (u - x r^2 mean(u x)).
 //
-// Every element is read once and written once and costs a few FMAs: the kernels
-// are bound by HBM, so they are laid out for coalesced 128-byte rows and loads
-// in flight.  G = d / 8 lanes (rounded up to a power of two) own a row, eight
-// elements each, chosen so that both members of a pair sit in one lane: the
-// rotation needs no exchange, and the norm one butterfly over the G lanes.  A
-// warp takes one token and walks over its heads, so the token's cos and sin are
-// loaded once into registers and serve every head; the warps of a block take
-// neighbouring tokens, whose rows of a head are neighbours in the output.
+// Every element is read once and written once: the floor is HBM's.  G = d / 8 lanes
+// (rounded up to a power of two) own a row, eight elements each, chosen so that both
+// members of a pair sit in one lane: the rotation needs no exchange, and the norm one
+// butterfly over the G lanes.  A warp takes some heads of one kind (q, k or v) of one
+// token, with all their loads in flight at once, and the token's angles serve them all;
+// the warps of a block take neighbouring tokens, whose rows of a head are neighbours in the
+// output.  What is left beside HBM is the chain position -> table row -> product and the
+// issue of some hundred instructions a row: positions go out before anything else and are
+// checked when they are used, and products run in pairs (f32x2).
 #include <cuda_bf16.h>
 
 #include "kernels.h"
@@ -27,30 +28,42 @@ namespace topk {
 
 namespace {
 
-constexpr int kWarps = 8;        // tokens per block
+constexpr int kWarps = 8;  // tokens of a block at a time
 constexpr unsigned kFull = 0xffffffffu;
-constexpr int kBwdBlocksPerSm = 3;
+// Measured on 65,536 tokens x 36 heads of 64 (bf16) forward, and 32,768 x 48 heads of 128 (fp32 gradients)
+// backward: 119 and 265 us with these (5.2 and 5.6 TB/s, 77 and 82 % of a copy's rate).  More
+// blocks per SM spill registers (151 and 386 us); two rows a lane in place of four in the backward pass reload the
+// angles twice as often (302 us); blocks of a single token (no walk) wait for position and table in turn (135 and 519 us).
+constexpr int kFwdBlocksPerSm = 4, kBwdBlocksPerSm = 2;
+constexpr int kRowsPerLane = 4;  // at most, held at once; in fp32 two forward and one backward
+constexpr int kWaves = 4;        // blocks for each place on the GPU: values cost less than queries, and are not waited for
 
 __device__ __forceinline__ void load4(const float* p, float (&v)[4]) {
   const float4 f = *reinterpret_cast<const float4*>(p);
   v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
 }
 
-__device__ __forceinline__ void load4(const __nv_bfloat16* p, float (&v)[4]) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xffff0000u);
-  v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xffff0000u);
+// Two fp32 values in a 64-bit register pair: one instruction for two products.
+struct F2 {
+  unsigned long long v;
+};
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+  return r;
 }
-
-__device__ __forceinline__ void store4(float* p, const float (&v)[4]) {
-  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
 }
-
-// the one rounding of a result to bf16, to nearest
-__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&v)[4]) {
-  const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
-  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
 }
+__device__ __forceinline__ float lo(F2 a) { return __uint_as_float(static_cast<uint32_t>(a.v)); }
+__device__ __forceinline__ float hi(F2 a) { return __uint_as_float(static_cast<uint32_t>(a.v >> 32)); }
 
 template <int G>
 __device__ __forceinline__ float group_sum(float s) {
@@ -64,8 +77,15 @@ __device__ __forceinline__ float group_sum(float s) {
 // unrotated tail) they are neighbours.
 struct Lane {
   int a, b;
+  int axis, split;  // the axis of its first pair, and how many of its four pairs (or more) are on it
   bool on, rotated;
 };
+
+__device__ __forceinline__ int axis_of(const QkArgs& p, int pair) {
+  int axis = 0;
+  for (int x = 0; x + 1 < p.axes; ++x) axis += pair >= p.bound[x];
+  return axis;
+}
 
 __device__ __forceinline__ Lane lane_of(const QkArgs& p, int j) {
   Lane l;
@@ -74,78 +94,172 @@ __device__ __forceinline__ Lane lane_of(const QkArgs& p, int j) {
   const bool half = l.rotated && !p.interleaved;
   l.a = half ? 4 * j : 8 * j;
   l.b = half ? p.rot / 2 + 4 * j : 8 * j + 4;
+  l.axis = axis_of(p, 4 * j);
+  l.split = p.positions && p.axes > 1 ? p.bound[l.axis] - 4 * j : 4;
   return l;
 }
 
-// cos and sin of the lane's four pairs 4j .. 4j + 3 for token (b, t); identity
-// where the lane does not rotate.  A position outside the tables is reported
-// and clamped.
-__device__ __forceinline__ void load_angles(const QkArgs& p, const Lane& l, int j, int b, int t, const DevCtl& ctl,
-                                            float (&c)[4], float (&s)[4]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) c[e] = 1.f, s[e] = 0.f;
-  if (!l.rotated) return;
-  const int half = p.rot / 2;
-  int row[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    int axis = 0;
-    for (int x = 0; x + 1 < p.axes; ++x) axis += 4 * j + e >= p.bound[x];
-    int pos = p.positions ? __ldg(p.positions + (static_cast<size_t>(axis) * p.B + b) * p.L + t) : t;
-    if (pos < 0 || pos >= p.table_rows) {
-      atomicOr(ctl.error, kDevErrRange);
-      pos = pos < 0 ? 0 : p.table_rows - 1;
-    }
-    row[e] = pos;
+// A lane's eight values of a row: [a, a + 4) in x[0], x[1] and [b, b + 4) in x[2], x[3].
+struct Eight {
+  F2 x[4];
+};
+
+// The same as they lie in memory: a bf16 row takes half the registers while it is in flight.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p, const Lane& l) {
+    a = *reinterpret_cast<const float4*>(p + l.a);
+    b = *reinterpret_cast<const float4*>(p + l.b);
   }
-  if (row[0] == row[3] && row[0] == row[1] && row[0] == row[2]) {
-    load4(p.cos + static_cast<size_t>(row[0]) * half + 4 * j, c);
-    load4(p.sin + static_cast<size_t>(row[0]) * half + 4 * j, s);
-  } else {
+  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ Eight get() const { return {f2(a.x, a.y), f2(a.z, a.w), f2(b.x, b.y), f2(b.z, b.w)}; }
+  __device__ __forceinline__ void set(const Eight& v) {
+    a = make_float4(lo(v.x[0]), hi(v.x[0]), lo(v.x[1]), hi(v.x[1]));
+    b = make_float4(lo(v.x[2]), hi(v.x[2]), lo(v.x[3]), hi(v.x[3]));
+  }
+  __device__ __forceinline__ void store(float* p, const Lane& l) const {
+    *reinterpret_cast<float4*>(p + l.a) = a;
+    *reinterpret_cast<float4*>(p + l.b) = b;
+  }
+};
+template <>
+struct Raw<__nv_bfloat16> {
+  uint2 a, b;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, const Lane& l) {
+    a = *reinterpret_cast<const uint2*>(p + l.a);
+    b = *reinterpret_cast<const uint2*>(p + l.b);
+  }
+  __device__ __forceinline__ void zero() { a = b = make_uint2(0u, 0u); }
+  static __device__ __forceinline__ F2 wide(uint32_t u) { return f2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)); }
+  // the one rounding of a result, to nearest
+  static __device__ __forceinline__ uint32_t narrow(F2 v) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo(v), hi(v));
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  __device__ __forceinline__ Eight get() const { return {wide(a.x), wide(a.y), wide(b.x), wide(b.y)}; }
+  __device__ __forceinline__ void set(const Eight& v) {
+    a = make_uint2(narrow(v.x[0]), narrow(v.x[1]));
+    b = make_uint2(narrow(v.x[2]), narrow(v.x[3]));
+  }
+  __device__ __forceinline__ void store(__nv_bfloat16* p, const Lane& l) const {
+    *reinterpret_cast<uint2*>(p + l.a) = a;
+    *reinterpret_cast<uint2*>(p + l.b) = b;
+  }
+};
+
+// The positions of the lane's four pairs 4j .. 4j + 3 for token (b, t), as they are given.  The four lie on one axis, or,
+// where an axis ends among them, on two; NARROW: on up to four.  Nothing here may wait for the loads, not even a
+// copy: they go out a token ahead.
+template <bool NARROW>
+struct Positions {
+  int row[NARROW ? 4 : 2];
+  __device__ __forceinline__ void load(const QkArgs& p, const Lane& l, int j, int b, int t) {
+    if (!l.rotated) return;
+    if (!p.positions) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      c[e] = __ldg(p.cos + static_cast<size_t>(row[e]) * half + 4 * j + e);
-      s[e] = __ldg(p.sin + static_cast<size_t>(row[e]) * half + 4 * j + e);
+      for (int& r : row) r = t;
+      return;
     }
+    const int32_t* at = p.positions + static_cast<size_t>(b) * p.L + t;
+    const size_t axis = static_cast<size_t>(p.B) * p.L;
+    if constexpr (NARROW) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) row[e] = __ldg(at + axis_of(p, 4 * j + e) * axis);
+    } else {
+      row[0] = __ldg(at + l.axis * axis);
+      if (l.split < 4) row[1] = __ldg(at + axis_of(p, 4 * j + 3) * axis);
+    }
+  }
+};
+
+// The angles of a lane's four pairs; minus the sines too, which a paired product cannot negate.
+struct Angles {
+  F2 c[2], s[2], m[2];
+};
+
+// cos and sin, times `scale`, of the four pairs; the scale alone where the lane does not rotate.  A
+// position outside the tables is reported and clamped.
+template <bool NARROW>
+__device__ __forceinline__ void load_angles(const QkArgs& p, const Lane& l, int j, const Positions<NARROW>& at, float scale,
+                                            const DevCtl& ctl, Angles& t) {
+  float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (l.rotated) {
+    const int half = p.rot / 2, last = p.table_rows - 1;
+    bool out = false;
+    auto inside = [&](int row) {
+      const int r = min(max(row, 0), last);
+      out |= r != row;
+      return static_cast<size_t>(r) * half + 4 * j;
+    };
+    if constexpr (NARROW) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const size_t r = inside(at.row[e]) + e;
+        c[e] = __ldg(p.cos + r);
+        s[e] = __ldg(p.sin + r);
+      }
+    } else {
+      const size_t r = inside(at.row[0]);
+      load4(p.cos + r, c);
+      load4(p.sin + r, s);
+      if (l.split < 4) {
+        const size_t r1 = inside(at.row[1]);
+        float c1[4], s1[4];
+        load4(p.cos + r1, c1);
+        load4(p.sin + r1, s1);
+#pragma unroll
+        for (int e = 1; e < 4; ++e)
+          if (e >= l.split) c[e] = c1[e], s[e] = s1[e];
+      }
+    }
+    if (out) atomicOr(ctl.error, kDevErrRange);
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    t.c[e] = f2(c[2 * e] * scale, c[2 * e + 1] * scale);
+    t.s[e] = f2(s[2 * e] * scale, s[2 * e + 1] * scale);
+    t.m[e] = f2(-s[2 * e] * scale, -s[2 * e + 1] * scale);
   }
 }
 
-// Rotates the lane's eight values by (c, s) in place.
-__device__ __forceinline__ void rotate(float (&a)[4], float (&b)[4], const float (&c)[4], const float (&s)[4],
-                                       bool interleaved) {
+// Turns the pairs by their angles, or back by the transpose (the other sign of the sines).
+template <bool BACK>
+__device__ __forceinline__ void rotate(Eight& v, const Angles& t, bool interleaved) {
   if (!interleaved) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float x = a[e], y = b[e];
-      a[e] = x * c[e] - y * s[e];
-      b[e] = y * c[e] + x * s[e];
+    for (int e = 0; e < 2; ++e) {
+      const F2 a = v.x[e], b = v.x[e + 2];
+      v.x[e] = fma2(b, BACK ? t.s[e] : t.m[e], mul2(a, t.c[e]));
+      v.x[e + 2] = fma2(a, BACK ? t.m[e] : t.s[e], mul2(b, t.c[e]));
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float x = a[2 * e], y = a[2 * e + 1];
-      a[2 * e] = x * c[e] - y * s[e];
-      a[2 * e + 1] = y * c[e] + x * s[e];
-      x = b[2 * e], y = b[2 * e + 1];
-      b[2 * e] = x * c[e + 2] - y * s[e + 2];
-      b[2 * e + 1] = y * c[e + 2] + x * s[e + 2];
+    for (int e = 0; e < 4; ++e) {
+      const float x = lo(v.x[e]), y = hi(v.x[e]);
+      const float c = e & 1 ? hi(t.c[e / 2]) : lo(t.c[e / 2]), s = e & 1 ? hi(t.s[e / 2]) : lo(t.s[e / 2]);
+      v.x[e] = BACK ? f2(x * c + y * s, y * c - x * s) : f2(x * c - y * s, y * c + x * s);
     }
   }
 }
 
 template <typename T>
-__device__ __forceinline__ void load_weight(const T* w, const Lane& l, float (&a)[4], float (&b)[4]) {
-  if (w && l.on) {
-    load4(w + l.a, a);
-    load4(w + l.b, b);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) a[e] = b[e] = 1.f;
-  }
+__device__ __forceinline__ Eight load_weight(const void* w, const Lane& l) {
+  if (!w || !l.on) return {f2(1.f, 1.f), f2(1.f, 1.f), f2(1.f, 1.f), f2(1.f, 1.f)};
+  Raw<T> r;
+  r.load(static_cast<const T*>(w), l);
+  return r.get();
 }
 
-// A warp's share of a token: `rows` heads of one kind (q, k or v), U x R at most.
-// The groups of a token are q's, then k's, then v's.
+__device__ __forceinline__ float dot8(const Eight& a, const Eight& b) {
+  const F2 s = fma2(a.x[0], b.x[0], mul2(a.x[1], b.x[1])), t = fma2(a.x[2], b.x[2], mul2(a.x[3], b.x[3]));
+  return (lo(s) + hi(s)) + (lo(t) + hi(t));
+}
+
+// A warp's share of a token: `rows` heads of one kind from h0 on, U x R at most.  The groups of a
+// token are q's, then k's, then v's.
 enum Kind { kQ, kK, kV };
 
 struct Group {
@@ -157,103 +271,73 @@ __device__ __forceinline__ Group group_of(const QkArgs& p, int g, int size) {
   Group o;
   o.kind = g < nq ? kQ : (g < nq + nk ? kK : kV);
   const int i = g - (o.kind == kQ ? 0 : (o.kind == kK ? nq : nq + nk));
-  const int heads = o.kind == kQ ? p.Hq : p.Hkv;
   o.h0 = i * size;
-  o.rows = min(size, heads - o.h0);
+  o.rows = min(size, (o.kind == kQ ? p.Hq : p.Hkv) - o.h0);
   return o;
 }
 
-// Loads as they lie in memory: a lane holds a row in four registers (bf16), and the loads of
-// all its rows go out before the first is used.
-template <typename T>
-struct Raw;
-template <>
-struct Raw<float> {
-  float4 u;
-  __device__ __forceinline__ void load(const float* p) { u = *reinterpret_cast<const float4*>(p); }
-  __device__ __forceinline__ void zero() { u = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w; }
-};
-template <>
-struct Raw<__nv_bfloat16> {
-  uint2 u;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = *reinterpret_cast<const uint2*>(p); }
-  __device__ __forceinline__ void zero() { u = make_uint2(0u, 0u); }
-  __device__ __forceinline__ void get(float (&v)[4]) const {
-    v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xffff0000u);
-    v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xffff0000u);
-  }
-};
-
-template <typename T, int G, int U>
-__global__ void __launch_bounds__(kWarps * 32, 4) qk_fwd_kernel(const __grid_constant__ QkArgs p, T* __restrict__ qo, T* __restrict__ ko,
-                                                               T* __restrict__ vo, int cap, const int32_t* __restrict__ start, DevCtl ctl) {
+template <typename T, int G, int U, bool NARROW>
+__global__ void __launch_bounds__(kWarps * 32, kFwdBlocksPerSm)
+    qk_fwd_kernel(const __grid_constant__ QkArgs p, T* __restrict__ qo, T* __restrict__ ko, T* __restrict__ vo, int cap,
+                  const int32_t* __restrict__ start, DevCtl ctl) {
   constexpr int R = 32 / G;  // rows (heads) of a warp at a time
   const int lane = threadIdx.x & 31, j = lane % G, sub = lane / G;
-  const long long token = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  if (token >= static_cast<long long>(p.B) * p.L) return;
-  const int b = static_cast<int>(token / p.L), t = static_cast<int>(token % p.L);
+  const unsigned tokens = static_cast<unsigned>(p.B) * p.L, stride = gridDim.x * kWarps;
+  unsigned token = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  if (token >= tokens) return;
   const Group g = group_of(p, blockIdx.y, R * U);
   const Lane l = lane_of(p, j);
-  const void* in = g.kind == kQ ? p.q : (g.kind == kK ? p.k : p.v);
-  const long long* stride = g.kind == kQ ? p.q_stride : (g.kind == kK ? p.k_stride : p.v_stride);
-  const T* src = static_cast<const T*>(in) + b * stride[0] + t * stride[1] + (g.h0 + sub) * stride[2];
-  const long long step = R * stride[2];
-  Raw<T> ra[U], rb[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (u * R + sub < g.rows && l.on) {
-      ra[u].load(src + u * step + l.a);
-      rb[u].load(src + u * step + l.b);
-    } else {
-      ra[u].zero();
-      rb[u].zero();
-    }
-  }
-  // the output row of the group's first head
+  const bool turns = g.kind != kV;
+  Positions<NARROW> at;
+  if (turns) at.load(p, l, j, token / p.L, token % p.L);
+  const long long* step = g.kind == kQ ? p.q_stride : (g.kind == kK ? p.k_stride : p.v_stride);
+  const T* in = static_cast<const T*>(g.kind == kQ ? p.q : (g.kind == kK ? p.k : p.v)) + (g.h0 + sub) * step[2];
   const int heads = g.kind == kQ ? p.Hq : p.Hkv, rows = g.kind == kQ ? p.L : cap;
-  long long row = t;
-  if (start && g.kind != kQ) {
-    row += __ldg(start + b);
-    if (row < 0 || row >= cap) {
-      if (lane == 0) atomicOr(ctl.error, kDevErrRange);
-      return;
-    }
-  }
-  T* dst = (g.kind == kQ ? qo : (g.kind == kK ? ko : vo)) + ((static_cast<long long>(b) * heads + g.h0 + sub) * rows + row) * p.d;
+  T* const out = (g.kind == kQ ? qo : (g.kind == kK ? ko : vo)) + static_cast<long long>(g.h0 + sub) * rows * p.d;
   const long long out_step = static_cast<long long>(R) * rows * p.d;
-  if (g.kind == kV) {
+  const float scale = g.kind == kQ ? p.q_scale : 1.f, inv_d = 1.f / p.d;
+  for (; token < tokens; token += stride) {
+    const int b = token / p.L, t = token % p.L;
+    const T* src = in + b * step[0] + t * step[1];
+    Raw<T> x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (u * R + sub >= g.rows || !l.on) continue;
-      *reinterpret_cast<Raw<T>*>(dst + u * out_step + l.a) = ra[u];
-      *reinterpret_cast<Raw<T>*>(dst + u * out_step + l.b) = rb[u];
+      if (u * R + sub < g.rows && l.on)
+        x[u].load(src + u * R * step[2], l);
+      else
+        x[u].zero();
     }
-    return;
-  }
-  float c[4], s[4], wa[4], wb[4];
-  load_angles(p, l, j, b, t, ctl, c, s);
-  load_weight(static_cast<const T*>(g.kind == kQ ? p.q_weight : p.k_weight), l, wa, wb);
-  const float scale = g.kind == kQ ? p.q_scale : 1.f, inv_d = 1.f / p.d;
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    float xa[4], xb[4];
-    ra[u].get(xa);
-    rb[u].get(xb);
-    if (p.normalize) {
-      float ss = 0.f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) ss += xa[e] * xa[e] + xb[e] * xb[e];
-      const float r = rsqrtf(group_sum<G>(ss) * inv_d + p.eps);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) xa[e] = xa[e] * r * wa[e], xb[e] = xb[e] * r * wb[e];
+    // the output row of the group's first head
+    long long to = t;
+    if (start && g.kind != kQ) {
+      to += __ldg(start + b);
+      if (to < 0 || to >= cap) {
+        if (lane == 0) atomicOr(ctl.error, kDevErrRange);
+        to = -1;
+      }
     }
-    rotate(xa, xb, c, s, p.interleaved);
+    if (turns) {
+      Angles turn;
+      load_angles(p, l, j, at, scale, ctl, turn);
+      if (token + stride < tokens) at.load(p, l, j, (token + stride) / p.L, (token + stride) % p.L);
+      const Eight w = load_weight<T>(g.kind == kQ ? p.q_weight : p.k_weight, l);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) xa[e] *= scale, xb[e] *= scale;
-    if (u * R + sub >= g.rows || !l.on) continue;
-    store4(dst + u * out_step + l.a, xa);
-    store4(dst + u * out_step + l.b, xb);
+      for (int u = 0; u < U; ++u) {
+        Eight v = x[u].get();
+        if (p.normalize) {
+          const float r = rsqrtf(group_sum<G>(dot8(v, v)) * inv_d + p.eps);
+          const F2 rr = f2(r, r);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v.x[e] = mul2(mul2(v.x[e], rr), w.x[e]);
+        }
+        rotate<false>(v, turn, p.interleaved);
+        x[u].set(v);
+      }
+    }
+    T* dst = out + (static_cast<long long>(b) * heads * rows + to) * p.d;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u * R + sub < g.rows && l.on && to >= 0) x[u].store(dst + u * out_step, l);
   }
 }
 
@@ -262,98 +346,84 @@ __global__ void __launch_bounds__(kWarps * 32, 4) qk_fwd_kernel(const __grid_con
 // block adds its lanes up in a fixed order and writes one partial row.
 // qk_bwd_weights_kernel adds the partial rows: the result does not depend on the order in
 // which blocks run.
-template <typename T, typename GT, int G, int U>
+template <typename T, typename GT, int G, int U, bool NARROW>
 __global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm)
     qk_bwd_kernel(const __grid_constant__ QkArgs p, const GT* __restrict__ dq, const GT* __restrict__ dk, const GT* __restrict__ dv,
                   T* __restrict__ dqkv, float* __restrict__ partial, DevCtl ctl) {
   constexpr int R = 32 / G;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane % G, sub = lane / G;
   const int all = p.Hq + (dv ? 2 : 1) * p.Hkv;
-  const long long tokens = static_cast<long long>(p.B) * p.L;
+  const unsigned tokens = static_cast<unsigned>(p.B) * p.L, stride = gridDim.x * kWarps;
   const Lane l = lane_of(p, j);
   const Group g = group_of(p, blockIdx.y, R * U);
   const int heads = g.kind == kQ ? p.Hq : p.Hkv;
-  const GT* grad = g.kind == kQ ? dq : (g.kind == kK ? dk : dv);
-  const T* in = static_cast<const T*>(g.kind == kQ ? p.q : p.k);
-  const long long* stride = g.kind == kQ ? p.q_stride : p.k_stride;
-  const bool norm = p.normalize && g.kind != kV;
-  float wa[4], wb[4], ga[4] = {}, gb[4] = {};
-  load_weight(static_cast<const T*>(g.kind == kQ ? p.q_weight : p.k_weight), l, wa, wb);
+  const GT* grad = (g.kind == kQ ? dq : (g.kind == kK ? dk : dv)) + static_cast<long long>(g.h0 + sub) * p.L * p.d;
+  const long long* step = g.kind == kQ ? p.q_stride : p.k_stride;
+  const T* in = static_cast<const T*>(g.kind == kQ ? p.q : p.k) + (g.h0 + sub) * step[2];
+  T* const out = dqkv + static_cast<long long>((g.kind == kQ ? 0 : (g.kind == kK ? p.Hq : p.Hq + p.Hkv)) + g.h0 + sub) * p.d;
+  const bool turns = g.kind != kV, norm = p.normalize && turns;
+  const Eight w = load_weight<T>(g.kind == kQ ? p.q_weight : p.k_weight, l);
   const float scale = g.kind == kQ ? p.q_scale : 1.f, inv_d = 1.f / p.d;
-  for (long long token = static_cast<long long>(blockIdx.x) * kWarps + warp; token < tokens;
-       token += static_cast<long long>(gridDim.x) * kWarps) {
-    const int b = static_cast<int>(token / p.L), t = static_cast<int>(token % p.L);
-    const GT* gs = grad + ((static_cast<long long>(b) * heads + g.h0 + sub) * p.L + t) * p.d;
-    const long long gstep = static_cast<long long>(R) * p.L * p.d;
-    const T* xs = in + b * stride[0] + t * stride[1] + (g.h0 + sub) * stride[2];
-    Raw<GT> qa[U], qb[U];
-    Raw<T> ra[U], rb[U];
+  Eight dw = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
+  Positions<NARROW> at;
+  unsigned token = blockIdx.x * kWarps + warp;
+  if (turns && token < tokens) at.load(p, l, j, token / p.L, token % p.L);
+  for (; token < tokens; token += stride) {
+    const int b = token / p.L, t = token % p.L;
+    Raw<GT> y[U];
+    Raw<T> x[U];
+    const GT* gs = grad + (static_cast<long long>(b) * heads * p.L + t) * p.d;
+    const T* xs = in + b * step[0] + t * step[1];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const bool on = u * R + sub < g.rows && l.on;
-      if (on) {
-        qa[u].load(gs + u * gstep + l.a);
-        qb[u].load(gs + u * gstep + l.b);
-      } else {
-        qa[u].zero();
-        qb[u].zero();
-      }
-      if (on && norm) {
-        ra[u].load(xs + u * R * stride[2] + l.a);
-        rb[u].load(xs + u * R * stride[2] + l.b);
-      } else {
-        ra[u].zero();
-        rb[u].zero();
-      }
+      if (on)
+        y[u].load(gs + static_cast<long long>(u * R) * p.L * p.d, l);
+      else
+        y[u].zero();
+      if (on && norm)
+        x[u].load(xs + u * R * step[2], l);
+      else
+        x[u].zero();
     }
-    T* dst = dqkv + (token * all + (g.kind == kQ ? 0 : (g.kind == kK ? p.Hq : p.Hq + p.Hkv)) + g.h0 + sub) * p.d;
-    float c[4], s[4];
-    if (g.kind != kV) load_angles(p, l, j, b, t, ctl, c, s);
+    Angles turn;
+    if (turns) {
+      load_angles(p, l, j, at, scale, ctl, turn);
+      if (token + stride < tokens) at.load(p, l, j, (token + stride) / p.L, (token + stride) % p.L);
+    }
+    T* dst = out + static_cast<long long>(token) * all * p.d;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float ya[4], yb[4];
-      qa[u].get(ya);
-      qb[u].get(yb);
-      if (g.kind != kV) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) ya[e] *= scale, yb[e] *= scale;
-        const float back[4] = {-s[0], -s[1], -s[2], -s[3]};  // the transpose turns the other way
-        rotate(ya, yb, c, back, p.interleaved);
-      }
+      Eight v = y[u].get();
+      if (turns) rotate<true>(v, turn, p.interleaved);
       if (norm) {
-        float xa[4], xb[4], ss = 0.f, dot = 0.f;
-        ra[u].get(xa);
-        rb[u].get(xb);
+        Eight z = x[u].get(), vz;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vz.x[e] = mul2(v.x[e], z.x[e]);
+        const float ss = group_sum<G>(dot8(z, z)), ux = group_sum<G>(dot8(vz, w));
+        const float r = rsqrtf(ss * inv_d + p.eps), k = -r * r * ux * inv_d;
+        const F2 rr = f2(r, r), kk = f2(k, k);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          ss += xa[e] * xa[e] + xb[e] * xb[e];
-          dot += ya[e] * wa[e] * xa[e] + yb[e] * wb[e] * xb[e];
-        }
-        const float r = rsqrtf(group_sum<G>(ss) * inv_d + p.eps), k3 = r * r * r * group_sum<G>(dot) * inv_d;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          ga[e] += ya[e] * xa[e] * r;
-          gb[e] += yb[e] * xb[e] * r;
-          ya[e] = r * (ya[e] * wa[e]) - xa[e] * k3;
-          yb[e] = r * (yb[e] * wb[e]) - xb[e] * k3;
+          dw.x[e] = fma2(vz.x[e], rr, dw.x[e]);
+          v.x[e] = mul2(rr, fma2(z.x[e], kk, mul2(v.x[e], w.x[e])));
         }
       }
       if (u * R + sub >= g.rows || !l.on) continue;
-      store4(dst + u * R * p.d + l.a, ya);
-      store4(dst + u * R * p.d + l.b, yb);
+      Raw<T> o;
+      o.set(v);
+      o.store(dst + static_cast<long long>(u * R) * p.d, l);
     }
   }
-  if (!partial || g.kind == kV) return;
+  if (!partial || !turns) return;
   // lanes of one j, then warps, in a fixed order
   __shared__ float sums[kWarps][G][8];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < 8; ++e) {
+    float a = e & 1 ? hi(dw.x[e / 2]) : lo(dw.x[e / 2]);
 #pragma unroll
-    for (int o = G; o < 32; o <<= 1) {
-      ga[e] += __shfl_xor_sync(kFull, ga[e], o);
-      gb[e] += __shfl_xor_sync(kFull, gb[e], o);
-    }
-    if (sub == 0) sums[warp][j][e] = ga[e], sums[warp][j][e + 4] = gb[e];
+    for (int o = G; o < 32; o <<= 1) a += __shfl_xor_sync(kFull, a, o);
+    if (sub == 0) sums[warp][j][e] = a;
   }
   __syncthreads();
   for (int i = threadIdx.x; i < G * 8; i += kWarps * 32) {
@@ -362,7 +432,7 @@ __global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm)
     if (!o.on) continue;
     float a = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) a += sums[w][jj][e];
+    for (int k = 0; k < kWarps; ++k) a += sums[k][jj][e];
     partial[(static_cast<size_t>(blockIdx.y) * gridDim.x + blockIdx.x) * p.d + (e < 4 ? o.a + e : o.b + e - 4)] = a;
   }
 }
@@ -401,37 +471,51 @@ int rows_per_lane(const QkArgs& p, int R, int most) {
   return best;
 }
 
-template <typename F>
-int by_rows(int u, F f) {
-  switch (u) {
-    case 1: return f(std::integral_constant<int, 1>());
-    case 2: return f(std::integral_constant<int, 2>());
-    case 3: return f(std::integral_constant<int, 3>());
-    default: return f(std::integral_constant<int, 4>());
+// Whether a lane's four pairs can lie on more than two axes.
+bool narrow_axes(const QkArgs& p) {
+  if (!p.positions) return false;
+  for (int x = 1; x + 1 < p.axes; ++x)
+    if (p.bound[x] - p.bound[x - 1] < 3) return true;
+  return false;
+}
+
+// f(rows a lane holds, NARROW).  Narrow axes cost four positions and eight table loads a lane: one row at a time.
+template <int MOST, typename F>
+int by_rows(const QkArgs& p, int u, F f) {
+  if (narrow_axes(p)) return f(std::integral_constant<int, 1>(), std::true_type());
+  if constexpr (MOST >= 4) {
+    if (u == 4) return f(std::integral_constant<int, 4>(), std::false_type());
   }
+  if constexpr (MOST >= 3) {
+    if (u == 3) return f(std::integral_constant<int, 3>(), std::false_type());
+  }
+  if constexpr (MOST >= 2) {
+    if (u == 2) return f(std::integral_constant<int, 2>(), std::false_type());
+  }
+  return f(std::integral_constant<int, 1>(), std::false_type());
+}
+
+// Blocks that walk over the tokens, for each group.
+int walkers(int B, int L, int groups, int places) {
+  const long long want = (static_cast<long long>(B) * L + kWarps - 1) / kWarps, most = places / groups;
+  return static_cast<int>(want < most ? want : (most > 1 ? most : 1));
 }
 
 template <typename T, int G>
 int launch_fwd(const QkArgs& p, void* qo, void* ko, void* vo, int cap, const int32_t* start, int num_sms, const DevCtl& ctl,
                cudaStream_t st) {
-  const long long tokens = static_cast<long long>(p.B) * p.L;
   constexpr int R = 32 / G;
-  const long long blocks = (tokens + kWarps - 1) / kWarps;
   // few tokens: one row a lane, for more warps
-  const int u = blocks < num_sms ? 1 : rows_per_lane(p, R, 4);
-  return by_rows(u, [&](auto n) {
+  const bool few = static_cast<long long>(p.B) * p.L <= static_cast<long long>(num_sms) * kWarps;
+  constexpr int kRows = sizeof(T) == 2 ? kRowsPerLane : 2;
+  return by_rows<kRows>(p, few ? 1 : rows_per_lane(p, R, kRows), [&](auto n, auto narrow) {
     constexpr int U = decltype(n)::value;
-    const dim3 grid(static_cast<unsigned>(blocks), groups_of(p.Hq, R * U) + (p.v ? 2 : 1) * groups_of(p.Hkv, R * U));
-    qk_fwd_kernel<T, G, U><<<grid, kWarps * 32, 0, st>>>(p, static_cast<T*>(qo), static_cast<T*>(ko), static_cast<T*>(vo), cap, start, ctl);
+    const int groups = groups_of(p.Hq, R * U) + (p.v ? 2 : 1) * groups_of(p.Hkv, R * U);
+    const dim3 grid(walkers(p.B, p.L, groups, num_sms * kFwdBlocksPerSm * kWaves), groups);
+    qk_fwd_kernel<T, G, U, decltype(narrow)::value><<<grid, kWarps * 32, 0, st>>>(p, static_cast<T*>(qo), static_cast<T*>(ko), static_cast<T*>(vo),
+                                                                                 cap, start, ctl);
     return cudaGetLastError() == cudaSuccess ? 1 : -1;
   });
-}
-
-// Blocks that walk over the tokens, for each group.
-int bwd_blocks(int B, int L, int groups, int num_sms) {
-  const long long want = (static_cast<long long>(B) * L + kWarps - 1) / kWarps;
-  const long long most = (static_cast<long long>(num_sms) * kBwdBlocksPerSm + groups - 1) / groups;
-  return static_cast<int>(want < most ? want : most);
 }
 
 template <typename T, typename GT, int G>
@@ -439,14 +523,14 @@ int launch_bwd(const QkArgs& p, const void* dq, const void* dk, const void* dv, 
                float* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
   constexpr int R = 32 / G;
   const bool weights = p.normalize && (dqw || dkw);
-  constexpr int kRows = sizeof(T) == 2 ? 2 : 1;  // what 80 registers hold of a row and its gradient
-  return by_rows(rows_per_lane(p, R, kRows), [&](auto n) {
-    constexpr int U = decltype(n)::value < kRows ? decltype(n)::value : kRows;
+  constexpr int kRows = sizeof(T) == 2 ? kRowsPerLane : 1;
+  return by_rows<kRows>(p, rows_per_lane(p, R, kRows), [&](auto n, auto narrow) {
+    constexpr int U = decltype(n)::value;
     const int nq = groups_of(p.Hq, R * U), nk = groups_of(p.Hkv, R * U), groups = nq + (dv ? 2 : 1) * nk;
-    const int blocks = bwd_blocks(p.B, p.L, groups, num_sms);
-    qk_bwd_kernel<T, GT, G, U><<<dim3(blocks, groups), kWarps * 32, 0, st>>>(p, static_cast<const GT*>(dq), static_cast<const GT*>(dk),
-                                                                            static_cast<const GT*>(dv), static_cast<T*>(dqkv),
-                                                                            weights ? workspace : nullptr, ctl);
+    const int blocks = walkers(p.B, p.L, groups, num_sms * kBwdBlocksPerSm * kWaves);
+    qk_bwd_kernel<T, GT, G, U, decltype(narrow)::value>
+        <<<dim3(blocks, groups), kWarps * 32, 0, st>>>(p, static_cast<const GT*>(dq), static_cast<const GT*>(dk), static_cast<const GT*>(dv),
+                                                       static_cast<T*>(dqkv), weights ? workspace : nullptr, ctl);
     if (cudaGetLastError() != cudaSuccess) return -1;
     if (!weights) return 1;
     qk_bwd_weights_kernel<<<dim3((p.d + 31) / 32, 2), dim3(32, 32), 0, st>>>(workspace, nq * blocks, nk * blocks, p.d, dqw, dkw);
@@ -457,7 +541,6 @@ int launch_bwd(const QkArgs& p, const void* dq, const void* dk, const void* dv, 
 template <typename F>
 int by_lanes(int d, F f) {
   const int lanes = (d + 7) / 8;
-  if (lanes <= 2) return f(std::integral_constant<int, 2>());
   if (lanes <= 4) return f(std::integral_constant<int, 4>());
   if (lanes <= 8) return f(std::integral_constant<int, 8>());
   if (lanes <= 16) return f(std::integral_constant<int, 16>());
@@ -469,7 +552,7 @@ int by_lanes(int d, F f) {
 // Partial rows of weight gradients: at most one for each block of a full grid and one more for each
 // group, or one for each eight tokens and head.
 int qk_bwd_partial_rows(int B, int L, int Hq, int Hkv, int num_sms) {
-  const long long heads = static_cast<long long>(Hq) + Hkv, full = static_cast<long long>(num_sms) * kBwdBlocksPerSm + heads;
+  const long long heads = static_cast<long long>(Hq) + Hkv, full = static_cast<long long>(num_sms) * kBwdBlocksPerSm * kWaves + heads;
   const long long few = (static_cast<long long>(B) * L + kWarps - 1) / kWarps * heads;
   return static_cast<int>(few < full ? few : full);
 }

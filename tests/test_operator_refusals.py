@@ -54,7 +54,7 @@ def test_qk_outputs(lib):
     assert b(ctypes.byref(_qk(dtype=0)), 16, 16, 16, 1, 16, 16, 16, None) == -2
     assert b(ref, 16, 16, 24, 0, 16, 16, 16, None) == -2
     assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 100, 2, 1, 64) == 13 * 3 * 64 * 4
-    assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 1 << 20, 32, 8, 64) <= (4 * 160 + 40) * 64 * 4
+    assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 1 << 20, 32, 8, 64) <= (8 * 160 + 40) * 64 * 4
     assert T.topk_qk_norm_rope_bwd_workspace_bytes(1, 100, 2, 1, 60) == 0
 
 
