@@ -20,9 +20,13 @@
 // the nearest the moments would never move.  bf16 parameters without a 32-bit master
 // are rounded stochastically for the same reason; a copy beside a master, which nothing
 // is added to, to the nearest.  The random bits are a hash of (seed, step, element): a step
-// gives the same bits whenever it is repeated.  States and roundings depend on the last
-// bit of the sums before them, so the sums use separately rounded products (no
-// fused multiply-add) and a test can state them exactly.
+// gives the same bits whenever it is repeated.
+//
+// With 8-bit states the memory time of an element (10 bytes with bf16 parameters and
+// gradients) is that of some 54 instructions: the scales take up b1, b2 and the
+// gradient's factors, roots and reciprocals are the hardware's approximations (2^-22; the
+// root's code is rounded to 2^-4 of it), the codes are cut out of fp32 patterns with byte
+// permutations and the blocks' maxima are three-input ones.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -55,16 +59,17 @@ struct Entry {
   int vec;            // every pointer allows a lane's vector accesses
 };
 
-constexpr int kMaxTensors = 352;
+constexpr int kMaxTensors = 352, kFewTensors = 32;
 
+template <int MAX>
 struct Table {
-  Entry e[kMaxTensors];
+  Entry e[MAX];
   const float* grad_scale;
-  float b1, c1, b2, c2, isb2, eps;  // c = 1 - b, isb2 = 1 / sqrt(1 - b2^t)
+  float b1, c1, b2, c2, rb2, rc2, isb2, eps;  // c = 1 - b, rb2 and rc2 the roots of b2 and c2, isb2 = 1 / sqrt(1 - b2^t)
   uint32_t key;
   int n_tensors, rounds;
 };
-static_assert(sizeof(Table) <= 32764, "kernel parameters");
+static_assert(sizeof(Table<kMaxTensors>) <= 32764, "kernel parameters");
 
 __host__ __device__ inline uint32_t mix32(uint32_t x) {
   x ^= x >> 16;
@@ -107,14 +112,15 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8], bool vec, 
   }
 }
 
-// eight 16-bit patterns (bf16)
+// eight bf16 patterns, each in the upper half of a word
 __device__ __forceinline__ void store8_16(__nv_bfloat16* p, const uint32_t (&h)[8], bool vec, int count) {
   if (vec && count == 8) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+    *reinterpret_cast<uint4*>(p) = make_uint4(__byte_perm(h[0], h[1], 0x7632), __byte_perm(h[2], h[3], 0x7632),
+                                              __byte_perm(h[4], h[5], 0x7632), __byte_perm(h[6], h[7], 0x7632));
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (e < count) p[e] = __ushort_as_bfloat16(static_cast<unsigned short>(h[e]));
+      if (e < count) p[e] = __ushort_as_bfloat16(static_cast<unsigned short>(h[e] >> 16));
   }
 }
 
@@ -137,49 +143,72 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint2 u, bool vec, int c
   }
 }
 
-__device__ __forceinline__ void decode8(uint2 u, float scale, float (&v)[8]) {
+// Codes as floats, without the scale.
+__device__ __forceinline__ void decode8(uint2 u, float (&v)[8]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const uint32_t w = e < 2 ? u.x : u.y;
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w >> (16 * (e & 1))), __NV_E4M3);
     const float2 f = __half22float2(__half2(h));
-    v[2 * e] = __fmul_rn(f.x, scale);
-    v[2 * e + 1] = __fmul_rn(f.y, scale);
+    v[2 * e] = f.x;
+    v[2 * e + 1] = f.y;
   }
 }
 
-// e4m3 codes of x / scale, stochastically: y = |x| / scale <= 448 has the bit
-// pattern of an e4m3 float 20 places up once its exponent is rebased by
-// 2^-120, subnormals included; ten random bits and half of their last place are
-// added below the last place kept, and the rest is cut off.
-template <int kShift>
+// e4m3 codes of x / scale, stochastically: y = |x| / scale <= 448 has the bit pattern of an e4m3 float 20
+// places up once its exponent is rebased by 2^-120, subnormals included; ten random bits and half of
+// their last place are added below the last place kept, and the rest is cut off.  At y = 448 the sum
+// stays below the next code by 511 units, more than y's rounding: no clamp.  Where y is not a number the
+// scale is not either, and the code does not matter.
+template <int kShift, bool kSigned>
 __device__ __forceinline__ uint2 encode8(const float (&x)[8], float inv, const uint32_t (&rnd)[8]) {
-  uint2 u = make_uint2(0, 0);
+  uint32_t c[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float y = __fmul_rn(fabsf(x[e]), inv);
-    uint32_t c = (__float_as_uint(__fmul_rn(y, 0x1p-120f)) + (((rnd[e] >> kShift) & 1023u) << 10) + 512u) >> 20;
-    c = y == y ? min(c, 0x7eu) : 0x7fu;  // rounding in y can pass the largest value; NaN stays NaN
-    c |= x[e] < 0.f ? 0x80u : 0u;
-    (e < 4 ? u.x : u.y) |= c << (8 * (e & 3));
+    const uint32_t r = kShift == 0 ? ((rnd[e] << 10) & 0xffc00u) | 512u : (rnd[e] & 0xffc00u) | 512u;
+    static_assert(kShift == 0 || kShift == 10, "the ten bits' place");
+    const float y = __fmul_rn(__fmul_rn(fabsf(x[e]), inv), 0x1p-120f);
+    c[e] = (__float_as_uint(y) + r) << 4;  // the code in the top byte
+    if (kSigned) c[e] = (c[e] & 0x7fffffffu) | (__float_as_uint(x[e]) & 0x80000000u);
   }
+  uint2 u;
+  u.x = __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
+  u.y = __byte_perm(__byte_perm(c[4], c[5], 0x0073), __byte_perm(c[6], c[7], 0x0073), 0x5410);
   return u;
 }
 
-// The block's scale from its lanes' largest magnitudes, and its reciprocal; blocks
-// below 2^-100 are held as zeros.
+// max(a, b, c); a NaN wins
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// The block's scale from its lanes' largest magnitudes, and its reciprocal; blocks below 2^-100 are held
+// as zeros.  Bit patterns of magnitudes order as the magnitudes do, a NaN above all.
 __device__ __forceinline__ float block_scale(const float (&x)[8], float* inv) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(fabsf(x[e])));
-  float s = __fmul_rn(__uint_as_float(__reduce_max_sync(kFull, top)), 1.f / kTop);
+  const float a = max3_nan(fabsf(x[0]), fabsf(x[1]), fabsf(x[2])), b = max3_nan(fabsf(x[3]), fabsf(x[4]), fabsf(x[5]));
+  const float top = max3_nan(max3_nan(a, b, fabsf(x[6])), fabsf(x[7]), 0.f);
+  float s = __fmul_rn(__uint_as_float(__reduce_max_sync(kFull, __float_as_uint(top))), 1.f / kTop);
   if (s < 0x1p-100f) s = 0.f;
   *inv = s == 0.f ? 0.f : __frcp_rn(s);
   return s;
 }
 
-template <typename P, typename G, bool k8>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Table t) {
+__device__ __forceinline__ float sqrt_fast(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ float rcp_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+template <typename P, typename G, bool k8, int MAX>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Table<MAX> t) {
   float gs = 1.f;
   if (t.grad_scale) {
     gs = __ldg(t.grad_scale);
@@ -208,24 +237,31 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     else
       load8(param, p, vec, count);
     const long long block = i / 256;
+    float root[8];
     if constexpr (k8) {
-      decode8(load_codes(static_cast<const uint8_t*>(en.m) + i, vec, count), en.m_scale[block], m);
-      decode8(load_codes(static_cast<const uint8_t*>(en.v) + i, vec, count), en.v_scale[block], v);
+      // b1 and the root of b2 go into the blocks' scales: v = (code scale sqrt(b2))^2 + (g sqrt(1 - b2))^2
+      decode8(load_codes(static_cast<const uint8_t*>(en.m) + i, vec, count), m);
+      decode8(load_codes(static_cast<const uint8_t*>(en.v) + i, vec, count), v);
+      const float ms = en.m_scale[block] * t.b1, vs = en.v_scale[block] * t.rb2, gc1 = gs * t.c1, gc2 = gs * t.rc2;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(v[e], v[e]);
+      for (int e = 0; e < 8; ++e) {
+        m[e] = fmaf(m[e], ms, g[e] * gc1);
+        const float r0 = v[e] * vs, r1 = g[e] * gc2;
+        root[e] = sqrt_fast(fmaf(r0, r0, r1 * r1));
+        const float u = m[e] * rcp_fast(fmaf(root[e], t.isb2, t.eps));
+        p[e] = fmaf(p[e], en.decay, -en.size * u);
+      }
     } else {
       load8(static_cast<const float*>(en.m) + i, m, vec, count);
       load8(static_cast<const float*>(en.v) + i, v, vec, count);
-    }
-    float root[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float x = t.grad_scale ? __fmul_rn(g[e], gs) : g[e];
-      m[e] = __fadd_rn(__fmul_rn(m[e], t.b1), __fmul_rn(x, t.c1));
-      v[e] = __fadd_rn(__fmul_rn(v[e], t.b2), __fmul_rn(__fmul_rn(x, x), t.c2));
-      root[e] = __fsqrt_rn(v[e]);
-      const float u = __fdiv_rn(m[e], __fadd_rn(__fmul_rn(root[e], t.isb2), t.eps));
-      p[e] = __fsub_rn(__fmul_rn(p[e], en.decay), __fmul_rn(u, en.size));
+      for (int e = 0; e < 8; ++e) {
+        const float x = g[e] * gs;
+        m[e] = __fadd_rn(__fmul_rn(m[e], t.b1), __fmul_rn(x, t.c1));
+        v[e] = __fadd_rn(__fmul_rn(v[e], t.b2), __fmul_rn(__fmul_rn(x, x), t.c2));
+        const float u = __fdiv_rn(m[e], __fadd_rn(__fmul_rn(__fsqrt_rn(v[e]), t.isb2), t.eps));
+        p[e] = __fsub_rn(__fmul_rn(p[e], en.decay), __fmul_rn(u, en.size));
+      }
     }
     uint32_t rnd[8];
     if (k8 || (sizeof(P) == 2 && !has_master)) {
@@ -240,12 +276,19 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
       if (has_master) {
         store8(en.master + i, p, vec, count);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = __bfloat16_as_ushort(__float2bfloat16_rn(p[e]));
+        for (int e = 0; e < 8; ++e) h[e] = static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(p[e]))) << 16;
       } else {
+        // a NaN's pattern must not be added to: 0 p is NaN for one, and for an infinity
+        float odd = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const uint32_t b = __float_as_uint(p[e]);
-          h[e] = (isfinite(p[e]) ? b + ((rnd[e] >> 20) << 4) + 8u : b) >> 16;
+          odd = fmaf(p[e], 0.f, odd);
+          h[e] = __float_as_uint(p[e]) + (((rnd[e] >> 16) & 0xfff0u) | 8u);
+        }
+        if (odd != odd) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (!isfinite(p[e])) h[e] = __float_as_uint(p[e]);
         }
       }
       store8_16(param, h, vec, count);
@@ -253,9 +296,9 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     if constexpr (k8) {
       float inv;
       const float ms = block_scale(m, &inv);
-      store_codes(static_cast<uint8_t*>(en.m) + i, encode8<0>(m, inv, rnd), vec, count);
+      store_codes(static_cast<uint8_t*>(en.m) + i, encode8<0, true>(m, inv, rnd), vec, count);
       const float vs = block_scale(root, &inv);
-      store_codes(static_cast<uint8_t*>(en.v) + i, encode8<10>(root, inv, rnd), vec, count);
+      store_codes(static_cast<uint8_t*>(en.v) + i, encode8<10, false>(root, inv, rnd), vec, count);
       if ((threadIdx.x & 31) == 0) en.m_scale[block] = ms, en.v_scale[block] = vs;
     } else {
       store8(static_cast<float*>(en.m) + i, m, vec, count);
@@ -264,44 +307,47 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
   }
 }
 
-template <typename P, typename G>
-int launch_adamw(const Table& t, int blocks, bool k8, cudaStream_t st) {
+template <typename P, typename G, int MAX>
+int launch_adamw(const Table<MAX>& t, int blocks, bool k8, cudaStream_t st) {
   if (k8)
-    adamw_kernel<P, G, true><<<blocks, kThreads, 0, st>>>(t);
+    adamw_kernel<P, G, true, MAX><<<blocks, kThreads, 0, st>>>(t);
   else
-    adamw_kernel<P, G, false><<<blocks, kThreads, 0, st>>>(t);
+    adamw_kernel<P, G, false, MAX><<<blocks, kThreads, 0, st>>>(t);
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
-}  // namespace
-
-int adamw_step(const AdamwArgs& a, int num_sms, cudaStream_t st) {
+template <int MAX>
+int step(const AdamwArgs& a, int num_sms, cudaStream_t st) {
   const double c1 = 1.0 - std::pow(a.beta1, static_cast<double>(a.step)), c2 = 1.0 - std::pow(a.beta2, static_cast<double>(a.step));
-  Table t;
+  Table<MAX> t;
   t.grad_scale = a.grad_scale;
   t.b1 = static_cast<float>(a.beta1), t.c1 = static_cast<float>(1.0 - a.beta1);
   t.b2 = static_cast<float>(a.beta2), t.c2 = static_cast<float>(1.0 - a.beta2);
+  t.rb2 = static_cast<float>(std::sqrt(a.beta2)), t.rc2 = static_cast<float>(std::sqrt(1.0 - a.beta2));
   t.isb2 = static_cast<float>(1.0 / std::sqrt(c2)), t.eps = static_cast<float>(a.eps);
   t.key = mix32(a.seed + static_cast<uint32_t>(a.step) * 0x9e3779b9u);
   long long total = 0;
   for (int k = 0; k < a.count; ++k) total += a.tensors[k].n;
+  // a block's start (the search for its tensor) is shared by four rounds where there are blocks enough
   t.rounds = total >= 16LL * kRound * num_sms ? 4 : 1;
+  const long long chunk = static_cast<long long>(t.rounds) * kRound;
   int launches = 0;
   for (int k = 0; k < a.count;) {
     t.n_tensors = 0;
     long long blocks = 0;
-    for (; k < a.count && t.n_tensors < kMaxTensors && blocks < (1 << 30); ++k) {
+    for (; k < a.count && t.n_tensors < MAX; ++k) {
       const topk_adamw_tensor& x = a.tensors[k];
       if (x.n == 0) continue;
-      Entry& e = t.e[t.n_tensors];
+      const long long more = (x.n + chunk - 1) / chunk;
+      if (blocks + more > (1ll << 30)) break;
+      Entry& e = t.e[t.n_tensors++];
       e = {x.param, x.grad, x.master, x.m, x.v, x.m_scale, x.v_scale, x.n, x.index,
            static_cast<float>(1.0 - x.lr * x.weight_decay), static_cast<float>(x.lr / c1), static_cast<int>(blocks), 0};
       e.vec = aligned(x.param, 16) && aligned(x.grad, 16) && aligned(x.master, 16) && aligned(x.m, a.bits8 ? 8 : 16) &&
               aligned(x.v, a.bits8 ? 8 : 16);
-      ++t.n_tensors;
-      blocks += (x.n + static_cast<long long>(t.rounds) * kRound - 1) / (static_cast<long long>(t.rounds) * kRound);
+      blocks += more;
     }
     if (t.n_tensors == 0) break;
     int n;
@@ -315,6 +361,13 @@ int adamw_step(const AdamwArgs& a, int num_sms, cudaStream_t st) {
     launches += n;
   }
   return launches;
+}
+
+}  // namespace
+
+int adamw_step(const AdamwArgs& a, int num_sms, cudaStream_t st) {
+  // the parameters of a launch are copied whole: a short table where it does
+  return a.count <= kFewTensors ? step<kFewTensors>(a, num_sms, st) : step<kMaxTensors>(a, num_sms, st);
 }
 
 }  // namespace topk
