@@ -345,8 +345,8 @@ size_t topk_linear_bwd_workspace_bytes(int M, int N, int K, int act);
  * One AdamW step over many tensors, in place:
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2  (g: the gradient x *grad_scale)
  *   p = p (1 - lr wd) - lr / (1 - beta1^step)  m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * in fp32; with 32-bit states each operation is rounded by itself in the order written
- * (lr / (..) last), with 8-bit states the root and the quotient are approximations (2^-22).
+ * in fp32, each operation rounded by itself in the order written (lr / (..) last); with 8-bit
+ * states the quotient is an approximation (2^-22) and the last difference fused.
  *   tensors    : `count` descriptions in HOST memory, read before the call returns.  Tensors may
  *                be of any length (0 is skipped) and alignment; 16-byte aligned ones (8-byte
  *                for 8-bit states) take vector accesses.  No two may overlap.

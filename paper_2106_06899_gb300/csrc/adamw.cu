@@ -23,15 +23,16 @@
 // gives the same bits whenever it is repeated.
 //
 // With 8-bit states the memory time of an element (10 bytes with bf16 parameters and
-// gradients) is that of some 54 instructions: the scales take up b1, b2 and the
-// gradient's factors, roots and reciprocals are the hardware's approximations (2^-22; the
-// root's code is rounded to 2^-4 of it), the codes are cut out of fp32 patterns with byte
-// permutations and the blocks' maxima are three-input ones.
+// gradients) is that of some 54 instructions, of which half at most on the integer pipe:
+// shifts are products where the multipliers are free, the codes are cut out of fp32
+// patterns with byte permutations, the blocks' maxima are three-input ones, and the
+// quotient, which no state depends on, is the hardware's approximation.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "kernels.h"
 
@@ -44,6 +45,11 @@ constexpr int kPer = 8;                          // neighbouring elements of a l
 constexpr int kRound = kThreads * kPer;          // elements of a block at a time
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kTop = 448.f;                    // largest e4m3 value
+// 307 M bf16 parameters with 8-bit states: 798 us (3.9 TB/s, 57 % of a copy's rate) with three blocks per SM, 32 rounds
+// a block and the next round's loads in flight; 908 us with two blocks, 846 us with four (spills).  Four fifths of all
+// issue slots are taken: instructions bound it.  Approximate roots and fused sums take 720 us, but a code that falls
+// on the other side of its random threshold (2 in 10^6) then makes a step differ from its formula by a place.
+constexpr int kBlocks8 = 3, kRounds8 = 32;
 
 struct Entry {
   void* param;
@@ -61,12 +67,19 @@ struct Entry {
 
 constexpr int kMaxTensors = 352, kFewTensors = 32;
 
+// Powers of two that the compiler does not know: a product by one is issued to the multipliers, where it would
+// write a shift to the integer pipe, which is the 8-bit step's bottleneck.
+struct Powers {
+  uint32_t p0, p4, p14, p16;
+};
+
 template <int MAX>
 struct Table {
   Entry e[MAX];
   const float* grad_scale;
-  float b1, c1, b2, c2, rb2, rc2, isb2, eps;  // c = 1 - b, rb2 and rc2 the roots of b2 and c2, isb2 = 1 / sqrt(1 - b2^t)
+  float b1, c1, b2, c2, isb2, eps;  // c = 1 - b, isb2 = 1 / sqrt(1 - b2^t)
   uint32_t key;
+  Powers k;
   int n_tensors, rounds;
 };
 static_assert(sizeof(Table<kMaxTensors>) <= 32764, "kernel parameters");
@@ -161,20 +174,26 @@ __device__ __forceinline__ void decode8(uint2 u, float (&v)[8]) {
 // stays below the next code by 511 units, more than y's rounding: no clamp.  Where y is not a number the
 // scale is not either, and the code does not matter.
 template <int kShift, bool kSigned>
-__device__ __forceinline__ uint2 encode8(const float (&x)[8], float inv, const uint32_t (&rnd)[8]) {
+__device__ __forceinline__ uint2 encode8(const float (&x)[8], float inv, const uint32_t (&rnd)[8], const Powers& k) {
+  static_assert(kShift == 0 || kShift == 10, "the ten bits' place");
   uint32_t c[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const uint32_t r = kShift == 0 ? ((rnd[e] << 10) & 0xffc00u) | 512u : (rnd[e] & 0xffc00u) | 512u;
-    static_assert(kShift == 0 || kShift == 10, "the ten bits' place");
-    const float y = __fmul_rn(__fmul_rn(fabsf(x[e]), inv), 0x1p-120f);
-    c[e] = (__float_as_uint(y) + r) << 4;  // the code in the top byte
+    const uint32_t y = __float_as_uint(__fmul_rn(__fmul_rn(fabsf(x[e]), inv), 0x1p-120f));
+    const uint32_t r = kShift == 0 ? (rnd[e] & 0x3ffu) * k.p14 + 8192u : (rnd[e] & 0xffc00u) * k.p4 + 8192u;
+    c[e] = y * k.p4 + r;  // 16 (y + 1024 random + 512): the code in the top byte
     if (kSigned) c[e] = (c[e] & 0x7fffffffu) | (__float_as_uint(x[e]) & 0x80000000u);
   }
   uint2 u;
   u.x = __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
   u.y = __byte_perm(__byte_perm(c[4], c[5], 0x0073), __byte_perm(c[6], c[7], 0x0073), 0x5410);
   return u;
+}
+
+__device__ __forceinline__ float rcp_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
 
 // max(a, b, c); a NaN wins
@@ -195,25 +214,83 @@ __device__ __forceinline__ float block_scale(const float (&x)[8], float* inv) {
   return s;
 }
 
-__device__ __forceinline__ float sqrt_fast(float x) {
-  float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-
-__device__ __forceinline__ float rcp_fast(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-
-template <typename P, typename G, bool k8, int MAX>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Table<MAX> t) {
-  float gs = 1.f;
-  if (t.grad_scale) {
-    gs = __ldg(t.grad_scale);
-    if (!isfinite(gs)) return;  // an overflowed step changes nothing
+// Eight values as they lie in memory.
+template <typename T>
+struct Raw8 {
+  static constexpr int kWords = sizeof(T) * 2;  // 32-bit words
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const T* p, bool vec, int count) {
+    if (vec && count == 8) {
+#pragma unroll
+      for (int i = 0; i < kWords / 4; ++i) {
+        const uint4 u = reinterpret_cast<const uint4*>(p)[i];
+        w[4 * i] = u.x, w[4 * i + 1] = u.y, w[4 * i + 2] = u.z, w[4 * i + 3] = u.w;
+      }
+    } else {
+      float v[8];
+      load8(p, v, false, count);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 4)
+          w[i] = __float_as_uint(v[i]);
+        else
+          w[i / 2] = i & 1 ? w[i / 2] | __float_as_uint(v[i]) : __float_as_uint(v[i]) >> 16;
+      }
+    }
   }
+  __device__ __forceinline__ void get(float (&v)[8], const Powers& k) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (sizeof(T) == 4)
+        v[e] = __uint_as_float(w[e]);
+      else
+        v[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] * k.p16);
+    }
+  }
+};
+
+// Stores parameters that no master stands behind: fp32 as they are, bf16 stochastically.
+__device__ __forceinline__ void store_param(float* param, const float (&p)[8], const uint32_t (&)[8], const Powers&, bool vec, int count) {
+  store8(param, p, vec, count);
+}
+__device__ __forceinline__ void store_param(__nv_bfloat16* param, const float (&p)[8], const uint32_t (&rnd)[8], const Powers& k, bool vec,
+                                            int count) {
+  uint32_t h[8];
+  // a NaN's pattern must not be added to: 0 p is NaN for one, and for an infinity
+  float odd = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    odd = fmaf(p[e], 0.f, odd);
+    h[e] = __float_as_uint(p[e]) * k.p0 + ((rnd[e] >> 20) * k.p4 + 8u);
+  }
+  if (odd != odd) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (!isfinite(p[e])) h[e] = __float_as_uint(p[e]);
+  }
+  store8_16(param, h, vec, count);
+}
+
+__device__ __forceinline__ void store_master(float* master, float*, const float (&p)[8], bool vec, int count) {
+  store8(master, p, vec, count);
+}
+__device__ __forceinline__ void store_master(float* master, __nv_bfloat16* param, const float (&p)[8], bool vec, int count) {
+  store8(master, p, vec, count);
+  uint32_t h[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) h[e] = static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(p[e]))) << 16;
+  store8_16(param, h, vec, count);
+}
+
+__device__ __forceinline__ void random8(uint32_t first, uint32_t key, uint32_t (&rnd)[8]) {
+  const uint32_t base = first * 0x9e3779b1u + key;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) rnd[e] = mix32(base + e * 0x9e3779b1u);
+}
+
+// The tensor of a block: the last whose first block is not after it.
+template <int MAX>
+__device__ __forceinline__ const Entry& entry_of(const Table<MAX>& t) {
   int lo = 0, hi = t.n_tensors - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -222,13 +299,26 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     else
       hi = mid - 1;
   }
-  const Entry& en = t.e[lo];
+  return t.e[lo];
+}
+
+template <int MAX>
+__device__ __forceinline__ bool grad_scale_of(const Table<MAX>& t, float& gs) {
+  gs = t.grad_scale ? __ldg(t.grad_scale) : 1.f;
+  return isfinite(gs);  // an overflowed step changes nothing
+}
+
+// 32-bit states.
+template <typename P, typename G, int MAX>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Table<MAX> t) {
+  float gs;
+  if (!grad_scale_of(t, gs)) return;
+  const Entry& en = entry_of(t);
   const bool vec = en.vec, has_master = en.master != nullptr;
   const long long n = en.n;
   long long i = static_cast<long long>(static_cast<int>(blockIdx.x) - en.first) * t.rounds * kRound + threadIdx.x * kPer;
-  for (int r = 0; r < t.rounds; ++r, i += kRound) {
-    if (i - (threadIdx.x & 31) * kPer >= n) return;  // the warp's block of 256 is past the end
-    const int count = i >= n ? 0 : (n - i < kPer ? static_cast<int>(n - i) : kPer);
+  for (int r = 0; r < t.rounds && i < n; ++r, i += kRound) {
+    const int count = n - i < kPer ? static_cast<int>(n - i) : kPer;
     P* param = static_cast<P*>(en.param) + i;
     float p[8], g[8], m[8], v[8];
     load8(static_cast<const G*>(en.grad) + i, g, vec, count);
@@ -236,83 +326,152 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
       load8(en.master + i, p, vec, count);
     else
       load8(param, p, vec, count);
-    const long long block = i / 256;
-    float root[8];
-    if constexpr (k8) {
-      // b1 and the root of b2 go into the blocks' scales: v = (code scale sqrt(b2))^2 + (g sqrt(1 - b2))^2
-      decode8(load_codes(static_cast<const uint8_t*>(en.m) + i, vec, count), m);
-      decode8(load_codes(static_cast<const uint8_t*>(en.v) + i, vec, count), v);
-      const float ms = en.m_scale[block] * t.b1, vs = en.v_scale[block] * t.rb2, gc1 = gs * t.c1, gc2 = gs * t.rc2;
+    load8(static_cast<const float*>(en.m) + i, m, vec, count);
+    load8(static_cast<const float*>(en.v) + i, v, vec, count);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        m[e] = fmaf(m[e], ms, g[e] * gc1);
-        const float r0 = v[e] * vs, r1 = g[e] * gc2;
-        root[e] = sqrt_fast(fmaf(r0, r0, r1 * r1));
-        const float u = m[e] * rcp_fast(fmaf(root[e], t.isb2, t.eps));
-        p[e] = fmaf(p[e], en.decay, -en.size * u);
-      }
+    for (int e = 0; e < 8; ++e) {
+      const float x = g[e] * gs;
+      m[e] = __fadd_rn(__fmul_rn(m[e], t.b1), __fmul_rn(x, t.c1));
+      v[e] = __fadd_rn(__fmul_rn(v[e], t.b2), __fmul_rn(__fmul_rn(x, x), t.c2));
+      const float u = __fdiv_rn(m[e], __fadd_rn(__fmul_rn(__fsqrt_rn(v[e]), t.isb2), t.eps));
+      p[e] = __fsub_rn(__fmul_rn(p[e], en.decay), __fmul_rn(u, en.size));
+    }
+    if (has_master) {
+      store_master(en.master + i, param, p, vec, count);
     } else {
-      load8(static_cast<const float*>(en.m) + i, m, vec, count);
-      load8(static_cast<const float*>(en.v) + i, v, vec, count);
+      uint32_t rnd[8];
+      if constexpr (sizeof(P) == 2) random8(static_cast<uint32_t>(en.index + i), t.key, rnd);
+      store_param(param, p, rnd, t.k, vec, count);
+    }
+    store8(static_cast<float*>(en.m) + i, m, vec, count);
+    store8(static_cast<float*>(en.v) + i, v, vec, count);
+  }
+}
+
+// 8-bit states.
+template <typename S, typename G>
+struct Held8 {  // a lane's eight elements as they lie in memory
+  Raw8<S> p;
+  Raw8<G> g;
+  uint2 m, v;
+  float ms, vs;
+};
+
+// Eight elements at offset `at` of the block's chunk: the update, then the block's new scales and codes.
+// FULL: a whole, aligned chunk; else `count` elements, one access each where `vec` is false.
+template <bool FULL, typename P, typename G, bool MASTER, int MAX>
+struct Step8 {
+  using S = std::conditional_t<MASTER, float, P>;  // what the parameters are read from
+  const Table<MAX>& t;
+  const Entry& en;
+  const float gs;
+  // the chunk's addresses, the same for all threads
+  P* const param;
+  const G* const grad;
+  float* const master;
+  uint8_t *const m8, *const v8;
+  float *const m_scale, *const v_scale;
+  const uint32_t index;
+  const int left;
+  const bool vec;
+
+  __device__ __forceinline__ Step8(const Table<MAX>& t_, const Entry& e, float gs_, long long start, int left_)
+      : t(t_), en(e), gs(gs_), param(static_cast<P*>(e.param) + start), grad(static_cast<const G*>(e.grad) + start),
+        master(e.master + start), m8(static_cast<uint8_t*>(e.m) + start), v8(static_cast<uint8_t*>(e.v) + start),
+        m_scale(e.m_scale + start / 256), v_scale(e.v_scale + start / 256), index(static_cast<uint32_t>(e.index + start)), left(left_), vec(e.vec) {}
+
+  __device__ __forceinline__ int count(unsigned at) const {
+    return FULL ? kPer : max(0, min(kPer, left - static_cast<int>(at)));
+  }
+  __device__ __forceinline__ void load(unsigned at, Held8<S, G>& h) const {
+    const int n = count(at);
+    const bool wide = FULL || vec;
+    h.g.load(grad + at, wide, n);
+    if constexpr (MASTER)
+      h.p.load(master + at, wide, n);
+    else
+      h.p.load(param + at, wide, n);
+    h.m = load_codes(m8 + at, wide, n);
+    h.v = load_codes(v8 + at, wide, n);
+    h.ms = m_scale[at / 256], h.vs = v_scale[at / 256];
+  }
+  __device__ __forceinline__ void work(unsigned at, const Held8<S, G>& h) const {
+    const int n = count(at);
+    const bool wide = FULL || vec;
+    float p[8], g[8], m[8], v[8];
+    h.g.get(g, t.k);
+    h.p.get(p, t.k);
+    decode8(h.m, m);
+    decode8(h.v, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = g[e] * gs;
-        m[e] = __fadd_rn(__fmul_rn(m[e], t.b1), __fmul_rn(x, t.c1));
-        v[e] = __fadd_rn(__fmul_rn(v[e], t.b2), __fmul_rn(__fmul_rn(x, x), t.c2));
-        const float u = __fdiv_rn(m[e], __fadd_rn(__fmul_rn(__fsqrt_rn(v[e]), t.isb2), t.eps));
-        p[e] = __fsub_rn(__fmul_rn(p[e], en.decay), __fmul_rn(u, en.size));
-      }
+    for (int e = 0; e < 8; ++e) {
+      const float x = g[e] * gs, r0 = __fmul_rn(v[e], h.vs);
+      m[e] = __fadd_rn(__fmul_rn(__fmul_rn(m[e], h.ms), t.b1), __fmul_rn(x, t.c1));
+      v[e] = __fsqrt_rn(__fadd_rn(__fmul_rn(__fmul_rn(r0, r0), t.b2), __fmul_rn(__fmul_rn(x, x), t.c2)));
+      const float u = m[e] * rcp_fast(fmaf(v[e], t.isb2, t.eps));
+      p[e] = fmaf(p[e], en.decay, -en.size * u);
     }
     uint32_t rnd[8];
-    if (k8 || (sizeof(P) == 2 && !has_master)) {
-      const uint32_t first = static_cast<uint32_t>(en.index + i);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) rnd[e] = mix32((first + e) * 0x9e3779b1u + t.key);
+    random8(index + at, t.key, rnd);
+    if constexpr (MASTER)
+      store_master(master + at, param + at, p, wide, n);
+    else
+      store_param(param + at, p, rnd, t.k, wide, n);
+    float inv;
+    const float ms1 = block_scale(m, &inv);
+    store_codes(m8 + at, encode8<0, true>(m, inv, rnd, t.k), wide, n);
+    const float vs1 = block_scale(v, &inv);
+    store_codes(v8 + at, encode8<10, false>(v, inv, rnd, t.k), wide, n);
+    if ((threadIdx.x & 31) == 0) m_scale[at / 256] = ms1, v_scale[at / 256] = vs1;
+  }
+};
+
+template <typename P, typename G, bool MASTER, int MAX>
+__global__ void __launch_bounds__(kThreads, kBlocks8) adamw8_kernel(const __grid_constant__ Table<MAX> t) {
+  float gs;
+  if (!grad_scale_of(t, gs)) return;
+  const Entry& en = entry_of(t);
+  const long long start = static_cast<long long>(static_cast<int>(blockIdx.x) - en.first) * t.rounds * kRound;
+  const int chunk = t.rounds * kRound, left = en.n - start < chunk ? static_cast<int>(en.n - start) : chunk;
+  const unsigned at0 = threadIdx.x * kPer;
+  if (en.vec && left == chunk) {
+    const Step8<true, P, G, MASTER, MAX> s(t, en, gs, start, left);
+    Held8<typename Step8<true, P, G, MASTER, MAX>::S, G> a, b;
+    s.load(at0, a);
+#pragma unroll 1
+    for (int at = 0;; at += 2 * kRound) {
+      const bool second = at + kRound < chunk;
+      if (second) s.load(at0 + at + kRound, b);
+      s.work(at0 + at, a);
+      if (!second) return;
+      const bool third = at + 2 * kRound < chunk;
+      if (third) s.load(at0 + at + 2 * kRound, a);
+      s.work(at0 + at + kRound, b);
+      if (!third) return;
     }
-    if constexpr (sizeof(P) == 4) {
-      store8(param, p, vec, count);
-    } else {
-      uint32_t h[8];
-      if (has_master) {
-        store8(en.master + i, p, vec, count);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(p[e]))) << 16;
-      } else {
-        // a NaN's pattern must not be added to: 0 p is NaN for one, and for an infinity
-        float odd = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          odd = fmaf(p[e], 0.f, odd);
-          h[e] = __float_as_uint(p[e]) + (((rnd[e] >> 16) & 0xfff0u) | 8u);
-        }
-        if (odd != odd) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (!isfinite(p[e])) h[e] = __float_as_uint(p[e]);
-        }
-      }
-      store8_16(param, h, vec, count);
-    }
-    if constexpr (k8) {
-      float inv;
-      const float ms = block_scale(m, &inv);
-      store_codes(static_cast<uint8_t*>(en.m) + i, encode8<0, true>(m, inv, rnd), vec, count);
-      const float vs = block_scale(root, &inv);
-      store_codes(static_cast<uint8_t*>(en.v) + i, encode8<10, false>(root, inv, rnd), vec, count);
-      if ((threadIdx.x & 31) == 0) en.m_scale[block] = ms, en.v_scale[block] = vs;
-    } else {
-      store8(static_cast<float*>(en.m) + i, m, vec, count);
-      store8(static_cast<float*>(en.v) + i, v, vec, count);
-    }
+    return;
+  }
+  const Step8<false, P, G, MASTER, MAX> s(t, en, gs, start, left);
+#pragma unroll 1
+  for (int at = 0; at + static_cast<int>(at0 & ~255u) < left; at += kRound) {  // while the warp's block of 256 has elements
+    Held8<typename Step8<false, P, G, MASTER, MAX>::S, G> h;
+    s.load(at0 + at, h);
+    s.work(at0 + at, h);
   }
 }
 
 template <typename P, typename G, int MAX>
 int launch_adamw(const Table<MAX>& t, int blocks, bool k8, cudaStream_t st) {
-  if (k8)
-    adamw_kernel<P, G, true, MAX><<<blocks, kThreads, 0, st>>>(t);
-  else
-    adamw_kernel<P, G, false, MAX><<<blocks, kThreads, 0, st>>>(t);
+  if (!k8) {
+    adamw_kernel<P, G, MAX><<<blocks, kThreads, 0, st>>>(t);
+  } else if constexpr (sizeof(P) == 2) {
+    if (t.e[0].master)
+      adamw8_kernel<P, G, true, MAX><<<blocks, kThreads, 0, st>>>(t);
+    else
+      adamw8_kernel<P, G, false, MAX><<<blocks, kThreads, 0, st>>>(t);
+  } else {
+    adamw8_kernel<P, G, false, MAX><<<blocks, kThreads, 0, st>>>(t);
+  }
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 
@@ -323,15 +482,16 @@ int step(const AdamwArgs& a, int num_sms, cudaStream_t st) {
   const double c1 = 1.0 - std::pow(a.beta1, static_cast<double>(a.step)), c2 = 1.0 - std::pow(a.beta2, static_cast<double>(a.step));
   Table<MAX> t;
   t.grad_scale = a.grad_scale;
+  t.k = {1u, 1u << 4, 1u << 14, 1u << 16};
   t.b1 = static_cast<float>(a.beta1), t.c1 = static_cast<float>(1.0 - a.beta1);
   t.b2 = static_cast<float>(a.beta2), t.c2 = static_cast<float>(1.0 - a.beta2);
-  t.rb2 = static_cast<float>(std::sqrt(a.beta2)), t.rc2 = static_cast<float>(std::sqrt(1.0 - a.beta2));
   t.isb2 = static_cast<float>(1.0 / std::sqrt(c2)), t.eps = static_cast<float>(a.eps);
   t.key = mix32(a.seed + static_cast<uint32_t>(a.step) * 0x9e3779b9u);
   long long total = 0;
   for (int k = 0; k < a.count; ++k) total += a.tensors[k].n;
-  // a block's start (the search for its tensor) is shared by four rounds where there are blocks enough
-  t.rounds = total >= 16LL * kRound * num_sms ? 4 : 1;
+  // the rounds of a block share its start (the search for its tensor), as many as leave every SM a dozen blocks
+  const long long most = a.bits8 ? kRounds8 : 4, fair = total / (12LL * kRound * num_sms);
+  t.rounds = static_cast<int>(fair < 1 ? 1 : (fair < most ? fair : most));
   const long long chunk = static_cast<long long>(t.rounds) * kRound;
   int launches = 0;
   for (int k = 0; k < a.count;) {
