@@ -21,6 +21,8 @@
 // bound by reading W once.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "kernels.h"
 
 namespace topk {
@@ -31,22 +33,83 @@ constexpr int BM = 128, BK = 64;
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 
-template <int BN>
+// CTAS = 2: two CTAs of a cluster (a pair of SMs) work on one 256 x BN tile.  Each stages its 128 rows of A and its
+// half of B's rows, the pair's first CTA issues the products for both, and each ends up with its
+// 128 x BN accumulator: B is read from shared memory once for two SMs.
+template <int CTAS, int BN>
 struct Layout {
-  static constexpr uint32_t A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2;
+  static constexpr uint32_t A_BYTES = BM * BK * 2, B_BYTES = BN / CTAS * BK * 2;
   static constexpr uint32_t STAGE = A_BYTES + B_BYTES;
   static constexpr uint32_t EPI = 4096;  // a warp's 32 rows of 128 bytes
-  static constexpr int S = (232448 - 2048 - kEpiWarps * EPI) / STAGE > 6 ? 6 : (232448 - 2048 - kEpiWarps * EPI) / STAGE;
+  static constexpr int FIT = (232448 - 2048 - kEpiWarps * EPI) / STAGE;
+  static constexpr int S = FIT > 6 ? 6 : FIT;
   static constexpr size_t OFF_EPI = static_cast<size_t>(S) * STAGE;
   static constexpr size_t OFF_BAR = OFF_EPI + kEpiWarps * EPI;
   static constexpr int NBARS = 2 * S + 5;  // full/empty per stage, accumulator full/empty x 2, drain
   static constexpr size_t BYTES = 1024 + OFF_BAR + NBARS * 8 + 16;
+  static constexpr uint32_t TMEM_COLS = 2 * BN <= 256 ? 256 : 512;
   static_assert(BYTES <= 232448 && S >= 3, "shared memory");
+  static_assert(STAGE % 1024 == 0, "swizzle atoms");
 };
 
+// ------------------------------------------------------------ pairs of CTAs
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// The address of the first CTA's barrier.
+__device__ __forceinline__ uint32_t leader_bar(const uint64_t* bar) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(bar)));
+  return r;
+}
+
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// Bounded wait (common.cuh's mbar_wait) that also acquires what the other CTA released.
+__device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, const DevCtl& ctl, volatile int* abort_flag) {
+  const unsigned long long t0 = global_ns();
+  for (uint32_t spin = 1;; ++spin) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if ((spin & 63u) == 0u) {
+      if (*abort_flag) return false;
+      if (global_ns() - t0 > ctl.wait_limit_ns) {
+        atomicOr(ctl.error, kDevErrTimeout);
+        *abort_flag = 1;
+        return false;
+      }
+    }
+  }
+}
+
+template <int CTAS>
+__device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, const DevCtl& ctl, volatile int* abort_flag) {
+  if constexpr (CTAS == 1)
+    return mbar_wait(bar, parity, ctl, abort_flag);
+  else
+    return wait_pair(bar, parity, ctl, abort_flag);
+}
+
+template <int CTAS>
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const DevCtl& ctl, volatile int* abort_flag) {
   int ok = 0;
-  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity, ctl, abort_flag) ? 1 : 0;
+  if ((threadIdx.x & 31) == 0) ok = wait_bar<CTAS>(bar, parity, ctl, abort_flag) ? 1 : 0;
   return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
 
@@ -58,6 +121,73 @@ __device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity, const
       return;
     }
   }
+}
+
+template <int CTAS>
+__device__ __forceinline__ void tmem_take(uint32_t* dst, uint32_t cols) {
+  if constexpr (CTAS == 1) {
+    tmem_alloc(dst, cols);
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst)), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+}
+
+template <int CTAS>
+__device__ __forceinline__ void tmem_give(uint32_t addr, uint32_t cols) {
+  if constexpr (CTAS == 1)
+    tmem_dealloc(addr, cols);
+  else
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
+}
+
+// `bar`: an address in the cluster's shared memory (the first CTA's barrier for a pair).
+template <int CTAS>
+__device__ __forceinline__ void load_box(void* dst, const void* map, uint32_t bar, int c0, int c1) {
+  if constexpr (CTAS == 1)
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(0)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(0)
+        : "memory");
+}
+
+template <int CTAS>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (CTAS == 1)
+    mma_bf16_ss(d, a, b, idesc, accumulate);
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// Arrives on the barrier (of both CTAs of a pair) when all products issued so far are done.
+template <int CTAS>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  if constexpr (CTAS == 1)
+    mma_commit(bar);
+  else
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+                 "h"(static_cast<uint16_t>(3))
+                 : "memory");
+}
+
+// Arrives on this CTA's barrier alone.
+template <int CTAS>
+__device__ __forceinline__ void commit_here(uint64_t* bar) {
+  if constexpr (CTAS == 1)
+    mma_commit(bar);
+  else
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
 // MN-major tile of 64 x 64 boxes (128-byte rows of 64 MN elements, one row per k): 64-element
@@ -138,28 +268,30 @@ __device__ __forceinline__ void unit_of(const Grid& g, int u, int& mt, int& nt, 
 }
 
 // Out: __nv_bfloat16 or float (the result, or a part's partial sums).
-template <int BN, bool A_MN, bool B_MN, typename Out>
+template <int CTAS, int BN, bool A_MN, bool B_MN, typename Out>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_mma_kernel(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUtensorMap tmb,
                       const __grid_constant__ CUtensorMap tmo, const __grid_constant__ CUtensorMap tmz, Epi epi, Grid grid, int M,
                       int N, DevCtl ctl) {
-  using L = Layout<BN>;
-  constexpr int S = L::S;
-  constexpr uint32_t IDESC = idesc_bf16_f32(BM, BN) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
-  constexpr uint32_t TMEM_COLS = 2 * BN <= 128 ? 128 : (2 * BN <= 256 ? 256 : 512);
+  using L = Layout<CTAS, BN>;
+  constexpr int S = L::S, NB = BN / CTAS;  // NB: rows of B that a CTA stages
+  constexpr uint32_t IDESC = idesc_bf16_f32(BM * CTAS, BN) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
+  static_assert(!B_MN || NB % 64 == 0, "whole boxes of B");
 
   extern __shared__ uint8_t smem_raw[];
+  // the same offset in both CTAs of a pair: their windows start alike
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
-  uint64_t* full = bars;
+  uint64_t* full = bars;                   // the first CTA's are used, for the loads of both
   uint64_t* empty = bars + S;
   uint64_t* acc_full = bars + 2 * S;       // [2]
-  uint64_t* acc_empty = bars + 2 * S + 2;  // [2]
+  uint64_t* acc_empty = bars + 2 * S + 2;  // [2], the first CTA's are used
   uint64_t* drain = bars + 2 * S + 4;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::NBARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = CTAS == 2 ? static_cast<int>(cluster_rank()) : 0;
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
       mbar_init(&full[s], 1);
@@ -167,18 +299,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&acc_full[b], 1);
-      mbar_init(&acc_empty[b], kEpiWarps);
+      mbar_init(&acc_empty[b], kEpiWarps * CTAS);
     }
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
-  if (warp == 1) tmem_alloc(tmem_slot, TMEM_COLS);
+  if (warp == 1) tmem_take<CTAS>(tmem_slot, L::TMEM_COLS);
   tc_fence_before();
   __syncthreads();
+  if constexpr (CTAS == 2) cluster_sync();  // the other CTA's barriers are there
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   const int units = grid.m_tiles * grid.n_tiles * grid.parts;
+  const int unit0 = blockIdx.x / CTAS, stride = gridDim.x / CTAS;
   auto k_first = [&](int part) { return static_cast<int>(static_cast<long long>(grid.k_blocks) * part / grid.parts); };
 
   if (warp == 0) {
@@ -188,53 +322,57 @@ __global__ void __launch_bounds__(kThreads, 1)
       tma_prefetch_desc(&tmb);
       uint32_t it = 0;
       bool ok = true;
-      for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      for (int u = unit0; ok && u < units; u += stride) {
         int mt, nt, part;
         unit_of(grid, u, mt, nt, part);
+        const int row = (mt * CTAS + rank) * BM, col = nt * BN + rank * NB;
         for (int kb = k_first(part), end = k_first(part + 1); kb < end; ++kb, ++it) {
           const int s = it % S;
-          if (!mbar_wait(&empty[s], ((it / S) & 1u) ^ 1u, ctl, abort_flag)) {
+          if (!wait_bar<CTAS>(&empty[s], ((it / S) & 1u) ^ 1u, ctl, abort_flag)) {
             ok = false;
             break;
           }
           uint8_t* a = smem + static_cast<size_t>(s) * L::STAGE;
           uint8_t* b = a + L::A_BYTES;
-          mbar_arrive_expect_tx(&full[s], L::STAGE);
+          // the first CTA's barrier counts the bytes of both
+          const uint32_t bar = CTAS == 2 ? leader_bar(&full[s]) : smem_u32(&full[s]);
+          if (rank == 0) mbar_arrive_expect_tx(&full[s], CTAS * L::STAGE);
           if constexpr (A_MN) {
-            for (int r = 0; r < BM / 64; ++r) tma_load_3d(a + r * 8192, &tma, &full[s], mt * BM + r * 64, kb * BK, 0);
+            for (int r = 0; r < BM / 64; ++r) load_box<CTAS>(a + r * 8192, &tma, bar, row + r * 64, kb * BK);
           } else {
-            tma_load_3d(a, &tma, &full[s], kb * BK, mt * BM, 0);
+            load_box<CTAS>(a, &tma, bar, kb * BK, row);
           }
           if constexpr (B_MN) {
-            for (int r = 0; r < BN / 64; ++r) tma_load_3d(b + r * 8192, &tmb, &full[s], nt * BN + r * 64, kb * BK, 0);
+            for (int r = 0; r < NB / 64; ++r) load_box<CTAS>(b + r * 8192, &tmb, bar, col + r * 64, kb * BK);
           } else {
-            tma_load_3d(b, &tmb, &full[s], kb * BK, nt * BN, 0);
+            load_box<CTAS>(b, &tmb, bar, kb * BK, col);
           }
         }
       }
-      // every issued copy must land before the CTA exits
+      // every issued copy must land before the CTA exits: the first CTA waits for both's, the second for the
+      // products' arrivals on its own barriers, which come after
       for (uint32_t back = 1; back <= static_cast<uint32_t>(S) && back <= it; ++back) {
         const uint32_t t = it - back;
-        drain_wait(&full[t % S], (t / S) & 1u, ctl);
+        drain_wait(rank == 0 ? &full[t % S] : &empty[t % S], (t / S) & 1u, ctl);
       }
     }
     __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ products
-    if (lane == 0) {
+    if (lane == 0 && rank == 0) {
       uint32_t it = 0, tile = 0;
       bool ok = true;
-      for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++tile) {
+      for (int u = unit0; ok && u < units; u += stride, ++tile) {
         int mt, nt, part;
         unit_of(grid, u, mt, nt, part);
         const uint32_t buf = tile & 1u;
-        if (!mbar_wait(&acc_empty[buf], ((tile >> 1) & 1u) ^ 1u, ctl, abort_flag)) break;
+        if (!wait_bar<CTAS>(&acc_empty[buf], ((tile >> 1) & 1u) ^ 1u, ctl, abort_flag)) break;
         tc_fence_after();
         const uint32_t acc = tmem_base + buf * BN;
         const int first = k_first(part), end = k_first(part + 1);
         for (int kb = first; kb < end; ++kb, ++it) {
           const int s = it % S;
-          if (!mbar_wait(&full[s], (it / S) & 1u, ctl, abort_flag)) {
+          if (!wait_bar<CTAS>(&full[s], (it / S) & 1u, ctl, abort_flag)) {
             ok = false;
             break;
           }
@@ -242,14 +380,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t a = smem_u32(smem + static_cast<size_t>(s) * L::STAGE), b = a + L::A_BYTES;
 #pragma unroll
           for (int k = 0; k < BK / 16; ++k)
-            mma_bf16_ss(acc, A_MN ? sdesc_mn128(a + k * 2048) : sdesc_k128(a + k * 32),
-                        B_MN ? sdesc_mn128(b + k * 2048) : sdesc_k128(b + k * 32), IDESC, kb > first || k > 0 ? 1u : 0u);
-          mma_commit(&empty[s]);
+            mma<CTAS>(acc, A_MN ? sdesc_mn128(a + k * 2048) : sdesc_k128(a + k * 32),
+                      B_MN ? sdesc_mn128(b + k * 2048) : sdesc_k128(b + k * 32), IDESC, kb > first || k > 0 ? 1u : 0u);
+          commit<CTAS>(&empty[s]);
         }
-        if (ok) mma_commit(&acc_full[buf]);
+        if (ok) commit<CTAS>(&acc_full[buf]);
       }
       // all issued MMAs must complete before TMEM is freed
-      mma_commit(drain);
+      commit_here<CTAS>(drain);
       drain_wait(drain, 0, ctl);
     }
     __syncwarp();
@@ -274,13 +412,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     };
     uint32_t tile = 0;
-    for (int u = blockIdx.x; u < units; u += gridDim.x, ++tile) {
+    for (int u = unit0; u < units; u += stride, ++tile) {
       int mt, nt, part;
       unit_of(grid, u, mt, nt, part);
       const uint32_t buf = tile & 1u;
-      if (!warp_wait(&acc_full[buf], (tile >> 1) & 1u, ctl, abort_flag)) break;
+      if (!warp_wait<CTAS>(&acc_full[buf], (tile >> 1) & 1u, ctl, abort_flag)) break;
       tc_fence_after();
-      const int row0 = mt * BM + quad * 32, row = row0 + lane;
+      const int row0 = (mt * CTAS + rank) * BM + quad * 32, row = row0 + lane;
       const uint32_t taddr = tmem_base + buf * BN + (static_cast<uint32_t>(quad * 32) << 16);
 #pragma unroll 1
       for (int c = half; c < BN / COLS; c += 2) {
@@ -343,7 +481,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&acc_empty[buf]);
+      if (lane == 0) {
+        if constexpr (CTAS == 2)
+          arrive_cluster(leader_bar(&acc_empty[buf]));
+        else
+          mbar_arrive(&acc_empty[buf]);
+      }
     }
     if (lane == 0) bulk_wait_all();
     __syncwarp();
@@ -351,9 +494,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   tc_fence_before();
   __syncthreads();
+  // a CTA of a pair may leave when the products that read its shared memory, and the loads into it, are done
+  if constexpr (CTAS == 2) cluster_sync();
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem_base, TMEM_COLS);
+    tmem_give<CTAS>(tmem_base, L::TMEM_COLS);
   }
 }
 
@@ -526,62 +671,90 @@ bool make_out_map(CUtensorMap* map, const void* base, bool f32, uint64_t cols, u
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How a product is cut: tile width and parts of the sum.  `out_rows` x `out_cols`, summed over `sum`.
+// What a tile costs beside its columns, in columns: a narrow one reads A for fewer products, a single CTA all of B.
+constexpr double kTileCost(int ctas, int bn) { return ctas == 1 ? 48.0 : (bn == 256 ? 0.0 : 16.0); }
+
+// How a product is cut: CTAs and width of a tile, parts of the sum.
 struct Cut {
-  int bn, parts;
+  int ctas, bn, parts;
 };
 
-Cut cut_of(int out_rows, int out_cols, int sum, int num_sms) {
-  const int mt = (out_rows + BM - 1) / BM, kb = (sum + BK - 1) / BK;
-  Cut best{128, 1};
-  // the time of a wave is that of its tiles; 256-wide tiles read less of A per product
+// `out_rows` x `out_cols`, summed over `sum`; `places`: SMs.
+Cut cut_of(int out_rows, int out_cols, int sum, bool b_mn, int places) {
+  const int kb = (sum + BK - 1) / BK;
+  Cut best{1, 128, 1};
   double least = 1e30;
-  for (int bn : {256, 128}) {
-    const long long tiles = static_cast<long long>(mt) * ((out_cols + bn - 1) / bn);
-    const double waves = static_cast<double>((tiles + num_sms - 1) / num_sms) * bn * (bn == 128 ? 1.15 : 1.0);
-    if (waves < least) least = waves, best.bn = bn;
+  long long best_tiles = 1;
+  for (const Cut& c : {Cut{2, 256, 1}, Cut{2, 192, 1}, Cut{2, 128, 1}, Cut{1, 128, 1}}) {
+    if (c.bn == 192 && b_mn) continue;  // half of 192 is no whole number of 64-wide boxes
+    const int rows = BM * c.ctas;
+    const long long tiles = static_cast<long long>((out_rows + rows - 1) / rows) * ((out_cols + c.bn - 1) / c.bn);
+    const long long units = places / c.ctas;
+    const double cost = static_cast<double>((tiles + units - 1) / units) * (c.bn + kTileCost(c.ctas, c.bn));
+    if (cost < least) least = cost, best = c, best_tiles = tiles;
   }
-  const long long tiles = static_cast<long long>(mt) * ((out_cols + best.bn - 1) / best.bn);
   // a part has at least eight blocks of the sum, so that its loads outlast its partial tile's store
-  if (tiles * 2 <= num_sms) {
-    long long p = num_sms / tiles;
+  const long long units = places / best.ctas;
+  if (best_tiles * 2 <= units) {
+    long long p = units / best_tiles;
     if (p > kb / 8) p = kb / 8;
     best.parts = p < 1 ? 1 : static_cast<int>(p);
   }
   return best;
 }
 
-template <int BN, bool A_MN, bool B_MN, typename Out>
+template <int CTAS, int BN, bool A_MN, bool B_MN, typename Out>
 int launch_mma(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to, const CUtensorMap& tz, const Epi& epi, const Grid& g, int rows,
                int cols, int num_sms, const DevCtl& ctl, cudaStream_t st) {
-  auto kern = linear_mma_kernel<BN, A_MN, B_MN, Out>;
-  constexpr int bytes = static_cast<int>(Layout<BN>::BYTES);
+  auto kern = linear_mma_kernel<CTAS, BN, A_MN, B_MN, Out>;
+  constexpr int bytes = static_cast<int>(Layout<CTAS, BN>::BYTES);
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return -1;
-  const long long units = static_cast<long long>(g.m_tiles) * g.n_tiles * g.parts;
-  kern<<<static_cast<int>(units < num_sms ? units : num_sms), kThreads, bytes, st>>>(ta, tb, to, tz, epi, g, rows, cols, ctl);
-  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+  const long long units = static_cast<long long>(g.m_tiles) * g.n_tiles * g.parts, most = num_sms / CTAS;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(units < most ? units : most) * CTAS);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = CTAS;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = CTAS > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kern, ta, tb, to, tz, epi, g, rows, cols, ctl) == cudaSuccess ? 1 : -1;
 }
 
 // D [rows][cols] = sum over `sum`; a is [rows][sum] or, A_MN, [sum][rows]; b likewise.
 template <bool A_MN, bool B_MN>
 int product(const void* a, const void* b, int rows, int cols, int sum, const Epi& epi, void* out, bool out_f32, void* z, float* partial,
             int num_sms, const DevCtl& ctl, cudaStream_t st) {
-  const Cut cut = cut_of(rows, cols, sum, num_sms);
+  const Cut cut = cut_of(rows, cols, sum, B_MN, num_sms);
   CUtensorMap ta, tb, to, tz;
   if (!(A_MN ? make_tmap_bf16_3d(&ta, a, rows, sum, 1, 64) : make_tmap_bf16_3d(&ta, a, sum, rows, 1, BM))) return -1;
-  if (!(B_MN ? make_tmap_bf16_3d(&tb, b, cols, sum, 1, 64) : make_tmap_bf16_3d(&tb, b, sum, cols, 1, cut.bn))) return -1;
+  if (!(B_MN ? make_tmap_bf16_3d(&tb, b, cols, sum, 1, 64) : make_tmap_bf16_3d(&tb, b, sum, cols, 1, cut.bn / cut.ctas))) return -1;
   const bool f32 = out_f32 || cut.parts > 1;
   if (!make_out_map(&to, cut.parts > 1 ? partial : out, f32, cols, rows, cut.parts)) return -1;
   tz = to;
   if (epi.keep && cut.parts == 1 && !make_out_map(&tz, z, false, cols, rows, 1)) return -1;
-  const Grid g{(rows + BM - 1) / BM, (cols + cut.bn - 1) / cut.bn, cut.parts, (sum + BK - 1) / BK};
-  int n;
-  if (cut.bn == 256)
-    n = f32 ? launch_mma<256, A_MN, B_MN, float>(ta, tb, to, tz, epi, g, rows, cols, num_sms, ctl, st)
-            : launch_mma<256, A_MN, B_MN, __nv_bfloat16>(ta, tb, to, tz, epi, g, rows, cols, num_sms, ctl, st);
-  else
-    n = f32 ? launch_mma<128, A_MN, B_MN, float>(ta, tb, to, tz, epi, g, rows, cols, num_sms, ctl, st)
-            : launch_mma<128, A_MN, B_MN, __nv_bfloat16>(ta, tb, to, tz, epi, g, rows, cols, num_sms, ctl, st);
+  const int tile = BM * cut.ctas;
+  const Grid g{(rows + tile - 1) / tile, (cols + cut.bn - 1) / cut.bn, cut.parts, (sum + BK - 1) / BK};
+  auto go = [&](auto ctas, auto bn) {
+    constexpr int C = decltype(ctas)::value, W = decltype(bn)::value;
+    return f32 ? launch_mma<C, W, A_MN, B_MN, float>(ta, tb, to, tz, epi, g, rows, cols, num_sms, ctl, st)
+               : launch_mma<C, W, A_MN, B_MN, __nv_bfloat16>(ta, tb, to, tz, epi, g, rows, cols, num_sms, ctl, st);
+  };
+  using One = std::integral_constant<int, 1>;
+  using Two = std::integral_constant<int, 2>;
+  int n = -1;
+  if (cut.ctas == 1) {
+    n = go(One(), std::integral_constant<int, 128>());
+  } else if (cut.bn == 256) {
+    n = go(Two(), std::integral_constant<int, 256>());
+  } else if (cut.bn == 128) {
+    n = go(Two(), std::integral_constant<int, 128>());
+  } else if constexpr (!B_MN) {
+    n = go(Two(), std::integral_constant<int, 192>());
+  }
   if (n < 0 || cut.parts == 1) return n;
   const long long MN = static_cast<long long>(rows) * cols;
   const int blocks = static_cast<int>((MN / 8 + 255) / 256);
@@ -593,8 +766,8 @@ int product(const void* a, const void* b, int rows, int cols, int sum, const Epi
   return cudaGetLastError() == cudaSuccess ? n + 1 : -1;
 }
 
-size_t partial_bytes(int rows, int cols, int sum, int num_sms) {
-  const Cut c = cut_of(rows, cols, sum, num_sms);
+size_t partial_bytes(int rows, int cols, int sum, bool b_mn, int num_sms) {
+  const Cut c = cut_of(rows, cols, sum, b_mn, num_sms);
   return c.parts > 1 ? static_cast<size_t>(c.parts) * rows * cols * sizeof(float) : 0;
 }
 
@@ -609,7 +782,7 @@ int launch_few(const LinearArgs& a, const Epi& epi, cudaStream_t st) {
 
 }  // namespace
 
-size_t linear_fwd_workspace_bytes(int M, int N, int K, int num_sms) { return M <= kFewRows ? 0 : partial_bytes(M, N, K, num_sms); }
+size_t linear_fwd_workspace_bytes(int M, int N, int K, int num_sms) { return M <= kFewRows ? 0 : partial_bytes(M, N, K, false, num_sms); }
 
 int linear_fwd(const LinearArgs& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
   const Epi epi{static_cast<const __nv_bfloat16*>(a.bias), static_cast<const __nv_bfloat16*>(a.residual), a.act, a.z != nullptr};
@@ -625,7 +798,7 @@ int linear_fwd(const LinearArgs& a, void* workspace, int num_sms, const DevCtl& 
 size_t linear_bwd_workspace_bytes(int M, int N, int K, int act, int num_sms) {
   const size_t dz = act == kActNone ? 0 : round256(static_cast<size_t>(M) * N * 2);
   const size_t db = round256(static_cast<size_t>((M + kDzRows - 1) / kDzRows) * N * sizeof(float));
-  const size_t p1 = partial_bytes(M, K, N, num_sms), p2 = partial_bytes(N, K, M, num_sms);
+  const size_t p1 = partial_bytes(M, K, N, true, num_sms), p2 = partial_bytes(N, K, M, true, num_sms);
   return dz + db + (p1 > p2 ? p1 : p2);
 }
 
