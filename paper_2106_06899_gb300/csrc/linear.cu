@@ -226,16 +226,36 @@ __device__ __forceinline__ void unpack8(uint4 u, float (&v)[8]) {
 
 __device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
 
+// The normal distribution's Phi(z), to 1e-7: with x = |z| / sqrt(2) and t = 1 / (1 + 0.3275911 x),
+// erfc(x) = t (a1 + t (a2 + ..)) e^(-x^2) (Abramowitz and Stegun, 7.1.26).  e^(-x^2) = e^(-z^2/2) is returned too.
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float x = fabsf(z) * 0.70710678f, t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
+  e = __expf(-x * x);
+  float q = fmaf(t, 1.061405429f, -1.453152027f);
+  q = fmaf(t, q, 1.421413741f);
+  q = fmaf(t, q, -0.284496736f);
+  q = fmaf(t, q, 0.254829592f);
+  q *= 0.5f * t * e;  // half of erfc
+  return z > 0.f ? 1.f - q : q;
+}
+
 __device__ __forceinline__ float act_of(float z, int act) {
   if (act == kActRelu) return z < 0.f ? 0.f : z;  // a NaN stays
-  if (act == kActGelu) return 0.5f * z * (1.f + erff(z * 0.70710678f));
+  if (act == kActGelu) {
+    float e;
+    return z * normal_cdf(z, e);
+  }
   if (act == kActSilu) return z * sigmoid(z);
   return z;
 }
 
 __device__ __forceinline__ float act_slope(float z, int act) {
   if (act == kActRelu) return z > 0.f ? 1.f : 0.f;
-  if (act == kActGelu) return 0.5f * (1.f + erff(z * 0.70710678f)) + z * 0.39894228f * __expf(-0.5f * z * z);
+  if (act == kActGelu) {
+    float e;
+    const float phi = normal_cdf(z, e);
+    return phi + z * 0.39894228f * e;
+  }
   if (act == kActSilu) {
     const float s = sigmoid(z);
     return s * (1.f + z * (1.f - s));
@@ -393,10 +413,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else {
     // ------------------------------------------------------------ epilogue
+    // A warp has 32 rows (its quarter of TMEM's lanes) and every other chunk of columns.
     const int quad = warp & 3, half = (warp - 2) >> 2;
     uint8_t* stage = smem + L::OFF_EPI + static_cast<size_t>(warp - 2) * L::EPI;
     uint8_t* row_s = stage + lane * 128;
     constexpr int COLS = sizeof(Out) == 2 ? 64 : 32;  // columns of a staged 128-byte row
+    constexpr int CHUNKS = BN / COLS / 2;             // of a warp
     // Stages 128 bytes a row (sixteen-byte chunk c at c ^ (row & 7)) and stores the 32 rows.
     auto put = [&](const CUtensorMap& map, const uint32_t (&w)[32], int col, int row0, int part) {
       if (lane == 0) bulk_wait_read();  // the buffer's previous store has been read
@@ -411,23 +433,46 @@ __global__ void __launch_bounds__(kThreads, 1)
         bulk_commit();
       }
     };
+    const bool has_residual = sizeof(Out) == 2 && epi.residual;
     uint32_t tile = 0;
     for (int u = unit0; u < units; u += stride, ++tile) {
       int mt, nt, part;
       unit_of(grid, u, mt, nt, part);
       const uint32_t buf = tile & 1u;
+      const int row0 = (mt * CTAS + rank) * BM + quad * 32, row = row0 + lane;
+      // the residual's chunk is loaded before the accumulator is there
+      uint4 res[8];
+      auto load_residual = [&](int col) {
+        if (!has_residual || row >= M) return;
+        const uint4* r = reinterpret_cast<const uint4*>(epi.residual + static_cast<size_t>(row) * N + col);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (col + 8 * e < N) res[e] = __ldg(r + e);
+      };
+      load_residual(nt * BN + half * COLS);
       if (!warp_wait<CTAS>(&acc_full[buf], (tile >> 1) & 1u, ctl, abort_flag)) break;
       tc_fence_after();
-      const int row0 = (mt * CTAS + rank) * BM + quad * 32, row = row0 + lane;
       const uint32_t taddr = tmem_base + buf * BN + (static_cast<uint32_t>(quad * 32) << 16);
+      // the accumulator is free for the next tile but one when its last chunk is in registers
+      auto release = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (CTAS == 2)
+            arrive_cluster(leader_bar(&acc_empty[buf]));
+          else
+            mbar_arrive(&acc_empty[buf]);
+        }
+      };
 #pragma unroll 1
-      for (int c = half; c < BN / COLS; c += 2) {
-        const int col = nt * BN + c * COLS;
+      for (int i = 0; i < CHUNKS; ++i) {
+        const int c = 2 * i + half, col = nt * BN + c * COLS;
         uint32_t w[32];
         if constexpr (sizeof(Out) == 4) {
           float v[32];
           tmem_ld32(taddr + c * COLS, v);
           tmem_wait_ld();
+          if (i == CHUNKS - 1) release();
 #pragma unroll
           for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(v[e]);
           if (row0 < M && col < N) put(tmo, w, col, row0, part);
@@ -435,6 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           float v[64];
           tmem_ld64(taddr + c * COLS, v);
           tmem_wait_ld();
+          if (i == CHUNKS - 1) release();
           if (row0 >= M || col >= N) continue;
           if (epi.bias) {
 #pragma unroll
@@ -462,30 +508,20 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int e = 0; e < 64; ++e) v[e] = act_of(v[e], kActSilu);
           }
-          if (epi.residual && row < M) {
-            const uint4* r = reinterpret_cast<const uint4*>(epi.residual + static_cast<size_t>(row) * N + col);
+          if (has_residual) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              if (col + 8 * e < N) {
-                float b[8];
-                unpack8(__ldg(r + e), b);
+              float b[8];
+              unpack8(res[e], b);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[8 * e + i] += b[i];
-              }
+              for (int i = 0; i < 8; ++i) v[8 * e + i] += b[i];  // rows and columns beyond the edge are not stored
             }
+            if (i + 1 < CHUNKS) load_residual(col + 2 * COLS);
           }
 #pragma unroll
           for (int e = 0; e < 32; ++e) w[e] = pack2(v[2 * e], v[2 * e + 1]);
           put(tmo, w, col, row0, 0);
         }
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if constexpr (CTAS == 2)
-          arrive_cluster(leader_bar(&acc_empty[buf]));
-        else
-          mbar_arrive(&acc_empty[buf]);
       }
     }
     if (lane == 0) bulk_wait_all();
@@ -671,34 +707,32 @@ bool make_out_map(CUtensorMap* map, const void* base, bool f32, uint64_t cols, u
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// What a tile costs beside its columns, in columns: a narrow one reads A for fewer products, a single CTA all of B.
-constexpr double kTileCost(int ctas, int bn) { return ctas == 1 ? 48.0 : (bn == 256 ? 0.0 : 16.0); }
-
 // How a product is cut: CTAs and width of a tile, parts of the sum.
 struct Cut {
   int ctas, bn, parts;
 };
 
-// `out_rows` x `out_cols`, summed over `sum`; `places`: SMs.
-Cut cut_of(int out_rows, int out_cols, int sum, bool b_mn, int places) {
+// `out_rows` x `out_cols`, summed over `sum`.  The cut with the least estimated time, in microseconds as measured: a
+// block of 64 of the sum takes 0.36 on a 256 x 256 tile of a pair, 0.40 on 128 x 256, and 0.33 on 128 x 128 (the
+// tensor pipe runs at half rate for 128 columns); a split sum writes and reads its partial tiles (about 5 TB/s) and
+// takes another launch (3).
+Cut cut_of(int out_rows, int out_cols, int sum, int num_sms) {
+  constexpr Cut kCuts[3] = {{2, 256, 1}, {1, 256, 1}, {1, 128, 1}};
+  constexpr double kBlock[3] = {0.36, 0.40, 0.33};
   const int kb = (sum + BK - 1) / BK;
-  Cut best{1, 128, 1};
+  Cut best = kCuts[0];
   double least = 1e30;
-  long long best_tiles = 1;
-  for (const Cut& c : {Cut{2, 256, 1}, Cut{2, 192, 1}, Cut{2, 128, 1}, Cut{1, 128, 1}}) {
-    if (c.bn == 192 && b_mn) continue;  // half of 192 is no whole number of 64-wide boxes
-    const int rows = BM * c.ctas;
-    const long long tiles = static_cast<long long>((out_rows + rows - 1) / rows) * ((out_cols + c.bn - 1) / c.bn);
-    const long long units = places / c.ctas;
-    const double cost = static_cast<double>((tiles + units - 1) / units) * (c.bn + kTileCost(c.ctas, c.bn));
-    if (cost < least) least = cost, best = c, best_tiles = tiles;
-  }
-  // a part has at least eight blocks of the sum, so that its loads outlast its partial tile's store
-  const long long units = places / best.ctas;
-  if (best_tiles * 2 <= units) {
-    long long p = units / best_tiles;
-    if (p > kb / 8) p = kb / 8;
-    best.parts = p < 1 ? 1 : static_cast<int>(p);
+  for (int i = 0; i < 3; ++i) {
+    const int rows = BM * kCuts[i].ctas;
+    const long long tiles = static_cast<long long>((out_rows + rows - 1) / rows) * ((out_cols + kCuts[i].bn - 1) / kCuts[i].bn);
+    const long long places = num_sms / kCuts[i].ctas;
+    // more parts than fill the places once do not pay; a part has at least four blocks
+    for (int p = 1; p == 1 || (p <= kb / 4 && tiles * (p - 1) < places); ++p) {
+      const double waves = static_cast<double>((tiles * p + places - 1) / places);
+      double us = waves * ((kb + p - 1) / p) * kBlock[i];
+      if (p > 1) us += 3.0 + static_cast<double>(p) * out_rows * out_cols * 8.0 / 5e6;
+      if (us < least) least = us, best = kCuts[i], best.parts = p;
+    }
   }
   return best;
 }
@@ -728,7 +762,7 @@ int launch_mma(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& 
 template <bool A_MN, bool B_MN>
 int product(const void* a, const void* b, int rows, int cols, int sum, const Epi& epi, void* out, bool out_f32, void* z, float* partial,
             int num_sms, const DevCtl& ctl, cudaStream_t st) {
-  const Cut cut = cut_of(rows, cols, sum, B_MN, num_sms);
+  const Cut cut = cut_of(rows, cols, sum, num_sms);
   CUtensorMap ta, tb, to, tz;
   if (!(A_MN ? make_tmap_bf16_3d(&ta, a, rows, sum, 1, 64) : make_tmap_bf16_3d(&ta, a, sum, rows, 1, BM))) return -1;
   if (!(B_MN ? make_tmap_bf16_3d(&tb, b, cols, sum, 1, 64) : make_tmap_bf16_3d(&tb, b, sum, cols, 1, cut.bn / cut.ctas))) return -1;
@@ -745,16 +779,9 @@ int product(const void* a, const void* b, int rows, int cols, int sum, const Epi
   };
   using One = std::integral_constant<int, 1>;
   using Two = std::integral_constant<int, 2>;
-  int n = -1;
-  if (cut.ctas == 1) {
-    n = go(One(), std::integral_constant<int, 128>());
-  } else if (cut.bn == 256) {
-    n = go(Two(), std::integral_constant<int, 256>());
-  } else if (cut.bn == 128) {
-    n = go(Two(), std::integral_constant<int, 128>());
-  } else if constexpr (!B_MN) {
-    n = go(Two(), std::integral_constant<int, 192>());
-  }
+  const int n = cut.ctas == 2   ? go(Two(), std::integral_constant<int, 256>())
+                : cut.bn == 256 ? go(One(), std::integral_constant<int, 256>())
+                                : go(One(), std::integral_constant<int, 128>());
   if (n < 0 || cut.parts == 1) return n;
   const long long MN = static_cast<long long>(rows) * cols;
   const int blocks = static_cast<int>((MN / 8 + 255) / 256);
@@ -766,8 +793,8 @@ int product(const void* a, const void* b, int rows, int cols, int sum, const Epi
   return cudaGetLastError() == cudaSuccess ? n + 1 : -1;
 }
 
-size_t partial_bytes(int rows, int cols, int sum, bool b_mn, int num_sms) {
-  const Cut c = cut_of(rows, cols, sum, b_mn, num_sms);
+size_t partial_bytes(int rows, int cols, int sum, int num_sms) {
+  const Cut c = cut_of(rows, cols, sum, num_sms);
   return c.parts > 1 ? static_cast<size_t>(c.parts) * rows * cols * sizeof(float) : 0;
 }
 
@@ -782,7 +809,7 @@ int launch_few(const LinearArgs& a, const Epi& epi, cudaStream_t st) {
 
 }  // namespace
 
-size_t linear_fwd_workspace_bytes(int M, int N, int K, int num_sms) { return M <= kFewRows ? 0 : partial_bytes(M, N, K, false, num_sms); }
+size_t linear_fwd_workspace_bytes(int M, int N, int K, int num_sms) { return M <= kFewRows ? 0 : partial_bytes(M, N, K, num_sms); }
 
 int linear_fwd(const LinearArgs& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
   const Epi epi{static_cast<const __nv_bfloat16*>(a.bias), static_cast<const __nv_bfloat16*>(a.residual), a.act, a.z != nullptr};
@@ -798,7 +825,7 @@ int linear_fwd(const LinearArgs& a, void* workspace, int num_sms, const DevCtl& 
 size_t linear_bwd_workspace_bytes(int M, int N, int K, int act, int num_sms) {
   const size_t dz = act == kActNone ? 0 : round256(static_cast<size_t>(M) * N * 2);
   const size_t db = round256(static_cast<size_t>((M + kDzRows - 1) / kDzRows) * N * sizeof(float));
-  const size_t p1 = partial_bytes(M, K, N, true, num_sms), p2 = partial_bytes(N, K, M, true, num_sms);
+  const size_t p1 = partial_bytes(M, K, N, num_sms), p2 = partial_bytes(N, K, M, num_sms);
   return dz + db + (p1 > p2 ? p1 : p2);
 }
 
