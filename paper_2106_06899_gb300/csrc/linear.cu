@@ -40,12 +40,12 @@ template <int CTAS, int BN>
 struct Layout {
   static constexpr uint32_t A_BYTES = BM * BK * 2, B_BYTES = BN / CTAS * BK * 2;
   static constexpr uint32_t STAGE = A_BYTES + B_BYTES;
-  static constexpr uint32_t EPI = 4096;  // a warp's 32 rows of 128 bytes
+  static constexpr uint32_t EPI = 2 * 4096;  // a warp's two buffers of 32 rows of 128 bytes
   static constexpr int FIT = (232448 - 2048 - kEpiWarps * EPI) / STAGE;
   static constexpr int S = FIT > 6 ? 6 : FIT;
   static constexpr size_t OFF_EPI = static_cast<size_t>(S) * STAGE;
   static constexpr size_t OFF_BAR = OFF_EPI + kEpiWarps * EPI;
-  static constexpr int NBARS = 2 * S + 5;  // full/empty per stage, accumulator full/empty x 2, drain
+  static constexpr int NBARS = 2 * S + 5 + 2 * kEpiWarps;  // full/empty per stage, accumulator full/empty x 2, drain, residual
   static constexpr size_t BYTES = 1024 + OFF_BAR + NBARS * 8 + 16;
   static constexpr uint32_t TMEM_COLS = 2 * BN <= 256 ? 256 : 512;
   static_assert(BYTES <= 232448 && S >= 3, "shared memory");
@@ -210,7 +210,11 @@ __device__ __forceinline__ void tma_store_3d(const void* map, const void* smem, 
 }
 
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+// Waits until all but the last PENDING groups have read their shared memory.
+template <int PENDING>
+__device__ __forceinline__ void bulk_wait_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory");
+}
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -224,18 +228,30 @@ __device__ __forceinline__ void unpack8(uint4 u, float (&v)[8]) {
   for (int e = 0; e < 4; ++e) v[2 * e] = __uint_as_float(w[e] << 16), v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
 }
 
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+// The hardware's 2^x and 1 / x, to 2^-22; results below 2^-126 are zero.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ float sigmoid(float z) { return rcp_fast(1.f + exp2_fast(z * -1.44269504f)); }
 
 // The normal distribution's Phi(z), to 1e-7: with x = |z| / sqrt(2) and t = 1 / (1 + 0.3275911 x),
-// erfc(x) = t (a1 + t (a2 + ..)) e^(-x^2) (Abramowitz and Stegun, 7.1.26).  e^(-x^2) = e^(-z^2/2) is returned too.
+// erfc(x) = t (a1 + t (a2 + ..)) e^(-x^2) (Abramowitz and Stegun, 7.1.26); half of it is Phi(-|z|).  e = e^(-z^2/2).
 __device__ __forceinline__ float normal_cdf(float z, float& e) {
-  const float x = fabsf(z) * 0.70710678f, t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
-  e = __expf(-x * x);
-  float q = fmaf(t, 1.061405429f, -1.453152027f);
-  q = fmaf(t, q, 1.421413741f);
-  q = fmaf(t, q, -0.284496736f);
-  q = fmaf(t, q, 0.254829592f);
-  q *= 0.5f * t * e;  // half of erfc
+  const float t = rcp_fast(fabsf(z) * 0.23164188f + 1.f);
+  e = exp2_fast(z * z * -0.72134752f);
+  float q = fmaf(t, 0.5307027145f, -0.7265760135f);
+  q = fmaf(t, q, 0.7107068705f);
+  q = fmaf(t, q, -0.142248368f);
+  q = fmaf(t, q, 0.127414796f);
+  q = q * t * e;
   return z > 0.f ? 1.f - q : q;
 }
 
@@ -291,8 +307,8 @@ __device__ __forceinline__ void unit_of(const Grid& g, int u, int& mt, int& nt, 
 template <int CTAS, int BN, bool A_MN, bool B_MN, typename Out>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_mma_kernel(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUtensorMap tmb,
-                      const __grid_constant__ CUtensorMap tmo, const __grid_constant__ CUtensorMap tmz, Epi epi, Grid grid, int M,
-                      int N, DevCtl ctl) {
+                      const __grid_constant__ CUtensorMap tmo, const __grid_constant__ CUtensorMap tmz,
+                      const __grid_constant__ CUtensorMap tmr, Epi epi, Grid grid, int M, int N, DevCtl ctl) {
   using L = Layout<CTAS, BN>;
   constexpr int S = L::S, NB = BN / CTAS;  // NB: rows of B that a CTA stages
   constexpr uint32_t IDESC = idesc_bf16_f32(BM * CTAS, BN) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
@@ -307,6 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* acc_full = bars + 2 * S;       // [2]
   uint64_t* acc_empty = bars + 2 * S + 2;  // [2], the first CTA's are used
   uint64_t* drain = bars + 2 * S + 4;
+  uint64_t* res_full = bars + 2 * S + 5;   // [warp][2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::NBARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -322,6 +339,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&acc_empty[b], kEpiWarps * CTAS);
     }
     mbar_init(drain, 1);
+    for (int b = 0; b < 2 * kEpiWarps; ++b) mbar_init(&res_full[b], 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -413,43 +431,59 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else {
     // ------------------------------------------------------------ epilogue
-    // A warp has 32 rows (its quarter of TMEM's lanes) and every other chunk of columns.
+    // A warp has 32 rows (its quarter of TMEM's lanes) and every other chunk of columns, staged in two buffers in
+    // turn: 128 bytes a row, sixteen-byte chunk c at c ^ (row & 7).  A residual is loaded into the
+    // buffer its results will take, before the accumulator is there (TMA: a lane's own row would be 32 lines a load).
     const int quad = warp & 3, half = (warp - 2) >> 2;
     uint8_t* stage = smem + L::OFF_EPI + static_cast<size_t>(warp - 2) * L::EPI;
-    uint8_t* row_s = stage + lane * 128;
+    uint64_t* res_bar = res_full + 2 * (warp - 2);
     constexpr int COLS = sizeof(Out) == 2 ? 64 : 32;  // columns of a staged 128-byte row
     constexpr int CHUNKS = BN / COLS / 2;             // of a warp
-    // Stages 128 bytes a row (sixteen-byte chunk c at c ^ (row & 7)) and stores the 32 rows.
-    auto put = [&](const CUtensorMap& map, const uint32_t (&w)[32], int col, int row0, int part) {
-      if (lane == 0) bulk_wait_read();  // the buffer's previous store has been read
-      __syncwarp();
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        *reinterpret_cast<uint4*>(row_s + ((c ^ (lane & 7)) << 4)) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+    uint32_t puts = 0;                                // buffers used so far
+    auto row_of = [&](uint32_t b) { return stage + (b & 1u) * 4096u + lane * 128; };
+    // Stores buffer `b`, which this warp has filled.
+    auto store = [&](const CUtensorMap& map, uint32_t b, int col, int row0, int part) {
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
-        tma_store_3d(&map, stage, col, row0, part);
+        tma_store_3d(&map, stage + (b & 1u) * 4096u, col, row0, part);
         bulk_commit();
       }
     };
+    auto put = [&](const CUtensorMap& map, const uint32_t (&w)[32], int col, int row0, int part) {
+      const uint32_t b = puts++;
+      if (lane == 0) bulk_wait_read<1>();  // the buffer's previous store has been read
+      __syncwarp();
+      uint8_t* row_s = row_of(b);
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        *reinterpret_cast<uint4*>(row_s + ((c ^ (lane & 7)) << 4)) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+      store(map, b, col, row0, part);
+    };
     const bool has_residual = sizeof(Out) == 2 && epi.residual;
+    const bool early = has_residual && !epi.keep;  // the kept pre-activations take the buffers first
+    uint32_t loads = 0, waits = 0;                 // residual chunks asked for, and waited for
+    auto load_residual = [&](int col, int row0) {
+      if (lane == 0) {
+        bulk_wait_read<0>();
+        uint64_t* bar = &res_bar[loads & 1u];
+        mbar_arrive_expect_tx(bar, 4096);
+        tma_load_3d(stage + (loads & 1u) * 4096u, &tmr, bar, col, row0, 0);
+      }
+      ++loads;
+    };
     uint32_t tile = 0;
     for (int u = unit0; u < units; u += stride, ++tile) {
       int mt, nt, part;
       unit_of(grid, u, mt, nt, part);
       const uint32_t buf = tile & 1u;
-      const int row0 = (mt * CTAS + rank) * BM + quad * 32, row = row0 + lane;
-      // the residual's chunk is loaded before the accumulator is there
-      uint4 res[8];
-      auto load_residual = [&](int col) {
-        if (!has_residual || row >= M) return;
-        const uint4* r = reinterpret_cast<const uint4*>(epi.residual + static_cast<size_t>(row) * N + col);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (col + 8 * e < N) res[e] = __ldg(r + e);
-      };
-      load_residual(nt * BN + half * COLS);
+      const int row0 = (mt * CTAS + rank) * BM + quad * 32;
+      if (early && row0 < M) {
+        for (int i = 0; i < CHUNKS; ++i) {
+          const int col = nt * BN + (2 * i + half) * COLS;
+          if (col < N) load_residual(col, row0);
+        }
+      }
       if (!warp_wait<CTAS>(&acc_full[buf], (tile >> 1) & 1u, ctl, abort_flag)) break;
       tc_fence_after();
       const uint32_t taddr = tmem_base + buf * BN + (static_cast<uint32_t>(quad * 32) << 16);
@@ -489,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 float b[8];
                 unpack8(__ldg(reinterpret_cast<const uint4*>(epi.bias + col) + e), b);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[8 * e + i] += b[i];
+                for (int j = 0; j < 8; ++j) v[8 * e + j] += b[j];
               }
             }
           }
@@ -509,21 +543,31 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int e = 0; e < 64; ++e) v[e] = act_of(v[e], kActSilu);
           }
           if (has_residual) {
+            if (!early) load_residual(col, row0);
+            const uint32_t b = waits++;
+            if (!warp_wait<1>(&res_bar[b & 1u], (b >> 1) & 1u, ctl, abort_flag)) break;
+            __syncwarp();
+            uint8_t* row_s = row_of(b);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              float b[8];
-              unpack8(res[e], b);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) v[8 * e + i] += b[i];  // rows and columns beyond the edge are not stored
+              uint4* at = reinterpret_cast<uint4*>(row_s + ((e ^ (lane & 7)) << 4));
+              float r[8];
+              unpack8(*at, r);
+              *at = make_uint4(pack2(v[8 * e] + r[0], v[8 * e + 1] + r[1]), pack2(v[8 * e + 2] + r[2], v[8 * e + 3] + r[3]),
+                               pack2(v[8 * e + 4] + r[4], v[8 * e + 5] + r[5]), pack2(v[8 * e + 6] + r[6], v[8 * e + 7] + r[7]));
             }
-            if (i + 1 < CHUNKS) load_residual(col + 2 * COLS);
-          }
+            store(tmo, b, col, row0, 0);
+          } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) w[e] = pack2(v[2 * e], v[2 * e + 1]);
-          put(tmo, w, col, row0, 0);
+            for (int e = 0; e < 32; ++e) w[e] = pack2(v[2 * e], v[2 * e + 1]);
+            put(tmo, w, col, row0, 0);
+          }
         }
       }
     }
+    // residual loads that no chunk waited for (a wait ran out) must land before the CTA exits
+    if (lane == 0)
+      for (; waits < loads; ++waits) drain_wait(&res_bar[waits & 1u], (waits >> 1) & 1u, ctl);
     if (lane == 0) bulk_wait_all();
     __syncwarp();
   }
@@ -738,7 +782,7 @@ Cut cut_of(int out_rows, int out_cols, int sum, int num_sms) {
 }
 
 template <int CTAS, int BN, bool A_MN, bool B_MN, typename Out>
-int launch_mma(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to, const CUtensorMap& tz, const Epi& epi, const Grid& g, int rows,
+int launch_mma(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to, const CUtensorMap& tz, const CUtensorMap& tr, const Epi& epi, const Grid& g, int rows,
                int cols, int num_sms, const DevCtl& ctl, cudaStream_t st) {
   auto kern = linear_mma_kernel<CTAS, BN, A_MN, B_MN, Out>;
   constexpr int bytes = static_cast<int>(Layout<CTAS, BN>::BYTES);
@@ -755,7 +799,7 @@ int launch_mma(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& 
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = CTAS > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kern, ta, tb, to, tz, epi, g, rows, cols, ctl) == cudaSuccess ? 1 : -1;
+  return cudaLaunchKernelEx(&cfg, kern, ta, tb, to, tz, tr, epi, g, rows, cols, ctl) == cudaSuccess ? 1 : -1;
 }
 
 // D [rows][cols] = sum over `sum`; a is [rows][sum] or, A_MN, [sum][rows]; b likewise.
@@ -763,19 +807,20 @@ template <bool A_MN, bool B_MN>
 int product(const void* a, const void* b, int rows, int cols, int sum, const Epi& epi, void* out, bool out_f32, void* z, float* partial,
             int num_sms, const DevCtl& ctl, cudaStream_t st) {
   const Cut cut = cut_of(rows, cols, sum, num_sms);
-  CUtensorMap ta, tb, to, tz;
+  CUtensorMap ta, tb, to, tz, tr;
   if (!(A_MN ? make_tmap_bf16_3d(&ta, a, rows, sum, 1, 64) : make_tmap_bf16_3d(&ta, a, sum, rows, 1, BM))) return -1;
   if (!(B_MN ? make_tmap_bf16_3d(&tb, b, cols, sum, 1, 64) : make_tmap_bf16_3d(&tb, b, sum, cols, 1, cut.bn / cut.ctas))) return -1;
   const bool f32 = out_f32 || cut.parts > 1;
   if (!make_out_map(&to, cut.parts > 1 ? partial : out, f32, cols, rows, cut.parts)) return -1;
-  tz = to;
+  tz = tr = to;
   if (epi.keep && cut.parts == 1 && !make_out_map(&tz, z, false, cols, rows, 1)) return -1;
+  if (epi.residual && cut.parts == 1 && !make_out_map(&tr, epi.residual, false, cols, rows, 1)) return -1;
   const int tile = BM * cut.ctas;
   const Grid g{(rows + tile - 1) / tile, (cols + cut.bn - 1) / cut.bn, cut.parts, (sum + BK - 1) / BK};
   auto go = [&](auto ctas, auto bn) {
     constexpr int C = decltype(ctas)::value, W = decltype(bn)::value;
-    return f32 ? launch_mma<C, W, A_MN, B_MN, float>(ta, tb, to, tz, epi, g, rows, cols, num_sms, ctl, st)
-               : launch_mma<C, W, A_MN, B_MN, __nv_bfloat16>(ta, tb, to, tz, epi, g, rows, cols, num_sms, ctl, st);
+    return f32 ? launch_mma<C, W, A_MN, B_MN, float>(ta, tb, to, tz, tr, epi, g, rows, cols, num_sms, ctl, st)
+               : launch_mma<C, W, A_MN, B_MN, __nv_bfloat16>(ta, tb, to, tz, tr, epi, g, rows, cols, num_sms, ctl, st);
   };
   using One = std::integral_constant<int, 1>;
   using Two = std::integral_constant<int, 2>;
