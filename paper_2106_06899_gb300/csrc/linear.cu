@@ -17,7 +17,7 @@
 // once, staged in shared memory and stored by TMA, which clips ragged edges.  Few tiles
 // and a long sum (dW, a few hundred tokens) are split along the sum: each part writes
 // fp32 partial tiles, and linear_join_kernel adds them in a fixed order with the same
-// epilogue.  Up to kFewRows tokens (decoding) go to linear_few_kernel, which is
+// epilogue.  A few tokens (decoding) go to linear_few_kernel, which is
 // bound by reading W once.
 #include <cuda_bf16.h>
 
@@ -625,59 +625,74 @@ __global__ void linear_join_kernel(const float* __restrict__ partial, int parts,
 }
 
 // ------------------------------------------------------------ few rows
-constexpr int kFewRows = 16;
+// y for at most 8 F tokens, where reading W once is the work: a block takes 16 rows of W, its eight warps 64 of the
+// sum each in turn, straight from memory into the operand registers of mma.m16n8k16 (W's rows are M, the tokens
+// N): a lane's 16 contiguous bytes of a row serve two steps, as the sum's order is free as long as W and x
+// agree on it.  The warps' sums are added in shared memory, in order.  tcgen05's way through shared memory and TMEM
+// costs 7 us for one tile of K = 768 (this kernel: 2 to 3).
+constexpr int kFewWarps = 8;
 
-// y for up to MR tokens: a warp takes eight rows of W (one 16-byte output a token), reads each
-// once, 512 bytes at a time, and holds 8 x MR sums a lane; x comes from L1.  The kWarps
-// warps of a block share the sum and are added up in shared memory.
-template <int MR, typename Out>
-__global__ void __launch_bounds__(256) linear_few_kernel(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ w, int M, int N,
-                                                         int K, Epi epi, Out* __restrict__ out, __nv_bfloat16* __restrict__ z) {
-  constexpr int kRows = 8 / (MR > 4 ? 2 : 1);  // rows of W a warp walks at a time
-  constexpr int kWarps = 8;
-  __shared__ float sums[kWarps][MR][8];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n0 = blockIdx.x * 8;
+// Up to 16 tokens always (8192 x 8192: 24 to 27 us, 5.5 TB/s; the tiles take 30).  Up to 64 where W is small: each
+// block reads all of x, and 4096 x 1024 weights take 6 to 7 us against 8 to 9 in tiles, 8192 x 8192 75 against 32.
+bool few_rows(int M, int N, int K) { return M <= 16 || (M <= 64 && K <= 1024 && static_cast<long long>(N) * K <= (4 << 20)); }
+
+__device__ __forceinline__ uint4 load_once(const __nv_bfloat16* p) {
+  uint4 u;
+  asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+  return u;
+}
+
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <int F>
+__global__ void __launch_bounds__(kFewWarps * 32) linear_few_kernel(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ w, int M,
+                                                                   int N, int K, Epi epi, __nv_bfloat16* __restrict__ out,
+                                                                   __nv_bfloat16* __restrict__ z) {
+  __shared__ float sums[kFewWarps][16][8 * F + 1];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int n0 = blockIdx.x * 16;
+  const bool upper = n0 + 8 < N;  // N is a multiple of 8: rows 8 to 15 are all there or all not
+  const __nv_bfloat16* w0 = w + static_cast<size_t>(n0 + g) * K + 8 * t;
+  const __nv_bfloat16* w1 = upper ? w0 + static_cast<size_t>(8) * K : w0;
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  float acc[F][4] = {};
+#pragma unroll 2
+  for (int k = warp * 64; k < K; k += kFewWarps * 64) {
+    uint4 a[2][2], b[2][F];
 #pragma unroll
-  for (int pass = 0; pass < 8 / kRows; ++pass) {
-    float acc[kRows][MR] = {};
-    for (int k = (warp * 32 + lane) * 8; k < K; k += kWarps * 256) {
-      uint4 wv[kRows];
+    for (int h = 0; h < 2; ++h) {
+      const int kk = k + 32 * h;
+      const bool in = kk + 8 * t < K;  // K is a multiple of 8
+      a[h][0] = in ? load_once(w0 + kk) : zero;
+      a[h][1] = in && upper ? load_once(w1 + kk) : zero;
 #pragma unroll
-      for (int r = 0; r < kRows; ++r)
-        wv[r] = __ldg(reinterpret_cast<const uint4*>(w + static_cast<size_t>(n0 + pass * kRows + r) * K + k));
-#pragma unroll
-      for (int m = 0; m < MR; ++m) {
-        if (m >= M) break;
-        float xv[8];
-        unpack8(__ldg(reinterpret_cast<const uint4*>(x + static_cast<size_t>(m) * K + k)), xv);
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-          float wf[8];
-          unpack8(wv[r], wf);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) acc[r][m] = fmaf(xv[e], wf[e], acc[r][m]);
-        }
-      }
+      for (int f = 0; f < F; ++f)
+        b[h][f] = in && 8 * f + g < M ? __ldg(reinterpret_cast<const uint4*>(x + static_cast<size_t>(8 * f + g) * K + 8 * t + kk)) : zero;
     }
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int m = 0; m < MR; ++m) {
-        float a = acc[r][m];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-        if (lane == 0) sums[warp][m][pass * kRows + r] = a;
+      for (int f = 0; f < F; ++f) {
+        mma_16x8x16(acc[f], a[h][0].x, a[h][1].x, a[h][0].y, a[h][1].y, b[h][f].x, b[h][f].y);
+        mma_16x8x16(acc[f], a[h][0].z, a[h][1].z, a[h][0].w, a[h][1].w, b[h][f].z, b[h][f].w);
       }
   }
-  __syncthreads();
-  const int m = threadIdx.x;
-  if (m < M) {
-    float v[8] = {};
-    for (int i = 0; i < kWarps; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += sums[i][m][e];
-    finish8(v, epi, out, z, static_cast<size_t>(m) * N + n0, n0);
+  for (int f = 0; f < F; ++f)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[warp][g + (e & 2) * 4][8 * f + 2 * t + (e & 1)] = acc[f][e];
+  __syncthreads();
+  const int m = threadIdx.x >> 1, half = threadIdx.x & 1;  // eight outputs of a token
+  if (m < M && (half == 0 || upper)) {
+    float v[8] = {};
+    for (int i = 0; i < kFewWarps; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += sums[i][8 * half + e][m];
+    finish8(v, epi, out, z, static_cast<size_t>(m) * N + n0 + 8 * half, n0 + 8 * half);
   }
 }
 
@@ -845,24 +860,25 @@ size_t partial_bytes(int rows, int cols, int sum, int num_sms) {
 
 size_t round256(size_t b) { return (b + 255) / 256 * 256; }
 
-template <int MR>
+template <int F>
 int launch_few(const LinearArgs& a, const Epi& epi, cudaStream_t st) {
-  linear_few_kernel<MR, __nv_bfloat16><<<a.N / 8, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(a.x), static_cast<const __nv_bfloat16*>(a.w), a.M,
-                                                                a.N, a.K, epi, static_cast<__nv_bfloat16*>(a.y), static_cast<__nv_bfloat16*>(a.z));
+  linear_few_kernel<F><<<(a.N + 15) / 16, kFewWarps * 32, 0, st>>>(static_cast<const __nv_bfloat16*>(a.x), static_cast<const __nv_bfloat16*>(a.w), a.M, a.N,
+                                                                  a.K, epi, static_cast<__nv_bfloat16*>(a.y), static_cast<__nv_bfloat16*>(a.z));
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 
 }  // namespace
 
-size_t linear_fwd_workspace_bytes(int M, int N, int K, int num_sms) { return M <= kFewRows ? 0 : partial_bytes(M, N, K, num_sms); }
+size_t linear_fwd_workspace_bytes(int M, int N, int K, int num_sms) { return few_rows(M, N, K) ? 0 : partial_bytes(M, N, K, num_sms); }
 
 int linear_fwd(const LinearArgs& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
   const Epi epi{static_cast<const __nv_bfloat16*>(a.bias), static_cast<const __nv_bfloat16*>(a.residual), a.act, a.z != nullptr};
-  if (a.M <= 1) return launch_few<1>(a, epi, st);
-  if (a.M <= 2) return launch_few<2>(a, epi, st);
-  if (a.M <= 4) return launch_few<4>(a, epi, st);
-  if (a.M <= 8) return launch_few<8>(a, epi, st);
-  if (a.M <= kFewRows) return launch_few<kFewRows>(a, epi, st);
+  if (few_rows(a.M, a.N, a.K)) {
+    if (a.M <= 8) return launch_few<1>(a, epi, st);
+    if (a.M <= 16) return launch_few<2>(a, epi, st);
+    if (a.M <= 32) return launch_few<4>(a, epi, st);
+    return launch_few<8>(a, epi, st);
+  }
   return product<false, false>(a.x, a.w, a.M, a.N, a.K, epi, a.y, false, a.z, static_cast<float*>(workspace), num_sms, ctl, st);
 }
 
