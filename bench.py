@@ -774,18 +774,20 @@ DECODER_METRIC = "12-layer decoder training step tokens/s (top-k attention, Sec.
 def run_decoder(args):
     """Forward + backward of the 12-layer decoder (d_model 768, 12 heads, d_ff 3072, top-64 causal
     attention, dense FF) over one sequence of L tokens (--L, default 32768): time per step and peak
-    device memory (PyTorch's allocator plus the library's pool)."""
+    device memory (PyTorch's allocator plus the library's pool); and of the fused decoder (the library's linear
+    layers, normalised and rotated queries and keys), with its AdamW step beside it."""
     import torch
 
     from paper_2106_06899_gb300 import topk as T
     from paper_2106_06899_gb300.decoder import Decoder
+    from paper_2106_06899_gb300.optim import AdamW
 
     torch.cuda.set_device(int(os.environ.get("LOCAL_RANK", "0")))
     L = args.L or 32768
     torch.manual_seed(0)
     results = {}
-    for name, topk in (("top64", 64), ("plain_sdpa", None)):
-        model = Decoder(12, 768, 12, 3072, topk=topk, ffn_topk=None)
+    for name, topk, fused in (("top64", 64, False), ("plain_sdpa", None, False), ("top64_fused", 64, True)):
+        model = Decoder(12, 768, 12, 3072, topk=topk, ffn_topk=None, fused=fused, max_positions=L)
         x = torch.randn(1, L, 768, device="cuda", dtype=torch.bfloat16)
 
         def step():
@@ -809,6 +811,18 @@ def run_decoder(args):
             pool_hi, _ = T.topk_pool_usage()
             results[name] = {"ms_per_step": ms, "tokens_per_s": L / (ms / 1e3),
                              "peak_torch_bytes": torch.cuda.max_memory_allocated(), "peak_library_pool_bytes": pool_hi}
+            if fused:  # the optimizer's step after it, with its moments in 32 bits and in 8
+                for bits in (32, 8):
+                    opt = AdamW(model.parameters(), state_bits=bits)
+                    opt.step()
+                    torch.cuda.synchronize()
+                    e0.record()
+                    for _ in range(args.steps):
+                        opt.step()
+                    e1.record()
+                    torch.cuda.synchronize()
+                    results[name][f"adamw_{bits}bit_ms"] = e0.elapsed_time(e1) / args.steps
+                    del opt
         except torch.OutOfMemoryError:
             results[name] = {"error": "out of device memory"}
         del model, x

@@ -92,32 +92,29 @@ class AdamW:
             grads = [p.grad for p in self.params]
         elif len(grads) != len(self.params):
             raise ValueError("one gradient for each parameter")
-        table, keep, gdt = self._table, [], None
-        for g, n in zip(grads, self._n):
-            if g is None:
-                keep.append(0)
-                continue
-            gdt = gdt or g.dtype
-            if g.dtype != gdt or g.numel() != n or g.device != self.device or not g.is_contiguous():
-                raise ValueError("gradients must be contiguous, of the parameters' sizes and of one dtype")
-            keep.append(g.data_ptr())
-        if gdt is None:
+        table, given = self._table, [g for g in grads if g is not None]
+        if not given:
             return
+        sizes = self._n if len(given) == len(grads) else [n for g, n in zip(grads, self._n) if g is not None]
+        gdt = given[0].dtype
+        if (any(g.dtype != gdt or not g.is_contiguous() or g.device != self.device for g in given)
+                or [g.numel() for g in given] != sizes):
+            raise ValueError("gradients must be contiguous, of the parameters' sizes and device, and of one dtype")
         if gdt not in (torch.float32, torch.bfloat16):
             raise TypeError("gradients must be float32 or bfloat16")
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1
                                        or grad_scale.device != self.device):
             raise ValueError("grad_scale must be one float32 element on the parameters' device")
         table["param"] = [p.data_ptr() for p in self.params]
-        table["grad"] = keep
+        table["grad"] = [0 if g is None else g.data_ptr() for g in grads]
         k = 0
         for group in self.param_groups:
             end = k + len(group["params"])
             table["lr"][k:end], table["weight_decay"][k:end] = group["lr"], group["weight_decay"]
             k = end
         address, count = self._address, len(table)
-        if 0 in keep:  # parameters without a gradient are left alone
-            table = table[np.array(keep) != 0]
+        if len(given) != len(grads):  # parameters without a gradient are left alone
+            table = table[[g is not None for g in grads]]
             address, count = table.ctypes.data, len(table)
         rc = self._step(address, count, self._param_code, T.TOPK_F32 if gdt == torch.float32 else T.TOPK_BF16, self.state_bits,
                         self.betas[0], self.betas[1], self.eps, self.state["step"] + 1, T._ptr(grad_scale),

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 
 import torch
@@ -23,17 +24,6 @@ _lock = threading.Lock()
 _lib = None
 
 
-class _QkArgs(ctypes.Structure):
-    """topk_qk_args"""
-    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "k", "v")]
-                + [(n, ctypes.c_longlong * 3) for n in ("q_stride", "k_stride", "v_stride")]
-                + [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "cos", "sin", "positions")]
-                + [(n, ctypes.c_int) for n in ("table_rows", "B", "L", "Hq", "Hkv", "d", "rot", "axes")]
-                + [("sections", ctypes.c_int * 4)]
-                + [(n, ctypes.c_int) for n in ("interleaved", "normalize", "dtype")]
-                + [(n, ctypes.c_float) for n in ("eps", "q_scale")])
-
-
 class TopkError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -43,6 +33,8 @@ class TopkError(RuntimeError):
 def lib() -> ctypes.CDLL:
     """The loaded libtopk.so.  Raises if it has not been built."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -75,8 +67,8 @@ def lib() -> ctypes.CDLL:
             L.topk_attn_bwd_workspace_bytes.restype = sz
             L.topk_ffn_bwd_workspace_bytes.argtypes = [i32] * 4
             L.topk_ffn_bwd_workspace_bytes.restype = sz
-            L.topk_qk_norm_rope_fwd.argtypes = [ctypes.POINTER(_QkArgs), vp, vp, vp, i32, vp, vp]
-            L.topk_qk_norm_rope_bwd.argtypes = [ctypes.POINTER(_QkArgs), vp, vp, vp, i32, vp, vp, vp, vp]
+            L.topk_qk_norm_rope_fwd.argtypes = [vp, vp, vp, vp, i32, vp, vp]
+            L.topk_qk_norm_rope_bwd.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp]
             L.topk_qk_norm_rope_bwd_workspace_bytes.argtypes = [i32] * 5
             L.topk_qk_norm_rope_bwd_workspace_bytes.restype = sz
             L.topk_linear_fwd.argtypes = [vp] * 6 + [i32] * 4 + [vp]
@@ -116,8 +108,14 @@ def _check(rc: int, where: str) -> None:
         raise TopkError(rc, where)
 
 
+# The current stream's handle without building a Stream object (0.3 us in place of 12).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
     if stream is None:
+        if _raw_stream is not None and torch.cuda.is_initialized():
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
@@ -345,33 +343,47 @@ def rope_tables(positions: int, rot: int, base: float = 10000.0, device="cuda"):
     return angle.cos().float(), angle.sin().float()
 
 
+_QK_PACK = struct.Struct("3P9q5P15i2f4x").pack  # topk_qk_args
+_NO_STRIDE = (0, 0, 0)
+
+
 def _qk_args(q, k, v, cos, sin, positions, q_weight, k_weight, eps, q_scale, sections, interleaved, normalize):
-    for name, t in (("q", q), ("k", k), ("v", v)):
-        if t is not None and (t.dim() != 4 or t.stride(3) != 1):
-            raise ValueError(f"{name} must be a [B, L, H, d] tensor with contiguous rows")
+    """topk_qk_args as bytes, and (B, L, Hq, Hkv, d)."""
+    sq, sk = q.stride(), k.stride()
+    sv = None if v is None else v.stride()
+    if len(sq) != 4 or sq[3] != 1 or len(sk) != 4 or sk[3] != 1 or (v is not None and (len(sv) != 4 or sv[3] != 1)):
+        raise ValueError("q, k and v must be [B, L, H, d] tensors with contiguous rows")
     B, L, Hq, d = q.shape
     Hkv = k.shape[2]
     if tuple(k.shape) != (B, L, Hkv, d) or (v is not None and v.shape != k.shape):
         raise ValueError("shape mismatch between q, k, v")
-    if k.dtype != q.dtype or (v is not None and v.dtype != q.dtype):
+    dtype = q.dtype
+    if k.dtype != dtype or (v is not None and v.dtype != dtype):
         raise TypeError("q, k, v must share a dtype")
-    half = cos.shape[-1]
-    for name, t in (("cos", cos), ("sin", sin)):
-        if t.dtype != torch.float32 or t.dim() != 2 or t.shape != cos.shape or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous [positions, rot / 2] float32 tensor")
-    sections = (half,) if sections is None else tuple(int(n) for n in sections)
-    if not 1 <= len(sections) <= 4:
+    if (cos.dtype != torch.float32 or sin.dtype != torch.float32 or cos.dim() != 2 or sin.shape != cos.shape
+            or not (cos.is_contiguous() and sin.is_contiguous())):
+        raise ValueError("cos and sin must be contiguous [positions, rot / 2] float32 tensors")
+    rows, half = cos.shape
+    sections = (half,) if sections is None else tuple(sections)
+    axes = len(sections)
+    if not 1 <= axes <= 4:
         raise ValueError("sections must name 1 to 4 axes")
-    if positions is not None and (positions.dtype != torch.int32 or tuple(positions.shape) != (len(sections), B, L)
+    if positions is not None and (positions.dtype != torch.int32 or tuple(positions.shape) != (axes, B, L)
                                   or not positions.is_contiguous()):
         raise ValueError("positions must be a contiguous [axes, B, L] int32 tensor")
-    for name, t in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if t is not None and (t.dtype != q.dtype or tuple(t.shape) != (d,) or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous [d] tensor of q's dtype")
-    a = _QkArgs(_ptr(q), _ptr(k), _ptr(v), q.stride()[:3], k.stride()[:3], (0, 0, 0) if v is None else v.stride()[:3],
-                _ptr(q_weight), _ptr(k_weight), _ptr(cos), _ptr(sin), _ptr(positions), cos.shape[0], B, L, Hq, Hkv, d,
-                2 * half, len(sections), sections, int(bool(interleaved)), int(bool(normalize)), _dtype_code(q), eps, q_scale)
-    return a, (B, L, Hq, Hkv, d)
+    for t in (q_weight, k_weight):
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != (d,) or not t.is_contiguous()):
+            raise ValueError("q_weight and k_weight must be contiguous [d] tensors of q's dtype")
+    args = _QK_PACK(q.data_ptr(), k.data_ptr(), _ptr(v) or 0, *sq[:3], *sk[:3], *(_NO_STRIDE if sv is None else sv[:3]),
+                    _ptr(q_weight) or 0, _ptr(k_weight) or 0, cos.data_ptr(), sin.data_ptr(), _ptr(positions) or 0, rows, B, L, Hq, Hkv, d,
+                    2 * half, axes, *sections, *_NO_STRIDE[axes - 1:], 1 if interleaved else 0, 1 if normalize else 0, _dtype_code(q), eps,
+                    q_scale)
+    return args, (B, L, Hq, Hkv, d)
+
+
+def _written(name, t, shape, dtype) -> None:
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {list(shape)} {dtype} tensor")
 
 
 def topk_qk_norm_rope_fwd(q, k, v, cos, sin, q_out, k_out, v_out, *, cache_start=None, positions=None, q_weight=None,
@@ -383,14 +395,13 @@ def topk_qk_norm_rope_fwd(q, k, v, cos, sin, q_out, k_out, v_out, *, cache_start
     a, (B, L, Hq, Hkv, d) = _qk_args(q, k, v, cos, sin, positions, q_weight, k_weight, eps, q_scale, sections, interleaved,
                                      normalize)
     cap = k_out.shape[2]
-    for name, t, shape in (("q_out", q_out, (B, Hq, L, d)), ("k_out", k_out, (B, Hkv, cap, d)),
-                           ("v_out", v_out, (B, Hkv, cap, d))):
-        if t is not None and (t.dtype != q.dtype or tuple(t.shape) != shape or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous {list(shape)} {q.dtype} tensor")
+    _written("q_out", q_out, (B, Hq, L, d), q.dtype)
+    _written("k_out", k_out, (B, Hkv, cap, d), q.dtype)
+    _written("v_out", v_out, (B, Hkv, cap, d), q.dtype)
     if cache_start is not None and (cache_start.dtype != torch.int32 or tuple(cache_start.shape) != (B,)
                                     or not cache_start.is_contiguous()):
         raise ValueError("cache_start must be a [B] int32 tensor")
-    rc = lib().topk_qk_norm_rope_fwd(ctypes.byref(a), _ptr(q_out), _ptr(k_out), _ptr(v_out), cap, _ptr(cache_start),
+    rc = lib().topk_qk_norm_rope_fwd(a, _ptr(q_out), _ptr(k_out), _ptr(v_out), cap, _ptr(cache_start),
                                      _stream(stream))
     _check(rc, "topk_qk_norm_rope_fwd")
 
@@ -402,16 +413,13 @@ def topk_qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, dqkv, dq_weight, dk_weight
     heads without dv) and the norms' weight gradients [d] fp32 (or None)."""
     a, (B, L, Hq, Hkv, d) = _qk_args(q, k, None, cos, sin, positions, q_weight, k_weight, eps, q_scale, sections, interleaved,
                                      normalize)
-    for name, t, h in (("dq", dq, Hq), ("dk", dk, Hkv), ("dv", dv, Hkv)):
-        if t is not None and (t.dtype != dq.dtype or tuple(t.shape) != (B, h, L, d) or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous {[B, h, L, d]} {dq.dtype} tensor")
-    want = (B, L, Hq + (Hkv if dv is None else 2 * Hkv), d)
-    if dqkv.dtype != q.dtype or tuple(dqkv.shape) != want or not dqkv.is_contiguous():
-        raise ValueError(f"dqkv must be a contiguous {list(want)} {q.dtype} tensor")
-    for name, t in (("dq_weight", dq_weight), ("dk_weight", dk_weight)):
-        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (d,) or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous [d] float32 tensor")
-    rc = lib().topk_qk_norm_rope_bwd(ctypes.byref(a), _ptr(dq), _ptr(dk), _ptr(dv), _dtype_code(dq), _ptr(dqkv), _ptr(dq_weight),
+    _written("dq", dq, (B, Hq, L, d), dq.dtype)
+    _written("dk", dk, (B, Hkv, L, d), dq.dtype)
+    _written("dv", dv, (B, Hkv, L, d), dq.dtype)
+    _written("dqkv", dqkv, (B, L, Hq + (Hkv if dv is None else 2 * Hkv), d), q.dtype)
+    _written("dq_weight", dq_weight, (d,), torch.float32)
+    _written("dk_weight", dk_weight, (d,), torch.float32)
+    rc = lib().topk_qk_norm_rope_bwd(a, _ptr(dq), _ptr(dk), _ptr(dv), _dtype_code(dq), _ptr(dqkv), _ptr(dq_weight),
                                      _ptr(dk_weight), _stream(stream))
     _check(rc, "topk_qk_norm_rope_bwd")
 
@@ -589,7 +597,8 @@ def qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, **options):
     dqkv = torch.empty(B, L, Hq + (Hkv if dv is None else 2 * Hkv), d, dtype=q.dtype, device=q.device)
     gq = gk = None
     if options.get("normalize", True):
-        gq, gk = (torch.empty(d, dtype=torch.float32, device=q.device) for _ in range(2))
+        both = torch.empty(2, d, dtype=torch.float32, device=q.device)
+        gq, gk = both[0], both[1]
     topk_qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, dqkv, gq, gk, **options)
     return dqkv, gq, gk
 

@@ -14,12 +14,34 @@ def lib():
     return T.lib()
 
 
+class _QkArgs(ctypes.Structure):
+    """topk_qk_args"""
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "k", "v")]
+                + [(n, ctypes.c_longlong * 3) for n in ("q_stride", "k_stride", "v_stride")]
+                + [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "cos", "sin", "positions")]
+                + [(n, ctypes.c_int) for n in ("table_rows", "B", "L", "Hq", "Hkv", "d", "rot", "axes")]
+                + [("sections", ctypes.c_int * 4)]
+                + [(n, ctypes.c_int) for n in ("interleaved", "normalize", "dtype")]
+                + [(n, ctypes.c_float) for n in ("eps", "q_scale")])
+
+
+def test_qk_record_matches_the_header():
+    # the binding packs topk_qk_args as bytes; the same values through the header's layout
+    values = [1, 2, 3, *range(10, 19), 4, 5, 6, 7, 8, *range(20, 28), *range(30, 34), 1, 0, 1, 0.5, 0.25]
+    fields, at = [], 0
+    for name, kind in _QkArgs._fields_:
+        n = getattr(kind, "_length_", 0)
+        fields.append(tuple(values[at:at + n]) if n else values[at])
+        at += n or 1
+    assert bytes(_QkArgs(*fields)) == T._QK_PACK(*values)
+
+
 def _qk(**kw):
     a = dict(q=16, k=16, v=16, q_stride=(64, 64, 64), k_stride=(64, 64, 64), v_stride=(64, 64, 64), q_weight=None, k_weight=None,
              cos=16, sin=16, positions=None, table_rows=8, B=1, L=8, Hq=2, Hkv=1, d=64, rot=64, axes=1, sections=(32, 0, 0, 0),
              interleaved=0, normalize=1, dtype=1, eps=1e-6, q_scale=1.0)
     a.update(kw)
-    return T._QkArgs(*[a[n] for n, _ in T._QkArgs._fields_])
+    return _QkArgs(*[a[n] for n, _ in _QkArgs._fields_])
 
 
 BAD = [
