@@ -17,7 +17,6 @@ namespace topk {
 // device error word values (bit flags, OR-ed together)
 constexpr unsigned kDevErrTimeout = 1u;
 constexpr unsigned kDevErrWorkspace = 2u;
-constexpr unsigned kDevErrRange = 4u;  // a position or cache row outside its table
 
 struct DevCtl {
   unsigned* error;          // device word, OR-ed with kDevErr* flags
@@ -293,28 +292,6 @@ __device__ __forceinline__ float max3f(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-
-// Two fp32 values in a 64-bit register pair: one instruction for two products.
-struct F2 {
-  unsigned long long v;
-};
-__device__ __forceinline__ F2 f2(float lo, float hi) {
-  F2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
-  F2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
-__device__ __forceinline__ float lo(F2 a) { return __uint_as_float(static_cast<uint32_t>(a.v)); }
-__device__ __forceinline__ float hi(F2 a) { return __uint_as_float(static_cast<uint32_t>(a.v >> 32)); }
 
 __device__ __forceinline__ bool elect_one() {
   uint32_t pred = 0;

@@ -11,6 +11,9 @@
 
 namespace topk {
 
+// flag of the device error word: a position or cache row outside its table (norm_rope.cu)
+constexpr unsigned kDevErrRange = 4u;
+
 // topk above this uses 32-row CTAs on the SIMT path (heap memory is
 // topk x rows x 8 bytes of shared memory).
 constexpr int kSimtSmallRowsMaxK = 128;

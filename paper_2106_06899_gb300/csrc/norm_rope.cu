@@ -23,6 +23,7 @@
 #include <cuda_bf16.h>
 
 #include "kernels.h"
+#include "pairs.cuh"
 
 namespace topk {
 

@@ -434,32 +434,34 @@ def _act_code(act: str) -> int:
     return ACTIVATIONS[act]
 
 
-def _linear_check(tensors) -> None:
-    for name, t, shape, dtypes in tensors:
-        if t is not None and (t.dtype not in dtypes or tuple(t.shape) != shape or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous {list(shape)} tensor of {' or '.join(map(str, dtypes))}")
+def _bf16(name, t, shape) -> int:
+    """t's address; t is None or a contiguous bf16 tensor of the shape."""
+    if t is None:
+        return 0
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} torch.bfloat16 tensor")
+    return t.data_ptr()
 
 
 def topk_linear_fwd(x, w, y, bias=None, residual=None, preact=None, act: str = "none", stream=None) -> None:
     """y = act(x w^T + bias) + residual: x [M,K], w [N,K], bias [N], residual, y and preact (z, written) [M,N], bf16."""
-    (M, K), N, bf = x.shape, w.shape[0], (torch.bfloat16,)
-    _linear_check((("x", x, (M, K), bf), ("w", w, (N, K), bf), ("bias", bias, (N,), bf), ("residual", residual, (M, N), bf),
-                   ("y", y, (M, N), bf), ("preact", preact, (M, N), bf)))
-    rc = lib().topk_linear_fwd(_ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(y), _ptr(preact), M, N, K, _act_code(act),
-                               _stream(stream))
+    (M, K), N = x.shape, w.shape[0]
+    out = (M, N)
+    rc = lib().topk_linear_fwd(_bf16("x", x, (M, K)), _bf16("w", w, (N, K)), _bf16("bias", bias, (N,)), _bf16("residual", residual, out),
+                               _bf16("y", y, out), _bf16("preact", preact, out), M, N, K, _act_code(act), _stream(stream))
     _check(rc, "topk_linear_fwd")
 
 
 def topk_linear_bwd(dy, x, w, dx, dw, db, preact=None, act: str = "none", stream=None) -> None:
     """Gradients of topk_linear_fwd: dx [M,K] bf16, dw [N,K] and db [N] bf16 or fp32 (one dtype); None where not wanted."""
-    (M, K), N, bf = x.shape, w.shape[0], (torch.bfloat16,)
-    grads = [t for t in (dw, db) if t is not None]
-    either = (grads[0].dtype,) if grads and grads[0].dtype in (torch.float32, torch.bfloat16) else (torch.float32, torch.bfloat16)
-    _linear_check((("dy", dy, (M, N), bf), ("x", x, (M, K), bf), ("w", w, (N, K), bf), ("preact", preact, (M, N), bf),
-                   ("dx", dx, (M, K), bf), ("dw", dw, (N, K), either), ("db", db, (N,), either)))
-    code = _dtype_code(grads[0]) if grads else TOPK_BF16
-    rc = lib().topk_linear_bwd(_ptr(dy), _ptr(x), _ptr(w), _ptr(preact), _ptr(dx), _ptr(dw), _ptr(db), M, N, K, _act_code(act), code,
-                               _stream(stream))
+    (M, K), N = x.shape, w.shape[0]
+    first = dw if dw is not None else db
+    dtype = torch.bfloat16 if first is None else first.dtype
+    _written("dw", dw, (N, K), dtype)
+    _written("db", db, (N,), dtype)
+    rc = lib().topk_linear_bwd(_bf16("dy", dy, (M, N)), _bf16("x", x, (M, K)), _bf16("w", w, (N, K)), _bf16("preact", preact, (M, N)),
+                               _bf16("dx", dx, (M, K)), _ptr(dw), _ptr(db), M, N, K, _act_code(act),
+                               TOPK_BF16 if first is None else _dtype_code(first), _stream(stream))
     _check(rc, "topk_linear_bwd")
 
 
