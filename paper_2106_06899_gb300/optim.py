@@ -6,6 +6,8 @@ bf16 with or without a 32-bit master.
 """
 from __future__ import annotations
 
+from operator import attrgetter
+
 import numpy as np
 import torch
 
@@ -14,6 +16,11 @@ from . import topk as T
 BLOCK = 256  # elements that share the scale of an 8-bit moment
 _TENSOR = np.dtype([(n, np.uint64) for n in ("param", "grad", "master", "m", "v", "m_scale", "v_scale")]
                    + [("n", np.int64), ("index", np.int64), ("lr", np.float64), ("weight_decay", np.float64)])
+
+
+_ADDRESS, _NUMEL, _CONTIGUOUS, _DEVICE = (
+    torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.get_device)
+_DTYPE = attrgetter("dtype")
 
 
 class AdamW:
@@ -67,6 +74,7 @@ class AdamW:
             t["m"], t["v"] = (s[k].data_ptr() + at[:-1] for k in ("exp_avg", "exp_avg_root"))
             t["m_scale"], t["v_scale"] = (s[k].data_ptr() + 4 * (at[:-1] // BLOCK) for k in ("exp_avg_scale", "exp_avg_root_scale"))
         self._address = self._table.ctypes.data
+        self._index, self._options = {self.params[0].get_device()}, None
         self._step = T.lib().topk_adamw_step
 
     def _buffers(self, total: int):
@@ -97,24 +105,28 @@ class AdamW:
             return
         sizes = self._n if len(given) == len(grads) else [n for g, n in zip(grads, self._n) if g is not None]
         gdt = given[0].dtype
-        if (any(g.dtype != gdt or not g.is_contiguous() or g.device != self.device for g in given)
-                or [g.numel() for g in given] != sizes):
+        if (set(map(_DTYPE, given)) != {gdt} or set(map(_DEVICE, given)) != self._index or not all(map(_CONTIGUOUS, given))
+                or list(map(_NUMEL, given)) != sizes):
             raise ValueError("gradients must be contiguous, of the parameters' sizes and device, and of one dtype")
         if gdt not in (torch.float32, torch.bfloat16):
             raise TypeError("gradients must be float32 or bfloat16")
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1
                                        or grad_scale.device != self.device):
             raise ValueError("grad_scale must be one float32 element on the parameters' device")
-        table["param"] = [p.data_ptr() for p in self.params]
-        table["grad"] = [0 if g is None else g.data_ptr() for g in grads]
-        k = 0
-        for group in self.param_groups:
-            end = k + len(group["params"])
-            table["lr"][k:end], table["weight_decay"][k:end] = group["lr"], group["weight_decay"]
-            k = end
+        table["param"] = list(map(_ADDRESS, self.params))
+        options = [(g["lr"], g["weight_decay"], len(g["params"])) for g in self.param_groups]
+        if options != self._options:
+            k = 0
+            for lr, wd, n in options:
+                table["lr"][k:k + n], table["weight_decay"][k:k + n] = lr, wd
+                k += n
+            self._options = options
         address, count = self._address, len(table)
-        if len(given) != len(grads):  # parameters without a gradient are left alone
+        if len(given) == len(grads):
+            table["grad"] = list(map(_ADDRESS, given))
+        else:  # parameters without a gradient are left alone
             table = table[[g is not None for g in grads]]
+            table["grad"] = list(map(_ADDRESS, given))
             address, count = table.ctypes.data, len(table)
         rc = self._step(address, count, self._param_code, T.TOPK_F32 if gdt == torch.float32 else T.TOPK_BF16, self.state_bits,
                         self.betas[0], self.betas[1], self.eps, self.state["step"] + 1, T._ptr(grad_scale),

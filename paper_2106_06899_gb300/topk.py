@@ -577,7 +577,7 @@ def qk_norm_rope(q, k, v, cos, sin, cache=None, cache_start=None, **options):
     into it from row cache_start[b] on ([B] int32) and the caches are returned.  v may be None (without a
     cache).  Options as topk_qk_norm_rope_fwd."""
     B, L, Hq, d = q.shape
-    qo = torch.empty(B, Hq, L, d, dtype=q.dtype, device=q.device)
+    qo = q.new_empty((B, Hq, L, d))
     if cache is not None:
         if cache_start is None or v is None:
             raise ValueError("a cache needs cache_start and v")
@@ -585,7 +585,7 @@ def qk_norm_rope(q, k, v, cos, sin, cache=None, cache_start=None, **options):
     else:
         if cache_start is not None:
             raise ValueError("cache_start needs a cache")
-        ko = torch.empty(B, k.shape[2], L, d, dtype=q.dtype, device=q.device)
+        ko = q.new_empty((B, k.shape[2], L, d))
         vo = None if v is None else torch.empty_like(ko)
     topk_qk_norm_rope_fwd(q, k, v, cos, sin, qo, ko, vo, cache_start=cache_start, **options)
     return qo, ko, vo
@@ -608,7 +608,7 @@ def qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, **options):
 def linear(x, w, bias=None, act: str = "none", residual=None, return_preact: bool = False, stream=None):
     """act(x w^T + bias) + residual for x [M,K] and w [N,K] (bf16); with return_preact also x w^T + bias, which
     linear_bwd takes for an activation."""
-    y = torch.empty(x.shape[0], w.shape[0], dtype=x.dtype, device=x.device)
+    y = x.new_empty((x.shape[0], w.shape[0]))
     z = torch.empty_like(y) if return_preact else None
     topk_linear_fwd(x, w, y, bias, residual, z, act, stream)
     return (y, z) if return_preact else y
