@@ -74,19 +74,23 @@ __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// Bounded wait (common.cuh's mbar_wait) that also acquires what the other CTA released.
-__device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, const DevCtl& ctl, volatile int* abort_flag) {
+// Bounded wait (as common.cuh's mbar_wait) that also acquires what the other CTA of the pair released.
+__device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
+static __device__ __noinline__ bool wait_cluster_slow(uint64_t* bar, uint32_t parity, const DevCtl& ctl, volatile int* abort_flag) {
   const unsigned long long t0 = global_ns();
   for (uint32_t spin = 1;; ++spin) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    if (ok) return true;
+    if (try_wait_cluster(bar, parity)) return true;
     if ((spin & 63u) == 0u) {
       if (*abort_flag) return false;
       if (global_ns() - t0 > ctl.wait_limit_ns) {
@@ -98,22 +102,21 @@ __device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, const 
   }
 }
 
+// For what the other CTA's threads arrive on; loads and products complete on a barrier by themselves.
 template <int CTAS>
-__device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, const DevCtl& ctl, volatile int* abort_flag) {
-  if constexpr (CTAS == 1)
-    return mbar_wait(bar, parity, ctl, abort_flag);
-  else
-    return wait_pair(bar, parity, ctl, abort_flag);
+__device__ __forceinline__ bool wait_arrivals(uint64_t* bar, uint32_t parity, const DevCtl& ctl, volatile int* abort_flag) {
+  if constexpr (CTAS == 1) return mbar_wait(bar, parity, ctl, abort_flag);
+  return try_wait_cluster(bar, parity) || wait_cluster_slow(bar, parity, ctl, abort_flag);
 }
 
-template <int CTAS>
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const DevCtl& ctl, volatile int* abort_flag) {
   int ok = 0;
-  if ((threadIdx.x & 31) == 0) ok = wait_bar<CTAS>(bar, parity, ctl, abort_flag) ? 1 : 0;
+  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity, ctl, abort_flag) ? 1 : 0;
   return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
 
 __device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity, const DevCtl& ctl) {
+  if (mbar_try_wait(bar, parity)) return;
   const unsigned long long t0 = global_ns();
   while (!mbar_try_wait(bar, parity)) {
     if (global_ns() - t0 > ctl.wait_limit_ns) {
@@ -366,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int row = (mt * CTAS + rank) * BM, col = nt * BN + rank * NB;
         for (int kb = k_first(part), end = k_first(part + 1); kb < end; ++kb, ++it) {
           const int s = it % S;
-          if (!wait_bar<CTAS>(&empty[s], ((it / S) & 1u) ^ 1u, ctl, abort_flag)) {
+          if (!mbar_wait(&empty[s], ((it / S) & 1u) ^ 1u, ctl, abort_flag)) {
             ok = false;
             break;
           }
@@ -404,13 +407,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         int mt, nt, part;
         unit_of(grid, u, mt, nt, part);
         const uint32_t buf = tile & 1u;
-        if (!wait_bar<CTAS>(&acc_empty[buf], ((tile >> 1) & 1u) ^ 1u, ctl, abort_flag)) break;
+        if (!wait_arrivals<CTAS>(&acc_empty[buf], ((tile >> 1) & 1u) ^ 1u, ctl, abort_flag)) break;
         tc_fence_after();
         const uint32_t acc = tmem_base + buf * BN;
         const int first = k_first(part), end = k_first(part + 1);
         for (int kb = first; kb < end; ++kb, ++it) {
           const int s = it % S;
-          if (!wait_bar<CTAS>(&full[s], (it / S) & 1u, ctl, abort_flag)) {
+          if (!mbar_wait(&full[s], (it / S) & 1u, ctl, abort_flag)) {
             ok = false;
             break;
           }
@@ -484,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (col < N) load_residual(col, row0);
         }
       }
-      if (!warp_wait<CTAS>(&acc_full[buf], (tile >> 1) & 1u, ctl, abort_flag)) break;
+      if (!warp_wait(&acc_full[buf], (tile >> 1) & 1u, ctl, abort_flag)) break;
       tc_fence_after();
       const uint32_t taddr = tmem_base + buf * BN + (static_cast<uint32_t>(quad * 32) << 16);
       // the accumulator is free for the next tile but one when its last chunk is in registers
@@ -545,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (has_residual) {
             if (!early) load_residual(col, row0);
             const uint32_t b = waits++;
-            if (!warp_wait<1>(&res_bar[b & 1u], (b >> 1) & 1u, ctl, abort_flag)) break;
+            if (!warp_wait(&res_bar[b & 1u], (b >> 1) & 1u, ctl, abort_flag)) break;
             __syncwarp();
             uint8_t* row_s = row_of(b);
 #pragma unroll
