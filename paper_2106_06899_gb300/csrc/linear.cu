@@ -306,6 +306,9 @@ __device__ __forceinline__ void unit_of(const Grid& g, int u, int& mt, int& nt, 
   mt = band * kBand + t - nt * rows;
 }
 
+// 16384 x 2048 x 8192: 312 us (1.76 PFLOP/s, 89 % of measured; the tensor pipe alone takes 279), 8192^3 611 us.  What
+// bounds it: an SM takes in 62.5 bytes a clock for products at full rate, of 65 that it can; for short sums the
+// fill of the first tile and the epilogue of the last.
 // Out: __nv_bfloat16 or float (the result, or a part's partial sums).
 template <int CTAS, int BN, bool A_MN, bool B_MN, typename Out>
 __global__ void __launch_bounds__(kThreads, 1)

@@ -32,7 +32,7 @@ namespace {
 constexpr int kWarps = 8;  // tokens of a block at a time
 constexpr unsigned kFull = 0xffffffffu;
 // Measured on 65,536 tokens x 36 heads of 64 (bf16) forward, and 32,768 x 48 heads of 128 (fp32 gradients)
-// backward: 119 and 265 us with these (5.2 and 5.6 TB/s, 77 and 82 % of a copy's rate).  More
+// backward: 116 and 262 us with these (5.3 and 5.7 TB/s, 78 and 83 % of a copy's rate).  More
 // blocks per SM spill registers (151 and 386 us); two rows a lane in place of four in the backward pass reload the
 // angles twice as often (302 us); blocks of a single token (no walk) wait for position and table in turn (135 and 519 us).
 constexpr int kFwdBlocksPerSm = 4, kBwdBlocksPerSm = 2;
