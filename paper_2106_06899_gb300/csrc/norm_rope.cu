@@ -32,11 +32,12 @@ namespace {
 constexpr int kWarps = 8;  // tokens of a block at a time
 constexpr unsigned kFull = 0xffffffffu;
 // Measured on 65,536 tokens x 36 heads of 64 (bf16) forward, and 32,768 x 48 heads of 128 (fp32 gradients)
-// backward: 116 and 262 us with these (5.3 and 5.7 TB/s, 78 and 83 % of a copy's rate).  More
-// blocks per SM spill registers (151 and 386 us); two rows a lane in place of four in the backward pass reload the
-// angles twice as often (302 us); blocks of a single token (no walk) wait for position and table in turn (135 and 519 us).
+// backward: 116 and 240 us with these (5.3 and 6.2 TB/s, 78 and 91 % of a copy's rate).  More forward blocks per SM
+// spill registers (151 us); blocks of a single token (no walk) wait for position and table in turn (135 us).  Backward,
+// rows held in registers take 262 us (fp32 rows 285 against 173 for 16,384 x 48 heads of 128), three blocks per
+// SM of fewer rows 322.
 constexpr int kFwdBlocksPerSm = 4, kBwdBlocksPerSm = 2;
-constexpr int kRowsPerLane = 4;  // at most, held at once; in fp32 two forward and one backward
+constexpr int kRowsPerLane = 4;  // at most, held at once (fp32: two)
 constexpr int kWaves = 4;        // blocks for each place on the GPU: values cost less than queries, and are not waited for
 
 __device__ __forceinline__ void load4(const float* p, float (&v)[4]) {
@@ -93,6 +94,10 @@ struct Raw<float> {
     a = *reinterpret_cast<const float4*>(p + l.a);
     b = *reinterpret_cast<const float4*>(p + l.b);
   }
+  __device__ __forceinline__ void from(const uint8_t* pa, const uint8_t* pb) {
+    a = *reinterpret_cast<const float4*>(pa);
+    b = *reinterpret_cast<const float4*>(pb);
+  }
   __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
   __device__ __forceinline__ Eight get() const { return {f2(a.x, a.y), f2(a.z, a.w), f2(b.x, b.y), f2(b.z, b.w)}; }
   __device__ __forceinline__ void set(const Eight& v) {
@@ -111,6 +116,10 @@ struct Raw<__nv_bfloat16> {
     a = *reinterpret_cast<const uint2*>(p + l.a);
     b = *reinterpret_cast<const uint2*>(p + l.b);
   }
+  __device__ __forceinline__ void from(const uint8_t* pa, const uint8_t* pb) {
+    a = *reinterpret_cast<const uint2*>(pa);
+    b = *reinterpret_cast<const uint2*>(pb);
+  }
   __device__ __forceinline__ void zero() { a = b = make_uint2(0u, 0u); }
   static __device__ __forceinline__ F2 wide(uint32_t u) { return f2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)); }
   // the one rounding of a result, to nearest
@@ -128,6 +137,17 @@ struct Raw<__nv_bfloat16> {
     *reinterpret_cast<uint2*>(p + l.b) = b;
   }
 };
+
+// A lane's pieces of the next token, copied into shared memory while it works on one: they take no registers, and only
+// the lane that asked for a piece reads it, so that its own wait is enough.  Nothing is read for a piece that is not
+// `on`; it is zero.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool on) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(on ? BYTES : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Until all but the newest group have landed.
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
 
 // The positions of the lane's four pairs 4j .. 4j + 3 for token (b, t), as they are given.  The four lie on one axis, or,
 // where an axis ends among them, on two; NARROW: on up to four.  Nothing here may wait for the loads, not even a
@@ -157,6 +177,14 @@ struct Positions {
 // The angles of a lane's four pairs; minus the sines too, which a paired product cannot negate.
 struct Angles {
   F2 c[2], s[2], m[2];
+  __device__ __forceinline__ void set(const float (&cs)[4], const float (&sn)[4], float scale) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      c[e] = f2(cs[2 * e] * scale, cs[2 * e + 1] * scale);
+      s[e] = f2(sn[2 * e] * scale, sn[2 * e + 1] * scale);
+      m[e] = f2(-sn[2 * e] * scale, -sn[2 * e + 1] * scale);
+    }
+  }
 };
 
 // cos and sin, times `scale`, of the four pairs; the scale alone where the lane does not rotate.  A
@@ -196,12 +224,44 @@ __device__ __forceinline__ void load_angles(const QkArgs& p, const Lane& l, int 
     }
     if (out) atomicOr(ctl.error, kDevErrRange);
   }
+  t.set(c, s, scale);
+}
+
+// The same in two steps: the copies into shared memory, and the reading of them.
+template <bool NARROW>
+__device__ __forceinline__ void fetch_angles(const QkArgs& p, const Lane& l, int j, const Positions<NARROW>& at, const DevCtl& ctl,
+                                             float* cos_s, float* sin_s) {
+  if (!l.rotated) return;
+  const int half = p.rot / 2, last = p.table_rows - 1;
+  bool out = false;
+  auto inside = [&](int row) {
+    const int r = min(max(row, 0), last);
+    out |= r != row;
+    return static_cast<size_t>(r) * half + 4 * j;
+  };
+  const uint32_t c = smem_u32(cos_s), s = smem_u32(sin_s);
+  if (!NARROW && l.split >= 4) {
+    const size_t r = inside(at.row[0]);
+    copy_async<16>(c, p.cos + r, true);
+    copy_async<16>(s, p.sin + r, true);
+  } else {
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    t.c[e] = f2(c[2 * e] * scale, c[2 * e + 1] * scale);
-    t.s[e] = f2(s[2 * e] * scale, s[2 * e + 1] * scale);
-    t.m[e] = f2(-s[2 * e] * scale, -s[2 * e + 1] * scale);
+    for (int e = 0; e < 4; ++e) {
+      const size_t r = inside(NARROW ? at.row[NARROW ? e : 0] : (e < l.split ? at.row[0] : at.row[1])) + e;
+      copy_async<4>(c + 4 * e, p.cos + r, true);
+      copy_async<4>(s + 4 * e, p.sin + r, true);
+    }
   }
+  if (out) atomicOr(ctl.error, kDevErrRange);
+}
+
+__device__ __forceinline__ void read_angles(const Lane& l, const float* cos_s, const float* sin_s, float scale, Angles& t) {
+  float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (l.rotated) {
+    load4(cos_s, c);
+    load4(sin_s, s);
+  }
+  t.set(c, s, scale);
 }
 
 // Turns the pairs by their angles, or back by the transpose (the other sign of the sines).
@@ -320,8 +380,15 @@ __global__ void __launch_bounds__(kWarps * 32, kFwdBlocksPerSm)
   }
 }
 
-// Backward.  A block keeps one group of heads and walks over tokens in strides of the grid, so
-// that its lanes sum their eight elements' weight gradient in registers; at the end the
+template <typename T, typename GT, int U>
+struct BwdStage {
+  float4 cos[kWarps * 32], sin[kWarps * 32];
+  uint8_t ya[U][kWarps * 32][4 * sizeof(GT)], yb[U][kWarps * 32][4 * sizeof(GT)];
+  uint8_t xa[U][kWarps * 32][4 * sizeof(T)], xb[U][kWarps * 32][4 * sizeof(T)];
+};
+
+// Backward.  A block keeps one group of heads and walks over tokens in strides of the grid, the next
+// token's rows and angles being copied into shared memory meanwhile, so that its lanes sum their eight elements' weight gradient in registers; at the end the
 // block adds its lanes up in a fixed order and writes one partial row.
 // qk_bwd_weights_kernel adds the partial rows: the result does not depend on the order in
 // which blocks run.
@@ -330,7 +397,9 @@ __global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm)
     qk_bwd_kernel(const __grid_constant__ QkArgs p, const GT* __restrict__ dq, const GT* __restrict__ dk, const GT* __restrict__ dv,
                   T* __restrict__ dqkv, float* __restrict__ partial, DevCtl ctl) {
   constexpr int R = 32 / G;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane % G, sub = lane / G;
+  extern __shared__ __align__(16) uint8_t smem[];
+  BwdStage<T, GT, U>* stages = reinterpret_cast<BwdStage<T, GT, U>*>(smem);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, j = lane % G, sub = lane / G;
   const int all = p.Hq + (dv ? 2 : 1) * p.Hkv;
   const unsigned tokens = static_cast<unsigned>(p.B) * p.L, stride = gridDim.x * kWarps;
   const Lane l = lane_of(p, j);
@@ -346,41 +415,56 @@ __global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm)
   Eight dw = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
   Positions<NARROW> at;
   unsigned token = blockIdx.x * kWarps + warp;
-  if (turns && token < tokens) at.load(p, l, j, token / p.L, token % p.L);
-  for (; token < tokens; token += stride) {
-    const int b = token / p.L, t = token % p.L;
-    Raw<GT> y[U];
-    Raw<T> x[U];
+  auto fetch = [&](unsigned tok, int s) {
+    const int b = tok / p.L, t = tok % p.L;
     const GT* gs = grad + (static_cast<long long>(b) * heads * p.L + t) * p.d;
     const T* xs = in + b * step[0] + t * step[1];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const bool on = u * R + sub < g.rows && l.on;
-      if (on)
-        y[u].load(gs + static_cast<long long>(u * R) * p.L * p.d, l);
-      else
-        y[u].zero();
-      if (on && norm)
-        x[u].load(xs + u * R * step[2], l);
-      else
-        x[u].zero();
+      const GT* yr = on ? gs + static_cast<long long>(u * R) * p.L * p.d : dq;
+      copy_async<4 * sizeof(GT)>(smem_u32(stages[s].ya[u][tid]), yr + (on ? l.a : 0), on);
+      copy_async<4 * sizeof(GT)>(smem_u32(stages[s].yb[u][tid]), yr + (on ? l.b : 0), on);
+      if (norm) {
+        const T* xr = on ? xs + u * R * step[2] : in;
+        copy_async<4 * sizeof(T)>(smem_u32(stages[s].xa[u][tid]), xr + (on ? l.a : 0), on);
+        copy_async<4 * sizeof(T)>(smem_u32(stages[s].xb[u][tid]), xr + (on ? l.b : 0), on);
+      }
     }
+    if (turns) fetch_angles(p, l, j, at, ctl, &stages[s].cos[tid].x, &stages[s].sin[tid].x);
+  };
+  if (token < tokens) {
+    if (turns) at.load(p, l, j, token / p.L, token % p.L);
+    fetch(token, 0);
+    if (turns && token + stride < tokens) at.load(p, l, j, (token + stride) / p.L, (token + stride) % p.L);
+  }
+  copies_commit();
+  for (int s = 0; token < tokens; token += stride, s ^= 1) {
+    const unsigned next = token + stride;
+    if (next < tokens) {
+      fetch(next, s ^ 1);
+      if (turns && next + stride < tokens) at.load(p, l, j, (next + stride) / p.L, (next + stride) % p.L);
+    }
+    copies_commit();
+    copies_wait();
     Angles turn;
-    if (turns) {
-      load_angles(p, l, j, at, scale, ctl, turn);
-      if (token + stride < tokens) at.load(p, l, j, (token + stride) / p.L, (token + stride) % p.L);
-    }
+    if (turns) read_angles(l, &stages[s].cos[tid].x, &stages[s].sin[tid].x, scale, turn);
     T* dst = out + static_cast<long long>(token) * all * p.d;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      Eight v = y[u].get();
+      Raw<GT> y;
+      y.from(stages[s].ya[u][tid], stages[s].yb[u][tid]);
+      Eight v = y.get();
       if (turns) rotate<true>(v, turn, p.interleaved);
       if (norm) {
-        Eight z = x[u].get(), vz;
+        Raw<T> x;
+        x.from(stages[s].xa[u][tid], stages[s].xb[u][tid]);
+        Eight z = x.get(), vz;
 #pragma unroll
         for (int e = 0; e < 4; ++e) vz.x[e] = mul2(v.x[e], z.x[e]);
         const float ss = group_sum<G>(dot8(z, z)), ux = group_sum<G>(dot8(vz, w));
-        const float r = rsqrtf(ss * inv_d + p.eps), k = -r * r * ux * inv_d;
+        // rows that are not there are zeros, whose root has no reciprocal without eps
+        const float r = u * R + sub < g.rows ? rsqrtf(ss * inv_d + p.eps) : 0.f, k = -r * r * ux * inv_d;
         const F2 rr = f2(r, r), kk = f2(k, k);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -502,14 +586,17 @@ int launch_bwd(const QkArgs& p, const void* dq, const void* dk, const void* dv, 
                float* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
   constexpr int R = 32 / G;
   const bool weights = p.normalize && (dqw || dkw);
-  constexpr int kRows = sizeof(T) == 2 ? kRowsPerLane : 1;
+  // what two blocks' shared memory holds of two tokens' rows and gradients (88 KB a block at most)
+  constexpr int kRows = sizeof(T) + sizeof(GT) == 4 ? 4 : (sizeof(T) + sizeof(GT) == 6 ? 3 : 2);
   return by_rows<kRows>(p, rows_per_lane(p, R, kRows), [&](auto n, auto narrow) {
     constexpr int U = decltype(n)::value;
     const int nq = groups_of(p.Hq, R * U), nk = groups_of(p.Hkv, R * U), groups = nq + (dv ? 2 : 1) * nk;
     const int blocks = walkers(p.B, p.L, groups, num_sms * kBwdBlocksPerSm * kWaves);
-    qk_bwd_kernel<T, GT, G, U, decltype(narrow)::value>
-        <<<dim3(blocks, groups), kWarps * 32, 0, st>>>(p, static_cast<const GT*>(dq), static_cast<const GT*>(dk), static_cast<const GT*>(dv),
-                                                       static_cast<T*>(dqkv), weights ? workspace : nullptr, ctl);
+    auto kern = qk_bwd_kernel<T, GT, G, U, decltype(narrow)::value>;
+    constexpr int bytes = 2 * sizeof(BwdStage<T, GT, U>);
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return -1;
+    kern<<<dim3(blocks, groups), kWarps * 32, bytes, st>>>(p, static_cast<const GT*>(dq), static_cast<const GT*>(dk), static_cast<const GT*>(dv),
+                                                           static_cast<T*>(dqkv), weights ? workspace : nullptr, ctl);
     if (cudaGetLastError() != cudaSuccess) return -1;
     if (!weights) return 1;
     qk_bwd_weights_kernel<<<dim3((p.d + 31) / 32, 2), dim3(32, 32), 0, st>>>(workspace, nq * blocks, nk * blocks, p.d, dqw, dkw);

@@ -178,6 +178,23 @@ def test_gradient_against_differences():
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_weight_gradients_without_eps(dtype):
+    # head counts that leave lanes without a row, eps = 0: the missing rows, zeros, must not reach the sums
+    B, L, Hq, Hkv, d = 2, 45, 5, 3, 64
+    q, k, v, qw, kw = _inputs(B, L, Hq, Hkv, d, dtype, 21)
+    cos, sin = T.rope_tables(64, d)
+    g = torch.Generator().manual_seed(22)
+    dq, dk, dv = (torch.randn(B, h, L, d, generator=g).cuda() for h in (Hq, Hkv, Hkv))
+    packed, dqw, dkw = T.qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, q_weight=qw, k_weight=kw, eps=0.0)
+    T.topk_check()
+    cs = _angles(cos, sin, None, (d // 2,), B, L)
+    for got, dy, x, w, dw in ((packed[:, :, :Hq], dq, q, qw, dqw), (packed[:, :, Hq:Hq + Hkv], dk, k, kw, dkw)):
+        dx, mag, rw, rwm = _ref_bwd(dy, x, w, cs, 0.0, 1.0, False, True)
+        _check(got, dx, mag)
+        assert ((dw.to(F64) - rw).abs() <= 400 * 2.0 ** -24 * rwm + 1e-30).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_cache_rows(dtype):
     B, L, Hq, Hkv, d, cap = 3, 5, 8, 4, 64, 100
     q, k, v, qw, kw = _inputs(B, L, Hq, Hkv, d, dtype, 4)
