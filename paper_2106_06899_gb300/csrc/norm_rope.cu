@@ -523,13 +523,16 @@ __global__ void __launch_bounds__(1024) qk_bwd_weights_kernel(const float* __res
 
 int groups_of(int heads, int size) { return (heads + size - 1) / size; }
 
-// Rows a lane holds at once: the fewest padded rows over q, k and v, and of those the most (more
-// loads in flight, the token's angles loaded less often).
-int rows_per_lane(const QkArgs& p, int R, int most) {
-  int best = 1, least = 1 << 30;
+// Rows a lane holds at once, u: a token's groups cost their rows, present or padded, and `group` rows' worth of angles,
+// weights and addresses each.  Forward a group costs 2.5 rows (16 query and 2 key heads of 64: two rows a lane take
+// 59 us where one, without padding, takes 80); backward, where the next token's copies hide it, next to nothing (16 and
+// 16 heads of 128: two rows 243 us, three 255).
+int rows_per_lane(const QkArgs& p, int R, int most, double group) {
+  int best = 1;
+  double least = 1e30;
   for (int u = 1; u <= most; ++u) {
-    const int rows = (groups_of(p.Hq, R * u) + 2 * groups_of(p.Hkv, R * u)) * u;
-    if (rows <= least) least = rows, best = u;
+    const double cost = (groups_of(p.Hq, R * u) + 2 * groups_of(p.Hkv, R * u)) * (u + group);
+    if (cost < least) least = cost, best = u;
   }
   return best;
 }
@@ -571,7 +574,7 @@ int launch_fwd(const QkArgs& p, void* qo, void* ko, void* vo, int cap, const int
   // few tokens: one row a lane, for more warps
   const bool few = static_cast<long long>(p.B) * p.L <= static_cast<long long>(num_sms) * kWarps;
   constexpr int kRows = sizeof(T) == 2 ? kRowsPerLane : 2;
-  return by_rows<kRows>(p, few ? 1 : rows_per_lane(p, R, kRows), [&](auto n, auto narrow) {
+  return by_rows<kRows>(p, few ? 1 : rows_per_lane(p, R, kRows, 2.5), [&](auto n, auto narrow) {
     constexpr int U = decltype(n)::value;
     const int groups = groups_of(p.Hq, R * U) + (p.v ? 2 : 1) * groups_of(p.Hkv, R * U);
     const dim3 grid(walkers(p.B, p.L, groups, num_sms * kFwdBlocksPerSm * kWaves), groups);
@@ -588,7 +591,7 @@ int launch_bwd(const QkArgs& p, const void* dq, const void* dk, const void* dv, 
   const bool weights = p.normalize && (dqw || dkw);
   // what two blocks' shared memory holds of two tokens' rows and gradients (88 KB a block at most)
   constexpr int kRows = sizeof(T) + sizeof(GT) == 4 ? 4 : (sizeof(T) + sizeof(GT) == 6 ? 3 : 2);
-  return by_rows<kRows>(p, rows_per_lane(p, R, kRows), [&](auto n, auto narrow) {
+  return by_rows<kRows>(p, rows_per_lane(p, R, kRows, 0.01), [&](auto n, auto narrow) {
     constexpr int U = decltype(n)::value;
     const int nq = groups_of(p.Hq, R * U), nk = groups_of(p.Hkv, R * U), groups = nq + (dv ? 2 : 1) * nk;
     const int blocks = walkers(p.B, p.L, groups, num_sms * kBwdBlocksPerSm * kWaves);
