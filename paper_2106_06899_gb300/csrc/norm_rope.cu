@@ -32,7 +32,7 @@ namespace {
 constexpr int kWarps = 8;  // tokens of a block at a time
 constexpr unsigned kFull = 0xffffffffu;
 // Measured on 65,536 tokens x 36 heads of 64 (bf16) forward, and 32,768 x 48 heads of 128 (fp32 gradients)
-// backward: 116 and 240 us with these (5.3 and 6.2 TB/s, 78 and 91 % of a copy's rate).  More forward blocks per SM
+// backward: 108 and 238 us with these (5.7 and 6.2 TB/s, 84 and 92 % of a copy's rate).  More forward blocks per SM
 // spill registers (151 us); blocks of a single token (no walk) wait for position and table in turn (135 us).  Backward,
 // rows held in registers take 262 us (fp32 rows 285 against 173 for 16,384 x 48 heads of 128), three blocks per
 // SM of fewer rows 322.
@@ -177,21 +177,20 @@ struct Positions {
 // The angles of a lane's four pairs; minus the sines too, which a paired product cannot negate.
 struct Angles {
   F2 c[2], s[2], m[2];
-  __device__ __forceinline__ void set(const float (&cs)[4], const float (&sn)[4], float scale) {
+  __device__ __forceinline__ void set(const float (&cs)[4], const float (&sn)[4]) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      c[e] = f2(cs[2 * e] * scale, cs[2 * e + 1] * scale);
-      s[e] = f2(sn[2 * e] * scale, sn[2 * e + 1] * scale);
-      m[e] = f2(-sn[2 * e] * scale, -sn[2 * e + 1] * scale);
+      c[e] = f2(cs[2 * e], cs[2 * e + 1]);
+      s[e] = f2(sn[2 * e], sn[2 * e + 1]);
+      m[e] = f2(-sn[2 * e], -sn[2 * e + 1]);
     }
   }
 };
 
-// cos and sin, times `scale`, of the four pairs; the scale alone where the lane does not rotate.  A
-// position outside the tables is reported and clamped.
+// cos and sin of the four pairs; identity where the lane does not rotate.  A position outside the tables is reported and clamped.
 template <bool NARROW>
-__device__ __forceinline__ void load_angles(const QkArgs& p, const Lane& l, int j, const Positions<NARROW>& at, float scale,
-                                            const DevCtl& ctl, Angles& t) {
+__device__ __forceinline__ void load_angles(const QkArgs& p, const Lane& l, int j, const Positions<NARROW>& at, const DevCtl& ctl,
+                                            Angles& t) {
   float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
   if (l.rotated) {
     const int half = p.rot / 2, last = p.table_rows - 1;
@@ -224,7 +223,7 @@ __device__ __forceinline__ void load_angles(const QkArgs& p, const Lane& l, int 
     }
     if (out) atomicOr(ctl.error, kDevErrRange);
   }
-  t.set(c, s, scale);
+  t.set(c, s);
 }
 
 // The same in two steps: the copies into shared memory, and the reading of them.
@@ -255,13 +254,13 @@ __device__ __forceinline__ void fetch_angles(const QkArgs& p, const Lane& l, int
   if (out) atomicOr(ctl.error, kDevErrRange);
 }
 
-__device__ __forceinline__ void read_angles(const Lane& l, const float* cos_s, const float* sin_s, float scale, Angles& t) {
+__device__ __forceinline__ void read_angles(const Lane& l, const float* cos_s, const float* sin_s, Angles& t) {
   float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
   if (l.rotated) {
     load4(cos_s, c);
     load4(sin_s, s);
   }
-  t.set(c, s, scale);
+  t.set(c, s);
 }
 
 // Turns the pairs by their angles, or back by the transpose (the other sign of the sines).
@@ -297,6 +296,22 @@ __device__ __forceinline__ float dot8(const Eight& a, const Eight& b) {
   return (lo(s) + hi(s)) + (lo(t) + hi(t));
 }
 
+// A warp's place in the batch, moved along by the grid's stride of tokens without a division a step.
+struct Place {
+  int b, t;
+};
+
+struct Walk {
+  int L, db, dt;
+  __device__ __forceinline__ Walk(int L_, unsigned stride) : L(L_), db(stride / L_), dt(stride % L_) {}
+  __device__ __forceinline__ Place at(unsigned token) const { return {static_cast<int>(token / L), static_cast<int>(token % L)}; }
+  __device__ __forceinline__ Place next(Place p) const {
+    p.b += db, p.t += dt;
+    if (p.t >= L) p.t -= L, ++p.b;
+    return p;
+  }
+};
+
 // A warp's share of a token: `rows` heads of one kind from h0 on, U x R at most.  The groups of a
 // token are q's, then k's, then v's.
 enum Kind { kQ, kK, kV };
@@ -328,7 +343,9 @@ __global__ void __launch_bounds__(kWarps * 32, kFwdBlocksPerSm)
   const Lane l = lane_of(p, j);
   const bool turns = g.kind != kV;
   Positions<NARROW> at;
-  if (turns) at.load(p, l, j, token / p.L, token % p.L);
+  const Walk walk(p.L, stride);
+  Place here = walk.at(token);
+  if (turns) at.load(p, l, j, here.b, here.t);
   const long long* step = g.kind == kQ ? p.q_stride : (g.kind == kK ? p.k_stride : p.v_stride);
   const T* in = static_cast<const T*>(g.kind == kQ ? p.q : (g.kind == kK ? p.k : p.v)) + (g.h0 + sub) * step[2];
   const int heads = g.kind == kQ ? p.Hq : p.Hkv, rows = g.kind == kQ ? p.L : cap;
@@ -336,7 +353,8 @@ __global__ void __launch_bounds__(kWarps * 32, kFwdBlocksPerSm)
   const long long out_step = static_cast<long long>(R) * rows * p.d;
   const float scale = g.kind == kQ ? p.q_scale : 1.f, inv_d = 1.f / p.d;
   for (; token < tokens; token += stride) {
-    const int b = token / p.L, t = token % p.L;
+    const int b = here.b, t = here.t;
+    here = walk.next(here);
     const T* src = in + b * step[0] + t * step[1];
     Raw<T> x[U];
 #pragma unroll
@@ -357,18 +375,17 @@ __global__ void __launch_bounds__(kWarps * 32, kFwdBlocksPerSm)
     }
     if (turns) {
       Angles turn;
-      load_angles(p, l, j, at, scale, ctl, turn);
-      if (token + stride < tokens) at.load(p, l, j, (token + stride) / p.L, (token + stride) % p.L);
+      load_angles(p, l, j, at, ctl, turn);
+      if (token + stride < tokens) at.load(p, l, j, here.b, here.t);
       const Eight w = load_weight<T>(g.kind == kQ ? p.q_weight : p.k_weight, l);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         Eight v = x[u].get();
-        if (p.normalize) {
-          const float r = rsqrtf(group_sum<G>(dot8(v, v)) * inv_d + p.eps);
-          const F2 rr = f2(r, r);
+        // one factor a row: the norm's and the scale's (weights are ones without the norm)
+        const float r = p.normalize ? rsqrtf(group_sum<G>(dot8(v, v)) * inv_d + p.eps) * scale : scale;
+        const F2 rr = f2(r, r);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v.x[e] = mul2(mul2(v.x[e], rr), w.x[e]);
-        }
+        for (int e = 0; e < 4; ++e) v.x[e] = mul2(mul2(v.x[e], rr), w.x[e]);
         rotate<false>(v, turn, p.interleaved);
         x[u].set(v);
       }
@@ -415,10 +432,10 @@ __global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm)
   Eight dw = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
   Positions<NARROW> at;
   unsigned token = blockIdx.x * kWarps + warp;
-  auto fetch = [&](unsigned tok, int s) {
-    const int b = tok / p.L, t = tok % p.L;
-    const GT* gs = grad + (static_cast<long long>(b) * heads * p.L + t) * p.d;
-    const T* xs = in + b * step[0] + t * step[1];
+  const Walk walk(p.L, stride);
+  auto fetch = [&](Place o, int s) {
+    const GT* gs = grad + (static_cast<long long>(o.b) * heads * p.L + o.t) * p.d;
+    const T* xs = in + o.b * step[0] + o.t * step[1];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const bool on = u * R + sub < g.rows && l.on;
@@ -433,22 +450,26 @@ __global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm)
     }
     if (turns) fetch_angles(p, l, j, at, ctl, &stages[s].cos[tid].x, &stages[s].sin[tid].x);
   };
+  Place next_at = {0, 0};  // of the token after the one worked on
   if (token < tokens) {
-    if (turns) at.load(p, l, j, token / p.L, token % p.L);
-    fetch(token, 0);
-    if (turns && token + stride < tokens) at.load(p, l, j, (token + stride) / p.L, (token + stride) % p.L);
+    const Place first = walk.at(token);
+    if (turns) at.load(p, l, j, first.b, first.t);
+    fetch(first, 0);
+    next_at = walk.next(first);
+    if (turns && token + stride < tokens) at.load(p, l, j, next_at.b, next_at.t);
   }
   copies_commit();
   for (int s = 0; token < tokens; token += stride, s ^= 1) {
     const unsigned next = token + stride;
     if (next < tokens) {
-      fetch(next, s ^ 1);
-      if (turns && next + stride < tokens) at.load(p, l, j, (next + stride) / p.L, (next + stride) % p.L);
+      fetch(next_at, s ^ 1);
+      next_at = walk.next(next_at);
+      if (turns && next + stride < tokens) at.load(p, l, j, next_at.b, next_at.t);
     }
     copies_commit();
     copies_wait();
     Angles turn;
-    if (turns) read_angles(l, &stages[s].cos[tid].x, &stages[s].sin[tid].x, scale, turn);
+    if (turns) read_angles(l, &stages[s].cos[tid].x, &stages[s].sin[tid].x, turn);
     T* dst = out + static_cast<long long>(token) * all * p.d;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -465,12 +486,15 @@ __global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm)
         const float ss = group_sum<G>(dot8(z, z)), ux = group_sum<G>(dot8(vz, w));
         // rows that are not there are zeros, whose root has no reciprocal without eps
         const float r = u * R + sub < g.rows ? rsqrtf(ss * inv_d + p.eps) : 0.f, k = -r * r * ux * inv_d;
-        const F2 rr = f2(r, r), kk = f2(k, k);
+        const F2 rr = f2(r * scale, r * scale), kk = f2(k, k);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           dw.x[e] = fma2(vz.x[e], rr, dw.x[e]);
           v.x[e] = mul2(rr, fma2(z.x[e], kk, mul2(v.x[e], w.x[e])));
         }
+      } else if (turns) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v.x[e] = mul2(v.x[e], f2(scale, scale));
       }
       if (u * R + sub >= g.rows || !l.on) continue;
       Raw<T> o;
