@@ -518,6 +518,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (row0 < M && col < N) put(tmo, w, col, row0, part);
         } else {
           float v[64];
+          // the bias is on its way while the sums are read
+          uint4 bias[8];
+          if (epi.bias) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              bias[e] = col + 8 * e < N ? __ldg(reinterpret_cast<const uint4*>(epi.bias + col) + e) : make_uint4(0u, 0u, 0u, 0u);
+          }
           tmem_ld64(taddr + c * COLS, v);
           tmem_wait_ld();
           if (i == CHUNKS - 1) release();
@@ -525,12 +532,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (epi.bias) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              if (col + 8 * e < N) {
-                float b[8];
-                unpack8(__ldg(reinterpret_cast<const uint4*>(epi.bias + col) + e), b);
+              float b[8];
+              unpack8(bias[e], b);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[8 * e + j] += b[j];
-              }
+              for (int j = 0; j < 8; ++j) v[8 * e + j] += b[j];
             }
           }
           if (epi.keep) {
