@@ -32,7 +32,7 @@ namespace {
 constexpr int kWarps = 8;  // tokens of a block at a time
 constexpr unsigned kFull = 0xffffffffu;
 // Measured on 65,536 tokens x 36 heads of 64 (bf16) forward, and 32,768 x 48 heads of 128 (fp32 gradients)
-// backward: 108 and 238 us with these (5.7 and 6.2 TB/s, 84 and 92 % of a copy's rate).  More forward blocks per SM
+// backward: 106 and 234 us with these (5.9 and 6.3 TB/s, 86 and 93 % of a copy's rate).  More forward blocks per SM
 // spill registers (151 us); blocks of a single token (no walk) wait for position and table in turn (135 us).  Backward,
 // rows held in registers take 262 us (fp32 rows 285 against 173 for 16,384 x 48 heads of 128), three blocks per
 // SM of fewer rows 322.
