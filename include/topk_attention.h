@@ -355,7 +355,9 @@ size_t topk_linear_bwd_workspace_bytes(int M, int N, int K, int act);
  *                every 256 elements in m_scale, v_scale [ceil(n / 256)] (value = float x scale,
  *                scale = largest magnitude / 448; a block whose scale is below 2^-100 is zero); v
  *                holds the ROOT of the second moment.  They are rounded stochastically; the
- *                update uses the values before rounding.
+ *                update uses the values before rounding.  A root above zero is held as the
+ *                smallest float (2^-9) at least: cut to zero, it would leave the m beside it, which
+ *                may be rounded up to a whole float, without a denominator in the next step.
  *   master     : NULL, or (TOPK_BF16 parameters, all tensors or none) fp32 [n] that the step
  *                reads and updates; param is then its copy, rounded to nearest.  bf16
  *                parameters without a master are rounded stochastically.

@@ -45,10 +45,11 @@ constexpr int kPer = 8;                          // neighbouring elements of a l
 constexpr int kRound = kThreads * kPer;          // elements of a block at a time
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kTop = 448.f;                    // largest e4m3 value
-// 307 M bf16 parameters with 8-bit states: 798 us (3.9 TB/s, 57 % of a copy's rate) with three blocks per SM, 32 rounds
-// a block and the next round's loads in flight; 908 us with two blocks, 846 us with four (spills).  Four fifths of all
-// issue slots are taken: instructions bound it.  Approximate roots and fused sums take 720 us, but a code that falls
-// on the other side of its random threshold (2 in 10^6) then makes a step differ from its formula by a place.
+// 307 M bf16 parameters with 8-bit states: 832 us (3.7 TB/s, 55 % of a copy's rate) with three blocks per SM, 32 rounds
+// a block and the next round's loads in flight (two blocks per SM, or four, with their spills, are slower).  Four fifths
+// of all issue slots are taken: instructions bound it.  Of these the floor under the roots (encode8) costs 39 us, and
+// exact roots and separate sums 8: approximate ones put 331 of one step's 614 M codes on the other side of their random
+// threshold, and the step would differ from its formula by a place there.
 constexpr int kBlocks8 = 3, kRounds8 = 32;
 
 struct Entry {
@@ -173,16 +174,24 @@ __device__ __forceinline__ void decode8(uint2 u, float (&v)[8]) {
 // their last place are added below the last place kept, and the rest is cut off.  At y = 448 the sum
 // stays below the next code by 511 units, more than y's rounding: no clamp.  Where y is not a number the
 // scale is not either, and the code does not matter.
+// A root (not kSigned) above zero gets the smallest code at least.  Cut to zero, it would leave the next update's
+// denominator to the next gradient alone, while the first moment, rounded by itself, may have grown to a whole code: a
+// step of any length.  Held, the smallest codes' quotient is max|m| / max root of the block, which Adam's moments bound.
 template <int kShift, bool kSigned>
 __device__ __forceinline__ uint2 encode8(const float (&x)[8], float inv, const uint32_t (&rnd)[8], const Powers& k) {
   static_assert(kShift == 0 || kShift == 10, "the ten bits' place");
   uint32_t c[8];
+  // a root is zero or above 2^-75 (it is that of an fp32 number): the smaller of it and 2^-125 has code 1's pattern
+  const float least = !kSigned && inv > 0.f ? 0x1p-125f : 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const uint32_t y = __float_as_uint(__fmul_rn(__fmul_rn(fabsf(x[e]), inv), 0x1p-120f));
     const uint32_t r = kShift == 0 ? (rnd[e] & 0x3ffu) * k.p14 + 8192u : (rnd[e] & 0xffc00u) * k.p4 + 8192u;
     c[e] = y * k.p4 + r;  // 16 (y + 1024 random + 512): the code in the top byte
-    if (kSigned) c[e] = (c[e] & 0x7fffffffu) | (__float_as_uint(x[e]) & 0x80000000u);
+    if (kSigned)
+      c[e] = (c[e] & 0x7fffffffu) | (__float_as_uint(x[e]) & 0x80000000u);
+    else
+      c[e] = max(c[e], __float_as_uint(fminf(x[e], least)));
   }
   uint2 u;
   u.x = __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
