@@ -621,6 +621,7 @@ int topk_adamw_step(const topk_adamw_tensor* tensors, int count, int param_dtype
   if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0)) return TOPK_ERR_INVALID_ARG;
   if (!aligned4(grad_scale)) return TOPK_ERR_UNSUPPORTED;
   const uintptr_t pa = param_dtype == TOPK_F32 ? 3 : 1, ga = grad_dtype == TOPK_F32 ? 3 : 1;
+  const topk_adamw_tensor* first = nullptr;  // of those with elements: the others have a master if it has
   for (int k = 0; k < count; ++k) {
     const topk_adamw_tensor& t = tensors[k];
     if (t.n < 0 || !std::isfinite(t.lr) || !std::isfinite(t.weight_decay)) return TOPK_ERR_INVALID_ARG;
@@ -628,7 +629,8 @@ int topk_adamw_step(const topk_adamw_tensor* tensors, int count, int param_dtype
     if (!t.param || !t.grad || !t.m || !t.v) return TOPK_ERR_INVALID_ARG;
     if (state_bits == 8 && (!t.m_scale || !t.v_scale)) return TOPK_ERR_INVALID_ARG;
     if (t.master && param_dtype != TOPK_BF16) return TOPK_ERR_INVALID_ARG;
-    if ((t.master != nullptr) != (tensors[0].master != nullptr) && tensors[0].n) return TOPK_ERR_INVALID_ARG;
+    if (!first) first = &t;
+    if ((t.master != nullptr) != (first->master != nullptr)) return TOPK_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(t.param) & pa) || (reinterpret_cast<uintptr_t>(t.grad) & ga) || !aligned4(t.master) ||
         !aligned4(t.m_scale) || !aligned4(t.v_scale) || (state_bits == 32 && (!aligned4(t.m) || !aligned4(t.v))))
       return TOPK_ERR_UNSUPPORTED;
