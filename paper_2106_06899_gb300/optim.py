@@ -25,7 +25,7 @@ _DTYPE = attrgetter("dtype")
 
 class AdamW:
     """params: tensors, or dicts {"params": [...], "lr": .., "weight_decay": ..} (groups).  All share a dtype
-    (float32 or bfloat16) and are contiguous CUDA tensors.
+    (float32 or bfloat16) and are contiguous tensors, on the current CUDA device when a step is taken.
 
     state_bits: 32 or 8.  masters: None, True (32-bit masters are made of bf16 parameters), or a
     list of fp32 tensors to use as masters.  state: buffers of an earlier optimizer (as state_dict
@@ -100,9 +100,13 @@ class AdamW:
             grads = [p.grad for p in self.params]
         elif len(grads) != len(self.params):
             raise ValueError("one gradient for each parameter")
-        table, given = self._table, [g for g in grads if g is not None]
+        table, given, params = self._table, [g for g in grads if g is not None], self.params
         if not given:
             return
+        # a parameter's data can have been replaced since the last step (Module.to, p.data = ..)
+        if (set(map(_DTYPE, params)) != {self.dtype} or set(map(_DEVICE, params)) != self._index or list(map(_NUMEL, params)) != self._n
+                or not all(map(_CONTIGUOUS, params))):
+            raise ValueError("the parameters are no longer of the dtype, sizes and device that the optimizer was made for")
         sizes = self._n if len(given) == len(grads) else [n for g, n in zip(grads, self._n) if g is not None]
         gdt = given[0].dtype
         if (set(map(_DTYPE, given)) != {gdt} or set(map(_DEVICE, given)) != self._index or not all(map(_CONTIGUOUS, given))
@@ -113,7 +117,8 @@ class AdamW:
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1
                                        or grad_scale.device != self.device):
             raise ValueError("grad_scale must be one float32 element on the parameters' device")
-        table["param"] = list(map(_ADDRESS, self.params))
+        T._on_gpu("parameters", params[0])
+        table["param"] = list(map(_ADDRESS, params))
         options = [(g["lr"], g["weight_decay"], len(g["params"])) for g in self.param_groups]
         if options != self._options:
             k = 0

@@ -134,6 +134,16 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _on_gpu(names: str, first, *others) -> None:
+    """Refuses tensors (or None) that are not on the current CUDA device, where the kernels run."""
+    device = first.get_device()  # -1: not on a GPU
+    for t in others:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{names} must be CUDA tensors of one device")
+    if device < 0 or device != torch.cuda.current_device():
+        raise ValueError(f"{names} must be CUDA tensors on the current device")
+
+
 def _attn_dims(q, k, v, out):
     for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
         if t.dim() != 4 or not t.is_contiguous():
