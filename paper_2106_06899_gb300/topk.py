@@ -411,6 +411,8 @@ def topk_qk_norm_rope_fwd(q, k, v, cos, sin, q_out, k_out, v_out, *, cache_start
     if cache_start is not None and (cache_start.dtype != torch.int32 or tuple(cache_start.shape) != (B,)
                                     or not cache_start.is_contiguous()):
         raise ValueError("cache_start must be a [B] int32 tensor")
+    _on_gpu("q, k, v, the tables, positions, weights, outputs and cache_start", q, k, v, cos, sin, positions, q_weight, k_weight, q_out,
+            k_out, v_out, cache_start)
     rc = lib().topk_qk_norm_rope_fwd(a, _ptr(q_out), _ptr(k_out), _ptr(v_out), cap, _ptr(cache_start),
                                      _stream(stream))
     _check(rc, "topk_qk_norm_rope_fwd")
@@ -429,6 +431,8 @@ def topk_qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, dqkv, dq_weight, dk_weight
     _written("dqkv", dqkv, (B, L, Hq + (Hkv if dv is None else 2 * Hkv), d), q.dtype)
     _written("dq_weight", dq_weight, (d,), torch.float32)
     _written("dk_weight", dk_weight, (d,), torch.float32)
+    _on_gpu("gradients, q, k, the tables, positions, weights and outputs", q, k, cos, sin, positions, q_weight, k_weight, dq, dk, dv, dqkv,
+            dq_weight, dk_weight)
     rc = lib().topk_qk_norm_rope_bwd(a, _ptr(dq), _ptr(dk), _ptr(dv), _dtype_code(dq), _ptr(dqkv), _ptr(dq_weight),
                                      _ptr(dk_weight), _stream(stream))
     _check(rc, "topk_qk_norm_rope_bwd")
@@ -457,8 +461,11 @@ def topk_linear_fwd(x, w, y, bias=None, residual=None, preact=None, act: str = "
     """y = act(x w^T + bias) + residual: x [M,K], w [N,K], bias [N], residual, y and preact (z, written) [M,N], bf16."""
     (M, K), N = x.shape, w.shape[0]
     out = (M, N)
-    rc = lib().topk_linear_fwd(_bf16("x", x, (M, K)), _bf16("w", w, (N, K)), _bf16("bias", bias, (N,)), _bf16("residual", residual, out),
-                               _bf16("y", y, out), _bf16("preact", preact, out), M, N, K, _act_code(act), _stream(stream))
+    tensors = (_bf16("x", x, (M, K)), _bf16("w", w, (N, K)), _bf16("bias", bias, (N,)), _bf16("residual", residual, out),
+               _bf16("y", y, out), _bf16("preact", preact, out))
+    code = _act_code(act)
+    _on_gpu("x, w, bias, residual, y and preact", x, w, bias, residual, y, preact)
+    rc = lib().topk_linear_fwd(*tensors, M, N, K, code, _stream(stream))
     _check(rc, "topk_linear_fwd")
 
 
@@ -469,9 +476,11 @@ def topk_linear_bwd(dy, x, w, dx, dw, db, preact=None, act: str = "none", stream
     dtype = torch.bfloat16 if first is None else first.dtype
     _written("dw", dw, (N, K), dtype)
     _written("db", db, (N,), dtype)
-    rc = lib().topk_linear_bwd(_bf16("dy", dy, (M, N)), _bf16("x", x, (M, K)), _bf16("w", w, (N, K)), _bf16("preact", preact, (M, N)),
-                               _bf16("dx", dx, (M, K)), _ptr(dw), _ptr(db), M, N, K, _act_code(act),
-                               TOPK_BF16 if first is None else _dtype_code(first), _stream(stream))
+    tensors = (_bf16("dy", dy, (M, N)), _bf16("x", x, (M, K)), _bf16("w", w, (N, K)), _bf16("preact", preact, (M, N)),
+               _bf16("dx", dx, (M, K)), _ptr(dw), _ptr(db))
+    code, grad_code = _act_code(act), TOPK_BF16 if first is None else _dtype_code(first)
+    _on_gpu("dy, x, w, preact, dx, dw and db", x, w, dy, preact, dx, dw, db)
+    rc = lib().topk_linear_bwd(*tensors, M, N, K, code, grad_code, _stream(stream))
     _check(rc, "topk_linear_bwd")
 
 
