@@ -205,6 +205,15 @@ class Decoder(torch.nn.Module):
         self.fused = fused
         self.tables = T.rope_tables(max_positions, d_model // heads, device=device) if fused else None
 
+    def _apply(self, fn, recurse=True):
+        super()._apply(fn, recurse)
+        # the tables go where the parameters go, but stay in 32 bits and out of the state_dict
+        device = self.norm.weight.device
+        if self.tables is not None and self.tables[0].device != device:
+            rows, half = self.tables[0].shape
+            self.tables = T.rope_tables(rows, 2 * half, device=device)
+        return self
+
     def forward(self, x):
         for layer in self.layers:
             x = layer.forward_fused(x, self.tables) if self.fused else layer(x)
