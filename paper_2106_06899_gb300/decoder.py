@@ -13,10 +13,14 @@ With fused=True (bf16) those, but for the LayerNorms, are the library's operator
 their activation and residual (topk_linear_fwd / _bwd), and between the q/k/v projection and the attention
 the norms of queries and keys with a rotation by position (topk_qk_norm_rope_fwd / _bwd).  The fused
 decoder also generates, a token a step, against key/value caches (Decoder.step).
+
+The library's gradients have no gradients of their own: a second differentiation through one of these functions is
+an error.
 """
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import topk as T
 
@@ -32,6 +36,7 @@ class TopKAttentionFunction(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         q, k, v, idx, score = ctx.saved_tensors
         dq, dk, dv = T.attention_bwd(q, k, v, dout.to(q.dtype).contiguous(), idx, score)
@@ -48,6 +53,7 @@ class TopKFFNFunction(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         x, w1, w2, idx, score = ctx.saved_tensors
         dx, d1, d2 = T.ffn_bwd(x, w1, w2, dout.float().contiguous(), idx, score)
@@ -66,6 +72,7 @@ class LinearFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, w, z = ctx.saved_tensors
         dy = dy.contiguous()
@@ -87,6 +94,7 @@ class RotaryAttentionFunction(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         qkv, q_weight, k_weight, cos, sin, q, k, v, idx, score = ctx.saved_tensors
         H = qkv.shape[2] // 3
@@ -107,6 +115,7 @@ class QKNormRopeFunction(torch.autograd.Function):
                               q_scale=qkv.shape[3] ** -0.5)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq, dk, dv):
         qkv, q_weight, k_weight, cos, sin = ctx.saved_tensors
         H = qkv.shape[2] // 3

@@ -1,0 +1,104 @@
+"""The library's autograd functions, with stand-ins for the library's calls on the CPU (no GPU needed)."""
+import pytest
+import torch
+
+from paper_2106_06899_gb300 import decoder
+
+
+def _act(z, act):
+    return {"none": lambda: z, "relu": lambda: z.relu(), "gelu": lambda: torch.nn.functional.gelu(z), "silu": lambda: torch.nn.functional.silu(z)}[act]()
+
+
+class _StandIn:
+    """linear, qk_norm_rope, attention and ffn with their gradients, as torch operations that leave no graph."""
+
+    def __init__(self):
+        self.calls = []
+
+    def linear(self, x, w, bias=None, act="none", residual=None, return_preact=False, stream=None):
+        self.calls.append(("linear", return_preact))
+        with torch.no_grad():
+            z = x @ w.t()
+            y = _act(z, act) + (0 if residual is None else residual)
+        return (y, z) if return_preact else y
+
+    def linear_bwd(self, dy, x, w, preact=None, act="none", bias=False, need_dx=True, need_dw=True, grad_dtype=None, stream=None):
+        assert need_dx or need_dw, "the library refuses a call that asks for nothing"
+        assert (preact is None) == (act == "none")
+        self.calls.append(("linear_bwd", need_dx, need_dw))
+        with torch.enable_grad():
+            z = (torch.zeros_like(dy) if preact is None else preact).detach().clone().requires_grad_()
+            (dz,) = torch.autograd.grad(_act(z, act), z, dy.detach())
+        return (dz @ w).detach() if need_dx else None, (dz.t() @ x).detach() if need_dw else None, None
+
+    def qk_norm_rope(self, q, k, v, cos, sin, q_weight=None, k_weight=None, q_scale=1.0):
+        self.calls.append(("qk_norm_rope",))
+        with torch.no_grad():
+            return tuple(t.transpose(1, 2).contiguous() for t in (q * q_weight * q_scale, k * k_weight, v))
+
+    def qk_norm_rope_bwd(self, dq, dk, dv, q, k, cos, sin, q_weight=None, k_weight=None, q_scale=1.0):
+        self.calls.append(("qk_norm_rope_bwd",))
+        with torch.no_grad():
+            dq, dk, dv = (t.transpose(1, 2).to(q.dtype) for t in (dq, dk, dv))
+            return (torch.cat((dq * q_weight * q_scale, dk * k_weight, dv), 2), (dq * q * q_scale).sum((0, 1, 2)), (dk * k).sum((0, 1, 2)))
+
+    def attention(self, q, k, v, topk, causal=False, return_indices=False):
+        with torch.no_grad():
+            out = q * k * v
+        return out, torch.zeros(1, dtype=torch.int32), torch.zeros(1)
+
+    def attention_bwd(self, q, k, v, dout, idx, score):
+        with torch.no_grad():
+            return dout * k * v, dout * q * v, dout * q * k
+
+    def ffn(self, x, w1, w2, topk, return_indices=False):
+        with torch.no_grad():
+            return (x @ w1.t()) @ w2, torch.zeros(1, dtype=torch.int32), torch.zeros(1)
+
+    def ffn_bwd(self, x, w1, w2, dout, idx, score):
+        with torch.no_grad():
+            return (dout @ w2.t()) @ w1, (dout @ w2.t()).t() @ x, (x @ w1.t()).t() @ dout
+
+
+@pytest.fixture
+def stand_in(monkeypatch):
+    s = _StandIn()
+    monkeypatch.setattr(decoder, "T", s)
+    return s
+
+
+def _rand(*shape):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(sum(shape))).requires_grad_()
+
+
+def _cases():
+    qkv, w, tables = _rand(1, 4, 6, 8), _rand(8), (torch.zeros(4, 4), torch.zeros(4, 4))
+    q, x, wx, w1, w2 = _rand(1, 2, 4, 8), _rand(4, 8), _rand(6, 8), _rand(16, 8), _rand(16, 8)
+    return {
+        "linear": (x, lambda: decoder.LinearFunction.apply(x, wx, "none", None)),
+        "linear with an activation and a residual": (x, lambda: decoder.LinearFunction.apply(x, wx, "silu", x[:, :6])),
+        "norms, rotation and attention": (qkv, lambda: decoder.RotaryAttentionFunction.apply(qkv, w, w, *tables, 4)),
+        "norms and rotation": (qkv, lambda: torch.cat(decoder.QKNormRopeFunction.apply(qkv, w, w, *tables))),
+        "attention": (q, lambda: decoder.TopKAttentionFunction.apply(q, q, q, 4, True)),
+        "feed-forward": (x, lambda: decoder.TopKFFNFunction.apply(x, w1, w2, 4)),
+    }
+
+
+NAMES = ["linear", "linear with an activation and a residual", "norms, rotation and attention", "norms and rotation", "attention", "feed-forward"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_second_derivatives_are_refused(stand_in, name):
+    # the gradient of a gradient would be that of the torch operations around alone: an error, not a part of it
+    x, run = _cases()[name]
+    (g,) = torch.autograd.grad(run().square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.square().sum().backward()
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_first_derivatives_are_the_same_with_create_graph(stand_in, name):
+    x, run = _cases()[name]
+    (a,) = torch.autograd.grad(run().square().sum(), x)
+    (b,) = torch.autograd.grad(run().square().sum(), x, create_graph=True)
+    assert torch.equal(a, b) and float(a.abs().max()) > 0
