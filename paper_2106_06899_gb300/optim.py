@@ -137,6 +137,11 @@ class AdamW:
                         self.betas[0], self.betas[1], self.eps, self.state["step"] + 1, T._ptr(grad_scale),
                         self.seed & 0xFFFFFFFF, T._stream(stream))
         T._check(rc, "topk_adamw_step")
+        whole = len(given) == len(grads)
+        for changed in (params, self.masters):
+            if changed is not None:
+                T._changed(*(changed if whole else [t for t, g in zip(changed, grads) if g is not None]))
+        T._changed(*(t for k, t in self.state.items() if k != "step"))
         self.state["step"] += 1
 
     def zero_grad(self, set_to_none: bool = True) -> None:

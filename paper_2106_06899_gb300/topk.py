@@ -144,6 +144,11 @@ def _on_gpu(names: str, first, *others) -> None:
         raise ValueError(f"{names} must be CUDA tensors on the current device")
 
 
+def _changed(*tensors) -> None:
+    """Counts tensors (or None) as changed in place, for graphs that hold them: autograd does not see a kernel's writes."""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+
+
 def _attn_dims(q, k, v, out):
     for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
         if t.dim() != 4 or not t.is_contiguous():
@@ -416,6 +421,7 @@ def topk_qk_norm_rope_fwd(q, k, v, cos, sin, q_out, k_out, v_out, *, cache_start
     rc = lib().topk_qk_norm_rope_fwd(a, _ptr(q_out), _ptr(k_out), _ptr(v_out), cap, _ptr(cache_start),
                                      _stream(stream))
     _check(rc, "topk_qk_norm_rope_fwd")
+    _changed(q_out, k_out, v_out)
 
 
 def topk_qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, dqkv, dq_weight, dk_weight, *, positions=None, q_weight=None,
@@ -436,6 +442,7 @@ def topk_qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, dqkv, dq_weight, dk_weight
     rc = lib().topk_qk_norm_rope_bwd(a, _ptr(dq), _ptr(dk), _ptr(dv), _dtype_code(dq), _ptr(dqkv), _ptr(dq_weight),
                                      _ptr(dk_weight), _stream(stream))
     _check(rc, "topk_qk_norm_rope_bwd")
+    _changed(dqkv, dq_weight, dk_weight)
 
 
 def topk_qk_norm_rope_bwd_workspace_bytes(B, L, Hq, Hkv, d) -> int:
@@ -467,6 +474,7 @@ def topk_linear_fwd(x, w, y, bias=None, residual=None, preact=None, act: str = "
     _on_gpu("x, w, bias, residual, y and preact", x, w, bias, residual, y, preact)
     rc = lib().topk_linear_fwd(*tensors, M, N, K, code, _stream(stream))
     _check(rc, "topk_linear_fwd")
+    _changed(y, preact)
 
 
 def topk_linear_bwd(dy, x, w, dx, dw, db, preact=None, act: str = "none", stream=None) -> None:
@@ -482,6 +490,7 @@ def topk_linear_bwd(dy, x, w, dx, dw, db, preact=None, act: str = "none", stream
     _on_gpu("dy, x, w, preact, dx, dw and db", x, w, dy, preact, dx, dw, db)
     rc = lib().topk_linear_bwd(*tensors, M, N, K, code, grad_code, _stream(stream))
     _check(rc, "topk_linear_bwd")
+    _changed(dx, dw, db)
 
 
 def topk_linear_workspace_bytes(M, N, K) -> int:
