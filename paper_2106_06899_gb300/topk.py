@@ -234,12 +234,27 @@ def topk_vanilla_attn_fwd(q, k, v, out, chunk: int = 1024, causal: bool = False,
     _check(rc, "topk_vanilla_attn_fwd")
 
 
+def _allocate(stream, make):
+    """make()'s tuple of output tensors (or None) for a call on `stream`: memory of that stream, as on another's its kernels
+    could write while work that was queued on the memory's last tenant still runs; and lent to the current stream, so that it is
+    not given away under what reads the outputs there."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))):
+        out = make()
+    current = torch.cuda.current_stream()
+    for t in out:
+        if t is not None:
+            t.record_stream(current)
+    return out
+
+
 def topk_vanilla_attn_workspace_bytes(B, H, Lq, Lk, d, dtype) -> int:
     return int(lib().topk_vanilla_attn_workspace_bytes(B, H, Lq, Lk, d, dtype))
 
 
 def vanilla_attention(q, k, v, chunk: int = 1024, causal: bool = False, kv_len=None, stream=None):
-    out = torch.empty_like(q)
+    (out,) = _allocate(stream, lambda: (torch.empty_like(q),))
     topk_vanilla_attn_fwd(q, k, v, out, chunk, causal, kv_len, stream)
     return out
 
@@ -256,7 +271,7 @@ def topk_vanilla_ffn_workspace_bytes(N, d_model, d_ff, chunk) -> int:
 
 
 def vanilla_ffn(x, W1, W2, chunk: int = 16384, stream=None):
-    out = torch.empty(x.shape[0], x.shape[1], dtype=torch.float32, device=x.device)
+    (out,) = _allocate(stream, lambda: (torch.empty(x.shape[0], x.shape[1], dtype=torch.float32, device=x.device),))
     topk_vanilla_ffn_fwd(x, W1, W2, out, chunk, stream)
     return out
 
@@ -545,37 +560,41 @@ def topk_pool_trim() -> None:
 
 # convenience wrappers that allocate the outputs ---------------------------------------------
 
+def _kept(rows, topk: int, device):
+    """Empty lists of the kept indices and scores."""
+    return (torch.empty(*rows, topk, dtype=torch.int32, device=device), torch.empty(*rows, topk, dtype=torch.float32, device=device))
+
+
 def attention(q, k, v, topk: int, chunk: int = 1024, causal: bool = False, return_indices: bool = False,
               stream=None, kv_len=None, mask=None):
     """Top-k attention; kv_len ([B] int32) and mask (bool [B|1, H|1, Lq, Lk], True = valid) add Eq. 2's
     general masks."""
-    out = torch.empty_like(q)
-    if kv_len is not None or mask is not None:
-        B, H, Lq, _ = q.shape
-        idx = score = None
-        if return_indices:
-            idx = torch.empty(B, H, Lq, topk, dtype=torch.int32, device=q.device)
-            score = torch.empty(B, H, Lq, topk, dtype=torch.float32, device=q.device)
-        words, bs, hs = pack_mask(mask) if mask is not None else (None, 0, 0)
-        topk_attn_fwd_masked(q, k, v, out, topk, chunk, causal, kv_len, words, bs, hs, idx, score, stream)
-        return (out, idx, score) if return_indices else out
-    if not return_indices:
-        topk_attn_fwd(q, k, v, out, topk, chunk, causal, stream)
-        return out
     B, H, Lq, _ = q.shape
-    idx = torch.empty(B, H, Lq, topk, dtype=torch.int32, device=q.device)
-    score = torch.empty(B, H, Lq, topk, dtype=torch.float32, device=q.device)
-    topk_attn_fwd_indices(q, k, v, out, topk, chunk, causal, idx, score, stream)
-    return out, idx, score
+    out, idx, score = _allocate(stream, lambda: (
+        torch.empty_like(q), *(_kept((B, H, Lq), topk, q.device) if return_indices else (None, None))))
+    if kv_len is not None or mask is not None:
+        strides = [0, 0]
+
+        def pack():  # on the call's stream, as the kernel that reads the words
+            words, *strides[:] = pack_mask(mask)
+            return (words,)
+
+        (words,) = _allocate(stream, pack) if mask is not None else (None,)
+        topk_attn_fwd_masked(q, k, v, out, topk, chunk, causal, kv_len, words, *strides, idx, score, stream)
+    elif return_indices:
+        topk_attn_fwd_indices(q, k, v, out, topk, chunk, causal, idx, score, stream)
+    else:
+        topk_attn_fwd(q, k, v, out, topk, chunk, causal, stream)
+    return (out, idx, score) if return_indices else out
 
 
 def ffn(x, W1, W2, topk: int, return_indices: bool = False, stream=None):
-    out = torch.empty(x.shape[0], x.shape[1], dtype=torch.float32, device=x.device)
+    out, idx, score = _allocate(stream, lambda: (
+        torch.empty(x.shape[0], x.shape[1], dtype=torch.float32, device=x.device),
+        *(_kept((x.shape[0],), topk, x.device) if return_indices else (None, None))))
     if not return_indices:
         topk_ffn_fwd(x, W1, W2, out, topk, stream)
         return out
-    idx = torch.empty(x.shape[0], topk, dtype=torch.int32, device=x.device)
-    score = torch.empty(x.shape[0], topk, dtype=torch.float32, device=x.device)
     topk_ffn_fwd_indices(x, W1, W2, out, topk, idx, score, stream)
     return out, idx, score
 
@@ -583,61 +602,55 @@ def ffn(x, W1, W2, topk: int, return_indices: bool = False, stream=None):
 def attention_bwd(q, k, v, dout, idx, score, stream=None):
     """Gradients (dq, dk, dv), fp32, of top-k attention for the cache (idx, score) of attention(...,
     return_indices=True)."""
-    dq = torch.empty(q.shape, dtype=torch.float32, device=q.device)
-    dk = torch.empty(k.shape, dtype=torch.float32, device=k.device)
-    dv = torch.empty(v.shape, dtype=torch.float32, device=v.device)
+    dq, dk, dv = _allocate(stream, lambda: tuple(torch.empty(t.shape, dtype=torch.float32, device=t.device) for t in (q, k, v)))
     topk_attn_bwd(q, k, v, dout, idx, score, dq, dk, dv, stream)
     return dq, dk, dv
 
 
 def ffn_bwd(x, W1, W2, dout, idx, score, stream=None):
     """Gradients (dx, dW1, dW2), fp32, of the top-k FF layer for the cache of ffn(..., return_indices=True)."""
-    dx = torch.empty(x.shape, dtype=torch.float32, device=x.device)
-    dW1 = torch.empty(W1.shape, dtype=torch.float32, device=W1.device)
-    dW2 = torch.empty(W2.shape, dtype=torch.float32, device=W2.device)
+    dx, dW1, dW2 = _allocate(stream, lambda: tuple(torch.empty(t.shape, dtype=torch.float32, device=t.device) for t in (x, W1, W2)))
     topk_ffn_bwd(x, W1, W2, dout, idx, score, dx, dW1, dW2, stream)
     return dx, dW1, dW2
 
 
-def qk_norm_rope(q, k, v, cos, sin, cache=None, cache_start=None, **options):
+def qk_norm_rope(q, k, v, cos, sin, cache=None, cache_start=None, stream=None, **options):
     """Norm, rotation and scale of a projection's q [B,L,Hq,d] and k, v [B,L,Hkv,d] for the attention:
     (q [B,Hq,L,d], k, v [B,Hkv,L,d]).  With cache = (keys, values), each [B,Hkv,cap,d], k and v are written
     into it from row cache_start[b] on ([B] int32) and the caches are returned.  v may be None (without a
     cache).  Options as topk_qk_norm_rope_fwd."""
     B, L, Hq, d = q.shape
-    qo = q.new_empty((B, Hq, L, d))
     if cache is not None:
         if cache_start is None or v is None:
             raise ValueError("a cache needs cache_start and v")
-        ko, vo = cache
+        (qo,), (ko, vo) = _allocate(stream, lambda: (q.new_empty((B, Hq, L, d)),)), cache
     else:
         if cache_start is not None:
             raise ValueError("cache_start needs a cache")
-        ko = q.new_empty((B, k.shape[2], L, d))
-        vo = None if v is None else torch.empty_like(ko)
-    topk_qk_norm_rope_fwd(q, k, v, cos, sin, qo, ko, vo, cache_start=cache_start, **options)
+        kv = (B, k.shape[2], L, d)
+        qo, ko, vo = _allocate(stream, lambda: (q.new_empty((B, Hq, L, d)), q.new_empty(kv), None if v is None else q.new_empty(kv)))
+    topk_qk_norm_rope_fwd(q, k, v, cos, sin, qo, ko, vo, cache_start=cache_start, stream=stream, **options)
     return qo, ko, vo
 
 
-def qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, **options):
+def qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, stream=None, **options):
     """Gradients (dqkv [B,L,Hq+2Hkv,d] packed in q's dtype, dq_weight, dk_weight fp32 [d]) of qk_norm_rope; the weight
     gradients are None with normalize=False.  dv may be None."""
     B, L, Hq, d = q.shape
     Hkv = k.shape[2]
-    dqkv = torch.empty(B, L, Hq + (Hkv if dv is None else 2 * Hkv), d, dtype=q.dtype, device=q.device)
-    gq = gk = None
-    if options.get("normalize", True):
-        both = torch.empty(2, d, dtype=torch.float32, device=q.device)
-        gq, gk = both[0], both[1]
-    topk_qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, dqkv, gq, gk, **options)
+    dqkv, both = _allocate(stream, lambda: (
+        torch.empty(B, L, Hq + (Hkv if dv is None else 2 * Hkv), d, dtype=q.dtype, device=q.device),
+        torch.empty(2, d, dtype=torch.float32, device=q.device) if options.get("normalize", True) else None))
+    gq, gk = (None, None) if both is None else (both[0], both[1])
+    topk_qk_norm_rope_bwd(dq, dk, dv, q, k, cos, sin, dqkv, gq, gk, stream=stream, **options)
     return dqkv, gq, gk
 
 
 def linear(x, w, bias=None, act: str = "none", residual=None, return_preact: bool = False, stream=None):
     """act(x w^T + bias) + residual for x [M,K] and w [N,K] (bf16); with return_preact also x w^T + bias, which
     linear_bwd takes for an activation."""
-    y = x.new_empty((x.shape[0], w.shape[0]))
-    z = torch.empty_like(y) if return_preact else None
+    shape = (x.shape[0], w.shape[0])
+    y, z = _allocate(stream, lambda: (x.new_empty(shape), x.new_empty(shape) if return_preact else None))
     topk_linear_fwd(x, w, y, bias, residual, z, act, stream)
     return (y, z) if return_preact else y
 
@@ -645,8 +658,8 @@ def linear(x, w, bias=None, act: str = "none", residual=None, return_preact: boo
 def linear_bwd(dy, x, w, preact=None, act: str = "none", bias: bool = False, need_dx: bool = True, need_dw: bool = True,
                grad_dtype=torch.bfloat16, stream=None):
     """Gradients (dx, dw, db) of linear; the residual's is dy.  dw and db are of grad_dtype; None where not wanted."""
-    dx = torch.empty_like(x) if need_dx else None
-    dw = torch.empty(w.shape, dtype=grad_dtype, device=w.device) if need_dw else None
-    db = torch.empty(w.shape[0], dtype=grad_dtype, device=w.device) if bias else None
+    dx, dw, db = _allocate(stream, lambda: (
+        torch.empty_like(x) if need_dx else None, torch.empty(w.shape, dtype=grad_dtype, device=w.device) if need_dw else None,
+        torch.empty(w.shape[0], dtype=grad_dtype, device=w.device) if bias else None))
     topk_linear_bwd(dy, x, w, dx, dw, db, preact, act, stream)
     return dx, dw, db
