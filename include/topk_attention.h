@@ -268,6 +268,9 @@ int topk_ffn_bwd(const void* x, const void* W1, const void* W2, const float* dou
  *              and is reported as TOPK_ERR_RANGE by topk_check().
  *   d        : a multiple of 8, at most 256.  rot: a multiple of 8, at most d (0: none).
  *   axes     : 1 to 4; their sections are >= 0 and sum to rot / 2.
+ *   Hq, Hkv  : at most 65,536 each.  A launch holds 65,535 groups of q's, k's and v's heads; what makes more
+ *              (in the worst case, axes of one or two pairs, 65,536 heads of over 128 elements together) is
+ *              TOPK_ERR_UNSUPPORTED.
  * Sums are taken in fp32 and each result is rounded once, to nearest.
  */
 typedef struct {

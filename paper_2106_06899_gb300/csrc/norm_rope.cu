@@ -547,6 +547,14 @@ __global__ void __launch_bounds__(1024) qk_bwd_weights_kernel(const float* __res
 
 int groups_of(int heads, int size) { return (heads + size - 1) / size; }
 
+// Groups are a grid's y: 65,535 at most.  Heads that make more, one row a lane, take more rows a lane.
+constexpr int kMostGroups = 65535;
+
+int rows_that_fit(const QkArgs& p, int R, int u, int most) {
+  while (u < most && groups_of(p.Hq, R * u) + 2 * groups_of(p.Hkv, R * u) > kMostGroups) ++u;
+  return u;
+}
+
 // Rows a lane holds at once, u: a token's groups cost their rows, present or padded, and `group` rows' worth of angles,
 // weights and addresses each.  Forward a group costs 2.5 rows (16 query and 2 key heads of 64: two rows a lane take
 // 59 us where one, without padding, takes 80); backward, where the next token's copies hide it, next to nothing (16 and
@@ -598,9 +606,10 @@ int launch_fwd(const QkArgs& p, void* qo, void* ko, void* vo, int cap, const int
   // few tokens: one row a lane, for more warps
   const bool few = static_cast<long long>(p.B) * p.L <= static_cast<long long>(num_sms) * kWarps;
   constexpr int kRows = sizeof(T) == 2 ? kRowsPerLane : 2;
-  return by_rows<kRows>(p, few ? 1 : rows_per_lane(p, R, kRows, 2.5), [&](auto n, auto narrow) {
+  return by_rows<kRows>(p, rows_that_fit(p, R, few ? 1 : rows_per_lane(p, R, kRows, 2.5), kRows), [&](auto n, auto narrow) {
     constexpr int U = decltype(n)::value;
     const int groups = groups_of(p.Hq, R * U) + (p.v ? 2 : 1) * groups_of(p.Hkv, R * U);
+    if (groups > kMostGroups) return 0;
     const dim3 grid(walkers(p.B, p.L, groups, num_sms * kFwdBlocksPerSm * kWaves), groups);
     qk_fwd_kernel<T, G, U, decltype(narrow)::value><<<grid, kWarps * 32, 0, st>>>(p, static_cast<T*>(qo), static_cast<T*>(ko), static_cast<T*>(vo),
                                                                                  cap, start, ctl);
@@ -615,9 +624,10 @@ int launch_bwd(const QkArgs& p, const void* dq, const void* dk, const void* dv, 
   const bool weights = p.normalize && (dqw || dkw);
   // what two blocks' shared memory holds of two tokens' rows and gradients (88 KB a block at most)
   constexpr int kRows = sizeof(T) + sizeof(GT) == 4 ? 4 : (sizeof(T) + sizeof(GT) == 6 ? 3 : 2);
-  return by_rows<kRows>(p, rows_per_lane(p, R, kRows, 0.01), [&](auto n, auto narrow) {
+  return by_rows<kRows>(p, rows_that_fit(p, R, rows_per_lane(p, R, kRows, 0.01), kRows), [&](auto n, auto narrow) {
     constexpr int U = decltype(n)::value;
     const int nq = groups_of(p.Hq, R * U), nk = groups_of(p.Hkv, R * U), groups = nq + (dv ? 2 : 1) * nk;
+    if (groups > kMostGroups) return 0;
     const int blocks = walkers(p.B, p.L, groups, num_sms * kBwdBlocksPerSm * kWaves);
     auto kern = qk_bwd_kernel<T, GT, G, U, decltype(narrow)::value>;
     constexpr int bytes = 2 * sizeof(BwdStage<T, GT, U>);
