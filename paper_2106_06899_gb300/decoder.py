@@ -76,7 +76,9 @@ class LinearFunction(torch.autograd.Function):
     def backward(ctx, dy):
         x, w, z = ctx.saved_tensors
         dy = dy.contiguous()
-        dx, dw, _ = T.linear_bwd(dy, x, w, z, ctx.act, need_dx=ctx.needs_input_grad[0], need_dw=ctx.needs_input_grad[1])
+        dx = dw = None
+        if any(ctx.needs_input_grad[:2]):
+            dx, dw, _ = T.linear_bwd(dy, x, w, z, ctx.act, need_dx=ctx.needs_input_grad[0], need_dw=ctx.needs_input_grad[1])
         return dx, dw, None, dy if ctx.has_residual else None
 
 

@@ -102,3 +102,11 @@ def test_first_derivatives_are_the_same_with_create_graph(stand_in, name):
     (a,) = torch.autograd.grad(run().square().sum(), x)
     (b,) = torch.autograd.grad(run().square().sum(), x, create_graph=True)
     assert torch.equal(a, b) and float(a.abs().max()) > 0
+
+
+def test_a_linear_layer_of_frozen_inputs_passes_the_residuals_gradient(stand_in):
+    x, w, r = _rand(4, 8).detach(), _rand(6, 8).detach(), _rand(4, 6)
+    for act in ("none", "gelu"):
+        (g,) = torch.autograd.grad(decoder.LinearFunction.apply(x, w, act, r).square().sum(), r)
+        y = decoder.LinearFunction.apply(x, w, act, r).detach()
+        assert torch.equal(g, 2 * y)
