@@ -61,12 +61,16 @@ class TopKFFNFunction(torch.autograd.Function):
 
 
 class LinearFunction(torch.autograd.Function):
-    """act(x w^T) + residual for x [M, K], w [N, K] (bf16); the pre-activations are kept for the backward pass."""
+    """act(x w^T) + residual for x [M, K], w [N, K] (bf16).  The backward pass needs the pre-activations, but for
+    ReLU, whose slope is the sign of its output, only where a residual was added to that."""
 
     @staticmethod
     def forward(ctx, x, w, act: str, residual):
-        y, z = T.linear(x, w, act=act, residual=residual, return_preact=True) if act != "none" else (
-            T.linear(x, w, residual=residual), None)
+        if act == "none" or (act == "relu" and residual is None):
+            y = T.linear(x, w, act=act, residual=residual)
+            z = None if act == "none" else y
+        else:
+            y, z = T.linear(x, w, act=act, residual=residual, return_preact=True)
         ctx.save_for_backward(x, w, z)
         ctx.act, ctx.has_residual = act, residual is not None
         return y
@@ -80,6 +84,13 @@ class LinearFunction(torch.autograd.Function):
         if any(ctx.needs_input_grad[:2]):
             dx, dw, _ = T.linear_bwd(dy, x, w, z, ctx.act, need_dx=ctx.needs_input_grad[0], need_dw=ctx.needs_input_grad[1])
         return dx, dw, None, dy if ctx.has_residual else None
+
+
+def linear(x, w, act: str = "none", residual=None):
+    """LinearFunction where a gradient is wanted, else the library's call, which then keeps nothing."""
+    if torch.is_grad_enabled() and (x.requires_grad or w.requires_grad or (residual is not None and residual.requires_grad)):
+        return LinearFunction.apply(x, w, act, residual)
+    return T.linear(x, w, act=act, residual=residual)
 
 
 class RotaryAttentionFunction(torch.autograd.Function):
@@ -159,16 +170,16 @@ class DecoderLayer(torch.nn.Module):
 
     def _fused_tail(self, a, x):
         """Output projection and feed-forward layer, each with its residual: a (attention, [M, D]), x [M, D]."""
-        x = LinearFunction.apply(a, self.proj.weight, "none", x)
+        x = linear(a, self.proj.weight, residual=x)
         h = self.ln2(x)
         if self.ffn_topk is None:
-            return LinearFunction.apply(LinearFunction.apply(h, self.w1, "relu", None), self.w2, "none", x)
+            return linear(linear(h, self.w1, "relu"), self.w2, residual=x)
         return x + TopKFFNFunction.apply(h.contiguous(), self.w1, self.w2, self.ffn_topk).to(h.dtype)
 
     def forward_fused(self, x, tables):
         B, L, D = x.shape
         x = x.reshape(B * L, D)
-        qkv = LinearFunction.apply(self.ln1(x), self.qkv.weight, "none", None).view(B, L, 3 * self.h, self.dh)
+        qkv = linear(self.ln1(x), self.qkv.weight).view(B, L, 3 * self.h, self.dh)
         if self.topk is None:
             a = self.attention(*QKNormRopeFunction.apply(qkv, self.q_norm, self.k_norm, *tables))
         else:

@@ -110,3 +110,44 @@ def test_a_linear_layer_of_frozen_inputs_passes_the_residuals_gradient(stand_in)
         (g,) = torch.autograd.grad(decoder.LinearFunction.apply(x, w, act, r).square().sum(), r)
         y = decoder.LinearFunction.apply(x, w, act, r).detach()
         assert torch.equal(g, 2 * y)
+
+
+def _held(fn):
+    """The bytes that the graph of fn's result holds, each storage once."""
+    seen = {}
+
+    def pack(t):
+        seen[t.untyped_storage().data_ptr()] = t.untyped_storage().nbytes()
+        return t
+
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t):
+        out = fn()
+    return out, seen
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("residual", [False, True])
+def test_linear_keeps_pre_activations_only_where_they_are_needed(stand_in, act, residual):
+    x, w = _rand(4, 8), _rand(6, 8)
+    r = _rand(4, 6).detach() if residual else None
+    y, held = _held(lambda: decoder.LinearFunction.apply(x, w, act, r))
+    # ReLU's slope is its output's sign, unless a residual was added to it
+    needs = act in ("gelu", "silu") or (act == "relu" and residual)
+    assert stand_in.calls[-1] == ("linear", needs)
+    more = {k for k in held if k not in (x.data_ptr(), w.data_ptr())}
+    assert len(more) == (act != "none") and (not more or needs or more == {y.data_ptr()})
+    gx, gw = torch.autograd.grad(y.square().sum(), (x, w))
+    u, v = (t.detach().clone().requires_grad_() for t in (x, w))
+    want = _act(u @ v.t(), act) + (0 if r is None else r)
+    hx, hw = torch.autograd.grad(want.square().sum(), (u, v))
+    assert torch.allclose(gx, hx, rtol=1e-5, atol=1e-6) and torch.allclose(gw, hw, rtol=1e-5, atol=1e-6)
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+def test_linear_keeps_nothing_without_gradients(stand_in, act):
+    x, w, r = _rand(4, 8), _rand(6, 8), _rand(4, 6)
+    with torch.no_grad():
+        decoder.linear(x, w, act, r)
+    decoder.linear(x.detach(), w.detach(), act)
+    assert [c for c in stand_in.calls if c[0] == "linear"] == [("linear", False)] * 2
+    assert decoder.linear(x, w, act).requires_grad and decoder.linear(x.detach(), w.detach(), act, r).requires_grad
