@@ -151,3 +151,15 @@ def test_linear_keeps_nothing_without_gradients(stand_in, act):
     decoder.linear(x.detach(), w.detach(), act)
     assert [c for c in stand_in.calls if c[0] == "linear"] == [("linear", False)] * 2
     assert decoder.linear(x, w, act).requires_grad and decoder.linear(x.detach(), w.detach(), act, r).requires_grad
+
+
+def test_attention_after_the_rotation_keeps_its_inputs_once(stand_in):
+    qkv, w, tables = _rand(1, 4, 6, 8), _rand(8), (torch.zeros(4, 4), torch.zeros(4, 4))
+    out, held = _held(lambda: decoder.RotaryAttentionFunction.apply(qkv, w, w, *tables, 4))
+    size = qkv.numel() * qkv.element_size()
+    assert sum(held.values()) < 1.5 * size  # the projection's output; what it is turned into is made again from it
+    g, gw = torch.autograd.grad(out.square().sum(), (qkv, w))
+    u, v = qkv.detach().clone().requires_grad_(), w.detach().clone().requires_grad_()
+    q, k, x = (t.transpose(1, 2) for t in (u[:, :, :2] * v * 8 ** -0.5, u[:, :, 2:4] * v, u[:, :, 4:]))
+    hu, hv = torch.autograd.grad((q * k * x).square().sum(), (u, v))
+    assert torch.allclose(g, hu, rtol=1e-5, atol=1e-6) and torch.allclose(gw, hv, rtol=1e-5, atol=1e-6)
