@@ -318,7 +318,8 @@ size_t topk_qk_norm_rope_bwd_workspace_bytes(int B, int L, int Hq, int Hkv, int 
  *   residual : [M, N] or NULL.  y: [M, N].  preact: NULL, or [M, N], which receives z for
  *              the backward pass.  All bf16, contiguous, 16-byte aligned; y and preact overlap no
  *              input, but y may be the residual itself.
- *   act      : TOPK_ACT_*; GELU is z Phi(z) (the exact form), SILU z / (1 + e^-z).
+ *   act      : TOPK_ACT_*; GELU is z Phi(z) (the erf form), SILU z / (1 + e^-z).  Phi is within 6e-7;
+ *              its relative error passes half a bf16 place (3.7e-3) below z = -6, where |y| < 1e-8.
  *   M >= 1; N and K multiples of 8.  Sums in fp32, every result rounded once, to nearest.
  *   Scratch: topk_linear_workspace_bytes(): 0, or fp32 partial sums (parts x M x N) where the
  *   outputs are too few tiles for the SMs and the sum is split; parts are added in order, so
