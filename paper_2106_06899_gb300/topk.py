@@ -240,7 +240,9 @@ def _allocate(stream, make):
     not given away under what reads the outputs there."""
     if stream is None:
         return make()
-    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))):
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(0 if int(stream) == 1 else int(stream))  # 1: the default stream's other handle
+    with torch.cuda.stream(stream):
         out = make()
     current = torch.cuda.current_stream()
     for t in out:

@@ -66,3 +66,13 @@ def test_outputs_belong_to_the_calls_stream(name, handle):
     for g, w in zip(got, want):
         assert _stream_of(g) == st.cuda_stream
         assert name in UNORDERED or torch.equal(g, w)
+
+
+@pytest.mark.parametrize("handle", [0, 1, 2])
+def test_default_streams_by_their_handles(handle):
+    x, w = (torch.randn(64, 64, device="cuda").to(BF) for _ in range(2))
+    want = T.linear(x, w)
+    torch.cuda.synchronize()
+    got = T.linear(x, w, stream=handle)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
