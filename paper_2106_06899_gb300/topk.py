@@ -427,6 +427,7 @@ def topk_qk_norm_rope_fwd(q, k, v, cos, sin, q_out, k_out, v_out, *, cache_start
     a, (B, L, Hq, Hkv, d) = _qk_args(q, k, v, cos, sin, positions, q_weight, k_weight, eps, q_scale, sections, interleaved,
                                      normalize)
     cap = k_out.shape[2]
+    _fits(cap)
     _written("q_out", q_out, (B, Hq, L, d), q.dtype)
     _written("k_out", k_out, (B, Hkv, cap, d), q.dtype)
     _written("v_out", v_out, (B, Hkv, cap, d), q.dtype)
@@ -466,6 +467,12 @@ def topk_qk_norm_rope_bwd_workspace_bytes(B, L, Hq, Hkv, d) -> int:
     return int(lib().topk_qk_norm_rope_bwd_workspace_bytes(B, L, Hq, Hkv, d))
 
 
+def _fits(*sizes) -> None:
+    """Refuses sizes that the C ABI's ints cannot hold: ctypes would pass their low 32 bits."""
+    if max(sizes) >= 1 << 31:
+        raise ValueError("sizes must be below 2^31")
+
+
 def _act_code(act: str) -> int:
     if act not in ACTIVATIONS:
         raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}")
@@ -484,6 +491,7 @@ def _bf16(name, t, shape) -> int:
 def topk_linear_fwd(x, w, y, bias=None, residual=None, preact=None, act: str = "none", stream=None) -> None:
     """y = act(x w^T + bias) + residual: x [M,K], w [N,K], bias [N], residual, y and preact (z, written) [M,N], bf16."""
     (M, K), N = x.shape, w.shape[0]
+    _fits(M, N, K)
     out = (M, N)
     tensors = (_bf16("x", x, (M, K)), _bf16("w", w, (N, K)), _bf16("bias", bias, (N,)), _bf16("residual", residual, out),
                _bf16("y", y, out), _bf16("preact", preact, out))
@@ -497,6 +505,7 @@ def topk_linear_fwd(x, w, y, bias=None, residual=None, preact=None, act: str = "
 def topk_linear_bwd(dy, x, w, dx, dw, db, preact=None, act: str = "none", stream=None) -> None:
     """Gradients of topk_linear_fwd: dx [M,K] bf16, dw [N,K] and db [N] bf16 or fp32 (one dtype); None where not wanted."""
     (M, K), N = x.shape, w.shape[0]
+    _fits(M, N, K)
     first = dw if dw is not None else db
     dtype = torch.bfloat16 if first is None else first.dtype
     _written("dw", dw, (N, K), dtype)
