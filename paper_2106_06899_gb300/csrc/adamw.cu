@@ -85,6 +85,7 @@ struct Table {
 };
 static_assert(sizeof(Table<kMaxTensors>) <= 32764, "kernel parameters");
 
+// Mixes all bits of x: shifts and two multipliers published by C. Wellons ("Prospecting for Hash Functions", 2018).
 __host__ __device__ inline uint32_t mix32(uint32_t x) {
   x ^= x >> 16;
   x *= 0x7feb352du;

@@ -95,7 +95,9 @@ class AdamW:
 
     def step(self, grads=None, grad_scale=None, stream=None) -> None:
         """One step with the parameters' .grad (or `grads`, one for each parameter; None skips it).
-        grad_scale: a float32 CUDA tensor of one element that multiplies the gradients."""
+        grad_scale: a float32 CUDA tensor of one element that multiplies the gradients.  If it is not finite nothing is
+        updated, but state["step"], which the host counts without waiting for the GPU, goes on; a caller that finds the scale
+        not finite takes the step back (opt.state["step"] -= 1), or the bias corrections run ahead of the moments."""
         if grads is None:
             grads = [p.grad for p in self.params]
         elif len(grads) != len(self.params):
