@@ -6,7 +6,7 @@ bf16 with or without a 32-bit master.
 """
 from __future__ import annotations
 
-from operator import attrgetter
+from operator import attrgetter, is_
 
 import numpy as np
 import torch
@@ -73,9 +73,14 @@ class AdamW:
         else:
             t["m"], t["v"] = (s[k].data_ptr() + at[:-1] for k in ("exp_avg", "exp_avg_root"))
             t["m_scale"], t["v_scale"] = (s[k].data_ptr() + 4 * (at[:-1] // BLOCK) for k in ("exp_avg_scale", "exp_avg_root_scale"))
+        self._names = tuple(k for k in s if k != "step")
+        self._held = self._buffers_now()  # the table has their addresses
         self._address = self._table.ctypes.data
         self._index, self._options = {self.params[0].get_device()}, None
         self._step = T.lib().topk_adamw_step
+
+    def _buffers_now(self):
+        return [*(self.masters or ()), *map(self.state.get, self._names)]
 
     def _buffers(self, total: int):
         if self.state_bits == 32:
@@ -116,6 +121,9 @@ class AdamW:
             raise ValueError("gradients must be contiguous, of the parameters' sizes and device, and of one dtype")
         if gdt not in (torch.float32, torch.bfloat16):
             raise TypeError("gradients must be float32 or bfloat16")
+        held = self._buffers_now()
+        if len(held) != len(self._held) or not all(map(is_, held, self._held)):
+            raise ValueError("the state's buffers or the masters were replaced: load_state_dict copies into them")
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1
                                        or grad_scale.device != self.device):
             raise ValueError("grad_scale must be one float32 element on the parameters' device")
@@ -143,7 +151,7 @@ class AdamW:
         for changed in (params, self.masters):
             if changed is not None:
                 T._changed(*(changed if whole else [t for t, g in zip(changed, grads) if g is not None]))
-        T._changed(*(t for k, t in self.state.items() if k != "step"))
+        T._changed(*held[0 if self.masters is None else len(self.masters):])
         self.state["step"] += 1
 
     def zero_grad(self, set_to_none: bool = True) -> None:
