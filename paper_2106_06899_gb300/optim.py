@@ -29,7 +29,9 @@ class AdamW:
 
     state_bits: 32 or 8.  masters: None, True (32-bit masters are made of bf16 parameters), or a
     list of fp32 tensors to use as masters.  state: buffers of an earlier optimizer (as state_dict
-    returns them) to continue with; they are used as they are, not copied."""
+    returns them) to continue with; they are used as they are, not copied.
+
+    Not a torch.optim.Optimizer.  A step's number goes to the kernel by value: a CUDA graph repeats the one it captured."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                  state_bits: int = 32, seed: int = 0, masters=None, state=None):
