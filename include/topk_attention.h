@@ -88,8 +88,9 @@ enum {
   TOPK_ERR_NO_DEVICE = -6,   /* no usable sm_103 device */
   TOPK_ERR_SCRATCH_LIMIT = -7, /* the problem needs more scratch than the fixed buffer of
                                  topk_ffn_fwd_noalloc holds */
-  TOPK_ERR_RANGE = -8        /* a position outside the rotation tables (its nearest row was used) or
-                                a row outside the cache (not written); reported by topk_check() */
+  TOPK_ERR_RANGE = -8        /* a position outside the rotation tables (its nearest row was used), a row
+                                outside the cache (not written), a token outside the vocabulary (taken as
+                                none) or sequences outside their tensors (cut); reported by topk_check() */
 };
 
 /*
@@ -389,6 +390,120 @@ typedef struct {
 int topk_adamw_step(const topk_adamw_tensor* tensors, int count, int param_dtype, int grad_dtype, int state_bits,
                     double beta1, double beta2, double eps, long long step, const float* grad_scale, uint32_t seed,
                     void* stream);
+
+/*
+ * Embedding lookup: out[n] = scale weight[ids[n]], rounded once, to nearest.
+ *   ids      : [N] int32 or int64 (id_bits 32 or 64).  A negative id is padding: its row of out is zero.  An id
+ *              of `rows` or more gives zeros too and is reported as TOPK_ERR_RANGE by topk_check().
+ *   weight   : [rows, D].  out: [N, D].  `dtype`, contiguous, 16-byte aligned; any D.
+ */
+int topk_embedding_fwd(const void* ids, int id_bits, const void* weight, void* out, int N, int rows, int D, float scale,
+                       int dtype, void* stream);
+
+/*
+ * Backward: dweight[v] = scale (sum of dy[n] over the n with ids[n] = v), in fp32 and always added up in the same
+ * order: two runs give the same bits.  Ids that are padding or out of range add to nothing (the latter are reported
+ * as TOPK_ERR_RANGE).
+ *   dy         : [N, D] of `dtype`.  dweight: [rows, D] of grad_dtype (TOPK_F32 or TOPK_BF16).
+ *   accumulate : 0: every row of dweight is written, zeros where no id points.  1: the sums are added to what dweight
+ *                holds (tied weights, several batches), rounded once; rows without an id are left alone.
+ *   Scratch: topk_embedding_bwd_workspace_bytes(): 16 bytes for each id and two rows of D floats for every 32 ids.
+ */
+int topk_embedding_bwd(const void* dy, const void* ids, int id_bits, void* dweight, int N, int rows, int D, float scale,
+                       int accumulate, int dtype, int grad_dtype, void* stream);
+size_t topk_embedding_bwd_workspace_bytes(int N, int rows, int D);
+
+/*
+ * What the logits of a row say of its tokens, in one pass over them.  With z = scale x for a row x of V logits:
+ *   lse = ln sum_j e^z_j,  log p_j = z_j - lse,  entropy = -sum_j p_j log p_j,
+ *   logp = log p of the target, and the `top` tokens of the largest logits, largest first, ties to the lower index.
+ *   logits  : [N, V] of `dtype`, rows row_stride elements apart (>= V; any alignment of a whole element).
+ *   targets : [N] int32 or int64 (target_bits 32 or 64), or NULL.  A negative target is none: its logp is 0.  One of V or
+ *             more is taken as none and reported as TOPK_ERR_RANGE by topk_check().
+ *   scale   : > 0, the inverse of a temperature.
+ *   logp, entropy, lse: [N] fp32, or NULL where not wanted (logp needs targets).
+ *   top     : 0 to 128.  top_logp [N, top] fp32 and top_ids [N, top] int32, both or neither.
+ * A logit of -inf is a masked token: p = 0, and it is never an alternative (missing ones have index -1 and -inf, as the
+ * kept lists of the attention have).  A row of nothing else has lse -inf, entropy 0 and logp -inf.  A row with a NaN or
+ * +inf has NaN in its fp32 outputs (but for a logp without a target) and alternatives of index -1.
+ * Sums in fp32.
+ */
+int topk_token_logprobs_fwd(const void* logits, long long row_stride, const void* targets, int target_bits, float scale,
+                            int top, float* logp, float* entropy, float* lse, float* top_logp, int32_t* top_ids, int N,
+                            int V, int dtype, void* stream);
+
+/*
+ * Backward, from lse (and, for dentropy, the entropy) of the forward pass.  With G = dlogp + sum of dtop:
+ *   dz_j = dlogp [j = target] + sum_m dtop_m [j = top_ids_m] - G p_j - dentropy p_j (log p_j + entropy),
+ *   dlogits = scale dz, of `dtype`, rounded once.
+ *   dlogp   : [N] fp32 with targets, both or neither.  dentropy: [N] fp32 with entropy, both or neither.
+ *   dtop    : [N, top] fp32 with top_ids [N, top], both or neither (an index outside [0, V) gets nothing).  At least
+ *             one of dlogp, dentropy and dtop.
+ *   dlogits : [N, V], rows dlogits_stride elements apart; logits itself is allowed (with its stride).
+ * A row none of whose gradients differs from 0 is written as zeros, whatever its logits hold; so is one with nothing but masked
+ * logits.
+ */
+int topk_token_logprobs_bwd(const void* logits, long long row_stride, const float* lse, const void* targets,
+                            int target_bits, const float* dlogp, const float* entropy, const float* dentropy,
+                            const int32_t* top_ids, const float* dtop, int top, float scale, void* dlogits,
+                            long long dlogits_stride, int N, int V, int dtype, void* stream);
+
+/*
+ * Plain attention (Eq. 1) over packed sequences of different lengths, with grouped heads: query head h reads key
+ * head h / (Hq / Hkv).  As in every attention call here the temperature is in q.
+ *   q        : [Tq, Hq, d].  k, v: [Tk, Hkv, d].  bf16, 16-byte aligned, contiguous rows of d, with element strides
+ *              {token, head}, multiples of 8 and at least 1 where there is more than one: views of a packed projection,
+ *              or of the [1, H, T, d] that topk_qk_norm_rope_fwd writes.
+ *   q_starts : [B + 1] int32, device: sequence b's queries are rows q_starts[b] to q_starts[b + 1] - 1.
+ *   k_starts : the same for its keys and values; NULL: q_starts.  Bounds that fall, or lie outside [0, Tq] ([0, Tk]), are
+ *              clamped and reported as TOPK_ERR_RANGE by topk_check().
+ *   causal   : a sequence's queries are the last of its positions: with Lq queries and Lk keys, query i reads keys
+ *              j <= i + Lk - Lq (Lk > Lq: a prompt that goes on from cached keys).  0: every key of the sequence.
+ *   out      : [Tq, Hq, d] bf16, contiguous.  A query without a key gets zeros.  Rows of no sequence are left alone, or
+ *              with clear_rest = 1 written as zeros.
+ *   d        : 64 or 128.  Hq a multiple of Hkv, Hq / Hkv at most 128.
+ * Keys and values outside a sequence are not read into its results, whatever they hold.  Scores and sums in fp32; weights are
+ * rounded to bf16 as the tensor cores' operand (not in the softmax's sum).
+ *   Scratch: topk_prompt_attn_workspace_bytes(), a fixed amount for each SM.
+ */
+typedef struct {
+  const void *q, *k, *v;
+  void* out;
+  long long q_stride[2], k_stride[2], v_stride[2];
+  const int32_t *q_starts, *k_starts;
+  int B, Tq, Tk, Hq, Hkv, d, causal, clear_rest;
+} topk_prompt_args;
+
+int topk_prompt_attn_fwd(const topk_prompt_args* args, void* stream);
+size_t topk_prompt_attn_workspace_bytes(int d);
+
+/*
+ * Plain attention of T drafted tokens of each sequence against its key/value cache.  The cache holds kv_len[b]
+ * tokens and, in the T rows behind them, the drafted tokens' own keys and values (as topk_qk_norm_rope_fwd with
+ * cache_start = kv_len writes them).  Token i reads all of the kv_len[b] rows and drafted row j where bit j of its word of
+ * `tree` is set: its ancestors and itself.  T = 1 without a tree is ordinary decoding.
+ *   q            : [B, Hq, T, d].  keys, values: [B, Hkv, cap, d].  bf16, 16-byte aligned, contiguous rows of d, element
+ *                  strides {batch, head, row} as in topk_prompt_attn_fwd.  Query head h reads key head h / (Hq / Hkv).
+ *   kv_len       : [B] int32, device.  A negative one is no sequence: zeros come out.  kv_len[b] + T above cap is reported
+ *                  as TOPK_ERR_RANGE by topk_check(); rows from cap on do not exist.
+ *   tree         : [B, T] int64, device, or NULL: token i reads drafted tokens 0 to i (a chain).
+ *   tree_stride  : words from one sequence's to the next (0: one tree for all).
+ *   out          : [B, Hq, T, d] bf16, contiguous.  A token that reads nothing gets zeros.
+ *   T            : 1 to 64.  d, Hq and Hkv as above.
+ * Rows of the cache that a sequence does not have are not read into its results, whatever they hold.
+ *   Scratch: topk_prompt_attn_workspace_bytes().
+ */
+typedef struct {
+  const void *q, *keys, *values;
+  void* out;
+  long long q_stride[3], key_stride[3], value_stride[3];
+  const int32_t* kv_len;
+  const int64_t* tree;
+  long long tree_stride;
+  int B, T, Hq, Hkv, cap, d;
+} topk_tree_args;
+
+int topk_tree_attn_fwd(const topk_tree_args* args, void* stream);
 
 /* Scratch bytes of the two backward calls for these arguments; 0 if invalid or unsupported. */
 size_t topk_attn_bwd_workspace_bytes(int B, int H, int Lq, int Lk, int d, int topk, int dtype);

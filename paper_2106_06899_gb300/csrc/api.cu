@@ -8,7 +8,9 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
+#include <utility>
 
 #include "topk_attention.h"
 #include "kernels.h"
@@ -646,6 +648,173 @@ int topk_adamw_step(const topk_adamw_tensor* tensors, int count, int param_dtype
   return TOPK_OK;
 }
 
+namespace {
+bool known_dtype(int dtype) { return dtype == TOPK_F32 || dtype == TOPK_BF16; }
+
+// Whole numbers of 32 or 64 bits, aligned to their size.
+int validate_whole(const void* p, int bits) {
+  if (bits != 32 && bits != 64) return TOPK_ERR_INVALID_ARG;
+  return reinterpret_cast<uintptr_t>(p) & (bits / 8 - 1) ? TOPK_ERR_UNSUPPORTED : TOPK_OK;
+}
+
+int validate_embed(const void* ids, int id_bits, int N, int rows, int D, float scale, int dtype) {
+  if (!ids || N <= 0 || rows <= 0 || D <= 0 || !known_dtype(dtype) || !std::isfinite(scale)) return TOPK_ERR_INVALID_ARG;
+  // kernels count ids, rows and blocks of them in 32 bits
+  if (N > (1 << 30) || rows > (1 << 30) || D > (1 << 20)) return TOPK_ERR_UNSUPPORTED;
+  return validate_whole(ids, id_bits);
+}
+}  // namespace
+
+int topk_embedding_fwd(const void* ids, int id_bits, const void* weight, void* out, int N, int rows, int D, float scale,
+                       int dtype, void* stream) {
+  if (!weight || !out) return TOPK_ERR_INVALID_ARG;
+  const int rc = validate_embed(ids, id_bits, N, rows, D, scale, dtype);
+  if (rc) return rc;
+  if (!aligned16(weight) || !aligned16(out)) return TOPK_ERR_UNSUPPORTED;
+  DeviceState* dev = gb300();
+  if (!dev) return TOPK_ERR_NO_DEVICE;
+  const EmbedArgs a{ids, id_bits == 64, N, rows, D, scale};
+  return launched(embed_fwd(a, weight, out, dtype == TOPK_BF16, dev->num_sms, make_ctl(dev), static_cast<cudaStream_t>(stream)));
+}
+
+int topk_embedding_bwd(const void* dy, const void* ids, int id_bits, void* dweight, int N, int rows, int D, float scale,
+                       int accumulate, int dtype, int grad_dtype, void* stream) {
+  if (!dy || !dweight || !known_dtype(grad_dtype) || (accumulate != 0 && accumulate != 1)) return TOPK_ERR_INVALID_ARG;
+  const int rc = validate_embed(ids, id_bits, N, rows, D, scale, dtype);
+  if (rc) return rc;
+  if (!aligned16(dy) || !aligned16(dweight)) return TOPK_ERR_UNSUPPORTED;
+  DeviceState* dev = gb300();
+  if (!dev) return TOPK_ERR_NO_DEVICE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  void* buf = nullptr;
+  if (!pool_alloc(&buf, embed_bwd_workspace_bytes(N, rows, D), st)) return TOPK_ERR_CUDA;
+  const EmbedArgs a{ids, id_bits == 64, N, rows, D, scale};
+  const int n = embed_bwd(a, dy, dweight, accumulate != 0, dtype == TOPK_BF16, grad_dtype == TOPK_BF16, buf, dev->num_sms, make_ctl(dev), st);
+  cudaFreeAsync(buf, st);
+  return launched(n);
+}
+
+size_t topk_embedding_bwd_workspace_bytes(int N, int rows, int D) {
+  if (validate_embed(reinterpret_cast<void*>(16), 32, N, rows, D, 1.f, TOPK_F32) != TOPK_OK) return 0;
+  return embed_bwd_workspace_bytes(N, rows, D);
+}
+
+namespace {
+int validate_logprobs(const void* logits, long long stride, const void* targets, int target_bits, float scale, int top, int N, int V,
+                      int dtype) {
+  if (!logits || N <= 0 || V <= 0 || stride < V || top < 0 || !known_dtype(dtype)) return TOPK_ERR_INVALID_ARG;
+  if (!(scale > 0.f) || !std::isfinite(scale)) return TOPK_ERR_INVALID_ARG;
+  if (top > kMaxAlternatives || N > (1 << 30) || V > (1 << 30) || stride > (1ll << 31)) return TOPK_ERR_UNSUPPORTED;
+  if (reinterpret_cast<uintptr_t>(logits) % elem_bytes(dtype)) return TOPK_ERR_UNSUPPORTED;
+  return targets ? validate_whole(targets, target_bits) : TOPK_OK;
+}
+}  // namespace
+
+int topk_token_logprobs_fwd(const void* logits, long long row_stride, const void* targets, int target_bits, float scale,
+                            int top, float* logp, float* entropy, float* lse, float* top_logp, int32_t* top_ids, int N,
+                            int V, int dtype, void* stream) {
+  const int rc = validate_logprobs(logits, row_stride, targets, target_bits, scale, top, N, V, dtype);
+  if (rc) return rc;
+  if ((logp && !targets) || (top_logp != nullptr) != (top > 0) || (top_ids != nullptr) != (top > 0)) return TOPK_ERR_INVALID_ARG;
+  if (!logp && !entropy && !lse && !top) return TOPK_ERR_INVALID_ARG;
+  for (const void* p : {static_cast<const void*>(logp), static_cast<const void*>(entropy), static_cast<const void*>(lse),
+                        static_cast<const void*>(top_logp), static_cast<const void*>(top_ids)})
+    if (!aligned4(p)) return TOPK_ERR_UNSUPPORTED;
+  DeviceState* dev = gb300();
+  if (!dev) return TOPK_ERR_NO_DEVICE;
+  const LogprobArgs a{logits, row_stride, targets, target_bits == 64, scale, top, N, V};
+  return launched(logprob_fwd(a, logp, entropy, lse, top_logp, top_ids, dtype == TOPK_BF16, dev->num_sms, make_ctl(dev),
+                              static_cast<cudaStream_t>(stream)));
+}
+
+int topk_token_logprobs_bwd(const void* logits, long long row_stride, const float* lse, const void* targets,
+                            int target_bits, const float* dlogp, const float* entropy, const float* dentropy,
+                            const int32_t* top_ids, const float* dtop, int top, float scale, void* dlogits,
+                            long long dlogits_stride, int N, int V, int dtype, void* stream) {
+  const int rc = validate_logprobs(logits, row_stride, targets, target_bits, scale, top, N, V, dtype);
+  if (rc) return rc;
+  if (!lse || !dlogits || dlogits_stride < V) return TOPK_ERR_INVALID_ARG;
+  if ((targets != nullptr) != (dlogp != nullptr) || (entropy != nullptr) != (dentropy != nullptr)) return TOPK_ERR_INVALID_ARG;
+  if ((top_ids != nullptr) != (top > 0) || (dtop != nullptr) != (top > 0) || (!dlogp && !dentropy && !dtop)) return TOPK_ERR_INVALID_ARG;
+  if (dlogits == logits && dlogits_stride != row_stride) return TOPK_ERR_INVALID_ARG;
+  if (dlogits_stride > (1ll << 31) || reinterpret_cast<uintptr_t>(dlogits) % elem_bytes(dtype)) return TOPK_ERR_UNSUPPORTED;
+  for (const void* p : {static_cast<const void*>(lse), static_cast<const void*>(dlogp), static_cast<const void*>(entropy),
+                        static_cast<const void*>(dentropy), static_cast<const void*>(top_ids), static_cast<const void*>(dtop)})
+    if (!aligned4(p)) return TOPK_ERR_UNSUPPORTED;
+  DeviceState* dev = gb300();
+  if (!dev) return TOPK_ERR_NO_DEVICE;
+  const LogprobArgs a{logits, row_stride, targets, target_bits == 64, scale, top, N, V};
+  return launched(logprob_bwd(a, lse, dlogp, entropy, dentropy, top_ids, dtop, dlogits, dlogits_stride, dtype == TOPK_BF16, dev->num_sms,
+                              static_cast<cudaStream_t>(stream)));
+}
+
+namespace {
+// What a tensor map holds: strides of whole 16 bytes below 2^40, and none of zero where there is more than one.
+int validate_strides(std::initializer_list<std::pair<int, long long>> dims) {
+  for (const auto& [n, stride] : dims) {
+    if (n > 1 && stride < 1) return TOPK_ERR_INVALID_ARG;
+    if (n > 1 && (stride % 8 || stride >= 1ll << 38)) return TOPK_ERR_UNSUPPORTED;
+  }
+  return TOPK_OK;
+}
+
+int validate_heads(int Hq, int Hkv, int d) {
+  if (Hq <= 0 || Hkv <= 0 || d <= 0 || Hq % Hkv) return TOPK_ERR_INVALID_ARG;
+  return (d != 64 && d != 128) || Hq / Hkv > 128 || Hq > 65536 ? TOPK_ERR_UNSUPPORTED : TOPK_OK;
+}
+
+// One of the two.
+int run_grouped(const topk_prompt_args* prompt, const topk_tree_args* tree, int d, void* stream) {
+  DeviceState* dev = gb300();
+  if (!dev) return TOPK_ERR_NO_DEVICE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  void* buf = nullptr;
+  const size_t ws = grouped_workspace_bytes(d, dev->num_sms);
+  if (ws && !pool_alloc(&buf, ws, st)) return TOPK_ERR_CUDA;
+  const DevCtl ctl = make_ctl(dev);
+  const int n = prompt ? prompt_attn(*prompt, buf, dev->num_sms, ctl, st) : tree_attn(*tree, buf, dev->num_sms, ctl, st);
+  if (buf) cudaFreeAsync(buf, st);
+  return launched(n);
+}
+}  // namespace
+
+int topk_prompt_attn_fwd(const topk_prompt_args* args, void* stream) {
+  if (!args || !args->q || !args->k || !args->v || !args->out || !args->q_starts) return TOPK_ERR_INVALID_ARG;
+  const topk_prompt_args& a = *args;
+  if (a.B <= 0 || a.Tq <= 0 || a.Tk <= 0 || (a.causal & ~1) || (a.clear_rest & ~1)) return TOPK_ERR_INVALID_ARG;
+  int rc = validate_heads(a.Hq, a.Hkv, a.d);
+  if (!rc)
+    rc = validate_strides({{a.Tq, a.q_stride[0]}, {a.Hq, a.q_stride[1]}, {a.Tk, a.k_stride[0]}, {a.Hkv, a.k_stride[1]}, {a.Tk, a.v_stride[0]},
+                           {a.Hkv, a.v_stride[1]}});
+  if (rc) return rc;
+  if (a.B > (1 << 20) || a.Tq > (1 << 28) || a.Tk > (1 << 28)) return TOPK_ERR_UNSUPPORTED;
+  if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.v) || !aligned16(a.out) || !aligned4(a.q_starts) || !aligned4(a.k_starts))
+    return TOPK_ERR_UNSUPPORTED;
+  return run_grouped(args, nullptr, a.d, stream);
+}
+
+size_t topk_prompt_attn_workspace_bytes(int d) {
+  if (d != 64 && d != 128) return 0;
+  const DeviceState* dev = device_state();
+  return grouped_workspace_bytes(d, dev ? dev->num_sms : kAssumedSms);
+}
+
+int topk_tree_attn_fwd(const topk_tree_args* args, void* stream) {
+  if (!args || !args->q || !args->keys || !args->values || !args->out || !args->kv_len) return TOPK_ERR_INVALID_ARG;
+  const topk_tree_args& a = *args;
+  if (a.B <= 0 || a.T <= 0 || a.cap <= 0 || a.tree_stride < 0) return TOPK_ERR_INVALID_ARG;
+  int rc = validate_heads(a.Hq, a.Hkv, a.d);
+  if (!rc)
+    rc = validate_strides({{a.B, a.q_stride[0]}, {a.Hq, a.q_stride[1]}, {a.T, a.q_stride[2]}, {a.B, a.key_stride[0]}, {a.Hkv, a.key_stride[1]},
+                           {a.cap, a.key_stride[2]}, {a.B, a.value_stride[0]}, {a.Hkv, a.value_stride[1]}, {a.cap, a.value_stride[2]}});
+  if (rc) return rc;
+  if (a.T > 64 || a.B > (1 << 20) || a.cap > (1 << 28)) return TOPK_ERR_UNSUPPORTED;
+  if (!aligned16(a.q) || !aligned16(a.keys) || !aligned16(a.values) || !aligned16(a.out) || !aligned4(a.kv_len) ||
+      (reinterpret_cast<uintptr_t>(a.tree) & 7u))
+    return TOPK_ERR_UNSUPPORTED;
+  return run_grouped(nullptr, args, a.d, stream);
+}
+
 size_t topk_qk_norm_rope_bwd_workspace_bytes(int B, int L, int Hq, int Hkv, int d) {
   if (B <= 0 || L <= 0 || Hq <= 0 || Hkv <= 0 || Hq > 65536 || Hkv > 65536 || d <= 0 || d % 8 != 0 || d > 256) return 0;
   const DeviceState* dev = device_state();
@@ -907,7 +1076,7 @@ const char* topk_error_string(int code) {
     case TOPK_ERR_WORKSPACE: return "per-row candidate list overflowed; outputs invalid";
     case TOPK_ERR_NO_DEVICE: return "no usable sm_103 device";
     case TOPK_ERR_SCRATCH_LIMIT: return "problem needs more scratch than the fixed no-allocation buffer holds";
-    case TOPK_ERR_RANGE: return "a position outside the rotation tables or a row outside the cache";
+    case TOPK_ERR_RANGE: return "a position, cache row, token or sequence outside its table";
     default: return "unknown error code";
   }
 }

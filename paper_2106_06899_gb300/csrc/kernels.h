@@ -11,7 +11,7 @@
 
 namespace topk {
 
-// flag of the device error word: a position or cache row outside its table (norm_rope.cu)
+// flag of the device error word: a position, cache row, token or sequence outside its table
 constexpr unsigned kDevErrRange = 4u;
 
 // topk above this uses 32-row CTAs on the SIMT path (heap memory is
@@ -196,6 +196,38 @@ size_t linear_fwd_workspace_bytes(int M, int N, int K, int num_sms);
 size_t linear_bwd_workspace_bytes(int M, int N, int K, int act, int num_sms);
 int linear_fwd(const LinearArgs& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st);
 int linear_bwd(const LinearBwdArgs& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st);
+
+// Embedding lookup and its gradient (embed.cu).
+struct EmbedArgs {
+  const void* ids;
+  bool ids64;
+  int N, rows, D;
+  float scale;
+};
+int embed_fwd(const EmbedArgs& a, const void* weight, void* out, bool bf16, int num_sms, const DevCtl& ctl, cudaStream_t st);
+size_t embed_bwd_workspace_bytes(int N, int rows, int D);
+int embed_bwd(const EmbedArgs& a, const void* dy, void* dweight, bool accumulate, bool bf16, bool grad_bf16, void* workspace, int num_sms,
+              const DevCtl& ctl, cudaStream_t st);
+
+// Log probabilities of tokens (logprob.cu).
+constexpr int kMaxAlternatives = 128;
+struct LogprobArgs {
+  const void* logits;
+  long long stride;
+  const void* targets;
+  bool targets64;
+  float scale;
+  int top, N, V;
+};
+int logprob_fwd(const LogprobArgs& a, float* logp, float* entropy, float* lse, float* top_logp, int32_t* top_ids, bool bf16, int num_sms,
+                const DevCtl& ctl, cudaStream_t st);
+int logprob_bwd(const LogprobArgs& a, const float* lse, const float* dlogp, const float* entropy, const float* dentropy, const int32_t* top_ids,
+                const float* dtop, void* dlogits, long long out_stride, bool bf16, int num_sms, cudaStream_t st);
+
+// Attention of grouped heads over packed prompts or over caches (grouped.cu).
+size_t grouped_workspace_bytes(int d, int num_sms);
+int prompt_attn(const topk_prompt_args& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st);
+int tree_attn(const topk_tree_args& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st);
 
 // Driver entry point for cuTensorMapEncodeTiled (resolved once, no libcuda link).
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,

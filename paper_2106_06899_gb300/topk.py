@@ -12,6 +12,7 @@ import ctypes
 import os
 import struct
 import threading
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -79,6 +80,17 @@ def lib() -> ctypes.CDLL:
             L.topk_linear_bwd_workspace_bytes.restype = sz
             L.topk_adamw_step.argtypes = [vp, i32, i32, i32, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                           ctypes.c_longlong, vp, ctypes.c_uint32, vp]
+            f32, i64 = ctypes.c_float, ctypes.c_longlong
+            L.topk_embedding_fwd.argtypes = [vp, i32, vp, vp, i32, i32, i32, f32, i32, vp]
+            L.topk_embedding_bwd.argtypes = [vp, vp, i32, vp, i32, i32, i32, f32, i32, i32, i32, vp]
+            L.topk_embedding_bwd_workspace_bytes.argtypes = [i32] * 3
+            L.topk_embedding_bwd_workspace_bytes.restype = sz
+            L.topk_token_logprobs_fwd.argtypes = [vp, i64, vp, i32, f32, i32] + [vp] * 5 + [i32] * 3 + [vp]
+            L.topk_token_logprobs_bwd.argtypes = [vp, i64, vp, vp, i32] + [vp] * 5 + [i32, f32, vp, i64] + [i32] * 3 + [vp]
+            L.topk_prompt_attn_fwd.argtypes = [vp, vp]
+            L.topk_prompt_attn_workspace_bytes.argtypes = [i32]
+            L.topk_prompt_attn_workspace_bytes.restype = sz
+            L.topk_tree_attn_fwd.argtypes = [vp, vp]
             L.topk_check.argtypes = [vp]
             L.topk_error_string.argtypes = [i32]
             L.topk_error_string.restype = ctypes.c_char_p
@@ -93,7 +105,9 @@ def lib() -> ctypes.CDLL:
                       "topk_last_launch_count",
                       "topk_debug_skip_arrive", "topk_pool_usage", "topk_pool_trim", "topk_attn_bwd",
                       "topk_ffn_bwd", "topk_attn_fwd_masked", "topk_vanilla_attn_fwd", "topk_vanilla_ffn_fwd",
-                      "topk_qk_norm_rope_fwd", "topk_qk_norm_rope_bwd", "topk_adamw_step", "topk_linear_fwd", "topk_linear_bwd"):
+                      "topk_qk_norm_rope_fwd", "topk_qk_norm_rope_bwd", "topk_adamw_step", "topk_linear_fwd", "topk_linear_bwd",
+                      "topk_embedding_fwd", "topk_embedding_bwd", "topk_token_logprobs_fwd", "topk_token_logprobs_bwd",
+                      "topk_prompt_attn_fwd", "topk_tree_attn_fwd"):
                 getattr(L, f).restype = i32
             _lib = L
     return _lib
@@ -527,6 +541,175 @@ def topk_linear_bwd_workspace_bytes(M, N, K, act: str = "none") -> int:
     return int(lib().topk_linear_bwd_workspace_bytes(M, N, K, _act_code(act)))
 
 
+def _whole(name, t, shape) -> int:
+    """The bits of t's whole numbers; t is a contiguous int32 or int64 tensor of the shape."""
+    if t.dtype not in (torch.int32, torch.int64) or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} int32 or int64 tensor")
+    return 32 if t.dtype == torch.int32 else 64
+
+
+def topk_embedding_fwd(ids, weight, out, scale: float = 1.0, stream=None) -> None:
+    """out [*ids.shape, D] = scale weight[ids]: ids int32 or int64 (a negative one is padding and gives zeros), weight
+    [rows, D] and out fp32 or bf16."""
+    if weight.dim() != 2 or not weight.is_contiguous():
+        raise ValueError("weight must be a contiguous [rows, D] tensor")
+    rows, D = weight.shape
+    N = ids.numel()
+    _fits(N, rows, D)
+    bits = _whole("ids", ids, ids.shape)
+    _written("out", out, (*ids.shape, D), weight.dtype)
+    code = _dtype_code(weight)
+    _on_gpu("ids, weight and out", weight, ids, out)
+    rc = lib().topk_embedding_fwd(_ptr(ids), bits, _ptr(weight), _ptr(out), N, rows, D, scale, code, _stream(stream))
+    _check(rc, "topk_embedding_fwd")
+    _changed(out)
+
+
+def topk_embedding_bwd(dy, ids, dweight, scale: float = 1.0, accumulate: bool = False, stream=None) -> None:
+    """dweight [rows, D] (fp32 or bf16) = scale x the sums of dy [*ids.shape, D] over each id's tokens, or with accumulate
+    that added to it."""
+    if dweight.dim() != 2 or not dweight.is_contiguous():
+        raise ValueError("dweight must be a contiguous [rows, D] tensor")
+    rows, D = dweight.shape
+    N = ids.numel()
+    _fits(N, rows, D)
+    bits = _whole("ids", ids, ids.shape)
+    _written("dy", dy, (*ids.shape, D), dy.dtype)
+    code, grad_code = _dtype_code(dy), _dtype_code(dweight)
+    _on_gpu("dy, ids and dweight", dweight, ids, dy)
+    rc = lib().topk_embedding_bwd(_ptr(dy), _ptr(ids), bits, _ptr(dweight), N, rows, D, scale, 1 if accumulate else 0, code, grad_code,
+                                  _stream(stream))
+    _check(rc, "topk_embedding_bwd")
+    _changed(dweight)
+
+
+def topk_embedding_bwd_workspace_bytes(N, rows, D) -> int:
+    return int(lib().topk_embedding_bwd_workspace_bytes(N, rows, D))
+
+
+def _rows_of(name, t):
+    """(N, V, row stride) of a [N, V] tensor with contiguous rows."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a [N, V] tensor with contiguous rows")
+    N, V = t.shape
+    stride = t.stride(0) if N > 1 else V
+    if stride < V:
+        raise ValueError(f"the rows of {name} must not overlap")
+    _fits(N, V, stride)
+    return N, V, stride
+
+
+def topk_token_logprobs_fwd(logits, targets=None, logp=None, entropy=None, lse=None, top_logp=None, top_ids=None, scale: float = 1.0,
+                            stream=None) -> None:
+    """Of each row of logits [N, V] (fp32 or bf16; rows may be strided) times scale: logp [N] of the targets ([N], int32 or int64,
+    negative: none), entropy [N], lse [N], and the largest tokens' top_logp and top_ids (int32) [N, top]; None where not wanted."""
+    N, V, stride = _rows_of("logits", logits)
+    top = 0 if top_ids is None else top_ids.shape[1]
+    bits = 32 if targets is None else _whole("targets", targets, (N,))
+    for name, t in (("logp", logp), ("entropy", entropy), ("lse", lse)):
+        _written(name, t, (N,), torch.float32)
+    _written("top_logp", top_logp, (N, top), torch.float32)
+    _written("top_ids", top_ids, (N, top), torch.int32)
+    code = _dtype_code(logits)
+    _on_gpu("logits, targets and outputs", logits, targets, logp, entropy, lse, top_logp, top_ids)
+    rc = lib().topk_token_logprobs_fwd(_ptr(logits), stride, _ptr(targets), bits, scale, top, _ptr(logp), _ptr(entropy), _ptr(lse),
+                                       _ptr(top_logp), _ptr(top_ids), N, V, code, _stream(stream))
+    _check(rc, "topk_token_logprobs_fwd")
+    _changed(logp, entropy, lse, top_logp, top_ids)
+
+
+def topk_token_logprobs_bwd(logits, lse, dlogits, targets=None, dlogp=None, entropy=None, dentropy=None, top_ids=None, dtop=None,
+                            scale: float = 1.0, stream=None) -> None:
+    """dlogits [N, V] (logits' dtype; may be logits itself) from the gradients of topk_token_logprobs_fwd's outputs: dlogp [N] with
+    targets, dentropy [N] with entropy, dtop [N, top] with top_ids, all fp32."""
+    N, V, stride = _rows_of("logits", logits)
+    if dlogits.shape != logits.shape or dlogits.dtype != logits.dtype:
+        raise ValueError("dlogits must have the shape and dtype of logits")
+    _, _, out_stride = _rows_of("dlogits", dlogits)
+    top = 0 if top_ids is None else top_ids.shape[1]
+    bits = 32 if targets is None else _whole("targets", targets, (N,))
+    for name, t in (("lse", lse), ("dlogp", dlogp), ("entropy", entropy), ("dentropy", dentropy)):
+        _written(name, t, (N,), torch.float32)
+    _written("top_ids", top_ids, (N, top), torch.int32)
+    _written("dtop", dtop, (N, top), torch.float32)
+    code = _dtype_code(logits)
+    _on_gpu("logits, dlogits, targets, lse, entropy and gradients", logits, dlogits, lse, targets, dlogp, entropy, dentropy, top_ids, dtop)
+    rc = lib().topk_token_logprobs_bwd(_ptr(logits), stride, _ptr(lse), _ptr(targets), bits, _ptr(dlogp), _ptr(entropy), _ptr(dentropy),
+                                       _ptr(top_ids), _ptr(dtop), top, scale, _ptr(dlogits), out_stride, N, V, code, _stream(stream))
+    _check(rc, "topk_token_logprobs_bwd")
+    _changed(dlogits)
+
+
+_PROMPT_PACK = struct.Struct("4P6q2P8i").pack  # topk_prompt_args
+_TREE_PACK = struct.Struct("4P9q2Pq6i").pack  # topk_tree_args
+
+
+def _heads_bf16(dims, **tensors) -> None:
+    for name, t in tensors.items():
+        if t.dtype != torch.bfloat16:
+            raise TypeError(f"{name} must be bfloat16")
+        if t.dim() != dims or (t.stride(-1) != 1 and t.shape[-1] > 1):
+            raise ValueError(f"{name} must be a {dims}-dimensional tensor with contiguous rows")
+        _fits(*t.shape)
+
+
+def _starts(name, t) -> None:
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] < 2 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [sequences + 1] int32 tensor")
+
+
+def topk_prompt_attn_fwd(q, k, v, out, q_starts, k_starts=None, causal: bool = True, clear_rest: bool = False, stream=None) -> None:
+    """Plain attention over packed sequences: q [Tq,Hq,d], k and v [Tk,Hkv,d] (bf16, strided views allowed), sequence b's queries in
+    rows q_starts[b] to q_starts[b + 1] - 1 ([B + 1] int32), its keys by k_starts likewise (None: q_starts); out [Tq,Hq,d], whose
+    rows of no sequence are left alone, or zeros with clear_rest."""
+    _heads_bf16(3, q=q, k=k, v=v)
+    Tq, Hq, d = q.shape
+    Tk, Hkv = k.shape[:2]
+    if k.shape[2] != d or v.shape != k.shape:
+        raise ValueError("shape mismatch between q, k, v")
+    _written("out", out, (Tq, Hq, d), torch.bfloat16)
+    _starts("q_starts", q_starts)
+    if k_starts is not None:
+        _starts("k_starts", k_starts)
+        if k_starts.shape != q_starts.shape:
+            raise ValueError("q_starts and k_starts must have the same length")
+    elif Tk != Tq:
+        raise ValueError("keys in other rows than the queries need k_starts")
+    _on_gpu("q, k, v, out and the starts", q, k, v, out, q_starts, k_starts)
+    args = _PROMPT_PACK(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), *q.stride()[:2], *k.stride()[:2], *v.stride()[:2],
+                        q_starts.data_ptr(), _ptr(k_starts) or 0, q_starts.shape[0] - 1, Tq, Tk, Hq, Hkv, d, 1 if causal else 0,
+                        1 if clear_rest else 0)
+    _check(lib().topk_prompt_attn_fwd(args, _stream(stream)), "topk_prompt_attn_fwd")
+    _changed(out)
+
+
+def topk_prompt_attn_workspace_bytes(d) -> int:
+    return int(lib().topk_prompt_attn_workspace_bytes(d))
+
+
+def topk_tree_attn_fwd(q, keys, values, out, kv_len, tree=None, stream=None) -> None:
+    """Plain attention of T drafted tokens of each sequence, q [B,Hq,T,d], over caches [B,Hkv,cap,d] (bf16, strided views allowed) of
+    kv_len[b] tokens ([B] int32) followed by the drafted ones; tree [B or 1, T] int64 has the drafted tokens that each one reads
+    (tree_mask), None: those up to it."""
+    _heads_bf16(4, q=q, keys=keys, values=values)
+    B, Hq, T, d = q.shape
+    Hkv, cap = keys.shape[1:3]
+    if keys.shape != (B, Hkv, cap, d) or values.shape != keys.shape:
+        raise ValueError("shape mismatch between q, keys, values")
+    _written("out", out, (B, Hq, T, d), torch.bfloat16)
+    if kv_len.dtype != torch.int32 or kv_len.shape != (B,) or not kv_len.is_contiguous():
+        raise ValueError("kv_len must be a contiguous [B] int32 tensor")
+    if tree is not None and (tree.dtype != torch.int64 or tree.dim() != 2 or tree.shape[0] not in (1, B) or tree.shape[1] != T
+                             or not tree.is_contiguous()):
+        raise ValueError("tree must be a contiguous [B or 1, T] int64 tensor")
+    _on_gpu("q, keys, values, out, kv_len and tree", q, keys, values, out, kv_len, tree)
+    args = _TREE_PACK(q.data_ptr(), keys.data_ptr(), values.data_ptr(), out.data_ptr(), *q.stride()[:3], *keys.stride()[:3],
+                      *values.stride()[:3], kv_len.data_ptr(), _ptr(tree) or 0, 0 if tree is None or tree.shape[0] == 1 else T, B, T, Hq, Hkv,
+                      cap, d)
+    _check(lib().topk_tree_attn_fwd(args, _stream(stream)), "topk_tree_attn_fwd")
+    _changed(out)
+
+
 def topk_attn_bwd_workspace_bytes(B, H, Lq, Lk, d, topk, dtype) -> int:
     return int(lib().topk_attn_bwd_workspace_bytes(B, H, Lq, Lk, d, topk, dtype))
 
@@ -674,3 +857,103 @@ def linear_bwd(dy, x, w, preact=None, act: str = "none", bias: bool = False, nee
         torch.empty(w.shape[0], dtype=grad_dtype, device=w.device) if bias else None))
     topk_linear_bwd(dy, x, w, dx, dw, db, preact, act, stream)
     return dx, dw, db
+
+
+def embedding(ids, weight, scale: float = 1.0, stream=None):
+    """scale weight[ids], [*ids.shape, D]; a negative id is padding: zeros."""
+    (out,) = _allocate(stream, lambda: (weight.new_empty((*ids.shape, weight.shape[-1])),))
+    if ids.numel():
+        topk_embedding_fwd(ids, weight, out, scale, stream)
+    return out
+
+
+def embedding_bwd(dy, ids, rows: int, scale: float = 1.0, grad_dtype=None, into=None, stream=None):
+    """The gradient [rows, D] of embedding's weight, of grad_dtype (None: dy's), or added to `into` (returned)."""
+    dtype = dy.dtype if grad_dtype is None else grad_dtype
+    shape = (rows, dy.shape[-1])
+    if into is not None:
+        _written("into", into, shape, into.dtype if grad_dtype is None else grad_dtype)
+        dweight = into
+    elif ids.numel():
+        (dweight,) = _allocate(stream, lambda: (torch.empty(shape, dtype=dtype, device=dy.device),))
+    else:
+        (dweight,) = _allocate(stream, lambda: (torch.zeros(shape, dtype=dtype, device=dy.device),))
+    if ids.numel():
+        topk_embedding_bwd(dy, ids, dweight, scale, into is not None, stream)
+    return dweight
+
+
+class TokenLogProbs(NamedTuple):
+    """token_logprobs' outputs; None where not asked for."""
+    logp: Optional[torch.Tensor]  # [N], of the targets
+    entropy: torch.Tensor  # [N]
+    lse: torch.Tensor  # [N]
+    top_logp: Optional[torch.Tensor]  # [N, top], largest first
+    top_ids: Optional[torch.Tensor]  # [N, top] int32
+
+
+def token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, stream=None) -> TokenLogProbs:
+    """Log probabilities, in fp32, under softmax(scale logits) for logits [N, V]: of the targets ([N]; negative: none, 0), the
+    entropy, the log of the sum, and the `top` likeliest tokens (ties to the lower id; a masked token, -inf, is none: id -1)."""
+    N = logits.shape[0]
+    ids, best, sums = _allocate(stream, lambda: (
+        torch.empty(N, top, dtype=torch.int32, device=logits.device) if top else None,
+        torch.empty(N, top, dtype=torch.float32, device=logits.device) if top else None,
+        torch.empty(2 if targets is None else 3, N, dtype=torch.float32, device=logits.device)))
+    entropy, lse, logp = (*sums, None)[:3]
+    if N:
+        topk_token_logprobs_fwd(logits, targets, logp, entropy, lse, best, ids, scale, stream)
+    return TokenLogProbs(logp, entropy, lse, best, ids)
+
+
+def token_logprobs_bwd(logits, lse, targets=None, dlogp=None, entropy=None, dentropy=None, top_ids=None, dtop=None, scale: float = 1.0,
+                       out=None, stream=None):
+    """The gradient of logits (their dtype) from those of token_logprobs' outputs; dentropy goes with its entropy, dtop with its
+    top_ids.  out: where to write it; logits itself is allowed."""
+    if dentropy is None:
+        entropy = None
+    if dlogp is None:
+        targets = None
+    if dtop is None:
+        top_ids = None
+    if out is None:
+        (out,) = _allocate(stream, lambda: (torch.empty(logits.shape, dtype=logits.dtype, device=logits.device),))
+    if logits.shape[0]:
+        topk_token_logprobs_bwd(logits, lse, out, targets, dlogp, entropy, dentropy, top_ids, dtop, scale, stream)
+    return out
+
+
+def prompt_attention(q, k, v, q_starts, k_starts=None, causal: bool = True, out=None, stream=None):
+    """Plain attention over packed sequences (topk_prompt_attn_fwd): [Tq,Hq,d], zeros in the rows of no sequence; with out those
+    rows are left alone."""
+    given = out is not None
+    if not given:
+        (out,) = _allocate(stream, lambda: (torch.empty(q.shape, dtype=q.dtype, device=q.device),))
+    if q.shape[0] and k.shape[0]:
+        topk_prompt_attn_fwd(q, k, v, out, q_starts, k_starts, causal, not given, stream)
+    elif q.shape[0]:
+        raise ValueError("no keys")
+    return out
+
+
+def tree_mask(parents: torch.Tensor) -> torch.Tensor:
+    """Drafted tokens' words for tree_attention from their parents [.., T] (T up to 64): parents[i] < i, or negative where token
+    i follows the cache directly.  Bit j of word i: token j is i or one of its ancestors."""
+    T = parents.shape[-1]
+    if T > 64:
+        raise ValueError("at most 64 drafted tokens")
+    i = torch.arange(T, device=parents.device)
+    step = (parents[..., None] == i) | (i[:, None] == i)  # to the parent, or to oneself
+    reach = step.float()
+    for _ in range(6):  # paths of up to 64 steps
+        reach = (reach @ reach).clamp_max(1)
+    words = torch.where(i == 63, torch.iinfo(torch.int64).min, 1 << i.clamp_max(62))
+    return (reach.long() * words).sum(-1)
+
+
+def tree_attention(q, keys, values, kv_len, tree=None, stream=None):
+    """Plain attention of drafted tokens over caches (topk_tree_attn_fwd): [B,Hq,T,d].  T = 1: ordinary decoding."""
+    (out,) = _allocate(stream, lambda: (torch.empty(q.shape, dtype=q.dtype, device=q.device),))
+    if out.numel():
+        topk_tree_attn_fwd(q, keys, values, out, kv_len, tree, stream)
+    return out
