@@ -1,86 +1,824 @@
-// grouped.cu -- plain attention (Eq. 1) of grouped heads: over packed prompts, and of drafted tokens over caches.
+// grouped.cu -- plain attention (Eq. 1) of grouped heads on the tensor cores: over packed prompts of different
+// lengths, and of drafted tokens over key/value caches.  One kernel serves both.
+//
+// A unit of work is a key head of a sequence with the rows of two 128-row tiles: a row is one query head of one
+// token, and a tile takes as many tokens as its 128 rows hold of the group's heads, so that a group's heads share
+// every key tile that is staged.  Per 128 keys and tile
+//   S = Q K^T      tcgen05.mma, fp32 in TMEM;
+//   P = 2^(S - m)  four warps, a row each thread, written over S as the bf16 operand that the next product
+//                  reads from TMEM;
+//   O += P V       tcgen05.mma, V as it lies in memory (its keys are the sum: the instruction transposes).
+// While the warps of one tile are at its exponentials, the tensor pipe works for the other.  A row's running maximum
+// m is raised only when a tile's exceeds it by more than kRaise; O and the sum are scaled then.
+//
+// Sequences differ in length by orders of magnitude, and only the device knows the lengths.  So the key tiles of all
+// units are numbered in one row, and every CTA takes an equal run of them: it computes from the lengths where
+// its run begins.  A run that begins or ends inside a unit leaves that unit's (m, sum, O) in scratch, at most two
+// such parts for each CTA, and grouped_join_kernel joins the parts of a unit in order.
 #include <cuda_bf16.h>
 
 #include "kernels.h"
+#include "pairs.cuh"
 
 namespace topk {
 
 namespace {
 
-// A warp for each query row: the softmax's running maximum and sum over its keys.
-template <typename Valid>
-__device__ void attend(const __nv_bfloat16* q, const __nv_bfloat16* k, long long k_stride, const __nv_bfloat16* v, long long v_stride, int keys, int d,
-                       __nv_bfloat16* out, Valid valid) {
-  const int lane = threadIdx.x & 31, each = d / 32;
-  float x[4], acc[4] = {}, m = -INFINITY, z = 0.f;
-  for (int e = 0; e < each; ++e) x[e] = __bfloat162float(q[lane * each + e]);
-  for (int j = 0; j < keys; ++j) {
-    if (!valid(j)) continue;
-    float s = 0.f;
-    for (int e = 0; e < each; ++e) s += x[e] * __bfloat162float(k[j * k_stride + lane * each + e]);
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    const float to = fmaxf(m, s), f = m == -INFINITY ? 0.f : expf(m - to), p = s == -INFINITY ? 0.f : expf(s - to);
-    m = to;
-    z = z * f + p;
-    for (int e = 0; e < each; ++e) acc[e] = acc[e] * f + p * __bfloat162float(v[j * v_stride + lane * each + e]);
+constexpr int BM = 128, BN = 128;  // rows of a tile, keys of a tile
+constexpr int kThreads = 384;      // loads, products, two idle warps; two groups of four softmax warps
+constexpr float kRaise = 8.0f;     // natural-log units
+constexpr float kLog2e = 1.4426950408889634f;
+
+template <int D>
+struct Layout {
+  static constexpr int R = D / 64;  // blocks of 128 bytes of a row
+  static constexpr uint32_t TILE = BM * D * 2;
+  static constexpr uint32_t BLOCK = BM * 128;  // a tile's rows of one 128-byte block
+  static constexpr int FIT = (232448 - 2048 - 2 * static_cast<int>(TILE)) / static_cast<int>(TILE);
+  static constexpr int S = FIT > 10 ? 10 : FIT;  // key and value tiles in turn: 5 for D = 128, 10 for 64
+  static constexpr size_t OFF_RING = 2 * static_cast<size_t>(TILE);
+  static constexpr size_t OFF_BAR = OFF_RING + static_cast<size_t>(S) * TILE;
+  static constexpr int NBARS = 2 * S + 13;
+  static constexpr size_t BYTES = 1024 + OFF_BAR + NBARS * 8 + 64;
+  static_assert(BYTES <= 232448 && S >= 4, "shared memory");
+  // TMEM columns: two score tiles, two outputs
+  static constexpr uint32_t O_COL = 2 * BN;
+  static constexpr uint32_t COLS = 512;
+};
+
+// A part of a unit in scratch: O as float4 [D / 4][256 rows], then m and the sum of each row.
+template <int D>
+constexpr size_t kPartFloats = 256 * (D + 2);
+
+struct Work {
+  const int32_t* q_starts;   // prompts
+  const int32_t* k_starts;
+  const int32_t* kv_len;     // caches
+  const int64_t* words;
+  long long word_stride;
+  __nv_bfloat16* out;
+  float* parts;
+  int B, Hq, Hkv, group, Tq, Tk, T, cap, causal, clear_rest;
+  int tokens;  // of a tile
+};
+
+// One sequence: its rows in q and k, and how many; with a cache, how many keys precede the drafted ones.
+struct Seq {
+  int q0, Lq, k0, Lk, prefix;
+  int blocks;  // pairs of tiles
+};
+
+template <bool TREE>
+__device__ __forceinline__ Seq seq_of(const Work& w, int b, bool* bad = nullptr) {
+  Seq s;
+  if constexpr (TREE) {
+    const int n = __ldg(w.kv_len + b);
+    s.q0 = s.k0 = 0;
+    s.Lq = w.T;
+    s.prefix = min(max(n, 0), w.cap);
+    s.Lk = n < 0 ? 0 : min(s.prefix + w.T, w.cap);
+    if (bad) *bad = static_cast<long long>(n) + w.T > w.cap;
+  } else {
+    const int q0 = __ldg(w.q_starts + b), q1 = __ldg(w.q_starts + b + 1);
+    s.q0 = min(max(q0, 0), w.Tq);
+    const int qe = max(s.q0, min(max(q1, 0), w.Tq));
+    const int k0 = __ldg(w.k_starts + b), k1 = __ldg(w.k_starts + b + 1);
+    s.k0 = min(max(k0, 0), w.Tk);
+    const int ke = max(s.k0, min(max(k1, 0), w.Tk));
+    s.Lq = qe - s.q0, s.Lk = ke - s.k0;
+    s.prefix = 0;
+    if (bad) *bad = q0 != s.q0 || q1 != qe || k0 != s.k0 || k1 != ke;
   }
-  for (int e = 0; e < each; ++e) out[lane * each + e] = __float2bfloat16_rn(z > 0.f ? acc[e] / z : z == 0.f ? 0.f : NAN);
+  s.blocks = (s.Lq + 2 * w.tokens - 1) / (2 * w.tokens);
+  return s;
 }
 
-// Sequence b's rows [first, end), cut to the tensor.
-__device__ bool bounds_of(const int32_t* starts, int b, int T, int& first, int& end) {
-  const int s = __ldg(starts + b), e = __ldg(starts + b + 1);
-  first = min(max(s, 0), T), end = max(first, min(max(e, 0), T));
-  return s == first && e == end;
+// Key tiles that the tokens up to `last` read: one at least, which is masked where they read nothing.
+template <bool TREE>
+__device__ __forceinline__ int key_tiles(const Work& w, const Seq& s, int last) {
+  const int lim = !TREE && w.causal ? last + 1 + s.Lk - s.Lq : s.Lk;
+  return max(1, (lim + BN - 1) / BN);
 }
 
-__global__ void prompt_kernel(topk_prompt_args a, DevCtl ctl) {
-  const int row = blockIdx.x, head = blockIdx.y * blockDim.y + threadIdx.y;
-  if (head >= a.Hq) return;
-  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (static_cast<size_t>(row) * a.Hq + head) * a.d;
-  for (int b = 0; b < a.B; ++b) {
-    int q0, q1, k0, k1;
-    bool ok = bounds_of(a.q_starts, b, a.Tq, q0, q1);
-    ok &= bounds_of(a.k_starts ? a.k_starts : a.q_starts, b, a.Tk, k0, k1);
-    if (!ok) atomicOr(ctl.error, kDevErrRange);
-    if (row < q0 || row >= q1) continue;
-    const int g = head / (a.Hq / a.Hkv), keys = k1 - k0, lim = a.causal ? row - q0 + keys - (q1 - q0) + 1 : keys;
-    attend(static_cast<const __nv_bfloat16*>(a.q) + row * a.q_stride[0] + head * a.q_stride[1],
-           static_cast<const __nv_bfloat16*>(a.k) + k0 * a.k_stride[0] + g * a.k_stride[1], a.k_stride[0],
-           static_cast<const __nv_bfloat16*>(a.v) + k0 * a.v_stride[0] + g * a.v_stride[1], a.v_stride[0], min(lim, keys), a.d, out,
-           [](int) { return true; });
-    return;
+template <bool TREE>
+__device__ __forceinline__ int block_tiles(const Work& w, const Seq& s, int block) {
+  return key_tiles<TREE>(w, s, min((block + 1) * 2 * w.tokens, s.Lq) - 1);
+}
+
+// sum over i < n of floor((a i + b) / m), by the steps of Euclid's algorithm for (a, m)
+__device__ __forceinline__ long long floor_sum(unsigned n, unsigned m, unsigned a, unsigned b) {
+  long long sum = 0;
+  while (n) {
+    sum += static_cast<long long>(a / m) * (static_cast<long long>(n) * (n - 1) / 2) + static_cast<long long>(b / m) * n;
+    a %= m, b %= m;
+    const unsigned y = a * n + b;
+    if (y < m) break;
+    n = y / m, b = y % m;
+    const unsigned t = a;
+    a = m, m = t;
   }
-  if (a.clear_rest)
-    for (int e = threadIdx.x; e < a.d; e += 32) out[e] = __float2bfloat16_rn(0.f);
+  return sum;
 }
 
-__global__ void tree_kernel(topk_tree_args a, DevCtl ctl) {
-  const int i = blockIdx.x % a.T, b = blockIdx.x / a.T, head = blockIdx.y * blockDim.y + threadIdx.y;
-  if (head >= a.Hq) return;
-  const int n = __ldg(a.kv_len + b), g = head / (a.Hq / a.Hkv);
-  if (static_cast<long long>(n) + a.T > a.cap) atomicOr(ctl.error, kDevErrRange);
-  const int prefix = min(max(n, 0), a.cap), keys = n < 0 ? 0 : min(prefix + a.T, a.cap);
-  const unsigned long long word = a.tree ? static_cast<unsigned long long>(a.tree[b * a.tree_stride + i]) : ~0ull >> (63 - i);
-  attend(static_cast<const __nv_bfloat16*>(a.q) + b * a.q_stride[0] + head * a.q_stride[1] + i * a.q_stride[2],
-         static_cast<const __nv_bfloat16*>(a.keys) + b * a.key_stride[0] + g * a.key_stride[1], a.key_stride[2],
-         static_cast<const __nv_bfloat16*>(a.values) + b * a.value_stride[0] + g * a.value_stride[1], a.value_stride[2], keys, a.d,
-         static_cast<__nv_bfloat16*>(a.out) + ((static_cast<size_t>(b) * a.Hq + head) * a.T + i) * a.d,
-         [=](int j) { return j < prefix || (word >> (j - prefix) & 1ull); });
+// Key tiles of a head's blocks before `block`.
+template <bool TREE>
+__device__ __forceinline__ long long tiles_before(const Work& w, const Seq& s, int block) {
+  if (block == 0) return 0;
+  if (TREE || !w.causal) return static_cast<long long>(block) * max(1, (s.Lk + BN - 1) / BN);
+  if (block == s.blocks) return tiles_before<TREE>(w, s, block - 1) + block_tiles<TREE>(w, s, block - 1);
+  // block i < blocks - 1 reads (i + 1) step + Lk - Lq keys
+  const int step = 2 * w.tokens, more = s.Lk - s.Lq;
+  const int none = more < 0 ? min(block, -more / step) : 0;  // blocks that read nothing
+  return none + floor_sum(block - none, BN, step, (none + 1) * step + more + BN - 1);
+}
+
+// The run of key tiles that CTA i of `ctas` begins with.
+__device__ __forceinline__ long long run_start(long long total, int ctas, int i) {
+  return total / ctas * i + total % ctas * i / ctas;
+}
+
+struct Place {
+  int b, h, block, kt;
+  long long total;
+};
+
+// Where the key tile number run_start(total, .., i) is; computed by a whole warp.  ctas: CTAs with work.
+template <bool TREE>
+__device__ Place locate(const Work& w, int i, int grid, int& ctas, unsigned* error) {
+  const int lane = threadIdx.x & 31;
+  Place p{0, 0, 0, 0, 0};
+  bool wrong = false;
+  for (int b = lane; b < w.B; b += 32) {
+    bool bad;
+    const Seq s = seq_of<TREE>(w, b, &bad);
+    wrong |= bad;
+    p.total += tiles_before<TREE>(w, s, s.blocks) * w.Hkv;
+  }
+  if (error && wrong) atomicOr(error, kDevErrRange);
+  for (int o = 16; o; o >>= 1) p.total += __shfl_xor_sync(0xffffffffu, p.total, o);
+  ctas = static_cast<int>(min(static_cast<long long>(grid), p.total));
+  if (i >= ctas) return p;
+  long long left = run_start(p.total, ctas, i);
+  for (int b0 = 0; b0 < w.B; b0 += 32) {
+    long long mine = 0;
+    Seq s{};
+    if (b0 + lane < w.B) {
+      s = seq_of<TREE>(w, b0 + lane);
+      mine = tiles_before<TREE>(w, s, s.blocks) * w.Hkv;
+    }
+    long long upto = mine;
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    const unsigned at = __ballot_sync(0xffffffffu, upto > left);
+    if (at) {
+      const int k = __ffs(at) - 1;
+      int h = 0, block = 0, kt = 0;
+      if (lane == k) {
+        left -= upto - mine;
+        const long long head = mine / w.Hkv;
+        h = static_cast<int>(left / head);
+        left -= h * head;
+        int lo = 0, hi = s.blocks - 1;  // the last block with tiles_before <= left
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) / 2;
+          if (tiles_before<TREE>(w, s, mid) <= left)
+            lo = mid;
+          else
+            hi = mid - 1;
+        }
+        block = lo;
+        kt = static_cast<int>(left - tiles_before<TREE>(w, s, lo));
+      }
+      p.b = b0 + k;
+      p.h = __shfl_sync(0xffffffffu, h, k);
+      p.block = __shfl_sync(0xffffffffu, block, k);
+      p.kt = __shfl_sync(0xffffffffu, kt, k);
+      return p;
+    }
+    left -= __shfl_sync(0xffffffffu, upto, 31);
+  }
+  return p;
+}
+
+// A run's part of one unit: key tiles [kt0, kt1) of its n; tile x of the two takes those below n_tile[x].
+struct Segment {
+  int b, h, block, kt0, kt1, n;
+  int n_tile[2];
+  Seq seq;
+  __device__ __forceinline__ int end(int x) const { return min(kt1, n_tile[x]); }
+  __device__ __forceinline__ bool active(int x) const { return kt0 < end(x); }
+  __device__ __forceinline__ bool whole() const { return kt0 == 0 && kt1 == n; }
+};
+
+template <bool TREE>
+struct Run {
+  const Work& w;
+  Seq seq;
+  int b, h, block, kt;
+  long long left;
+
+  __device__ __forceinline__ Run(const Work& work, const Place& p, long long tiles) : w(work), b(p.b), h(p.h), block(p.block), kt(p.kt), left(tiles) {
+    if (left > 0) seq = seq_of<TREE>(w, b);
+  }
+  __device__ __forceinline__ bool next(Segment& s) {
+    if (left <= 0) return false;
+    if (block >= seq.blocks) {
+      block = 0;
+      if (++h == w.Hkv) {
+        h = 0;
+        do {
+          if (++b >= w.B) return false;
+          seq = seq_of<TREE>(w, b);
+        } while (seq.blocks == 0);
+      }
+    }
+    s.b = b, s.h = h, s.block = block, s.kt0 = kt;
+    s.seq = seq;
+    s.n = 0;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int t0 = (2 * block + x) * w.tokens;
+      s.n_tile[x] = t0 < seq.Lq ? key_tiles<TREE>(w, seq, min(t0 + w.tokens, seq.Lq) - 1) : 0;
+      s.n = max(s.n, s.n_tile[x]);
+    }
+    s.kt1 = static_cast<int>(min(static_cast<long long>(s.n), kt + left));
+    left -= s.kt1 - kt;
+    kt = 0;
+    ++block;
+    return true;
+  }
+};
+
+// ------------------------------------------------------------ instructions
+__device__ __forceinline__ void load_4d(void* dst, const void* map, uint64_t* bar, int c0, int c1, int c2, int c3) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
+}
+
+// D[tmem] (+)= A[tmem] B[smem]: A's rows are lanes, two bf16 of a row in each column.
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// V's tile, keys x d, as an operand whose sum runs over the rows: 64-column blocks a whole tile of rows apart, groups of eight
+// keys 1024 bytes.
+__device__ __forceinline__ uint64_t sdesc_values(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>((BN * 128) >> 4) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), "r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
+      "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+
+// 2^x (ex2.approx, 2^-22); 2^-inf = 0
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const DevCtl& ctl, volatile int* abort_flag) {
+  int ok = 0;
+  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity, ctl, abort_flag) ? 1 : 0;
+  return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
+
+__device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity, const DevCtl& ctl) {
+  if (mbar_try_wait(bar, parity)) return;
+  const unsigned long long t0 = global_ns();
+  while (!mbar_try_wait(bar, parity)) {
+    if (global_ns() - t0 > ctl.wait_limit_ns) {
+      atomicOr(ctl.error, kDevErrTimeout);
+      return;
+    }
+  }
+}
+
+// Which of the keys j0 .. j0 + 127 a row reads, a bit each: those below `lim`, and drafted key i, at prefix + i, where bit
+// i of `word` is set.
+template <bool TREE>
+__device__ __forceinline__ void key_bits(uint32_t (&bits)[4], int j0, int lim, int prefix, unsigned long long word) {
+  const auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int j = j0 + 32 * i;
+    if constexpr (TREE) {
+      const int first = prefix - j;  // of the drafted keys
+      uint32_t drafted = 0;
+      if (first <= 0 && first > -64) drafted = static_cast<uint32_t>(word >> -first);
+      if (first > 0 && first < 32) drafted = static_cast<uint32_t>(word << first);
+      bits[i] = below(first) | (drafted & below(lim - j));
+    } else {
+      bits[i] = below(lim - j);
+    }
+  }
+}
+
+// ------------------------------------------------------------ the kernel
+template <int D, bool TREE>
+__global__ void __launch_bounds__(kThreads, 1)
+    grouped_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv,
+                   const __grid_constant__ Work w, DevCtl ctl) {
+  using L = Layout<D>;
+  constexpr int S = L::S, R = L::R;
+  constexpr uint32_t IDESC_S = idesc_bf16_f32(BM, BN), IDESC_O = idesc_bf16_f32(BM, D) | (1u << 16);
+
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint8_t* ring = smem + L::OFF_RING;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
+  uint64_t* empty = full + S;
+  uint64_t* q_full = full + 2 * S;        // [2], a tile each, as all below
+  uint64_t* q_empty = full + 2 * S + 2;
+  uint64_t* s_full = full + 2 * S + 4;
+  uint64_t* p_full = full + 2 * S + 6;
+  uint64_t* o_full = full + 2 * S + 8;
+  uint64_t* o_free = full + 2 * S + 10;
+  uint64_t* drain = full + 2 * S + 12;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + L::NBARS);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  Place* place_s = reinterpret_cast<Place*>(tmem_slot + 2);  // 8-byte aligned
+  long long* tiles_s = reinterpret_cast<long long*>(place_s + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(&q_full[x], 1);
+      mbar_init(&q_empty[x], 1);
+      mbar_init(&s_full[x], 1);
+      mbar_init(&p_full[x], 4);
+      mbar_init(&o_full[x], 1);
+      mbar_init(&o_free[x], 4);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, L::COLS);
+  if (warp == 2) {
+    int ctas;
+    const Place p = locate<TREE>(w, blockIdx.x, gridDim.x, ctas, blockIdx.x == 0 ? ctl.error : nullptr);
+    if (lane == 0) {
+      const int i = blockIdx.x;
+      *place_s = p;
+      *tiles_s = i < ctas ? run_start(p.total, ctas, i + 1) - run_start(p.total, ctas, i) : 0;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the join's blocks may wait from now on
+  const uint32_t tmem = *tmem_slot;
+  const long long tiles = *tiles_s;
+  const Place place = *place_s;
+
+  if (warp < 4) {
+    Run<TREE> run(w, place, tiles);
+    Segment seg;
+    if (warp == 0) {
+      // ------------------------------------------------------------ loads
+      if (lane == 0) {
+        tma_prefetch_desc(&tmq);
+        tma_prefetch_desc(&tmk);
+        tma_prefetch_desc(&tmv);
+        uint32_t it = 0, used[2] = {0, 0};  // ring tiles and query tiles loaded
+        bool ok = true;
+        auto load = [&](const CUtensorMap& map, int row, int h, int b) {
+          const uint32_t s = it % S;
+          if (!mbar_wait(&empty[s], ((it / S) & 1u) ^ 1u, ctl, abort_flag)) return false;
+          mbar_arrive_expect_tx(&full[s], L::TILE);
+#pragma unroll
+          for (int r = 0; r < R; ++r) load_4d(ring + s * L::TILE + r * L::BLOCK, &map, &full[s], r * 64, row, h, b);
+          ++it;
+          return true;
+        };
+        while (ok && run.next(seg)) {
+          const int b = TREE ? seg.b : 0;
+          for (int kt = seg.kt0; ok && kt < seg.kt1; ++kt) {
+            const int row = seg.seq.k0 + kt * BN;
+            ok = load(tmk, row, seg.h, b);
+            if (kt == seg.kt0) {
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                if (!ok || !seg.active(x)) continue;
+                if (!mbar_wait(&q_empty[x], (used[x] & 1u) ^ 1u, ctl, abort_flag)) {
+                  ok = false;
+                  continue;
+                }
+                mbar_arrive_expect_tx(&q_full[x], static_cast<uint32_t>(R * 128 * w.tokens * w.group));
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                  load_4d(smem + x * L::TILE + r * L::BLOCK, &tmq, &q_full[x], r * 64, seg.h * w.group, seg.seq.q0 + (2 * seg.block + x) * w.tokens, b);
+                ++used[x];
+              }
+            }
+            ok = ok && load(tmv, row, seg.h, b);
+          }
+        }
+        // every issued copy must land before the CTA exits
+        for (uint32_t back = 1; back <= static_cast<uint32_t>(S) && back <= it; ++back) drain_wait(&full[(it - back) % S], ((it - back) / S) & 1u, ctl);
+        for (int x = 0; x < 2; ++x)
+          if (used[x]) drain_wait(&q_full[x], (used[x] - 1) & 1u, ctl);
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      // ------------------------------------------------------------ products
+      // S of the next key tile is asked for right after O += P V of this one, tile by tile: P lies where S will.
+      if (lane == 0) {
+        Run<TREE> run_o(w, place, tiles);
+        Segment so;
+        bool more_s = run.next(seg), more_o = run_o.next(so), ok = true;
+        int kt_s = seg.kt0, kt_o = so.kt0;
+        uint32_t step_s = 0, step_o = 0;                          // key tiles so far
+        uint32_t q_used[2] = {0, 0}, p_used[2] = {0, 0}, o_used[2] = {0, 0};
+        auto scores = [&](int x) {  // of tile x and the key tile kt_s
+          if (kt_s >= seg.end(x)) return true;
+          const uint32_t s = (2 * step_s) % S;
+          if (!mbar_wait(&full[s], ((2 * step_s) / S) & 1u, ctl, abort_flag)) return false;
+          if (kt_s == seg.kt0 && !mbar_wait(&q_full[x], q_used[x]++ & 1u, ctl, abort_flag)) return false;
+          tc_fence_after();
+          const uint32_t qa = smem_u32(smem + x * L::TILE), ka = smem_u32(ring + s * L::TILE);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t at = (k / 4) * L::BLOCK + (k % 4) * 32;
+            mma_bf16_ss(tmem + x * BN, sdesc_k128(qa + at), sdesc_k128(ka + at), IDESC_S, k > 0 ? 1u : 0u);
+          }
+          mma_commit(&s_full[x]);
+          if (kt_s + 1 == seg.end(x)) mma_commit(&q_empty[x]);
+          return true;
+        };
+        auto values = [&](int x) {
+          if (kt_o >= so.end(x)) return true;
+          const uint32_t s = (2 * step_o + 1) % S;
+          if (!mbar_wait(&full[s], ((2 * step_o + 1) / S) & 1u, ctl, abort_flag)) return false;
+          // O of the unit before has been read
+          if (kt_o == so.kt0 && !mbar_wait(&o_free[x], (o_used[x]++ & 1u) ^ 1u, ctl, abort_flag)) return false;
+          if (!mbar_wait(&p_full[x], p_used[x]++ & 1u, ctl, abort_flag)) return false;
+          tc_fence_after();
+          const uint32_t va = smem_u32(ring + s * L::TILE);
+#pragma unroll
+          for (int k = 0; k < BN / 16; ++k)
+            mma_bf16_ts(tmem + L::O_COL + x * D, tmem + x * BN + k * 8, sdesc_values(va + k * 2048), IDESC_O, kt_o > so.kt0 || k > 0 ? 1u : 0u);
+          if (kt_o + 1 == so.end(x)) mma_commit(&o_full[x]);
+          return true;
+        };
+        auto advance_s = [&]() {
+          mma_commit(&empty[(2 * step_s) % S]);
+          ++step_s;
+          if (++kt_s == seg.kt1) {
+            more_s = run.next(seg);
+            kt_s = seg.kt0;
+          }
+        };
+        if (more_s) {
+          ok = scores(0) && scores(1);
+          if (ok) advance_s();
+        }
+        while (ok && more_o) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            ok = ok && values(x);
+            if (ok && more_s) ok = scores(x);
+          }
+          if (!ok) break;
+          mma_commit(&empty[(2 * step_o + 1) % S]);
+          if (more_s) advance_s();
+          ++step_o;
+          if (++kt_o == so.kt1) {
+            more_o = run_o.next(so);
+            kt_o = so.kt0;
+          }
+        }
+        // all products must be done before TMEM is freed
+        mma_commit(drain);
+        drain_wait(drain, 0, ctl);
+      }
+      __syncwarp();
+    } else if (!TREE && w.clear_rest) {
+      // rows of no sequence
+      const int first = min(max(__ldg(w.q_starts), 0), w.Tq), last = max(first, min(max(__ldg(w.q_starts + w.B), 0), w.Tq));
+      const long long row = static_cast<long long>(w.Hq) * D / 8, n = row * (first + w.Tq - last);
+      for (long long i = blockIdx.x * 64 + (threadIdx.x - 64); i < n; i += gridDim.x * 64)
+        reinterpret_cast<uint4*>(w.out)[i < first * row ? i : i + (last - first) * row] = make_uint4(0u, 0u, 0u, 0u);
+    }
+  } else {
+    // ------------------------------------------------------------ softmax
+    const int x = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;  // TMEM lane
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem + lanes + x * BN, o_addr = tmem + lanes + L::O_COL + x * D;
+    const int token_in = row / w.group, head_in = row % w.group;
+    uint32_t step = 0, s_used = 0, o_used = 0;
+    bool ok = true;
+    Run<TREE> run(w, place, tiles);
+    Segment seg;
+    while (ok && run.next(seg)) {
+      const int token = (2 * seg.block + x) * w.tokens + token_in;
+      const bool real = row < w.tokens * w.group && token < seg.seq.Lq;
+      const int end = seg.end(x);
+      float m = -INFINITY, z = 0.f;
+      if (seg.kt0 < end) {
+        const int Lk = seg.seq.Lk, prefix = seg.seq.prefix;
+        const int lim = !TREE && w.causal ? min(token + 1 + Lk - seg.seq.Lq, Lk) : Lk;
+        unsigned long long word = 0;
+        if (TREE && real) word = w.words ? static_cast<unsigned long long>(__ldg(w.words + seg.b * w.word_stride + token)) : ~0ull >> (63 - token);
+        const int clear = TREE ? min(prefix, Lk) : lim;  // keys below it are read without a look at the mask
+        for (int kt = seg.kt0; kt < end; ++kt, ++s_used) {
+          if (!warp_wait(&s_full[x], s_used & 1u, ctl, abort_flag)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          float s[BN];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, *reinterpret_cast<float(*)[32]>(s + 32 * c));
+          tmem_wait_ld();
+          const int j0 = kt * BN;
+          if (__any_sync(0xffffffffu, j0 + BN > clear)) {
+            uint32_t bits[4];
+            key_bits<TREE>(bits, j0, lim, prefix, word);
+#pragma unroll
+            for (int e = 0; e < BN; ++e)
+              if (!(bits[e / 32] >> (e % 32) & 1u)) s[e] = -INFINITY;
+            // a product takes 0 x value for a key that no row reads: values behind the sequence must be finite
+            if (j0 + BN > Lk) {
+              const uint32_t at = 2 * (step + kt - seg.kt0) + 1;
+              if (!warp_wait(&full[at % S], (at / S) & 1u, ctl, abort_flag)) {
+                ok = false;
+                break;
+              }
+              if (j0 + row >= Lk) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                  uint4* p = reinterpret_cast<uint4*>(ring + (at % S) * L::TILE + r * L::BLOCK + row * 128);
+#pragma unroll
+                  for (int c = 0; c < 8; ++c) p[c] = make_uint4(0u, 0u, 0u, 0u);
+                }
+              }
+              fence_proxy_async_smem();
+            }
+          }
+          float top = fmaxf(s[0], s[BN - 1]);
+#pragma unroll
+          for (int e = 1; e + 1 < BN; e += 2) top = max3f(top, s[e], s[e + 1]);
+          const bool raise = top > m + kRaise || (m == -INFINITY && top > -INFINITY);
+          const float to = raise ? top : m;
+          const float alpha = raise && m > -INFINITY ? exp2_fast((m - to) * kLog2e) : 1.f;
+          m = to;
+          // S of this key tile is there, so the product of the one before is done
+          if (kt > seg.kt0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll 1
+            for (int c = 0; c < D; c += 16) {
+              uint32_t o[16];
+              asm volatile(
+                  "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                  : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]), "=r"(o[8]), "=r"(o[9]), "=r"(o[10]),
+                    "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
+                  : "r"(o_addr + c));
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+              tmem_st16(o_addr + c, o);
+            }
+          }
+          const float ml = m == -INFINITY ? 0.f : m * kLog2e;
+          const F2 scale = f2(kLog2e, kLog2e), minus = f2(-ml, -ml);
+          F2 sum[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t p[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const F2 d = fma2(f2(s[32 * c + 2 * e], s[32 * c + 2 * e + 1]), scale, minus);
+              const float a = exp2_fast(lo(d)), b = exp2_fast(hi(d));
+              p[e] = pack2(a, b);
+              sum[e & 1] = add2(sum[e & 1], f2(a, b));
+            }
+            tmem_st16(s_addr + 16 * c, p);
+          }
+          const F2 both = add2(sum[0], sum[1]);
+          z = z * alpha + (lo(both) + hi(both));
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&p_full[x]);
+        }
+        if (!ok) break;
+        if (!warp_wait(&o_full[x], o_used++ & 1u, ctl, abort_flag)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+      }
+      if (seg.whole()) {
+        if (seg.kt0 < end) {
+          const float f = z == 0.f ? 0.f : 1.f / z;
+          const int head = seg.h * w.group + head_in;
+          __nv_bfloat16* out = w.out + (TREE ? (static_cast<size_t>(seg.b) * w.Hq + head) * w.T + token : static_cast<size_t>(seg.seq.q0 + token) * w.Hq + head) * D;
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            float o[32];
+            tmem_ld32(o_addr + c, o);
+            tmem_wait_ld();
+            uint32_t u[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) u[e] = z == 0.f ? 0u : pack2(o[2 * e] * f, o[2 * e + 1] * f);
+            if (real) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(out + c)[e] = make_uint4(u[4 * e], u[4 * e + 1], u[4 * e + 2], u[4 * e + 3]);
+            }
+          }
+        }
+      } else {
+        // the run's first unit goes to its first part, unless it begins with it
+        float* part = w.parts + (2 * static_cast<size_t>(blockIdx.x) + (seg.kt0 > 0 ? 0 : 1)) * kPartFloats<D>;
+        const int at = x * BM + row;
+        if (seg.kt0 < end) {
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            float o[32];
+            tmem_ld32(o_addr + c, o);
+            tmem_wait_ld();
+            if (real) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                reinterpret_cast<float4*>(part)[(c / 4 + e) * 256 + at] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            }
+          }
+        }
+        part[256 * D + at] = m;
+        part[256 * D + 256 + at] = z;
+      }
+      if (seg.kt0 < end) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&o_free[x]);
+      }
+      step += seg.kt1 - seg.kt0;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, L::COLS);
+  }
+}
+
+// Joins a unit's parts: block (i, c) looks at the place where CTA i + 1's run begins; where that is the first such place
+// inside its unit, it adds up the unit's parts in order, for 32 of the columns.
+template <int D, bool TREE>
+__global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant__ Work w, int grid) {
+  __shared__ Place place_s;
+  __shared__ int ctas_s;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int i = blockIdx.x + 1;
+  if (threadIdx.x < 32) {
+    int ctas;
+    const Place p = locate<TREE>(w, i, grid, ctas, nullptr);
+    if (threadIdx.x == 0) place_s = p, ctas_s = ctas;
+  }
+  __syncthreads();
+  const Place p = place_s;
+  const int ctas = ctas_s;
+  if (i >= ctas || p.kt == 0) return;
+  const Seq s = seq_of<TREE>(w, p.b);
+  const long long first = run_start(p.total, ctas, i) - p.kt, last = first + block_tiles<TREE>(w, s, p.block);
+  if (run_start(p.total, ctas, i - 1) > first) return;
+  int end = i + 1;  // CTAs i - 1 .. end - 1 have parts
+  while (end < ctas && run_start(p.total, ctas, end) < last) ++end;
+
+  const int at = threadIdx.x, row = at % BM, x = at / BM;
+  const int token = (2 * p.block + x) * w.tokens + row / w.group;
+  if (row >= w.tokens * w.group || token >= s.Lq) return;
+  const auto part = [&](int c) { return w.parts + (2 * static_cast<size_t>(c) + (c == i - 1 ? 1 : 0)) * kPartFloats<D>; };
+  float m = -INFINITY;
+  for (int c = i - 1; c < end; ++c) m = fmaxf(m, part(c)[256 * D + at]);
+  const float base = m == -INFINITY ? 0.f : m;
+  const int c0 = blockIdx.y * 32;
+  float z = 0.f, o[32] = {};
+  for (int c = i - 1; c < end; ++c) {
+    const float* from = part(c);
+    const float zc = from[256 * D + 256 + at];
+    if (zc == 0.f) continue;
+    const float f = exp2_fast((from[256 * D + at] - base) * kLog2e);
+    z += zc * f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float4 v = reinterpret_cast<const float4*>(from)[(c0 / 4 + e) * 256 + at];
+      o[4 * e] += v.x * f, o[4 * e + 1] += v.y * f, o[4 * e + 2] += v.z * f, o[4 * e + 3] += v.w * f;
+    }
+  }
+  const float f = z == 0.f ? 0.f : 1.f / z;
+  const int head = p.h * w.group + row % w.group;
+  __nv_bfloat16* out = w.out + (TREE ? (static_cast<size_t>(p.b) * w.Hq + head) * w.T + token : static_cast<size_t>(s.q0 + token) * w.Hq + head) * D + c0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    reinterpret_cast<uint4*>(out)[e] = make_uint4(pack2(o[8 * e] * f, o[8 * e + 1] * f), pack2(o[8 * e + 2] * f, o[8 * e + 3] * f),
+                                                  pack2(o[8 * e + 4] * f, o[8 * e + 5] * f), pack2(o[8 * e + 6] * f, o[8 * e + 7] * f));
+}
+
+// bf16 [n3][n2][n1][n0], strides in elements, boxes of 64 x b1 x b2 elements.
+bool make_map(CUtensorMap* map, const void* base, uint64_t n0, uint64_t n1, long long s1, uint64_t n2, long long s2, uint64_t n3, long long s3, uint32_t b1,
+              uint32_t b2) {
+  const cuuint64_t dims[4] = {n0, n1, n2, n3};
+  // the stride of an axis of one is never used
+  const cuuint64_t strides[3] = {(n1 > 1 ? static_cast<cuuint64_t>(s1) : n0) * 2, (n2 > 1 ? static_cast<cuuint64_t>(s2) : n0) * 2,
+                                 (n3 > 1 ? static_cast<cuuint64_t>(s3) : n0) * 2};
+  const cuuint32_t box[4] = {64, b1, b2, 1}, one[4] = {1, 1, 1, 1};
+  return encode_tiled_fn()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool TREE>
+int launch(const CUtensorMap& tmq, const CUtensorMap& tmk, const CUtensorMap& tmv, const Work& w, int grid, const DevCtl& ctl, cudaStream_t st) {
+  using L = Layout<D>;
+  const auto kernel = grouped_kernel<D, TREE>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::BYTES)) != cudaSuccess) return -1;
+  kernel<<<grid, kThreads, L::BYTES, st>>>(tmq, tmk, tmv, w, ctl);
+  if (cudaGetLastError() != cudaSuccess) return -1;
+  if (grid == 1) return 1;
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3(grid - 1, D / 32), config.blockDim = dim3(256), config.stream = st;
+  cudaLaunchAttribute early = {};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  config.attrs = &early, config.numAttrs = 1;
+  return cudaLaunchKernelEx(&config, grouped_join_kernel<D, TREE>, w, grid) == cudaSuccess ? 2 : -1;
 }
 
 }  // namespace
 
-size_t grouped_workspace_bytes(int, int) { return 0; }
-
-int prompt_attn(const topk_prompt_args& a, void*, int, const DevCtl& ctl, cudaStream_t st) {
-  prompt_kernel<<<dim3(a.Tq, (a.Hq + 7) / 8), dim3(32, 8), 0, st>>>(a, ctl);
-  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+size_t grouped_workspace_bytes(int d, int num_sms) {
+  return static_cast<size_t>(num_sms) * 2 * (d == 64 ? kPartFloats<64> : kPartFloats<128>) * sizeof(float);
 }
 
-int tree_attn(const topk_tree_args& a, void*, int, const DevCtl& ctl, cudaStream_t st) {
-  tree_kernel<<<dim3(a.B * a.T, (a.Hq + 7) / 8), dim3(32, 8), 0, st>>>(a, ctl);
-  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+int prompt_attn(const topk_prompt_args& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
+  if (!encode_tiled_fn()) return -1;
+  Work w = {};
+  w.q_starts = a.q_starts, w.k_starts = a.k_starts ? a.k_starts : a.q_starts;
+  w.out = static_cast<__nv_bfloat16*>(a.out), w.parts = static_cast<float*>(workspace);
+  w.B = a.B, w.Hq = a.Hq, w.Hkv = a.Hkv, w.group = a.Hq / a.Hkv, w.Tq = a.Tq, w.Tk = a.Tk, w.causal = a.causal, w.clear_rest = a.clear_rest;
+  w.tokens = BM / w.group;
+  CUtensorMap q, k, v;
+  if (!make_map(&q, a.q, a.d, a.Hq, a.q_stride[1], a.Tq, a.q_stride[0], 1, 0, w.group, w.tokens) ||
+      !make_map(&k, a.k, a.d, a.Tk, a.k_stride[0], a.Hkv, a.k_stride[1], 1, 0, BN, 1) ||
+      !make_map(&v, a.v, a.d, a.Tk, a.v_stride[0], a.Hkv, a.v_stride[1], 1, 0, BN, 1))
+    return -1;
+  return a.d == 64 ? launch<64, false>(q, k, v, w, num_sms, ctl, st) : launch<128, false>(q, k, v, w, num_sms, ctl, st);
+}
+
+int tree_attn(const topk_tree_args& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
+  if (!encode_tiled_fn()) return -1;
+  Work w = {};
+  w.kv_len = a.kv_len, w.words = a.tree, w.word_stride = a.tree_stride;
+  w.out = static_cast<__nv_bfloat16*>(a.out), w.parts = static_cast<float*>(workspace);
+  w.B = a.B, w.Hq = a.Hq, w.Hkv = a.Hkv, w.group = a.Hq / a.Hkv, w.T = a.T, w.cap = a.cap;
+  w.tokens = BM / w.group;
+  CUtensorMap q, k, v;
+  if (!make_map(&q, a.q, a.d, a.Hq, a.q_stride[1], a.T, a.q_stride[2], a.B, a.q_stride[0], w.group, w.tokens) ||
+      !make_map(&k, a.keys, a.d, a.cap, a.key_stride[2], a.Hkv, a.key_stride[1], a.B, a.key_stride[0], BN, 1) ||
+      !make_map(&v, a.values, a.d, a.cap, a.value_stride[2], a.Hkv, a.value_stride[1], a.B, a.value_stride[0], BN, 1))
+    return -1;
+  // key tiles of all units at most
+  const long long most = static_cast<long long>(a.B) * a.Hkv * ((a.T + 2 * w.tokens - 1) / (2 * w.tokens)) * ((a.cap + BN - 1) / BN);
+  const int grid = static_cast<int>(most < num_sms ? most : num_sms);
+  return a.d == 64 ? launch<64, true>(q, k, v, w, grid, ctl, st) : launch<128, true>(q, k, v, w, grid, ctl, st);
 }
 
 }  // namespace topk
