@@ -24,25 +24,27 @@ namespace topk {
 
 namespace {
 
-constexpr int BM = 128, BN = 128;  // rows of a tile, keys of a tile
-constexpr int kThreads = 384;      // loads, products, two idle warps; two groups of four softmax warps
-constexpr float kRaise = 8.0f;     // natural-log units
+constexpr int BM = 128, BN = 64;  // rows of a tile, keys of a step
+constexpr int kThreads = 384;     // loads, scores of each tile, products with the values; two groups of four softmax warps
+constexpr float kRaise = 8.0f;    // natural-log units
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <int D>
 struct Layout {
-  static constexpr int R = D / 64;  // blocks of 128 bytes of a row
-  static constexpr uint32_t TILE = BM * D * 2;
-  static constexpr uint32_t BLOCK = BM * 128;  // a tile's rows of one 128-byte block
-  static constexpr int FIT = (232448 - 2048 - 2 * static_cast<int>(TILE)) / static_cast<int>(TILE);
-  static constexpr int S = FIT > 10 ? 10 : FIT;  // key and value tiles in turn: 5 for D = 128, 10 for 64
-  static constexpr size_t OFF_RING = 2 * static_cast<size_t>(TILE);
+  static constexpr int R = D / 64;                 // blocks of 128 bytes of a row
+  static constexpr uint32_t Q_TILE = BM * D * 2, Q_BLOCK = BM * 128;
+  static constexpr uint32_t TILE = BN * D * 2, BLOCK = BN * 128;  // keys or values of a step
+  static constexpr int FIT = (232448 - 3072 - 2 * static_cast<int>(Q_TILE)) / static_cast<int>(TILE);
+  static constexpr int S = FIT > 16 ? 16 : FIT;    // keys and values of a step in turn: 10 for D = 128, 16 for 64
+  static constexpr size_t OFF_RING = 2 * static_cast<size_t>(Q_TILE);
   static constexpr size_t OFF_BAR = OFF_RING + static_cast<size_t>(S) * TILE;
-  static constexpr int NBARS = 2 * S + 13;
-  static constexpr size_t BYTES = 1024 + OFF_BAR + NBARS * 8 + 64;
-  static_assert(BYTES <= 232448 && S >= 4, "shared memory");
-  // TMEM columns: two score tiles, two outputs
-  static constexpr uint32_t O_COL = 2 * BN;
+  static constexpr int NBARS = 2 * S + 20;
+  static constexpr size_t OFF_EXCH = OFF_BAR + NBARS * 8 + 64;
+  static constexpr size_t BYTES = 1024 + OFF_EXCH + BM * 8;
+  static_assert(BYTES <= 232448, "shared memory");
+  static_assert(S >= 8 && S % 2 == 0, "scores run at most three steps ahead of the products with the values; keys lie in the even slots");
+  // TMEM columns: two score buffers of each tile, two outputs
+  static constexpr uint32_t O_COL = 4 * BN;
   static constexpr uint32_t COLS = 512;
 };
 
@@ -202,13 +204,16 @@ __device__ Place locate(const Work& w, int i, int grid, int& ctas, unsigned* err
   return p;
 }
 
-// A run's part of one unit: key tiles [kt0, kt1) of its n; tile x of the two takes those below n_tile[x].
+// A run's part of one unit: steps [kt0, kt1) of its n; tile x of the two takes those below n_tile[x].  Of a unit of one
+// tile the two groups of warps take every other step, each with an output of its own.
 struct Segment {
   int b, h, block, kt0, kt1, n;
   int n_tile[2];
   Seq seq;
-  __device__ __forceinline__ int end(int x) const { return min(kt1, n_tile[x]); }
-  __device__ __forceinline__ bool active(int x) const { return kt0 < end(x); }
+  __device__ __forceinline__ bool split() const { return n_tile[1] == 0; }
+  __device__ __forceinline__ bool own(int x, int kt) const { return split() ? ((kt - kt0) & 1) == x : kt < n_tile[x]; }
+  __device__ __forceinline__ bool active(int x) const { return split() ? kt1 - kt0 > x : kt0 < min(kt1, n_tile[x]); }
+  __device__ __forceinline__ bool last(int x, int kt) const { return split() ? kt + 2 >= kt1 : kt + 1 == min(kt1, n_tile[x]); }
   __device__ __forceinline__ bool whole() const { return kt0 == 0 && kt1 == n; }
 };
 
@@ -326,13 +331,13 @@ __device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity, const
   }
 }
 
-// Which of the keys j0 .. j0 + 127 a row reads, a bit each: those below `lim`, and drafted key i, at prefix + i, where bit
+// Which of the keys j0 .. j0 + 63 a row reads, a bit each: those below `lim`, and drafted key i, at prefix + i, where bit
 // i of `word` is set.
 template <bool TREE>
-__device__ __forceinline__ void key_bits(uint32_t (&bits)[4], int j0, int lim, int prefix, unsigned long long word) {
+__device__ __forceinline__ void key_bits(uint32_t (&bits)[BN / 32], int j0, int lim, int prefix, unsigned long long word) {
   const auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < BN / 32; ++i) {
     const int j = j0 + 32 * i;
     if constexpr (TREE) {
       const int first = prefix - j;  // of the drafted keys
@@ -360,33 +365,40 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* ring = smem + L::OFF_RING;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
   uint64_t* empty = full + S;
-  uint64_t* q_full = full + 2 * S;        // [2], a tile each, as all below
-  uint64_t* q_empty = full + 2 * S + 2;
-  uint64_t* s_full = full + 2 * S + 4;
-  uint64_t* p_full = full + 2 * S + 6;
-  uint64_t* o_full = full + 2 * S + 8;
-  uint64_t* o_free = full + 2 * S + 10;
-  uint64_t* drain = full + 2 * S + 12;
+  uint64_t* q_full = full + 2 * S;
+  uint64_t* q_empty = q_full + 1;
+  uint64_t* s_full = q_full + 2;    // [tile][buffer]
+  uint64_t* p_full = q_full + 6;    // [tile][buffer]
+  uint64_t* pv_done = q_full + 10;  // [tile][buffer]
+  uint64_t* o_full = q_full + 14;   // [tile]
+  uint64_t* o_free = q_full + 16;   // [tile]
+  uint64_t* exch_full = q_full + 18;
+  uint64_t* drain = q_full + 19;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + L::NBARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   Place* place_s = reinterpret_cast<Place*>(tmem_slot + 2);  // 8-byte aligned
-  long long* tiles_s = reinterpret_cast<long long*>(place_s + 1);
+  long long* steps_s = reinterpret_cast<long long*>(place_s + 1);
+  float2* exch = reinterpret_cast<float2*>(smem + L::OFF_EXCH);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], 1);
+      mbar_init(&empty[s], s % 2 == 0 ? 2 : 1);  // keys: the scores of both tiles
     }
-    for (int x = 0; x < 2; ++x) {
-      mbar_init(&q_full[x], 1);
-      mbar_init(&q_empty[x], 1);
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 2);
+    for (int x = 0; x < 4; ++x) {
       mbar_init(&s_full[x], 1);
       mbar_init(&p_full[x], 4);
+      mbar_init(&pv_done[x], 1);
+    }
+    for (int x = 0; x < 2; ++x) {
       mbar_init(&o_full[x], 1);
       mbar_init(&o_free[x], 4);
     }
-    mbar_init(drain, 1);
+    mbar_init(exch_full, 4);
+    mbar_init(drain, 3);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -397,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) {
       const int i = blockIdx.x;
       *place_s = p;
-      *tiles_s = i < ctas ? run_start(p.total, ctas, i + 1) - run_start(p.total, ctas, i) : 0;
+      *steps_s = i < ctas ? run_start(p.total, ctas, i + 1) - run_start(p.total, ctas, i) : 0;
     }
   }
   tc_fence_before();
@@ -405,172 +417,170 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the join's blocks may wait from now on
   const uint32_t tmem = *tmem_slot;
-  const long long tiles = *tiles_s;
+  const long long steps = *steps_s;
   const Place place = *place_s;
 
-  if (warp < 4) {
-    Run<TREE> run(w, place, tiles);
-    Segment seg;
-    if (warp == 0) {
-      // ------------------------------------------------------------ loads
-      if (lane == 0) {
-        tma_prefetch_desc(&tmq);
-        tma_prefetch_desc(&tmk);
-        tma_prefetch_desc(&tmv);
-        uint32_t it = 0, used[2] = {0, 0};  // ring tiles and query tiles loaded
-        bool ok = true;
-        auto load = [&](const CUtensorMap& map, int row, int h, int b) {
-          const uint32_t s = it % S;
-          if (!mbar_wait(&empty[s], ((it / S) & 1u) ^ 1u, ctl, abort_flag)) return false;
-          mbar_arrive_expect_tx(&full[s], L::TILE);
+  if (warp == 0) {
+    // ------------------------------------------------------------ loads
+    if (elect_one()) {
+      tma_prefetch_desc(&tmq);
+      tma_prefetch_desc(&tmk);
+      tma_prefetch_desc(&tmv);
+      Run<TREE> run(w, place, steps);
+      Segment seg;
+      uint32_t it = 0, segs = 0;  // ring tiles and units' queries loaded
+      bool ok = true;
+      auto load = [&](const CUtensorMap& map, int row, int h, int b) {
+        const uint32_t s = it % S;
+        if (!mbar_wait(&empty[s], ((it / S) & 1u) ^ 1u, ctl, abort_flag)) return false;
+        mbar_arrive_expect_tx(&full[s], L::TILE);
 #pragma unroll
-          for (int r = 0; r < R; ++r) load_4d(ring + s * L::TILE + r * L::BLOCK, &map, &full[s], r * 64, row, h, b);
-          ++it;
-          return true;
-        };
-        while (ok && run.next(seg)) {
-          const int b = TREE ? seg.b : 0;
-          for (int kt = seg.kt0; ok && kt < seg.kt1; ++kt) {
-            const int row = seg.seq.k0 + kt * BN;
-            ok = load(tmk, row, seg.h, b);
-            if (kt == seg.kt0) {
-#pragma unroll
-              for (int x = 0; x < 2; ++x) {
-                if (!ok || !seg.active(x)) continue;
-                if (!mbar_wait(&q_empty[x], (used[x] & 1u) ^ 1u, ctl, abort_flag)) {
-                  ok = false;
-                  continue;
-                }
-                mbar_arrive_expect_tx(&q_full[x], static_cast<uint32_t>(R * 128 * w.tokens * w.group));
+        for (int r = 0; r < R; ++r) load_4d(ring + s * L::TILE + r * L::BLOCK, &map, &full[s], r * 64, row, h, b);
+        ++it;
+        return true;
+      };
+      while (ok && run.next(seg)) {
+        const int b = TREE ? seg.b : 0;
+        for (int kt = seg.kt0; ok && kt < seg.kt1; ++kt) {
+          const int row = seg.seq.k0 + kt * BN;
+          ok = load(tmk, row, seg.h, b);
+          if (ok && kt == seg.kt0) {
+            ok = mbar_wait(q_empty, (segs & 1u) ^ 1u, ctl, abort_flag);
+            if (ok) {
+              const int n = seg.split() ? 1 : 2;
+              mbar_arrive_expect_tx(q_full, static_cast<uint32_t>(n * R * 128 * w.tokens * w.group));
+              for (int x = 0; x < n; ++x)
 #pragma unroll
                 for (int r = 0; r < R; ++r)
-                  load_4d(smem + x * L::TILE + r * L::BLOCK, &tmq, &q_full[x], r * 64, seg.h * w.group, seg.seq.q0 + (2 * seg.block + x) * w.tokens, b);
-                ++used[x];
-              }
+                  load_4d(smem + x * L::Q_TILE + r * L::Q_BLOCK, &tmq, q_full, r * 64, seg.h * w.group, seg.seq.q0 + (2 * seg.block + x) * w.tokens, b);
+              ++segs;
             }
-            ok = ok && load(tmv, row, seg.h, b);
           }
+          ok = ok && load(tmv, row, seg.h, b);
         }
-        // every issued copy must land before the CTA exits
-        for (uint32_t back = 1; back <= static_cast<uint32_t>(S) && back <= it; ++back) drain_wait(&full[(it - back) % S], ((it - back) / S) & 1u, ctl);
-        for (int x = 0; x < 2; ++x)
-          if (used[x]) drain_wait(&q_full[x], (used[x] - 1) & 1u, ctl);
       }
-      __syncwarp();
-    } else if (warp == 1) {
-      // ------------------------------------------------------------ products
-      // S of the next key tile is asked for right after O += P V of this one, tile by tile: P lies where S will.
-      if (lane == 0) {
-        Run<TREE> run_o(w, place, tiles);
-        Segment so;
-        bool more_s = run.next(seg), more_o = run_o.next(so), ok = true;
-        int kt_s = seg.kt0, kt_o = so.kt0;
-        uint32_t step_s = 0, step_o = 0;                          // key tiles so far
-        uint32_t q_used[2] = {0, 0}, p_used[2] = {0, 0}, o_used[2] = {0, 0};
-        auto scores = [&](int x) {  // of tile x and the key tile kt_s
-          if (kt_s >= seg.end(x)) return true;
-          const uint32_t s = (2 * step_s) % S;
-          if (!mbar_wait(&full[s], ((2 * step_s) / S) & 1u, ctl, abort_flag)) return false;
-          if (kt_s == seg.kt0 && !mbar_wait(&q_full[x], q_used[x]++ & 1u, ctl, abort_flag)) return false;
-          tc_fence_after();
-          const uint32_t qa = smem_u32(smem + x * L::TILE), ka = smem_u32(ring + s * L::TILE);
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            const uint32_t at = (k / 4) * L::BLOCK + (k % 4) * 32;
-            mma_bf16_ss(tmem + x * BN, sdesc_k128(qa + at), sdesc_k128(ka + at), IDESC_S, k > 0 ? 1u : 0u);
-          }
-          mma_commit(&s_full[x]);
-          if (kt_s + 1 == seg.end(x)) mma_commit(&q_empty[x]);
-          return true;
-        };
-        auto values = [&](int x) {
-          if (kt_o >= so.end(x)) return true;
-          const uint32_t s = (2 * step_o + 1) % S;
-          if (!mbar_wait(&full[s], ((2 * step_o + 1) / S) & 1u, ctl, abort_flag)) return false;
-          // O of the unit before has been read
-          if (kt_o == so.kt0 && !mbar_wait(&o_free[x], (o_used[x]++ & 1u) ^ 1u, ctl, abort_flag)) return false;
-          if (!mbar_wait(&p_full[x], p_used[x]++ & 1u, ctl, abort_flag)) return false;
-          tc_fence_after();
-          const uint32_t va = smem_u32(ring + s * L::TILE);
-#pragma unroll
-          for (int k = 0; k < BN / 16; ++k)
-            mma_bf16_ts(tmem + L::O_COL + x * D, tmem + x * BN + k * 8, sdesc_values(va + k * 2048), IDESC_O, kt_o > so.kt0 || k > 0 ? 1u : 0u);
-          if (kt_o + 1 == so.end(x)) mma_commit(&o_full[x]);
-          return true;
-        };
-        auto advance_s = [&]() {
-          mma_commit(&empty[(2 * step_s) % S]);
-          ++step_s;
-          if (++kt_s == seg.kt1) {
-            more_s = run.next(seg);
-            kt_s = seg.kt0;
-          }
-        };
-        if (more_s) {
-          ok = scores(0) && scores(1);
-          if (ok) advance_s();
-        }
-        while (ok && more_o) {
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            ok = ok && values(x);
-            if (ok && more_s) ok = scores(x);
-          }
-          if (!ok) break;
-          mma_commit(&empty[(2 * step_o + 1) % S]);
-          if (more_s) advance_s();
-          ++step_o;
-          if (++kt_o == so.kt1) {
-            more_o = run_o.next(so);
-            kt_o = so.kt0;
-          }
-        }
-        // all products must be done before TMEM is freed
-        mma_commit(drain);
-        drain_wait(drain, 0, ctl);
-      }
-      __syncwarp();
-    } else if (!TREE && w.clear_rest) {
-      // rows of no sequence
-      const int first = min(max(__ldg(w.q_starts), 0), w.Tq), last = max(first, min(max(__ldg(w.q_starts + w.B), 0), w.Tq));
-      const long long row = static_cast<long long>(w.Hq) * D / 8, n = row * (first + w.Tq - last);
-      for (long long i = blockIdx.x * 64 + (threadIdx.x - 64); i < n; i += gridDim.x * 64)
-        reinterpret_cast<uint4*>(w.out)[i < first * row ? i : i + (last - first) * row] = make_uint4(0u, 0u, 0u, 0u);
+      // every issued copy must land before the CTA exits
+      for (uint32_t back = 1; back <= static_cast<uint32_t>(S) && back <= it; ++back) drain_wait(&full[(it - back) % S], ((it - back) / S) & 1u, ctl);
+      if (segs) drain_wait(q_full, (segs - 1) & 1u, ctl);
     }
+    __syncwarp();
+  } else if (warp < 3) {
+    // ------------------------------------------------------------ scores of tile x
+    // A tile has two score buffers (P takes its scores' place), so that the scores of its next step are there when its warps
+    // are done with this one.  Every warp that issues products does so under elect: under a test of the lane the compiler does
+    // not know that one thread is left, and each product costs 110 cycles in place of 40.
+    const int x = warp - 1;
+    if (elect_one()) {
+      Run<TREE> run(w, place, steps);
+      Segment seg;
+      uint32_t step = 0, used = 0, segs = 0;
+      bool ok = true;
+      while (ok && run.next(seg)) {
+        ok = mbar_wait(q_full, segs++ & 1u, ctl, abort_flag);
+        const uint64_t qd = sdesc_k128(smem_u32(smem + (seg.split() ? 0 : x) * L::Q_TILE));
+        for (int kt = seg.kt0; ok && kt < seg.kt1; ++kt, ++step) {
+          const uint32_t s = (2 * step) % S;
+          ok = mbar_wait(&full[s], ((2 * step) / S) & 1u, ctl, abort_flag);
+          if (!ok) break;
+          if (!seg.own(x, kt)) {
+            mbar_arrive(&empty[s]);
+            continue;
+          }
+          const uint32_t buf = 2 * x + (used & 1u);
+          // the product with the P that lies there is done
+          if (used >= 2) ok = mbar_wait(&pv_done[buf], ((used >> 1) - 1) & 1u, ctl, abort_flag);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t kd = sdesc_k128(smem_u32(ring + s * L::TILE));
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+            mma_bf16_ss(tmem + buf * BN, qd + (((k / 4) * L::Q_BLOCK + (k % 4) * 32) >> 4), kd + (((k / 4) * L::BLOCK + (k % 4) * 32) >> 4), IDESC_S,
+                        k > 0 ? 1u : 0u);
+          mma_commit(&s_full[buf]);
+          mma_commit(&empty[s]);
+          ++used;
+        }
+        if (ok) mma_commit(q_empty);
+      }
+      // all products must be done before TMEM is freed
+      mma_commit(drain);
+      drain_wait(drain, 0, ctl);
+    }
+    __syncwarp();
+  } else if (warp == 3) {
+    // ------------------------------------------------------------ products with the values
+    if (elect_one()) {
+      Run<TREE> run(w, place, steps);
+      Segment seg;
+      uint32_t step = 0, used0 = 0, used1 = 0, units0 = 0, units1 = 0;
+      bool ok = true;
+      while (ok && run.next(seg)) {
+        bool first0 = true, first1 = true;
+        for (int kt = seg.kt0; ok && kt < seg.kt1; ++kt, ++step) {
+          const uint32_t s = (2 * step + 1) % S;
+          ok = mbar_wait(&full[s], ((2 * step + 1) / S) & 1u, ctl, abort_flag);
+          const uint64_t vd = sdesc_values(smem_u32(ring + s * L::TILE));
+          auto values = [&](int x, uint32_t& used, uint32_t& units, bool& first) {
+            if (!ok || !seg.own(x, kt)) return;
+            if (first) ok = mbar_wait(&o_free[x], (units++ & 1u) ^ 1u, ctl, abort_flag);  // O of the unit before has been read
+            const uint32_t buf = 2 * x + (used & 1u);
+            ok = ok && mbar_wait(&p_full[buf], (used >> 1) & 1u, ctl, abort_flag);
+            if (!ok) return;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < BN / 16; ++k)
+              mma_bf16_ts(tmem + L::O_COL + x * D, tmem + buf * BN + k * 8, vd + ((k * 2048) >> 4), IDESC_O, first && k == 0 ? 0u : 1u);
+            mma_commit(&pv_done[buf]);
+            if (seg.last(x, kt)) mma_commit(&o_full[x]);
+            first = false;
+            ++used;
+          };
+          values(0, used0, units0, first0);
+          values(1, used1, units1, first1);
+          if (ok) mma_commit(&empty[s]);
+        }
+      }
+      mma_commit(drain);
+      drain_wait(drain, 0, ctl);
+    }
+    __syncwarp();
   } else {
     // ------------------------------------------------------------ softmax
     const int x = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;  // TMEM lane
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_addr = tmem + lanes + x * BN, o_addr = tmem + lanes + L::O_COL + x * D;
+    const uint32_t s_addr = tmem + lanes + 2 * x * BN, o_addr = tmem + lanes + L::O_COL + x * D;
     const int token_in = row / w.group, head_in = row % w.group;
-    uint32_t step = 0, s_used = 0, o_used = 0;
+    uint32_t step = 0, used = 0;      // steps of the run, and of this tile
+    uint32_t outs[2] = {0, 0}, exchanges = 0;
     bool ok = true;
-    Run<TREE> run(w, place, tiles);
+    Run<TREE> run(w, place, steps);
     Segment seg;
     while (ok && run.next(seg)) {
-      const int token = (2 * seg.block + x) * w.tokens + token_in;
+      const bool split = seg.split(), mine = seg.active(x);
+      const int token = (2 * seg.block + (split ? 0 : x)) * w.tokens + token_in;
       const bool real = row < w.tokens * w.group && token < seg.seq.Lq;
-      const int end = seg.end(x);
       float m = -INFINITY, z = 0.f;
-      if (seg.kt0 < end) {
+      if (mine) {
         const int Lk = seg.seq.Lk, prefix = seg.seq.prefix;
         const int lim = !TREE && w.causal ? min(token + 1 + Lk - seg.seq.Lq, Lk) : Lk;
         unsigned long long word = 0;
         if (TREE && real) word = w.words ? static_cast<unsigned long long>(__ldg(w.words + seg.b * w.word_stride + token)) : ~0ull >> (63 - token);
         const int clear = TREE ? min(prefix, Lk) : lim;  // keys below it are read without a look at the mask
-        for (int kt = seg.kt0; kt < end; ++kt, ++s_used) {
-          if (!warp_wait(&s_full[x], s_used & 1u, ctl, abort_flag)) {
+        const int kt_first = seg.kt0 + (split ? x : 0), kt_step = split ? 2 : 1, kt_end = split ? seg.kt1 : min(seg.kt1, seg.n_tile[x]);
+        for (int kt = kt_first; kt < kt_end; kt += kt_step, ++used) {
+          const uint32_t buf = used & 1u;
+          if (!warp_wait(&s_full[2 * x + buf], (used >> 1) & 1u, ctl, abort_flag)) {
             ok = false;
             break;
           }
           tc_fence_after();
           float s[BN];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, *reinterpret_cast<float(*)[32]>(s + 32 * c));
+          tmem_ld32(s_addr + buf * BN, *reinterpret_cast<float(*)[32]>(s));
+          tmem_ld32(s_addr + buf * BN + 32, *reinterpret_cast<float(*)[32]>(s + 32));
           tmem_wait_ld();
           const int j0 = kt * BN;
           if (__any_sync(0xffffffffu, j0 + BN > clear)) {
-            uint32_t bits[4];
+            uint32_t bits[BN / 32];
             key_bits<TREE>(bits, j0, lim, prefix, word);
 #pragma unroll
             for (int e = 0; e < BN; ++e)
@@ -582,7 +592,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ok = false;
                 break;
               }
-              if (j0 + row >= Lk) {
+              if (row < BN && j0 + row >= Lk) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                   uint4* p = reinterpret_cast<uint4*>(ring + (at % S) * L::TILE + r * L::BLOCK + row * 128);
@@ -593,34 +603,50 @@ __global__ void __launch_bounds__(kThreads, 1)
               fence_proxy_async_smem();
             }
           }
-          float top = fmaxf(s[0], s[BN - 1]);
+          float tops[4];
 #pragma unroll
-          for (int e = 1; e + 1 < BN; e += 2) top = max3f(top, s[e], s[e + 1]);
+          for (int i = 0; i < 4; ++i) {
+            tops[i] = s[16 * i];
+#pragma unroll
+            for (int e = 1; e + 1 < 16; e += 2) tops[i] = max3f(tops[i], s[16 * i + e], s[16 * i + e + 1]);
+            tops[i] = fmaxf(tops[i], s[16 * i + 15]);
+          }
+          const float top = fmaxf(max3f(tops[0], tops[1], tops[2]), tops[3]);
           const bool raise = top > m + kRaise || (m == -INFINITY && top > -INFINITY);
-          const float to = raise ? top : m;
-          const float alpha = raise && m > -INFINITY ? exp2_fast((m - to) * kLog2e) : 1.f;
-          m = to;
-          // S of this key tile is there, so the product of the one before is done
-          if (kt > seg.kt0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+          float alpha = 1.f;
+          if (__any_sync(0xffffffffu, raise)) {
+            if (raise) {
+              if (m > -INFINITY) alpha = exp2_fast((m - top) * kLog2e);
+              m = top;
+              z *= alpha;
+            }
+            if (kt > kt_first && __any_sync(0xffffffffu, alpha != 1.f)) {
+              // O is between two products: the one before this step's is done
+              if (!warp_wait(&pv_done[2 * x + (buf ^ 1u)], ((used - 1) >> 1) & 1u, ctl, abort_flag)) {
+                ok = false;
+                break;
+              }
+              tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < D; c += 16) {
-              uint32_t o[16];
-              asm volatile(
-                  "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                  : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]), "=r"(o[8]), "=r"(o[9]), "=r"(o[10]),
-                    "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
-                  : "r"(o_addr + c));
-              tmem_wait_ld();
+              for (int c = 0; c < D; c += 16) {
+                uint32_t o[16];
+                asm volatile(
+                    "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                    : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]), "=r"(o[8]), "=r"(o[9]), "=r"(o[10]),
+                      "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
+                    : "r"(o_addr + c));
+                tmem_wait_ld();
 #pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-              tmem_st16(o_addr + c, o);
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                tmem_st16(o_addr + c, o);
+              }
             }
           }
           const float ml = m == -INFINITY ? 0.f : m * kLog2e;
           const F2 scale = f2(kLog2e, kLog2e), minus = f2(-ml, -ml);
           F2 sum[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < BN / 32; ++c) {
             uint32_t p[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -629,32 +655,71 @@ __global__ void __launch_bounds__(kThreads, 1)
               p[e] = pack2(a, b);
               sum[e & 1] = add2(sum[e & 1], f2(a, b));
             }
-            tmem_st16(s_addr + 16 * c, p);
+            tmem_st16(s_addr + buf * BN + 16 * c, p);
           }
           const F2 both = add2(sum[0], sum[1]);
-          z = z * alpha + (lo(both) + hi(both));
+          z += lo(both) + hi(both);
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&p_full[x]);
+          if (lane == 0) mbar_arrive(&p_full[2 * x + buf]);
         }
         if (!ok) break;
-        if (!warp_wait(&o_full[x], o_used++ & 1u, ctl, abort_flag)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
       }
+      // the outputs are there when their last products are done
+      const uint32_t wanted = (mine ? 1u << x : 0u) | (split && x == 0 && seg.active(1) ? 2u : 0u);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        if (ok && (wanted >> y & 1u)) ok = warp_wait(&o_full[y], outs[y] & 1u, ctl, abort_flag);
+        if (seg.active(y)) ++outs[y];
+      }
+      if (!ok) break;
+      tc_fence_after();
+      step += seg.kt1 - seg.kt0;
+      float f0 = 1.f, f1 = 0.f;  // of the two outputs of a split unit
+      if (split && seg.active(1)) {
+        // the second group hands its rows' maxima and sums over, and the first one adds up
+        if (x == 1) {
+          exch[row] = make_float2(m, z);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(exch_full);
+        } else {
+          if (!warp_wait(exch_full, exchanges & 1u, ctl, abort_flag)) {
+            ok = false;
+            break;
+          }
+          const float2 e = exch[row];
+          const float both = fmaxf(m, e.x), base = both == -INFINITY ? 0.f : both;
+          f0 = z == 0.f ? 0.f : exp2_fast((m - base) * kLog2e);
+          f1 = e.y == 0.f ? 0.f : exp2_fast((e.x - base) * kLog2e);
+          z = (z == 0.f ? 0.f : z * f0) + (e.y == 0.f ? 0.f : e.y * f1);
+          m = both;
+        }
+        ++exchanges;
+      }
+      if (split && x == 1) continue;
+      const bool two = split && seg.active(1);
+      auto sums = [&](int c, float (&o)[32]) {  // 32 columns of the row's weighted values
+        tmem_ld32(o_addr + c, o);
+        if (two) {
+          float p[32];
+          tmem_ld32(o_addr + D + c, p);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = o[e] * f0 + p[e] * f1;
+        } else {
+          tmem_wait_ld();
+        }
+      };
       if (seg.whole()) {
-        if (seg.kt0 < end) {
-          const float f = z == 0.f ? 0.f : 1.f / z;
-          const int head = seg.h * w.group + head_in;
-          __nv_bfloat16* out = w.out + (TREE ? (static_cast<size_t>(seg.b) * w.Hq + head) * w.T + token : static_cast<size_t>(seg.seq.q0 + token) * w.Hq + head) * D;
+        const float f = z == 0.f ? 0.f : 1.f / z;
+        const int head = seg.h * w.group + head_in;
+        __nv_bfloat16* out = w.out + (TREE ? (static_cast<size_t>(seg.b) * w.Hq + head) * w.T + token : static_cast<size_t>(seg.seq.q0 + token) * w.Hq + head) * D;
+        if (mine) {
 #pragma unroll 1
           for (int c = 0; c < D; c += 32) {
             float o[32];
-            tmem_ld32(o_addr + c, o);
-            tmem_wait_ld();
+            sums(c, o);
             uint32_t u[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) u[e] = z == 0.f ? 0u : pack2(o[2 * e] * f, o[2 * e + 1] * f);
@@ -668,12 +733,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         // the run's first unit goes to its first part, unless it begins with it
         float* part = w.parts + (2 * static_cast<size_t>(blockIdx.x) + (seg.kt0 > 0 ? 0 : 1)) * kPartFloats<D>;
         const int at = x * BM + row;
-        if (seg.kt0 < end) {
+        if (mine) {
 #pragma unroll 1
           for (int c = 0; c < D; c += 32) {
             float o[32];
-            tmem_ld32(o_addr + c, o);
-            tmem_wait_ld();
+            sums(c, o);
             if (real) {
 #pragma unroll
               for (int e = 0; e < 8; ++e)
@@ -684,12 +748,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         part[256 * D + at] = m;
         part[256 * D + 256 + at] = z;
       }
-      if (seg.kt0 < end) {
+      if (mine) {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&o_free[x]);
+        if (lane == 0) {
+          mbar_arrive(&o_free[x]);
+          if (two) mbar_arrive(&o_free[1]);
+        }
       }
-      step += seg.kt1 - seg.kt0;
+    }
+    if (!TREE && w.clear_rest) {
+      // rows of no sequence
+      const int first = min(max(__ldg(w.q_starts), 0), w.Tq), last = max(first, min(max(__ldg(w.q_starts + w.B), 0), w.Tq));
+      const long long row_words = static_cast<long long>(w.Hq) * D / 8, n = row_words * (first + w.Tq - last);
+      for (long long i = blockIdx.x * 256 + (threadIdx.x - 128); i < n; i += gridDim.x * 256)
+        reinterpret_cast<uint4*>(w.out)[i < first * row_words ? i : i + (last - first) * row_words] = make_uint4(0u, 0u, 0u, 0u);
     }
   }
   tc_fence_before();
