@@ -38,7 +38,7 @@ struct Layout {
   static constexpr int S = FIT > 16 ? 16 : FIT;    // keys and values of a step in turn: 10 for D = 128, 16 for 64
   static constexpr size_t OFF_RING = 2 * static_cast<size_t>(Q_TILE);
   static constexpr size_t OFF_BAR = OFF_RING + static_cast<size_t>(S) * TILE;
-  static constexpr int NBARS = 2 * S + 20;
+  static constexpr int NBARS = 2 * S + 22;
   static constexpr size_t OFF_EXCH = OFF_BAR + NBARS * 8 + 64;
   static constexpr size_t BYTES = 1024 + OFF_EXCH + BM * 8;
   static_assert(BYTES <= 232448, "shared memory");
@@ -52,6 +52,13 @@ struct Layout {
 template <int D>
 constexpr size_t kPartFloats = 256 * (D + 2);
 
+// Where a CTA's run of steps begins, of how many steps and CTAs with work.
+struct Place {
+  int b, h, block, kt;
+  long long total;
+  int ctas;
+};
+
 struct Work {
   const int32_t* q_starts;   // prompts
   const int32_t* k_starts;
@@ -60,6 +67,7 @@ struct Work {
   long long word_stride;
   __nv_bfloat16* out;
   float* parts;
+  Place* places;  // of every CTA, for the join
   int B, Hq, Hkv, group, Tq, Tk, T, cap, causal, clear_rest;
   int tokens;  // of a tile
 };
@@ -139,16 +147,11 @@ __device__ __forceinline__ long long run_start(long long total, int ctas, int i)
   return total / ctas * i + total % ctas * i / ctas;
 }
 
-struct Place {
-  int b, h, block, kt;
-  long long total;
-};
-
-// Where the key tile number run_start(total, .., i) is; computed by a whole warp.  ctas: CTAs with work.
+// Where the step number run_start(total, .., i) is; computed by a whole warp.
 template <bool TREE>
-__device__ Place locate(const Work& w, int i, int grid, int& ctas, unsigned* error) {
+__device__ Place locate(const Work& w, int i, int grid, unsigned* error) {
   const int lane = threadIdx.x & 31;
-  Place p{0, 0, 0, 0, 0};
+  Place p{};
   bool wrong = false;
   for (int b = lane; b < w.B; b += 32) {
     bool bad;
@@ -158,9 +161,9 @@ __device__ Place locate(const Work& w, int i, int grid, int& ctas, unsigned* err
   }
   if (error && wrong) atomicOr(error, kDevErrRange);
   for (int o = 16; o; o >>= 1) p.total += __shfl_xor_sync(0xffffffffu, p.total, o);
-  ctas = static_cast<int>(min(static_cast<long long>(grid), p.total));
-  if (i >= ctas) return p;
-  long long left = run_start(p.total, ctas, i);
+  p.ctas = static_cast<int>(min(static_cast<long long>(grid), p.total));
+  if (i >= p.ctas) return p;
+  long long left = run_start(p.total, p.ctas, i);
   for (int b0 = 0; b0 < w.B; b0 += 32) {
     long long mine = 0;
     Seq s{};
@@ -372,8 +375,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* pv_done = q_full + 10;  // [tile][buffer]
   uint64_t* o_full = q_full + 14;   // [tile]
   uint64_t* o_free = q_full + 16;   // [tile]
-  uint64_t* exch_full = q_full + 18;
-  uint64_t* drain = q_full + 19;
+  uint64_t* v_tail = q_full + 18;   // [tile]
+  uint64_t* exch_full = q_full + 20;
+  uint64_t* drain = q_full + 21;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + L::NBARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   Place* place_s = reinterpret_cast<Place*>(tmem_slot + 2);  // 8-byte aligned
@@ -396,6 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int x = 0; x < 2; ++x) {
       mbar_init(&o_full[x], 1);
       mbar_init(&o_free[x], 4);
+      mbar_init(&v_tail[x], 1);
     }
     mbar_init(exch_full, 4);
     mbar_init(drain, 3);
@@ -404,11 +409,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   if (warp == 1) tmem_alloc(tmem_slot, L::COLS);
   if (warp == 2) {
-    int ctas;
-    const Place p = locate<TREE>(w, blockIdx.x, gridDim.x, ctas, blockIdx.x == 0 ? ctl.error : nullptr);
+    const Place p = locate<TREE>(w, blockIdx.x, gridDim.x, blockIdx.x == 0 ? ctl.error : nullptr);
     if (lane == 0) {
-      const int i = blockIdx.x;
+      const int i = blockIdx.x, ctas = p.ctas;
       *place_s = p;
+      w.places[i] = p;
       *steps_s = i < ctas ? run_start(p.total, ctas, i + 1) - run_start(p.total, ctas, i) : 0;
     }
   }
@@ -467,7 +472,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp < 3) {
     // ------------------------------------------------------------ scores of tile x
     // A tile has two score buffers (P takes its scores' place), so that the scores of its next step are there when its warps
-    // are done with this one.  Every warp that issues products does so under elect: under a test of the lane the compiler does
+    // are done with this one.  A barrier's phase is known by its parity alone, so whoever waits on one waits for its every phase: both
+    // tiles take note of keys that only one of them reads.  Every warp that issues products does so under elect: under a test of the lane the compiler does
     // not know that one thread is left, and each product costs 110 cycles in place of 40.
     const int x = warp - 1;
     if (elect_one()) {
@@ -522,6 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint64_t vd = sdesc_values(smem_u32(ring + s * L::TILE));
           auto values = [&](int x, uint32_t& used, uint32_t& units, bool& first) {
             if (!ok || !seg.own(x, kt)) return;
+            if ((kt + 1) * BN > seg.seq.Lk) mbar_arrive(&v_tail[x]);
             if (first) ok = mbar_wait(&o_free[x], (units++ & 1u) ^ 1u, ctl, abort_flag);  // O of the unit before has been read
             const uint32_t buf = 2 * x + (used & 1u);
             ok = ok && mbar_wait(&p_full[buf], (used >> 1) & 1u, ctl, abort_flag);
@@ -551,7 +558,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t s_addr = tmem + lanes + 2 * x * BN, o_addr = tmem + lanes + L::O_COL + x * D;
     const int token_in = row / w.group, head_in = row % w.group;
     uint32_t step = 0, used = 0;      // steps of the run, and of this tile
-    uint32_t outs[2] = {0, 0}, exchanges = 0;
+    uint32_t outs = 0, exchanges = 0, tails = 0;
     bool ok = true;
     Run<TREE> run(w, place, steps);
     Segment seg;
@@ -565,7 +572,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int lim = !TREE && w.causal ? min(token + 1 + Lk - seg.seq.Lq, Lk) : Lk;
         unsigned long long word = 0;
         if (TREE && real) word = w.words ? static_cast<unsigned long long>(__ldg(w.words + seg.b * w.word_stride + token)) : ~0ull >> (63 - token);
-        const int clear = TREE ? min(prefix, Lk) : lim;  // keys below it are read without a look at the mask
+        // the first step with a key that one of the warp's rows does not read
+        const int masked = __reduce_min_sync(0xffffffffu, max(0, TREE ? min(prefix, Lk) : lim)) / BN;
         const int kt_first = seg.kt0 + (split ? x : 0), kt_step = split ? 2 : 1, kt_end = split ? seg.kt1 : min(seg.kt1, seg.n_tile[x]);
         for (int kt = kt_first; kt < kt_end; kt += kt_step, ++used) {
           const uint32_t buf = used & 1u;
@@ -579,19 +587,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_ld32(s_addr + buf * BN + 32, *reinterpret_cast<float(*)[32]>(s + 32));
           tmem_wait_ld();
           const int j0 = kt * BN;
-          if (__any_sync(0xffffffffu, j0 + BN > clear)) {
+          if (kt >= masked) {
             uint32_t bits[BN / 32];
             key_bits<TREE>(bits, j0, lim, prefix, word);
 #pragma unroll
             for (int e = 0; e < BN; ++e)
               if (!(bits[e / 32] >> (e % 32) & 1u)) s[e] = -INFINITY;
-            // a product takes 0 x value for a key that no row reads: values behind the sequence must be finite
+            // a product takes 0 x value for a key that no row reads: values behind the sequence must be finite.  v_tail says
+            // which phase of the slot is the one to look at
             if (j0 + BN > Lk) {
               const uint32_t at = 2 * (step + kt - seg.kt0) + 1;
-              if (!warp_wait(&full[at % S], (at / S) & 1u, ctl, abort_flag)) {
-                ok = false;
-                break;
-              }
+              ok = warp_wait(&v_tail[x], tails++ & 1u, ctl, abort_flag) && warp_wait(&full[at % S], (at / S) & 1u, ctl, abort_flag);
+              if (!ok) break;
               if (row < BN && j0 + row >= Lk) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
@@ -666,14 +673,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!ok) break;
       }
-      // the outputs are there when their last products are done
-      const uint32_t wanted = (mine ? 1u << x : 0u) | (split && x == 0 && seg.active(1) ? 2u : 0u);
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        if (ok && (wanted >> y & 1u)) ok = warp_wait(&o_full[y], outs[y] & 1u, ctl, abort_flag);
-        if (seg.active(y)) ++outs[y];
+      if (mine && !warp_wait(&o_full[x], outs++ & 1u, ctl, abort_flag)) {  // the last product is done
+        ok = false;
+        break;
       }
-      if (!ok) break;
       tc_fence_after();
       step += seg.kt1 - seg.kt0;
       float f0 = 1.f, f1 = 0.f;  // of the two outputs of a split unit
@@ -681,6 +684,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // the second group hands its rows' maxima and sums over, and the first one adds up
         if (x == 1) {
           exch[row] = make_float2(m, z);
+          tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(exch_full);
         } else {
@@ -688,6 +692,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             ok = false;
             break;
           }
+          tc_fence_after();
           const float2 e = exch[row];
           const float both = fmaxf(m, e.x), base = both == -INFINITY ? 0.f : both;
           f0 = z == 0.f ? 0.f : exp2_fast((m - base) * kLog2e);
@@ -773,57 +778,90 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// Joins a unit's parts: block (i, c) looks at the place where CTA i + 1's run begins; where that is the first such place
-// inside its unit, it adds up the unit's parts in order, for 32 of the columns.
+// Joins a unit's parts.  Block (i, y) looks at the place where CTA i + 1's run begins: where that is the first such place
+// inside its unit, it adds up the unit's parts, for 64 of the columns and 32 of the rows.  A few rows of many parts (one token over
+// a long cache) are shared out over the parts, and the shares added in order: 152 parts of 6 rows take 6 us, 120 with
+// a thread for each row.
 template <int D, bool TREE>
-__global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant__ Work w, int grid) {
-  __shared__ Place place_s;
-  __shared__ int ctas_s;
+__global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant__ Work w) {
+  constexpr int kMostParts = 256;
+  __shared__ float weight[kMostParts][32];
+  __shared__ float4 share[256];
+  __shared__ float shared[8][32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int i = blockIdx.x + 1;
-  if (threadIdx.x < 32) {
-    int ctas;
-    const Place p = locate<TREE>(w, i, grid, ctas, nullptr);
-    if (threadIdx.x == 0) place_s = p, ctas_s = ctas;
-  }
-  __syncthreads();
-  const Place p = place_s;
-  const int ctas = ctas_s;
-  if (i >= ctas || p.kt == 0) return;
+  const Place p = w.places[i];
+  if (i >= p.ctas || p.kt == 0) return;
   const Seq s = seq_of<TREE>(w, p.b);
-  const long long first = run_start(p.total, ctas, i) - p.kt, last = first + block_tiles<TREE>(w, s, p.block);
-  if (run_start(p.total, ctas, i - 1) > first) return;
+  const long long first = run_start(p.total, p.ctas, i) - p.kt, last = first + block_tiles<TREE>(w, s, p.block);
+  if (run_start(p.total, p.ctas, i - 1) > first) return;
+  // rows of this block: at most 32 of tile x
+  const int c0 = blockIdx.y % (D / 64) * 64, at0 = blockIdx.y / (D / 64) * 32, x = at0 / BM, row0 = at0 % BM;
+  const int t0 = (2 * p.block + x) * w.tokens;
+  const int rows = min(32, min(w.tokens, s.Lq - t0) * w.group - row0);
+  if (rows <= 0) return;
   int end = i + 1;  // CTAs i - 1 .. end - 1 have parts
-  while (end < ctas && run_start(p.total, ctas, end) < last) ++end;
+  while (end < p.ctas && run_start(p.total, p.ctas, end) < last) ++end;
+  const int parts = end - i + 1;
+  const auto part = [&](int k) { return w.parts + (2 * static_cast<size_t>(i - 1 + k) + (k == 0 ? 1 : 0)) * kPartFloats<D>; };
 
-  const int at = threadIdx.x, row = at % BM, x = at / BM;
-  const int token = (2 * p.block + x) * w.tokens + row / w.group;
-  if (row >= w.tokens * w.group || token >= s.Lq) return;
-  const auto part = [&](int c) { return w.parts + (2 * static_cast<size_t>(c) + (c == i - 1 ? 1 : 0)) * kPartFloats<D>; };
+  const int row = threadIdx.x % 32, group = threadIdx.x / 32;
   float m = -INFINITY;
-  for (int c = i - 1; c < end; ++c) m = fmaxf(m, part(c)[256 * D + at]);
-  const float base = m == -INFINITY ? 0.f : m;
-  const int c0 = blockIdx.y * 32;
-  float z = 0.f, o[32] = {};
-  for (int c = i - 1; c < end; ++c) {
-    const float* from = part(c);
-    const float zc = from[256 * D + 256 + at];
-    if (zc == 0.f) continue;
-    const float f = exp2_fast((from[256 * D + at] - base) * kLog2e);
-    z += zc * f;
+  for (int k = group; k < parts; k += 8) {
+    const float mk = row < rows ? part(k)[256 * D + at0 + row] : -INFINITY;
+    weight[k][row] = mk;
+    m = fmaxf(m, mk);
+  }
+  shared[group][row] = m;
+  __syncthreads();
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float4 v = reinterpret_cast<const float4*>(from)[(c0 / 4 + e) * 256 + at];
-      o[4 * e] += v.x * f, o[4 * e + 1] += v.y * f, o[4 * e + 2] += v.z * f, o[4 * e + 3] += v.w * f;
+  for (int g = 0; g < 8; ++g) m = fmaxf(m, shared[g][row]);
+  const float base = m == -INFINITY ? 0.f : m;
+  __syncthreads();
+  float z = 0.f;
+  for (int k = group; k < parts; k += 8) {
+    const float zk = row < rows ? part(k)[256 * D + 256 + at0 + row] : 0.f;
+    const float f = zk == 0.f ? 0.f : exp2_fast((weight[k][row] - base) * kLog2e);  // a part without a key has no O
+    weight[k][row] = f;
+    z += zk == 0.f ? 0.f : zk * f;
+  }
+  shared[group][row] = z;
+  __syncthreads();
+
+  // 16 columns of four for each row; the rest of the block's threads take other parts
+  int wide = 1;
+  while (wide < rows) wide *= 2;
+  const int items = 16 * wide, lanes = items >= 256 ? 1 : 256 / items;  // lanes: over the parts
+  for (int j = threadIdx.x; j < items * lanes; j += 256) {
+    const int r = j % wide, c = j / wide % 16, lane = j / items;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r < rows)
+#pragma unroll 4
+      for (int k = lane; k < parts; k += lanes) {
+        const float f = weight[k][r];
+        if (f == 0.f) continue;
+        const float4 v = reinterpret_cast<const float4*>(part(k))[(c0 / 4 + c) * 256 + at0 + r];
+        o.x += v.x * f, o.y += v.y * f, o.z += v.z * f, o.w += v.w * f;
+      }
+    if (lanes > 1) {
+      share[threadIdx.x] = o;
+      __syncthreads();
+      for (int l = 1; l < lanes && lane == 0; ++l) {
+        const float4 v = share[threadIdx.x + l * items];
+        o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
+      }
+    }
+    if (lane == 0 && r < rows) {
+      float sum = 0.f;
+#pragma unroll
+      for (int g = 0; g < 8; ++g) sum += shared[g][r];
+      const float f = sum == 0.f ? 0.f : 1.f / sum;
+      const int token = t0 + (row0 + r) / w.group, head = p.h * w.group + (row0 + r) % w.group;
+      __nv_bfloat16* out =
+          w.out + (TREE ? (static_cast<size_t>(p.b) * w.Hq + head) * w.T + token : static_cast<size_t>(s.q0 + token) * w.Hq + head) * D + c0 + 4 * c;
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack2(o.x * f, o.y * f), pack2(o.z * f, o.w * f));
     }
   }
-  const float f = z == 0.f ? 0.f : 1.f / z;
-  const int head = p.h * w.group + row % w.group;
-  __nv_bfloat16* out = w.out + (TREE ? (static_cast<size_t>(p.b) * w.Hq + head) * w.T + token : static_cast<size_t>(s.q0 + token) * w.Hq + head) * D + c0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    reinterpret_cast<uint4*>(out)[e] = make_uint4(pack2(o[8 * e] * f, o[8 * e + 1] * f), pack2(o[8 * e + 2] * f, o[8 * e + 3] * f),
-                                                  pack2(o[8 * e + 4] * f, o[8 * e + 5] * f), pack2(o[8 * e + 6] * f, o[8 * e + 7] * f));
 }
 
 // bf16 [n3][n2][n1][n0], strides in elements, boxes of 64 x b1 x b2 elements.
@@ -847,25 +885,28 @@ int launch(const CUtensorMap& tmq, const CUtensorMap& tmk, const CUtensorMap& tm
   if (cudaGetLastError() != cudaSuccess) return -1;
   if (grid == 1) return 1;
   cudaLaunchConfig_t config = {};
-  config.gridDim = dim3(grid - 1, D / 32), config.blockDim = dim3(256), config.stream = st;
+  // rows that a unit can have: the second tile's begin at 128
+  const int rows = TREE && w.T <= w.tokens ? w.T * w.group : 2 * BM;
+  config.gridDim = dim3(grid - 1, D / 64 * ((rows + 31) / 32)), config.blockDim = dim3(256), config.stream = st;
   cudaLaunchAttribute early = {};
   early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   early.val.programmaticStreamSerializationAllowed = 1;
   config.attrs = &early, config.numAttrs = 1;
-  return cudaLaunchKernelEx(&config, grouped_join_kernel<D, TREE>, w, grid) == cudaSuccess ? 2 : -1;
+  return cudaLaunchKernelEx(&config, grouped_join_kernel<D, TREE>, w) == cudaSuccess ? 2 : -1;
 }
 
 }  // namespace
 
 size_t grouped_workspace_bytes(int d, int num_sms) {
-  return static_cast<size_t>(num_sms) * 2 * (d == 64 ? kPartFloats<64> : kPartFloats<128>) * sizeof(float);
+  return num_sms * (2 * (d == 64 ? kPartFloats<64> : kPartFloats<128>) * sizeof(float) + sizeof(Place));
 }
 
 int prompt_attn(const topk_prompt_args& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
-  if (!encode_tiled_fn()) return -1;
+  if (!encode_tiled_fn() || num_sms > 256) return -1;  // the join's parts in shared memory
   Work w = {};
   w.q_starts = a.q_starts, w.k_starts = a.k_starts ? a.k_starts : a.q_starts;
   w.out = static_cast<__nv_bfloat16*>(a.out), w.parts = static_cast<float*>(workspace);
+  w.places = reinterpret_cast<Place*>(w.parts + num_sms * 2 * (a.d == 64 ? kPartFloats<64> : kPartFloats<128>));
   w.B = a.B, w.Hq = a.Hq, w.Hkv = a.Hkv, w.group = a.Hq / a.Hkv, w.Tq = a.Tq, w.Tk = a.Tk, w.causal = a.causal, w.clear_rest = a.clear_rest;
   w.tokens = BM / w.group;
   CUtensorMap q, k, v;
@@ -877,10 +918,11 @@ int prompt_attn(const topk_prompt_args& a, void* workspace, int num_sms, const D
 }
 
 int tree_attn(const topk_tree_args& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
-  if (!encode_tiled_fn()) return -1;
+  if (!encode_tiled_fn() || num_sms > 256) return -1;
   Work w = {};
   w.kv_len = a.kv_len, w.words = a.tree, w.word_stride = a.tree_stride;
   w.out = static_cast<__nv_bfloat16*>(a.out), w.parts = static_cast<float*>(workspace);
+  w.places = reinterpret_cast<Place*>(w.parts + num_sms * 2 * (a.d == 64 ? kPartFloats<64> : kPartFloats<128>));
   w.B = a.B, w.Hq = a.Hq, w.Hkv = a.Hkv, w.group = a.Hq / a.Hkv, w.T = a.T, w.cap = a.cap;
   w.tokens = BM / w.group;
   CUtensorMap q, k, v;

@@ -176,3 +176,17 @@ def test_graph_and_streams():
         a, b = T.tree_attention(*data[0]), T.tree_attention(*data[1], stream=side)
     torch.cuda.synchronize()
     assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,n,cap,d", [(6, 32, 8, 4, 7944, 128), (2, 1, 1, 6, 55568, 128), (4, 12, 12, 1, 8192, 64), (16, 32, 8, 16, 20000, 128)])
+def test_long_caches_again_and_again(B, Hq, Hkv, n, cap, d):
+    # loads that arrive in any order, over many key tiles: every run gives the same bits, and the first one is right
+    q, keys, values = _inputs(B, Hq, Hkv, n, cap, d, seed=9)
+    lens = [max(0, cap - n - 1000 * b - 13 * b * b) for b in range(B)]
+    kv_len = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    first = T.tree_attention(q, keys, values, kv_len)
+    T.topk_check()
+    _verify(first[:, :, -1:], q[:, :, -1:], keys, values, [m + n - 1 for m in lens], torch.ones(B, 1, 1, dtype=torch.bool, device="cuda"), cap)
+    for _ in range(60):
+        assert torch.equal(T.tree_attention(q, keys, values, kv_len), first)
+    T.topk_check()
