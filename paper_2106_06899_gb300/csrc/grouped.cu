@@ -25,19 +25,21 @@ namespace topk {
 namespace {
 
 constexpr int BM = 128, BN = 64;  // rows of a tile, keys of a step
-constexpr int kThreads = 384;     // loads, scores of each tile, products with the values; two groups of four softmax warps
+constexpr int kThreads = 384;     // loads, scores, products of each tile with the values; two groups of four softmax warps
 constexpr float kRaise = 8.0f;    // natural-log units
 constexpr float kLog2e = 1.4426950408889634f;
 
-template <int D>
+template <int D, bool TREE>
 struct Layout {
   static constexpr int R = D / 64;                 // blocks of 128 bytes of a row
   static constexpr uint32_t Q_TILE = BM * D * 2, Q_BLOCK = BM * 128;
   static constexpr uint32_t TILE = BN * D * 2, BLOCK = BN * 128;  // keys or values of a step
-  static constexpr int FIT = (232448 - 3072 - 2 * static_cast<int>(Q_TILE)) / static_cast<int>(TILE);
-  static constexpr int S = FIT > 16 ? 16 : FIT;    // keys and values of a step in turn: 10 for D = 128, 16 for 64
+  static constexpr int STAGE = TREE ? 0 : 32 * 128;  // a softmax warp's outputs on their way out (prompts, whose units are short)
+  static constexpr int FIT = (232448 - 3072 - 8 * STAGE - 2 * static_cast<int>(Q_TILE)) / static_cast<int>(TILE);
+  static constexpr int S = FIT > 16 ? 16 : FIT;      // keys and values of a step in turn: 8 or 10 for D = 128, 16 for 64
   static constexpr size_t OFF_RING = 2 * static_cast<size_t>(Q_TILE);
-  static constexpr size_t OFF_BAR = OFF_RING + static_cast<size_t>(S) * TILE;
+  static constexpr size_t OFF_STAGE = OFF_RING + static_cast<size_t>(S) * TILE;
+  static constexpr size_t OFF_BAR = OFF_STAGE + 8 * STAGE;
   static constexpr int NBARS = 2 * S + 22;
   static constexpr size_t OFF_EXCH = OFF_BAR + NBARS * 8 + 64;
   static constexpr size_t BYTES = 1024 + OFF_EXCH + BM * 8;
@@ -214,9 +216,7 @@ struct Segment {
   int n_tile[2];
   Seq seq;
   __device__ __forceinline__ bool split() const { return n_tile[1] == 0; }
-  __device__ __forceinline__ bool own(int x, int kt) const { return split() ? ((kt - kt0) & 1) == x : kt < n_tile[x]; }
   __device__ __forceinline__ bool active(int x) const { return split() ? kt1 - kt0 > x : kt0 < min(kt1, n_tile[x]); }
-  __device__ __forceinline__ bool last(int x, int kt) const { return split() ? kt + 2 >= kt1 : kt + 1 == min(kt1, n_tile[x]); }
   __device__ __forceinline__ bool whole() const { return kt0 == 0 && kt1 == n; }
 };
 
@@ -256,6 +256,15 @@ struct Run {
     kt = 0;
     ++block;
     return true;
+  }
+};
+
+// A place in the ring of keys and values, which alternate, and the parity of its phase.
+struct Slot {
+  uint32_t slot, parity;
+  __device__ __forceinline__ void advance(uint32_t slots) {
+    slot += 2;
+    if (slot >= slots) slot -= slots, parity ^= 1u;
   }
 };
 
@@ -359,7 +368,7 @@ template <int D, bool TREE>
 __global__ void __launch_bounds__(kThreads, 1)
     grouped_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv,
                    const __grid_constant__ Work w, DevCtl ctl) {
-  using L = Layout<D>;
+  using L = Layout<D, TREE>;
   constexpr int S = L::S, R = L::R;
   constexpr uint32_t IDESC_S = idesc_bf16_f32(BM, BN), IDESC_O = idesc_bf16_f32(BM, D) | (1u << 16);
 
@@ -388,10 +397,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], s % 2 == 0 ? 2 : 1);  // keys: the scores of both tiles
+      mbar_init(&empty[s], s % 2 == 0 ? 1 : 2);  // values: the products of both tiles
     }
     mbar_init(q_full, 1);
-    mbar_init(q_empty, 2);
+    mbar_init(q_empty, 1);
     for (int x = 0; x < 4; ++x) {
       mbar_init(&s_full[x], 1);
       mbar_init(&p_full[x], 4);
@@ -469,42 +478,44 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (segs) drain_wait(q_full, (segs - 1) & 1u, ctl);
     }
     __syncwarp();
-  } else if (warp < 3) {
-    // ------------------------------------------------------------ scores of tile x
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ scores
     // A tile has two score buffers (P takes its scores' place), so that the scores of its next step are there when its warps
     // are done with this one.  A barrier's phase is known by its parity alone, so whoever waits on one waits for its every phase: both
-    // tiles take note of keys that only one of them reads.  Every warp that issues products does so under elect: under a test of the lane the compiler does
-    // not know that one thread is left, and each product costs 110 cycles in place of 40.
-    const int x = warp - 1;
+    // tiles take note of values that only one of them reads.  Every warp that issues products does so under elect: under a test
+    // of the lane the compiler does not know that one thread is left, and each product costs 110 cycles in place of 40.
     if (elect_one()) {
       Run<TREE> run(w, place, steps);
       Segment seg;
-      uint32_t step = 0, used = 0, segs = 0;
+      uint32_t used0 = 0, used1 = 0, segs = 0;
+      Slot at{0, 0};
+      const uint64_t ring_k = sdesc_k128(smem_u32(ring)), q0 = sdesc_k128(smem_u32(smem)), q1 = sdesc_k128(smem_u32(smem + L::Q_TILE));
       bool ok = true;
       while (ok && run.next(seg)) {
         ok = mbar_wait(q_full, segs++ & 1u, ctl, abort_flag);
-        const uint64_t qd = sdesc_k128(smem_u32(smem + (seg.split() ? 0 : x) * L::Q_TILE));
-        for (int kt = seg.kt0; ok && kt < seg.kt1; ++kt, ++step) {
-          const uint32_t s = (2 * step) % S;
-          ok = mbar_wait(&full[s], ((2 * step) / S) & 1u, ctl, abort_flag);
-          if (!ok) break;
-          if (!seg.own(x, kt)) {
-            mbar_arrive(&empty[s]);
-            continue;
-          }
-          const uint32_t buf = 2 * x + (used & 1u);
-          // the product with the P that lies there is done
-          if (used >= 2) ok = mbar_wait(&pv_done[buf], ((used >> 1) - 1) & 1u, ctl, abort_flag);
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t kd = sdesc_k128(smem_u32(ring + s * L::TILE));
+        const bool split = seg.split();
+        const int end0 = min(seg.kt1, seg.n_tile[0]), end1 = min(seg.kt1, seg.n_tile[1]);
+        for (int kt = seg.kt0; ok && kt < seg.kt1; ++kt, at.advance(S)) {
+          ok = mbar_wait(&full[at.slot], at.parity, ctl, abort_flag);
+          const uint64_t kd = ring_k + at.slot * (L::TILE >> 4);
+          auto scores = [&](int x, uint32_t& used) {
+            if (!ok || (split ? ((kt - seg.kt0) & 1) != x : kt >= (x ? end1 : end0))) return;
+            const uint32_t buf = 2 * x + (used & 1u);
+            // the product with the P that lies there is done
+            if (used >= 2) ok = mbar_wait(&pv_done[buf], ((used >> 1) - 1) & 1u, ctl, abort_flag);
+            if (!ok) return;
+            tc_fence_after();
+            const uint64_t qd = split || x == 0 ? q0 : q1;
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k)
-            mma_bf16_ss(tmem + buf * BN, qd + (((k / 4) * L::Q_BLOCK + (k % 4) * 32) >> 4), kd + (((k / 4) * L::BLOCK + (k % 4) * 32) >> 4), IDESC_S,
-                        k > 0 ? 1u : 0u);
-          mma_commit(&s_full[buf]);
-          mma_commit(&empty[s]);
-          ++used;
+            for (int k = 0; k < D / 16; ++k)
+              mma_bf16_ss(tmem + buf * BN, qd + (((k / 4) * L::Q_BLOCK + (k % 4) * 32) >> 4), kd + (((k / 4) * L::BLOCK + (k % 4) * 32) >> 4), IDESC_S,
+                          k > 0 ? 1u : 0u);
+            mma_commit(&s_full[buf]);
+            ++used;
+          };
+          scores(0, used0);
+          scores(1, used1);
+          if (ok) mma_commit(&empty[at.slot]);
         }
         if (ok) mma_commit(q_empty);
       }
@@ -513,38 +524,42 @@ __global__ void __launch_bounds__(kThreads, 1)
       drain_wait(drain, 0, ctl);
     }
     __syncwarp();
-  } else if (warp == 3) {
-    // ------------------------------------------------------------ products with the values
+  } else if (warp < 4) {
+    // ------------------------------------------------------------ products of tile x with the values
+    const int x = warp - 2;
     if (elect_one()) {
       Run<TREE> run(w, place, steps);
       Segment seg;
-      uint32_t step = 0, used0 = 0, used1 = 0, units0 = 0, units1 = 0;
+      uint32_t used = 0, units = 0;
+      Slot at{1, 0};
+      const uint64_t ring_v = sdesc_values(smem_u32(ring));
       bool ok = true;
       while (ok && run.next(seg)) {
-        bool first0 = true, first1 = true;
-        for (int kt = seg.kt0; ok && kt < seg.kt1; ++kt, ++step) {
-          const uint32_t s = (2 * step + 1) % S;
-          ok = mbar_wait(&full[s], ((2 * step + 1) / S) & 1u, ctl, abort_flag);
-          const uint64_t vd = sdesc_values(smem_u32(ring + s * L::TILE));
-          auto values = [&](int x, uint32_t& used, uint32_t& units, bool& first) {
-            if (!ok || !seg.own(x, kt)) return;
-            if ((kt + 1) * BN > seg.seq.Lk) mbar_arrive(&v_tail[x]);
-            if (first) ok = mbar_wait(&o_free[x], (units++ & 1u) ^ 1u, ctl, abort_flag);  // O of the unit before has been read
-            const uint32_t buf = 2 * x + (used & 1u);
-            ok = ok && mbar_wait(&p_full[buf], (used >> 1) & 1u, ctl, abort_flag);
-            if (!ok) return;
-            tc_fence_after();
+        bool first = true;
+        const bool split = seg.split();
+        const int end = min(seg.kt1, seg.n_tile[x]);
+        for (int kt = seg.kt0; ok && kt < seg.kt1; ++kt, at.advance(S)) {
+          ok = mbar_wait(&full[at.slot], at.parity, ctl, abort_flag);
+          if (!ok) break;
+          if (split ? ((kt - seg.kt0) & 1) != x : kt >= end) {
+            mbar_arrive(&empty[at.slot]);
+            continue;
+          }
+          if ((kt + 1) * BN > seg.seq.Lk) mbar_arrive(&v_tail[x]);
+          if (first) ok = mbar_wait(&o_free[x], (units++ & 1u) ^ 1u, ctl, abort_flag);  // O of the unit before has been read
+          const uint32_t buf = 2 * x + (used & 1u);
+          ok = ok && mbar_wait(&p_full[buf], (used >> 1) & 1u, ctl, abort_flag);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t vd = ring_v + at.slot * (L::TILE >> 4);
 #pragma unroll
-            for (int k = 0; k < BN / 16; ++k)
-              mma_bf16_ts(tmem + L::O_COL + x * D, tmem + buf * BN + k * 8, vd + ((k * 2048) >> 4), IDESC_O, first && k == 0 ? 0u : 1u);
-            mma_commit(&pv_done[buf]);
-            if (seg.last(x, kt)) mma_commit(&o_full[x]);
-            first = false;
-            ++used;
-          };
-          values(0, used0, units0, first0);
-          values(1, used1, units1, first1);
-          if (ok) mma_commit(&empty[s]);
+          for (int k = 0; k < BN / 16; ++k)
+            mma_bf16_ts(tmem + L::O_COL + x * D, tmem + buf * BN + k * 8, vd + ((k * 2048) >> 4), IDESC_O, first && k == 0 ? 0u : 1u);
+          mma_commit(&pv_done[buf]);
+          mma_commit(&empty[at.slot]);
+          if (split ? kt + 2 >= seg.kt1 : kt + 1 == end) mma_commit(&o_full[x]);
+          first = false;
+          ++used;
         }
       }
       mma_commit(drain);
@@ -572,8 +587,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int lim = !TREE && w.causal ? min(token + 1 + Lk - seg.seq.Lq, Lk) : Lk;
         unsigned long long word = 0;
         if (TREE && real) word = w.words ? static_cast<unsigned long long>(__ldg(w.words + seg.b * w.word_stride + token)) : ~0ull >> (63 - token);
-        // the first step with a key that one of the warp's rows does not read
-        const int masked = __reduce_min_sync(0xffffffffu, max(0, TREE ? min(prefix, Lk) : lim)) / BN;
+        const int clear = TREE ? min(prefix, Lk) : lim;  // keys below it are read without a look at the mask
         const int kt_first = seg.kt0 + (split ? x : 0), kt_step = split ? 2 : 1, kt_end = split ? seg.kt1 : min(seg.kt1, seg.n_tile[x]);
         for (int kt = kt_first; kt < kt_end; kt += kt_step, ++used) {
           const uint32_t buf = used & 1u;
@@ -587,7 +601,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_ld32(s_addr + buf * BN + 32, *reinterpret_cast<float(*)[32]>(s + 32));
           tmem_wait_ld();
           const int j0 = kt * BN;
-          if (kt >= masked) {
+          if (__any_sync(0xffffffffu, j0 + BN > clear)) {
             uint32_t bits[BN / 32];
             key_bits<TREE>(bits, j0, lim, prefix, word);
 #pragma unroll
@@ -720,17 +734,39 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float f = z == 0.f ? 0.f : 1.f / z;
         const int head = seg.h * w.group + head_in;
         __nv_bfloat16* out = w.out + (TREE ? (static_cast<size_t>(seg.b) * w.Hq + head) * w.T + token : static_cast<size_t>(seg.seq.q0 + token) * w.Hq + head) * D;
+        // Rows lie apart: a lane that stored its own row would make a warp's store touch 32 lines, which the load/store unit
+        // takes one a cycle (4,700 cycles a unit of 128 columns, now 1,000).  Prompts' rows go through shared memory, eight lanes to a row.
         if (mine) {
 #pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
-            float o[32];
-            sums(c, o);
-            uint32_t u[16];
+          for (int c = 0; c < D; c += TREE ? 32 : 64) {
+            uint32_t u[32];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) u[e] = z == 0.f ? 0u : pack2(o[2 * e] * f, o[2 * e + 1] * f);
-            if (real) {
+            for (int h = 0; h < (TREE ? 1 : 2); ++h) {
+              float o[32];
+              sums(c + 32 * h, o);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(out + c)[e] = make_uint4(u[4 * e], u[4 * e + 1], u[4 * e + 2], u[4 * e + 3]);
+              for (int e = 0; e < 16; ++e) u[16 * h + e] = z == 0.f ? 0u : pack2(o[2 * e] * f, o[2 * e + 1] * f);
+            }
+            if constexpr (TREE) {
+              if (real) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(out + c)[e] = make_uint4(u[4 * e], u[4 * e + 1], u[4 * e + 2], u[4 * e + 3]);
+              }
+            } else {
+              uint8_t* stage = smem + L::OFF_STAGE + (warp - 4) * L::STAGE;
+              __syncwarp();  // what was there has been read
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                *reinterpret_cast<uint4*>(stage + lane * 128 + ((e ^ (lane & 7)) << 4)) = make_uint4(u[4 * e], u[4 * e + 1], u[4 * e + 2], u[4 * e + 3]);
+              __syncwarp();
+              const unsigned long long mine_at = real ? reinterpret_cast<unsigned long long>(out + c) : 0ull;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const int r = 4 * e + lane / 8, chunk = lane % 8;
+                const unsigned long long at = __shfl_sync(0xffffffffu, mine_at, r);
+                const uint4 v = *reinterpret_cast<const uint4*>(stage + r * 128 + ((chunk ^ (r & 7)) << 4));
+                if (at) reinterpret_cast<uint4*>(at)[chunk] = v;
+              }
             }
           }
         }
@@ -878,7 +914,7 @@ bool make_map(CUtensorMap* map, const void* base, uint64_t n0, uint64_t n1, long
 
 template <int D, bool TREE>
 int launch(const CUtensorMap& tmq, const CUtensorMap& tmk, const CUtensorMap& tmv, const Work& w, int grid, const DevCtl& ctl, cudaStream_t st) {
-  using L = Layout<D>;
+  using L = Layout<D, TREE>;
   const auto kernel = grouped_kernel<D, TREE>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::BYTES)) != cudaSuccess) return -1;
   kernel<<<grid, kThreads, L::BYTES, st>>>(tmq, tmk, tmv, w, ctl);
