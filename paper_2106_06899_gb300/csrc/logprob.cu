@@ -4,7 +4,7 @@
 // Forward, one pass over a row: with a reference r near the maximum and d = c (x - r), c = scale log2 e, the sums S of 2^d and
 // T of 2^d d give lse = scale r + ln S and the entropy ln S - ln 2 T / S.  A thread keeps its own reference and raises it
 // only where an element exceeds it by more than kRaise; references are brought together at the end.
-// Alternatives: after a block's first tile the top-th largest of 256 groups' maxima is a value that at least `top` elements
+// Alternatives: after a block's first tile the top-th largest of 64 to 256 groups' maxima is a value that at least `top` elements
 // reach, and hardly more do (1.1 to 1.4 times as many, for each tile); what reaches it goes to a buffer in
 // shared memory, where the candidates are ranked at the end.  A row that overflows the buffer (values that rise along the
 // row, or thousands of equal ones) is read a second time with a threshold that is raised whenever the buffer fills.
@@ -28,9 +28,8 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 6.f;  // in powers of two
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
 constexpr int kKept = 2048;    // alternatives' candidates of a block
-constexpr int kGroups = kThreads / 2;
 constexpr int kMostBlocks = 8; // of a row: the portable size of a cluster
 
 __device__ __forceinline__ float to_f(float x) { return x; }
@@ -190,9 +189,9 @@ __device__ void sort_keys(unsigned long long* k, int n) {
 }
 
 struct Shared {
-  unsigned long long kept[kKept];
+  alignas(16) unsigned long long kept[kKept];
   unsigned long long best[kMaxAlternatives];
-  float groups[kGroups];
+  float groups[kThreads];
   Sums sums[kThreads / 32];
   Sums total;
   unsigned long long threshold;
@@ -204,11 +203,17 @@ struct Shared {
 __device__ void rank(Shared& sh, int top) {
   __syncthreads();
   const int n = min(sh.count, kKept);
-  if (n <= kThreads) {
-    if (static_cast<int>(threadIdx.x) < n) {
-      const unsigned long long k = sh.kept[threadIdx.x];
+  if (n <= 2 * kThreads) {
+    if (threadIdx.x == 0 && n % 2) sh.kept[n] = 0;
+    __syncthreads();
+    for (int t = threadIdx.x; t < n; t += kThreads) {
+      const unsigned long long k = sh.kept[t];
       int before = 0;
-      for (int i = 0; i < n; ++i) before += sh.kept[i] > k;
+#pragma unroll 4
+      for (int i = 0; i < n; i += 2) {  // kept has an even length, and 0 behind an odd number of candidates
+        const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(sh.kept + i);
+        before += (two.x > k) + (two.y > k);
+      }
       if (before < top) sh.best[before] = k;
     }
   } else {
@@ -253,7 +258,7 @@ __device__ __noinline__ void rescan(Shared& sh, const T* x, int e0, int e1, int 
 // 4,099 rows of 50,001 bf16 logits with 8 alternatives: see the table of measured cases; what bounds it is memory, then the issue of
 // about six instructions an element.
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, 4)
     logprob_fwd_kernel(LogprobArgs a, float* logp, float* entropy, float* lse, float* top_logp, int32_t* top_ids, DevCtl ctl) {
   constexpr int N = Vec<T>::N, UNROLL = 4;
   __shared__ Shared sh;
@@ -274,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     edge = k < lead ? k : k - lead < a.V - tail ? tail + k - lead : -1;
   }
   Running mine;
-  float edge_x = -INFINITY, high = -INFINITY;  // high: the thread's largest element of the first tile
+  float edge_x = -INFINITY;
   if (edge >= 0) {
     edge_x = to_f(x[edge]);
     mine.take_one(edge_x, c);
@@ -287,14 +292,21 @@ __global__ void __launch_bounds__(kThreads, 2)
     }
   };
   if (TOP && threadIdx.x == 0) sh.count = 0;
+  Vec<T> ahead[UNROLL];
+  const auto fetch = [&](int v) {
+#pragma unroll
+    for (int i = 0; i < UNROLL; ++i) {
+      const int at = v + i * kThreads + threadIdx.x;
+      if (at < v1) ahead[i] = load_vec(body + static_cast<size_t>(at) * N);
+    }
+  };
+  fetch(v0);
   for (int v = v0; v == v0 || v < v1; v += kThreads * UNROLL) {
     Vec<T> u[UNROLL];
     float most[UNROLL];
 #pragma unroll
-    for (int i = 0; i < UNROLL; ++i) {
-      const int at = v + i * kThreads + threadIdx.x;
-      if (at < v1) u[i] = load_vec(body + static_cast<size_t>(at) * N);
-    }
+    for (int i = 0; i < UNROLL; ++i) u[i] = ahead[i];
+    fetch(v + kThreads * UNROLL);
 #pragma unroll
     for (int i = 0; i < UNROLL; ++i) {
       most[i] = -INFINITY;
@@ -305,16 +317,19 @@ __global__ void __launch_bounds__(kThreads, 2)
     }
     if constexpr (TOP) {
       if (v == v0) {
-        high = fmaxf(edge_x, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
-        high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, 1));
-        if (threadIdx.x % 2 == 0) sh.groups[threadIdx.x / 2] = high;
+        // 64 to 256 groups of neighbouring threads, twice as many as alternatives or more where there are
+        const int lanes = a.top <= 32 ? 4 : a.top <= 64 ? 2 : 1, groups = kThreads / lanes;
+        float high = fmaxf(edge_x, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
+        for (int o = 1; o < lanes; o *= 2) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+        if (threadIdx.x % lanes == 0) sh.groups[threadIdx.x / lanes] = high;
         if (threadIdx.x == 0) sh.bar = -INFINITY;
         __syncthreads();
-        if (threadIdx.x < kGroups) {
+        if (static_cast<int>(threadIdx.x) < groups) {
           const float g = sh.groups[threadIdx.x];
           int before = 0;
-          for (int i = 0; i < kGroups; ++i) before += sh.groups[i] > g || (sh.groups[i] == g && i < static_cast<int>(threadIdx.x));
-          if (before == a.top - 1) sh.bar = g;  // NaN and +inf are no larger than others; the row is void then
+#pragma unroll 8
+          for (int i = 0; i < groups; ++i) before += sh.groups[i] > g || (sh.groups[i] == g && i < static_cast<int>(threadIdx.x));
+          if (before == a.top - 1) sh.bar = g;
         }
         __syncthreads();
         bar = sh.bar;
@@ -347,25 +362,54 @@ __global__ void __launch_bounds__(kThreads, 2)
     all = threadIdx.x < kThreads / 32 ? sh.sums[threadIdx.x] : Sums{-INFINITY, 0.f, 0.f};
 #pragma unroll
     for (int o = kThreads / 64; o; o >>= 1) all.add_lane(o, c);
-    if (threadIdx.x == 0) sh.total = all;
+    if (threadIdx.x == 0) sh.total = all, sh.count = 0;
   }
   if (blocks > 1) {
     cluster.sync();
     if (rank_here == 0) {
-      if (threadIdx.x == 0) {
-        for (int b = 1; b < blocks; ++b) all.add(*cluster.map_shared_rank(&sh.total, b), c);
-        sh.total = all;
-        sh.count = 0;
+      // a warp for each block's alternatives, a lane for each one's sums: other blocks' memory is far away
+      const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+      if (warp == 0) {
+        all = lane < blocks ? *cluster.map_shared_rank(&sh.total, lane) : Sums{-INFINITY, 0.f, 0.f};
+#pragma unroll
+        for (int o = kMostBlocks / 2; o; o >>= 1) all.add_lane(o, c);
       }
       if constexpr (TOP) {
-        __syncthreads();
-        for (int b = 0; b < blocks; ++b) {
-          const Shared* from = cluster.map_shared_rank(&sh, b);
+        static_assert(kThreads / 32 >= kMostBlocks && kMostBlocks * kMaxAlternatives <= kKept, "a warp and a list for each block");
+        if (warp < blocks) {
+          const Shared* from = cluster.map_shared_rank(&sh, warp);
           const int have = from->have;
-          for (int i = threadIdx.x; i < have; i += kThreads) sh.kept[atomicAdd(&sh.count, 1)] = from->best[i];  // 8 x 128 at most
+#pragma unroll
+          for (int i = 0; i < kMaxAlternatives; i += 32)  // best holds anything from `have` on
+            if (i + lane < a.top) {
+              const unsigned long long k = from->best[i + lane];
+              sh.kept[warp * kMaxAlternatives + i + lane] = i + lane < have ? k : 0;
+            }
         }
-        rank(sh, a.top);
+        __syncthreads();
+        // the lists are sorted: an element's rank is its place in its own and how many of each other one are larger
+        for (int t = threadIdx.x; t < blocks * a.top; t += kThreads) {
+          const int list = t / a.top, i = t % a.top;
+          const unsigned long long k = sh.kept[list * kMaxAlternatives + i];
+          int before = i;
+          for (int o = 0; o < blocks && before < a.top; ++o) {
+            if (o == list) continue;
+            int lo = 0, hi = a.top;  // elements below lo are larger, from hi on they are not
+            while (lo < hi) {
+              const int mid = (lo + hi) / 2;
+              if (sh.kept[o * kMaxAlternatives + mid] > k)
+                lo = mid + 1;
+              else
+                hi = mid;
+            }
+            before += lo;
+          }
+          if (k && before < a.top) sh.best[before] = k;
+          if (k && before < a.top) atomicAdd(&sh.count, 1);
+        }
       }
+      __syncthreads();
+      if (threadIdx.x == 0) sh.total = all, sh.have = sh.count;
     }
     cluster.sync();  // no block leaves before its shared memory has been read
   }
@@ -496,9 +540,9 @@ __global__ void __launch_bounds__(kBwdThreads) logprob_bwd_kernel(LogprobArgs a,
 template <typename T>
 int fwd(const LogprobArgs& a, float* logp, float* entropy, float* lse, float* top_logp, int32_t* top_ids, int num_sms, const DevCtl& ctl,
         cudaStream_t st) {
-  // two blocks fit an SM; a share below 4,096 elements is not worth a block
+  // four blocks fit an SM; a share below 4,096 elements is not worth a block
   int blocks = 1;
-  while (blocks < kMostBlocks && 2ll * a.N * blocks <= 2ll * num_sms && a.V / (2 * blocks) >= 4096) blocks *= 2;
+  while (blocks < kMostBlocks && 2ll * a.N * blocks <= 4ll * num_sms && a.V / (2 * blocks) >= 4096) blocks *= 2;
   cudaLaunchConfig_t config = {};
   config.gridDim = dim3(static_cast<unsigned>(a.N) * blocks), config.blockDim = dim3(kThreads), config.stream = st;
   cudaLaunchAttribute attr = {};
