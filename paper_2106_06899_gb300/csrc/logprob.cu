@@ -18,7 +18,6 @@
 #include <cuda_bf16.h>
 
 #include "kernels.h"
-#include "pairs.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -115,64 +114,77 @@ struct Sums {
   }
 };
 
-__device__ __forceinline__ F2 add2(F2 a, F2 b) {
-  F2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-
-// The largest and the smallest of a vector's elements, NaN left out.
-__device__ __forceinline__ void range_of(const Vec<__nv_bfloat16>& v, float& most, float& least) {
+// The largest of a vector's elements, NaN left out.
+__device__ __forceinline__ float most_of(const Vec<__nv_bfloat16>& v) {
   const __nv_bfloat162* w = reinterpret_cast<const __nv_bfloat162*>(&v.u);
-  const __nv_bfloat162 hi = __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3])), lo = __hmin2(__hmin2(w[0], w[1]), __hmin2(w[2], w[3]));
-  most = fmaxf(__low2float(hi), __high2float(hi)), least = fminf(__low2float(lo), __high2float(lo));
+  const __nv_bfloat162 m = __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3]));
+  return fmaxf(__low2float(m), __high2float(m));
 }
-__device__ __forceinline__ void range_of(const Vec<float>& v, float& most, float& least) {
+__device__ __forceinline__ float most_of(const Vec<float>& v) {
   float x[4];
   v.get(x);
-  most = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), least = fminf(fminf(x[0], x[1]), fminf(x[2], x[3]));
+  return fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
 }
 
-// A thread's sums, in pairs.
+// Elements raised to `floor`; NaN stays.
+__device__ __forceinline__ Vec<__nv_bfloat16> at_least(Vec<__nv_bfloat16> v, float floor) {
+  __nv_bfloat162* w = reinterpret_cast<__nv_bfloat162*>(&v.u);
+  const __nv_bfloat162 f = __float2bfloat162_rn(floor);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = __hmax2_nan(w[e], f);
+  return v;
+}
+__device__ __forceinline__ Vec<float> at_least(Vec<float> v, float floor) {
+  uint32_t* w = reinterpret_cast<uint32_t*>(&v.u);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) asm("max.NaN.f32 %0, %1, %2;" : "=r"(w[e]) : "r"(w[e]), "f"(floor));
+  return v;
+}
+
+// A thread's sums; t without the factor c.
 struct Running {
-  float r = -INFINITY;
-  F2 s = f2(0.f, 0.f), t = f2(0.f, 0.f);
+  float r = -INFINITY, s = 0.f, t = 0.f;
+  float floor = -INFINITY;  // elements below it are taken for it: their 2^d is 0, and 0 x d must not be NaN
 
   __device__ __forceinline__ void raise(float top, float c) {
     if ((top - r) * c > kRaise) {  // the first element too: r is -inf
       if (r > -INFINITY) {
-        const float d = fmaxf((r - top) * c, -300.f), f = exp2_fast(d);
-        t = mul2(f2(f, f), fma2(f2(d, d), s, t)), s = mul2(f2(f, f), s);
+        const float d = r - top, f = exp2_fast(d * c);
+        t = f == 0.f ? 0.f : f * fmaf(d, s, t), s *= f;
       }
       r = top;
+      floor = top - 300.f / c - fabsf(top) * 0.03125f;  // the last part outlasts its rounding
     }
   }
-  // the vector's elements, between `least` and `most`
+  // the vector's elements, `most` the largest of them
   template <typename T>
-  __device__ __forceinline__ void take(const Vec<T>& v, float c, float most, float least) {
-    float x[Vec<T>::N];
-    v.get(x);
+  __device__ __forceinline__ void take(const Vec<T>& v, float c, float most) {
     raise(most, c);
-    const float base = r == -INFINITY ? 0.f : -r;
-    const bool far = !((least + base) * c > -300.f);  // 2^d is 0, and 0 x d must not be NaN
+    float x[Vec<T>::N];
+    if (floor == -INFINITY) {  // no element that counts yet, or none above the type's lowest values
+      v.get(x);
 #pragma unroll
-    for (int e = 0; e < Vec<T>::N; e += 2) {
-      F2 d = mul2(add2(f2(x[e], x[e + 1]), f2(base, base)), f2(c, c));
-      const F2 p = f2(exp2_fast(lo(d)), exp2_fast(hi(d)));
-      s = add2(s, p);
-      if (far) d = f2(fmaxf(lo(d), -300.f), fmaxf(hi(d), -300.f));
-      t = fma2(p, d, t);
+      for (int e = 0; e < Vec<T>::N; ++e) add_one(x[e], c);
+      return;
+    }
+    at_least(v, floor).get(x);
+#pragma unroll
+    for (int e = 0; e < Vec<T>::N; ++e) {
+      const float d = x[e] - r, p = exp2_fast(d * c);
+      s += p;
+      t = fmaf(p, d, t);
     }
   }
   __device__ __forceinline__ void take_one(float x, float c) {
     raise(x, c);
-    const float d = (x + (r == -INFINITY ? 0.f : -r)) * c, p = exp2_fast(d);
-    s = add2(s, f2(p, 0.f));
-    t = fma2(f2(p, 0.f), f2(fmaxf(d, -300.f), 0.f), t);
+    add_one(x, c);
   }
-  __device__ __forceinline__ Sums sums() const {
-    return Sums{r, lo(s) + hi(s), lo(t) + hi(t)};
+  __device__ __forceinline__ void add_one(float x, float c) {
+    const float d = x - (r == -INFINITY ? 0.f : r), p = exp2_fast(d * c);
+    s += p;
+    t = p == 0.f ? t : fmaf(p, d, t);
   }
+  __device__ __forceinline__ Sums sums(float c) const { return Sums{r, s, t * c}; }
 };
 
 // Sorts `n` (a power of two) keys, largest first; all threads.
@@ -311,9 +323,8 @@ __global__ void __launch_bounds__(kThreads, 4)
     for (int i = 0; i < UNROLL; ++i) {
       most[i] = -INFINITY;
       if (v + i * kThreads + static_cast<int>(threadIdx.x) >= v1) continue;
-      float least;
-      range_of(u[i], most[i], least);
-      mine.take(u[i], c, most[i], least);
+      most[i] = most_of(u[i]);
+      mine.take(u[i], c, most[i]);
     }
     if constexpr (TOP) {
       if (v == v0) {
@@ -341,8 +352,17 @@ __global__ void __launch_bounds__(kThreads, 4)
         float e[N];
         u[i].get(e);
         const int at = v + i * kThreads + threadIdx.x;
+        uint32_t hits = 0;
 #pragma unroll
-        for (int k = 0; k < N; ++k) offer(e[k], lead + at * N + k);
+        for (int k = 0; k < N; ++k) hits |= e[k] >= bar ? 1u << k : 0u;
+        while (hits) {  // one turn for nearly every warp
+          const int k = __ffs(hits) - 1;
+          hits &= hits - 1;
+          float ek = e[0];
+#pragma unroll
+          for (int q = 1; q < N; ++q) ek = q == k ? e[q] : ek;
+          offer(ek, lead + at * N + k);
+        }
       }
     }
   }
@@ -353,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   }
 
   // sums: lanes, warps, blocks, in this order
-  Sums all = mine.sums();
+  Sums all = mine.sums(c);
 #pragma unroll
   for (int o = 16; o; o >>= 1) all.add_lane(o, c);
   if (threadIdx.x % 32 == 0) sh.sums[threadIdx.x / 32] = all;
