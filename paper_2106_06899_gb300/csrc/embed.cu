@@ -1,7 +1,25 @@
 // embed.cu -- the embedding lookup and its gradient.
+//
+// Lookup: a warp for each token's row, sixteen bytes a lane where rows are aligned to them.  Memory bounds it.
+//
+// Gradient: a row of it is the sum of dy over the tokens with its id, and a few ids have most of the tokens.  The tokens are
+// sorted by id, stably, so that a row's terms lie together in the order of the tokens; the sorted list is cut into runs
+// of kRun tokens whatever their ids, and a warp adds up a run, a slice of columns each, with a run's rows all on
+// their way at once.  Ids that end inside the run are written; those that a run's edge cuts go to scratch (the run's
+// first and last id), and embed_join_kernel adds their parts up in the order of the runs: every sum is always
+// formed in the same order.
+//
+// The sort is least digit first over the bits that ids have, by one cluster of CTAs: each has a share of the tokens, counts
+// digits, learns from the others' shared memory where its tokens go, and places them.  That is latency, a few
+// microseconds a digit; the other SMs write the zeros of rows without a token meanwhile, in the same launch.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "kernels.h"
+
+namespace cg = cooperative_groups;
 
 namespace topk {
 
@@ -16,84 +34,402 @@ __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
-// A block for each token.
-template <typename T>
-__global__ void embed_fwd_kernel(EmbedArgs a, const T* __restrict__ weight, T* __restrict__ out, DevCtl ctl) {
-  const long long id = id_at(a.ids, a.ids64, blockIdx.x);
-  if (id >= a.rows && threadIdx.x == 0) atomicOr(ctl.error, kDevErrRange);
-  const bool real = id >= 0 && id < a.rows;
-  const T* w = weight + (real ? static_cast<size_t>(id) * a.D : 0);
-  for (int c = threadIdx.x; c < a.D; c += blockDim.x)
-    put(out + static_cast<size_t>(blockIdx.x) * a.D + c, real ? to_f(w[c]) * a.scale : 0.f);
+// E neighbouring elements, loaded and stored as one access.
+template <typename T, int E>
+struct Pack {
+  using Raw = std::conditional_t<sizeof(T) * E == 16, uint4,
+                                 std::conditional_t<sizeof(T) * E == 8, uint2, std::conditional_t<sizeof(T) * E == 4, uint32_t, uint16_t>>>;
+  Raw raw;
+  __device__ __forceinline__ float get(int e) const {
+    const T* x = reinterpret_cast<const T*>(&raw);
+    return to_f(x[e]);
+  }
+  __device__ __forceinline__ void set(int e, float v) { put(reinterpret_cast<T*>(&raw) + e, v); }
+};
+
+template <typename T, int E>
+__device__ __forceinline__ Pack<T, E> load_pack(const T* p) {
+  Pack<T, E> r;
+  r.raw = __ldg(reinterpret_cast<const typename Pack<T, E>::Raw*>(p));
+  return r;
 }
 
-// A block for each row of the gradient: it reads all ids and adds up its tokens in order.
-template <typename T, typename G>
-__global__ void __launch_bounds__(256) embed_bwd_kernel(EmbedArgs a, const T* __restrict__ dy, G* __restrict__ dw, bool accumulate, DevCtl ctl) {
-  __shared__ int found[256];
-  __shared__ int count[8];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int c0 = 0; c0 < a.D; c0 += 256) {
-    const int c = c0 + threadIdx.x;
-    float sum = 0.f;
-    bool any = false;
-    for (int n0 = 0; n0 < a.N; n0 += 256) {
-      const int n = n0 + threadIdx.x;
-      const long long id = n < a.N ? id_at(a.ids, a.ids64, n) : -1;
-      if (id >= a.rows && blockIdx.x == 0) atomicOr(ctl.error, kDevErrRange);
-      const bool mine = id == static_cast<long long>(blockIdx.x);
-      const unsigned votes = __ballot_sync(0xffffffffu, mine);
-      if (lane == 0) count[warp] = __popc(votes);
-      __syncthreads();
-      int at = __popc(votes & ((1u << lane) - 1u)), total = 0;
-      for (int w = 0; w < 8; ++w) {
-        if (w < warp) at += count[w];
-        total += count[w];
+// ------------------------------------------------------------ lookup
+constexpr int kFwdThreads = 256;
+
+// Unit u: the token u / parts and the part u % parts of its row, a warp each.
+template <typename T, int E>
+__global__ void __launch_bounds__(kFwdThreads) embed_fwd_kernel(EmbedArgs a, const T* __restrict__ weight, T* __restrict__ out, int parts, DevCtl ctl) {
+  constexpr int FLIGHT = 5;  // loads of a lane under way
+  const int lane = threadIdx.x % 32, packs = a.D / E, each = (packs + parts - 1) / parts;
+  const long long units = static_cast<long long>(a.N) * parts, stride = static_cast<long long>(gridDim.x) * (kFwdThreads / 32);
+  for (long long u = static_cast<long long>(blockIdx.x) * (kFwdThreads / 32) + threadIdx.x / 32; u < units; u += stride) {
+    const int n = static_cast<int>(u / parts), part = static_cast<int>(u % parts);
+    const long long id = id_at(a.ids, a.ids64, n);
+    const bool real = id >= 0 && id < a.rows;
+    if (id >= a.rows && lane == 0) atomicOr(ctl.error, kDevErrRange);
+    const T* from = weight + (real ? id : 0) * a.D;
+    T* to = out + static_cast<size_t>(n) * a.D;
+    for (int c0 = part * each + lane, end = min(packs, (part + 1) * each); c0 < end; c0 += 32 * FLIGHT) {
+      Pack<T, E> x[FLIGHT];
+#pragma unroll
+      for (int i = 0; i < FLIGHT; ++i)
+        if (c0 + 32 * i < end && real) x[i] = load_pack<T, E>(from + static_cast<size_t>(c0 + 32 * i) * E);
+#pragma unroll
+      for (int i = 0; i < FLIGHT; ++i) {
+        if (c0 + 32 * i >= end) continue;
+        if (!real) {
+          x[i].raw = typename Pack<T, E>::Raw{};
+        } else if (a.scale != 1.f) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[i].set(e, x[i].get(e) * a.scale);
+        }
+        *reinterpret_cast<typename Pack<T, E>::Raw*>(to + static_cast<size_t>(c0 + 32 * i) * E) = x[i].raw;
       }
-      if (mine) found[at] = n;
-      __syncthreads();
-      any |= total > 0;
-      if (c < a.D)
-        for (int i = 0; i < total; ++i) sum += to_f(dy[static_cast<size_t>(found[i]) * a.D + c]);
-      __syncthreads();
-    }
-    if (c < a.D) {
-      G* p = dw + static_cast<size_t>(blockIdx.x) * a.D + c;
-      if (!accumulate)
-        put(p, sum * a.scale);
-      else if (any)
-        put(p, to_f(*p) + sum * a.scale);
     }
   }
 }
 
-}  // namespace
+// ------------------------------------------------------------ sorting the tokens
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+constexpr int kSortBlocks = 8;  // of the cluster: the portable size
+constexpr int kDigitBits = 8, kDigits = 1 << kDigitBits;
 
-int embed_fwd(const EmbedArgs& a, const void* weight, void* out, bool bf16, int, const DevCtl& ctl, cudaStream_t st) {
-  if (bf16)
-    embed_fwd_kernel<<<a.N, 256, 0, st>>>(a, static_cast<const __nv_bfloat16*>(weight), static_cast<__nv_bfloat16*>(out), ctl);
-  else
-    embed_fwd_kernel<<<a.N, 256, 0, st>>>(a, static_cast<const float*>(weight), static_cast<float*>(out), ctl);
-  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+struct Scratch {
+  uint2* a;     // (id, token), sorted
+  uint2* b;
+  float* parts; // [runs][2][D]
+  int* real;    // tokens with an id in the table
+};
+
+constexpr int kRun = 32;  // sorted tokens that a warp adds up
+int runs_of(int N) { return (N + kRun - 1) / kRun; }
+
+struct SortShared {
+  unsigned count[kSortWarps][kDigits];  // of each warp's tokens, then where they go
+  unsigned total[kDigits];              // of the block
+  unsigned first[kDigits];              // where the block's tokens of a digit go
+  unsigned scan[kSortWarps];
+};
+
+// One digit of the cluster's sort: tokens [n0, n1) of `from` (or the ids themselves) into `to`.
+template <typename Get>
+__device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, uint2* to, int n0, int n1, int shift) {
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, blocks = cluster.num_blocks(), rank = cluster.block_rank();
+  for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&sh.count[0][0])[i] = 0;
+  __syncthreads();
+  // each warp has a share of its own, in order: places within it follow the tokens
+  const int each = ((n1 - n0 + kSortWarps - 1) / kSortWarps + 31) / 32 * 32, w0 = min(n1, n0 + warp * each), w1 = min(n1, w0 + each);
+  for (int i = w0; i < w1; i += 32) {
+    const bool in = i + lane < w1;
+    const unsigned digit = in ? get(i + lane).x >> shift & (kDigits - 1) : kDigits;
+    const unsigned same = __match_any_sync(0xffffffffu, digit);
+    if (in && (same & ((1u << lane) - 1u)) == 0) sh.count[warp][digit] += __popc(same);  // the first of its kind
+    __syncwarp();
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < kDigits; d += kSortThreads) {
+    unsigned sum = 0;
+    for (int w = 0; w < kSortWarps; ++w) {
+      const unsigned c = sh.count[w][d];
+      sh.count[w][d] = sum;
+      sum += c;
+    }
+    sh.total[d] = sum;
+  }
+  cluster.sync();
+  // where a digit begins: all smaller digits' tokens, and the earlier blocks' of its own
+  unsigned mine = 0, all = 0;
+  if (threadIdx.x < kDigits) {
+    unsigned got[kSortBlocks];
+#pragma unroll
+    for (int b = 0; b < kSortBlocks; ++b) got[b] = b < blocks ? cluster.map_shared_rank(&sh, b)->total[threadIdx.x] : 0;
+#pragma unroll
+    for (int b = 0; b < kSortBlocks; ++b) {
+      mine += b < rank ? got[b] : 0;
+      all += got[b];
+    }
+  }
+  unsigned upto = all;
+  for (int o = 1; o < 32; o *= 2) {
+    const unsigned x = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 31) sh.scan[warp] = upto;
+  __syncthreads();
+  if (threadIdx.x < kDigits) {
+    unsigned before = 0;
+    for (int w = 0; w < warp; ++w) before += sh.scan[w];
+    sh.first[threadIdx.x] = before + upto - all + mine;
+  }
+  __syncthreads();
+  for (int i = w0; i < w1; i += 32) {
+    const bool in = i + lane < w1;
+    const uint2 x = in ? get(i + lane) : make_uint2(0u, 0u);
+    const unsigned digit = in ? x.x >> shift & (kDigits - 1) : kDigits;
+    const unsigned same = __match_any_sync(0xffffffffu, digit), before = __popc(same & ((1u << lane) - 1u));
+    unsigned base = 0;
+    if (in) base = sh.count[warp][digit];
+    __syncwarp();
+    if (in) {
+      if (before == 0) sh.count[warp][digit] = base + __popc(same);
+      to[sh.first[digit] + base + before] = x;
+    }
+    __syncwarp();
+  }
+  __threadfence();
+  cluster.sync();  // the placed tokens are there, and no block's counts are read any more
 }
 
-size_t embed_bwd_workspace_bytes(int, int, int) { return 16; }
+// The first cluster sorts; the other blocks write zeros (into dw where it is to be written, [bytes16] of 16 bytes and a tail).
+__global__ void __launch_bounds__(kSortThreads)
+    embed_sort_kernel(EmbedArgs a, Scratch s, int passes, int sorters, uint4* zero, long long bytes16, int tail_bytes, DevCtl ctl) {
+  __shared__ SortShared sh;
+  cg::cluster_group cluster = cg::this_cluster();
+  if (static_cast<int>(blockIdx.x) >= sorters) {
+    const long long at = static_cast<long long>(blockIdx.x - sorters) * kSortThreads + threadIdx.x,
+                    stride = static_cast<long long>(gridDim.x - sorters) * kSortThreads;
+    for (long long i = at; i < bytes16; i += stride) zero[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (at < tail_bytes) reinterpret_cast<uint8_t*>(zero + bytes16)[at] = 0;
+    return;
+  }
+  const int rank = blockIdx.x;
+  const int each = (a.N + sorters - 1) / sorters, n0 = min(a.N, rank * each), n1 = min(a.N, n0 + each);
+  const unsigned none = static_cast<unsigned>(a.rows);  // the id of tokens without one: behind all others
+  if (rank == 0 && threadIdx.x == 0) *s.real = 0;
+  cluster.sync();
+  int real = 0;
+  bool wrong = false;
+  for (int i = n0 + threadIdx.x; i < n1; i += kSortThreads) {
+    const long long id = id_at(a.ids, a.ids64, i);
+    wrong |= id >= a.rows;
+    real += id >= 0 && id < a.rows;
+  }
+  if (wrong) atomicOr(ctl.error, kDevErrRange);
+  for (int o = 16; o; o /= 2) real += __shfl_xor_sync(0xffffffffu, real, o);
+  if (threadIdx.x % 32 == 0 && real) atomicAdd(s.real, real);
+  uint2 *from = s.b, *to = s.a;
+  if (passes % 2 == 0) {
+    uint2* t = from;
+    from = to, to = t;
+  }
+  for (int p = 0; p < passes; ++p) {
+    if (p == 0)
+      sort_digit(
+          cluster, sh,
+          [&](int i) {
+            const long long id = id_at(a.ids, a.ids64, i);
+            return make_uint2(id >= 0 && id < a.rows ? static_cast<unsigned>(id) : none, static_cast<unsigned>(i));
+          },
+          to, n0, n1, 0);
+    else
+      sort_digit(cluster, sh, [&](int i) { return __ldcg(from + i); }, to, n0, n1, p * kDigitBits);
+    uint2* t = from;
+    from = to, to = t;
+  }
+}
+
+// ------------------------------------------------------------ adding up
+constexpr int kSumWarps = 4;
+
+struct SumArgs {
+  int N, rows, D, parts;  // parts: of a row's columns
+  float scale;
+  bool accumulate;
+};
+
+// Writes an id's finished sum of E columns.
+template <typename G, int E>
+__device__ __forceinline__ void finish(G* at, const float (&sum)[E], float scale, bool accumulate) {
+  Pack<G, E> old, now;
+  if (accumulate) old = *reinterpret_cast<const Pack<G, E>*>(at);
+#pragma unroll
+  for (int e = 0; e < E; ++e) now.set(e, accumulate ? fmaf(sum[e], scale, old.get(e)) : sum[e] * scale);
+  *reinterpret_cast<typename Pack<G, E>::Raw*>(at) = now.raw;
+}
+
+// A warp: run `run` of sorted tokens, 32 E columns.
+template <typename T, typename G, int E>
+__global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(SumArgs a, Scratch s, const T* __restrict__ dy, G* __restrict__ dw) {
+  constexpr int FLIGHT = 8;
+  const int lane = threadIdx.x % 32;
+  const long long unit = static_cast<long long>(blockIdx.x) * kSumWarps + threadIdx.x / 32;
+  const int run = static_cast<int>(unit / a.parts), c = static_cast<int>(unit % a.parts) * 32 + lane;
+  const int real = *s.real, i0 = run * kRun, n = min(kRun, real - i0);
+  if (n <= 0) return;
+  const uint2 mine = lane < n ? __ldg(s.a + i0 + lane) : make_uint2(~0u, 0u);
+  const unsigned before = i0 > 0 ? __ldg(&s.a[i0 - 1].x) : ~0u, after = i0 + n < real ? __ldg(&s.a[i0 + n].x) : ~0u;
+  const bool in = c * E < a.D;
+  float sum[E] = {};
+  unsigned id = __shfl_sync(0xffffffffu, mine.x, 0);
+  bool first = true;  // the run's first id
+  const auto close = [&](bool last) {
+    if (!in) return;
+    const bool cut_front = first && id == before, cut_back = last && id == after;
+    if (cut_front || cut_back) {
+      float* to = s.parts + (static_cast<size_t>(run) * 2 + (first ? 0 : 1)) * a.D + c * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) to[e] = sum[e];
+    } else {
+      finish<G, E>(dw + static_cast<size_t>(id) * a.D + c * E, sum, a.scale, a.accumulate);
+    }
+  };
+  for (int k0 = 0; k0 < n; k0 += FLIGHT) {
+    Pack<T, E> x[FLIGHT];
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) {
+      const unsigned token = __shfl_sync(0xffffffffu, mine.y, k0 + k);
+      if (k0 + k < n && in) x[k] = load_pack<T, E>(dy + static_cast<size_t>(token) * a.D + c * E);
+    }
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) {
+      if (k0 + k >= n) break;
+      const unsigned now = __shfl_sync(0xffffffffu, mine.x, k0 + k);
+      if (now != id) {
+        close(false);
+        first = false, id = now;
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] = 0.f;
+      }
+      if (in) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] += x[k].get(e);
+      }
+    }
+  }
+  close(true);
+}
+
+// A warp for each run whose last id goes on in the next one and begins in it: it adds up that id's parts.
+template <typename G, int E>
+__global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(SumArgs a, Scratch s, G* __restrict__ dw) {
+  const int lane = threadIdx.x % 32;
+  const long long unit = static_cast<long long>(blockIdx.x) * kSumWarps + threadIdx.x / 32;
+  const int run = static_cast<int>(unit / a.parts), c = static_cast<int>(unit % a.parts) * 32 + lane;
+  const int real = *s.real, i0 = run * kRun, next = i0 + kRun;
+  if (next >= real) return;
+  const unsigned id = __ldg(&s.a[next - 1].x);
+  if (__ldg(&s.a[next].x) != id) return;               // it ends here
+  const bool all = __ldg(&s.a[i0].x) == id;            // the run is all of that id
+  if (all && i0 > 0 && __ldg(&s.a[i0 - 1].x) == id) return;  // it began before
+  // the runs that it covers: up to the last one that begins with it
+  int lo = run + 1, hi = (real - 1) / kRun;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (__ldg(&s.a[mid * kRun].x) == id)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  if (c * E >= a.D) return;
+  float sum[E];
+  const float* first = s.parts + (static_cast<size_t>(run) * 2 + (all ? 0 : 1)) * a.D + c * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) sum[e] = first[e];
+#pragma unroll 8
+  for (int r = run + 1; r <= lo; ++r) {
+    const float* p = s.parts + static_cast<size_t>(r) * 2 * a.D + c * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] += __ldg(p + e);
+  }
+  finish<G, E>(dw + static_cast<size_t>(id) * a.D + c * E, sum, a.scale, a.accumulate);
+}
+
+// Elements of an access: the most that divide a row and fill sixteen bytes at the wider type.
+int pack_of(int D, size_t narrow_bytes) {
+  int e = static_cast<int>(16 / narrow_bytes);
+  while (D % e) e /= 2;
+  return e;
+}
 
 template <typename T>
-static void bwd_of(const EmbedArgs& a, const void* dy, void* dw, bool accumulate, bool grad_bf16, const DevCtl& ctl, cudaStream_t st) {
-  if (grad_bf16)
-    embed_bwd_kernel<<<a.rows, 256, 0, st>>>(a, static_cast<const T*>(dy), static_cast<__nv_bfloat16*>(dw), accumulate, ctl);
-  else
-    embed_bwd_kernel<<<a.rows, 256, 0, st>>>(a, static_cast<const T*>(dy), static_cast<float*>(dw), accumulate, ctl);
+int fwd(const EmbedArgs& a, const T* weight, T* out, int num_sms, const DevCtl& ctl, cudaStream_t st) {
+  const int e = pack_of(a.D, sizeof(T)), packs = a.D / e;
+  // few tokens: a row is shared out over warps, one load a lane
+  int parts = 1;
+  while (static_cast<long long>(a.N) * parts < 16ll * num_sms && packs > 32 * parts) ++parts;
+  const long long units = static_cast<long long>(a.N) * parts, warps = kFwdThreads / 32;
+  const long long want = (units + warps - 1) / warps, most = 8ll * num_sms;
+  const unsigned grid = static_cast<unsigned>(want < most ? want : most);
+  switch (e) {
+    case 8:
+      if constexpr (sizeof(T) == 2) embed_fwd_kernel<T, 8><<<grid, kFwdThreads, 0, st>>>(a, weight, out, parts, ctl);
+      break;
+    case 4: embed_fwd_kernel<T, 4><<<grid, kFwdThreads, 0, st>>>(a, weight, out, parts, ctl); break;
+    case 2: embed_fwd_kernel<T, 2><<<grid, kFwdThreads, 0, st>>>(a, weight, out, parts, ctl); break;
+    default: embed_fwd_kernel<T, 1><<<grid, kFwdThreads, 0, st>>>(a, weight, out, parts, ctl);
+  }
+  return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 
-int embed_bwd(const EmbedArgs& a, const void* dy, void* dweight, bool accumulate, bool bf16, bool grad_bf16, void*, int, const DevCtl& ctl,
-              cudaStream_t st) {
-  if (bf16)
-    bwd_of<__nv_bfloat16>(a, dy, dweight, accumulate, grad_bf16, ctl, st);
-  else
-    bwd_of<float>(a, dy, dweight, accumulate, grad_bf16, ctl, st);
-  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+template <typename T, typename G, int E>
+int sums(SumArgs p, const Scratch& s, const T* dy, G* dw, cudaStream_t st) {
+  p.parts = (p.D / E + 31) / 32;
+  const long long units = static_cast<long long>(runs_of(p.N)) * p.parts;
+  const unsigned grid = static_cast<unsigned>((units + kSumWarps - 1) / kSumWarps);
+  embed_sum_kernel<T, G, E><<<grid, 32 * kSumWarps, 0, st>>>(p, s, dy, dw);
+  if (cudaGetLastError() != cudaSuccess) return -1;
+  if (p.N <= kRun) return 1;
+  embed_join_kernel<G, E><<<grid, 32 * kSumWarps, 0, st>>>(p, s, dw);
+  return cudaGetLastError() == cudaSuccess ? 2 : -1;
+}
+
+template <typename T, typename G>
+int sums_of(const SumArgs& p, const Scratch& s, const void* dy, void* dw, cudaStream_t st) {
+  const T* x = static_cast<const T*>(dy);
+  G* y = static_cast<G*>(dw);
+  switch (pack_of(p.D, sizeof(T) > sizeof(G) ? sizeof(T) : sizeof(G))) {
+    case 8:
+      if constexpr (sizeof(T) == 2 && sizeof(G) == 2) return sums<T, G, 8>(p, s, x, y, st);
+      return -1;
+    case 4: return sums<T, G, 4>(p, s, x, y, st);
+    case 2: return sums<T, G, 2>(p, s, x, y, st);
+    default: return sums<T, G, 1>(p, s, x, y, st);
+  }
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+int embed_fwd(const EmbedArgs& a, const void* weight, void* out, bool bf16, int num_sms, const DevCtl& ctl, cudaStream_t st) {
+  return bf16 ? fwd(a, static_cast<const __nv_bfloat16*>(weight), static_cast<__nv_bfloat16*>(out), num_sms, ctl, st)
+              : fwd(a, static_cast<const float*>(weight), static_cast<float*>(out), num_sms, ctl, st);
+}
+
+size_t embed_bwd_workspace_bytes(int N, int, int D) {
+  return 256 + 2 * align256(static_cast<size_t>(N) * sizeof(uint2)) + static_cast<size_t>(runs_of(N)) * 2 * D * sizeof(float);
+}
+
+int embed_bwd(const EmbedArgs& a, const void* dy, void* dweight, bool accumulate, bool bf16, bool grad_bf16, void* workspace, int num_sms,
+              const DevCtl& ctl, cudaStream_t st) {
+  uint8_t* at = static_cast<uint8_t*>(workspace);
+  Scratch s;
+  s.real = reinterpret_cast<int*>(at);
+  s.a = reinterpret_cast<uint2*>(at + 256);
+  s.b = reinterpret_cast<uint2*>(at + 256 + align256(static_cast<size_t>(a.N) * sizeof(uint2)));
+  s.parts = reinterpret_cast<float*>(at + 256 + 2 * align256(static_cast<size_t>(a.N) * sizeof(uint2)));
+  int passes = 1;
+  while (passes * kDigitBits < 31 && a.rows >> (passes * kDigitBits)) ++passes;  // ids up to `rows` itself
+  const long long bytes = accumulate ? 0 : static_cast<long long>(a.rows) * a.D * (grad_bf16 ? 2 : 4);
+  // a sorter for every thousand tokens; the others fill the GPU where there are zeros to write
+  int sorters = 1;
+  while (sorters < kSortBlocks && a.N > 1024 * sorters) sorters *= 2;
+  const long long zeroers = bytes ? (bytes / 16 + 4 * kSortThreads) / (4 * kSortThreads) : 0, most = num_sms - sorters;
+  const int grid = sorters + static_cast<int>((zeroers < most ? zeroers : most) + sorters - 1) / sorters * sorters;
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3(grid), config.blockDim = dim3(kSortThreads), config.stream = st;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = sorters, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  config.attrs = &attr, config.numAttrs = 1;
+  if (cudaLaunchKernelEx(&config, embed_sort_kernel, a, s, passes, sorters, static_cast<uint4*>(dweight), bytes / 16, static_cast<int>(bytes % 16), ctl) !=
+      cudaSuccess)
+    return -1;
+  const SumArgs p{a.N, a.rows, a.D, 1, a.scale, accumulate};
+  const int n = bf16 ? (grad_bf16 ? sums_of<__nv_bfloat16, __nv_bfloat16>(p, s, dy, dweight, st) : sums_of<__nv_bfloat16, float>(p, s, dy, dweight, st))
+                     : (grad_bf16 ? sums_of<float, __nv_bfloat16>(p, s, dy, dweight, st) : sums_of<float, float>(p, s, dy, dweight, st));
+  return n < 0 ? -1 : 1 + n;
 }
 
 }  // namespace topk
