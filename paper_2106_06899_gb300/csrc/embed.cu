@@ -4,10 +4,10 @@
 //
 // Gradient: a row of it is the sum of dy over the tokens with its id, and a few ids have most of the tokens.  The tokens are
 // sorted by id, stably, so that a row's terms lie together in the order of the tokens; the sorted list is cut into runs
-// of kRun tokens whatever their ids, and a warp adds up a run, a slice of columns each, with a run's rows all on
-// their way at once.  Ids that end inside the run are written; those that a run's edge cuts go to scratch (the run's
-// first and last id), and embed_join_kernel adds their parts up in the order of the runs: every sum is always
-// formed in the same order.
+// of kRun tokens whatever their ids, and a warp adds up a run, a slice of columns each.  Ids that lie in one run are
+// written by its warp, those that its edges cut are put together by the block over its eight runs, and those that a
+// block's edges cut go to scratch (its first and its last id), where embed_join_kernel adds their parts up in order:
+// every sum is always formed in the same order.
 //
 // The sort is least digit first over the bits that ids have, by one cluster of CTAs: each has a share of the tokens, counts
 // digits, learns from the others' shared memory where its tokens go, and places them.  That is latency, a few
@@ -91,19 +91,20 @@ __global__ void __launch_bounds__(kFwdThreads) embed_fwd_kernel(EmbedArgs a, con
 }
 
 // ------------------------------------------------------------ sorting the tokens
-constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
 constexpr int kSortBlocks = 8;  // of the cluster: the portable size
-constexpr int kDigitBits = 8, kDigits = 1 << kDigitBits;
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;  // two digits for tables of up to 262,143 rows
+static_assert(kDigits == kSortThreads, "a digit for each thread");
 
 struct Scratch {
   uint2* a;     // (id, token), sorted
   uint2* b;
-  float* parts; // [runs][2][D]
+  float* parts; // [pieces][2][D]
   int* real;    // tokens with an id in the table
 };
 
-constexpr int kRun = 32;  // sorted tokens that a warp adds up
-int runs_of(int N) { return (N + kRun - 1) / kRun; }
+constexpr int kRun = 32, kSumWarps = 8, kPiece = kRun * kSumWarps;  // sorted tokens that a warp and a block add up
+int pieces_of(int N) { return (N + kPiece - 1) / kPiece; }
 
 struct SortShared {
   unsigned count[kSortWarps][kDigits];  // of each warp's tokens, then where they go
@@ -120,35 +121,48 @@ __device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, 
   __syncthreads();
   // each warp has a share of its own, in order: places within it follow the tokens
   const int each = ((n1 - n0 + kSortWarps - 1) / kSortWarps + 31) / 32 * 32, w0 = min(n1, n0 + warp * each), w1 = min(n1, w0 + each);
-  for (int i = w0; i < w1; i += 32) {
-    const bool in = i + lane < w1;
-    const unsigned digit = in ? get(i + lane).x >> shift & (kDigits - 1) : kDigits;
-    const unsigned same = __match_any_sync(0xffffffffu, digit);
-    if (in && (same & ((1u << lane) - 1u)) == 0) sh.count[warp][digit] += __popc(same);  // the first of its kind
-    __syncwarp();
+  constexpr int AHEAD = 8;  // a lane's tokens under way: their loads are what the sort waits for
+  uint2 x[AHEAD];
+  const auto fetch = [&](int i0) {
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (i0 + 32 * k + lane < w1) x[k] = get(i0 + 32 * k + lane);
+  };
+  for (int i0 = w0; i0 < w1; i0 += 32 * AHEAD) {
+    fetch(i0);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (i0 + 32 * k < w1) {
+        const bool in = i0 + 32 * k + lane < w1;
+        const unsigned digit = in ? x[k].x >> shift & (kDigits - 1) : kDigits;
+        const unsigned same = __match_any_sync(0xffffffffu, digit);
+        if (in && (same & ((1u << lane) - 1u)) == 0) sh.count[warp][digit] += __popc(same);  // the first of its kind
+        __syncwarp();
+      }
+    }
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < kDigits; d += kSortThreads) {
-    unsigned sum = 0;
+  {
+    const int d = threadIdx.x;
+    unsigned c[kSortWarps], sum = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) c[w] = sh.count[w][d];
+#pragma unroll
     for (int w = 0; w < kSortWarps; ++w) {
-      const unsigned c = sh.count[w][d];
       sh.count[w][d] = sum;
-      sum += c;
+      sum += c[w];
     }
     sh.total[d] = sum;
   }
   cluster.sync();
   // where a digit begins: all smaller digits' tokens, and the earlier blocks' of its own
-  unsigned mine = 0, all = 0;
-  if (threadIdx.x < kDigits) {
-    unsigned got[kSortBlocks];
+  unsigned mine = 0, all = 0, got[kSortBlocks];
 #pragma unroll
-    for (int b = 0; b < kSortBlocks; ++b) got[b] = b < blocks ? cluster.map_shared_rank(&sh, b)->total[threadIdx.x] : 0;
+  for (int b = 0; b < kSortBlocks; ++b) got[b] = b < blocks ? cluster.map_shared_rank(&sh, b)->total[threadIdx.x] : 0;
 #pragma unroll
-    for (int b = 0; b < kSortBlocks; ++b) {
-      mine += b < rank ? got[b] : 0;
-      all += got[b];
-    }
+  for (int b = 0; b < kSortBlocks; ++b) {
+    mine += b < rank ? got[b] : 0;
+    all += got[b];
   }
   unsigned upto = all;
   for (int o = 1; o < 32; o *= 2) {
@@ -157,25 +171,29 @@ __device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, 
   }
   if (lane == 31) sh.scan[warp] = upto;
   __syncthreads();
-  if (threadIdx.x < kDigits) {
-    unsigned before = 0;
-    for (int w = 0; w < warp; ++w) before += sh.scan[w];
-    sh.first[threadIdx.x] = before + upto - all + mine;
-  }
+  unsigned before = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWarps; ++w) before += w < warp ? sh.scan[w] : 0;
+  sh.first[threadIdx.x] = before + upto - all + mine;
   __syncthreads();
-  for (int i = w0; i < w1; i += 32) {
-    const bool in = i + lane < w1;
-    const uint2 x = in ? get(i + lane) : make_uint2(0u, 0u);
-    const unsigned digit = in ? x.x >> shift & (kDigits - 1) : kDigits;
-    const unsigned same = __match_any_sync(0xffffffffu, digit), before = __popc(same & ((1u << lane) - 1u));
-    unsigned base = 0;
-    if (in) base = sh.count[warp][digit];
-    __syncwarp();
-    if (in) {
-      if (before == 0) sh.count[warp][digit] = base + __popc(same);
-      to[sh.first[digit] + base + before] = x;
+  for (int i0 = w0; i0 < w1; i0 += 32 * AHEAD) {
+    if (w1 - w0 > 32 * AHEAD) fetch(i0);  // else they are there
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (i0 + 32 * k < w1) {
+        const bool in = i0 + 32 * k + lane < w1;
+        const unsigned digit = in ? x[k].x >> shift & (kDigits - 1) : kDigits;
+        const unsigned same = __match_any_sync(0xffffffffu, digit), ahead = __popc(same & ((1u << lane) - 1u));
+        unsigned base = 0;
+        if (in) base = sh.count[warp][digit];
+        __syncwarp();
+        if (in) {
+          if (ahead == 0) sh.count[warp][digit] = base + __popc(same);
+          to[sh.first[digit] + base + ahead] = x[k];
+        }
+        __syncwarp();
+      }
     }
-    __syncwarp();
   }
   __threadfence();
   cluster.sync();  // the placed tokens are there, and no block's counts are read any more
@@ -230,109 +248,164 @@ __global__ void __launch_bounds__(kSortThreads)
 }
 
 // ------------------------------------------------------------ adding up
-constexpr int kSumWarps = 4;
-
 struct SumArgs {
   int N, rows, D, parts;  // parts: of a row's columns
   float scale;
   bool accumulate;
 };
 
-// Writes an id's finished sum of E columns.
+// An id's finished sum of E columns, added to `old` where there is something.
 template <typename G, int E>
-__device__ __forceinline__ void finish(G* at, const float (&sum)[E], float scale, bool accumulate) {
-  Pack<G, E> old, now;
-  if (accumulate) old = *reinterpret_cast<const Pack<G, E>*>(at);
+__device__ __forceinline__ void finish(G* at, const float (&sum)[E], const SumArgs& a, const Pack<G, E>& old) {
+  Pack<G, E> now;
 #pragma unroll
-  for (int e = 0; e < E; ++e) now.set(e, accumulate ? fmaf(sum[e], scale, old.get(e)) : sum[e] * scale);
+  for (int e = 0; e < E; ++e) now.set(e, a.accumulate ? fmaf(sum[e], a.scale, old.get(e)) : sum[e] * a.scale);
   *reinterpret_cast<typename Pack<G, E>::Raw*>(at) = now.raw;
 }
+template <typename G, int E>
+__device__ __forceinline__ Pack<G, E> old_of(const G* at) {
+  return *reinterpret_cast<const Pack<G, E>*>(at);
+}
 
-// A warp: run `run` of sorted tokens, 32 E columns.
+// A block: a piece of eight runs, 32 E columns; a warp for each run.
 template <typename T, typename G, int E>
 __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(SumArgs a, Scratch s, const T* __restrict__ dy, G* __restrict__ dw) {
   constexpr int FLIGHT = 8;
-  const int lane = threadIdx.x % 32;
-  const long long unit = static_cast<long long>(blockIdx.x) * kSumWarps + threadIdx.x / 32;
-  const int run = static_cast<int>(unit / a.parts), c = static_cast<int>(unit % a.parts) * 32 + lane;
-  const int real = *s.real, i0 = run * kRun, n = min(kRun, real - i0);
-  if (n <= 0) return;
-  const uint2 mine = lane < n ? __ldg(s.a + i0 + lane) : make_uint2(~0u, 0u);
-  const unsigned before = i0 > 0 ? __ldg(&s.a[i0 - 1].x) : ~0u, after = i0 + n < real ? __ldg(&s.a[i0 + n].x) : ~0u;
-  const bool in = c * E < a.D;
-  float sum[E] = {};
-  unsigned id = __shfl_sync(0xffffffffu, mine.x, 0);
-  bool first = true;  // the run's first id
-  const auto close = [&](bool last) {
-    if (!in) return;
-    const bool cut_front = first && id == before, cut_back = last && id == after;
-    if (cut_front || cut_back) {
-      float* to = s.parts + (static_cast<size_t>(run) * 2 + (first ? 0 : 1)) * a.D + c * E;
+  // the sums of a run's first and last id, where the run's edges cut them (head alone where the run is all of one id)
+  __shared__ float head[kSumWarps][E][32], tail[kSumWarps][E][32];
+  __shared__ unsigned tail_id[kSumWarps];
+  __shared__ int state[kSumWarps];  // kFront: the first id began before; kBack: the last one goes on; kOne: they are the same
+  constexpr int kFront = 1, kBack = 2, kOne = 4;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, piece = blockIdx.x / a.parts;
+  const int c = (blockIdx.x % a.parts * 32 + lane) * E;
+  const bool in = c < a.D;
+  const int real = *s.real, i0 = piece * kPiece + warp * kRun, n = min(kRun, real - i0);
+  if (piece * kPiece >= real) return;
+  if (n > 0) {
+    const uint2 mine = lane < n ? __ldg(s.a + i0 + lane) : make_uint2(~0u, 0u);
+    const unsigned before = i0 > 0 ? __ldg(&s.a[i0 - 1].x) : ~0u, after = i0 + n < real ? __ldg(&s.a[i0 + n].x) : ~0u;
+    float sum[E] = {};
+    bool first = true;
+    int flags = 0;
+    for (int k0 = 0; k0 < n; k0 += FLIGHT) {
+      Pack<T, E> x[FLIGHT];
+      Pack<G, E> old[FLIGHT];
 #pragma unroll
-      for (int e = 0; e < E; ++e) to[e] = sum[e];
-    } else {
-      finish<G, E>(dw + static_cast<size_t>(id) * a.D + c * E, sum, a.scale, a.accumulate);
-    }
-  };
-  for (int k0 = 0; k0 < n; k0 += FLIGHT) {
-    Pack<T, E> x[FLIGHT];
+      for (int k = 0; k < FLIGHT; ++k) {
+        const unsigned token = __shfl_sync(0xffffffffu, mine.y, k0 + k), id = __shfl_sync(0xffffffffu, mine.x, k0 + k);
+        const unsigned next = __shfl_sync(0xffffffffu, mine.x, (k0 + k + 1) & 31);
+        if (k0 + k >= n || !in) continue;
+        x[k] = load_pack<T, E>(dy + static_cast<size_t>(token) * a.D + c);
+        if (a.accumulate && (k0 + k + 1 == n || next != id)) old[k] = old_of<G, E>(dw + static_cast<size_t>(id) * a.D + c);
+      }
 #pragma unroll
-    for (int k = 0; k < FLIGHT; ++k) {
-      const unsigned token = __shfl_sync(0xffffffffu, mine.y, k0 + k);
-      if (k0 + k < n && in) x[k] = load_pack<T, E>(dy + static_cast<size_t>(token) * a.D + c * E);
-    }
+      for (int k = 0; k < FLIGHT; ++k) {
+        if (k0 + k >= n) continue;
+        const unsigned id = __shfl_sync(0xffffffffu, mine.x, k0 + k);
+        const unsigned next = k0 + k + 1 < n ? __shfl_sync(0xffffffffu, mine.x, (k0 + k + 1) & 31) : after;
+        const bool last = k0 + k + 1 == n;
+        if (in) {
 #pragma unroll
-    for (int k = 0; k < FLIGHT; ++k) {
-      if (k0 + k >= n) break;
-      const unsigned now = __shfl_sync(0xffffffffu, mine.x, k0 + k);
-      if (now != id) {
-        close(false);
-        first = false, id = now;
+          for (int e = 0; e < E; ++e) sum[e] += x[k].get(e);
+        }
+        if (!last && next == id) continue;
+        // the id's tokens in this run end here
+        const bool front = first && id == before, back = last && id == after;
+        if (front || back) {
+          float(*to)[32] = first ? head[warp] : tail[warp];
+#pragma unroll
+          for (int e = 0; e < E; ++e) to[e][lane] = sum[e];
+          flags |= (front ? kFront : 0) | (back ? kBack : 0);
+          if (back && lane == 0) tail_id[warp] = id;
+        } else if (in) {
+          finish<G, E>(dw + static_cast<size_t>(id) * a.D + c, sum, a, old[k]);
+        }
+        if (first && last) flags |= kOne;
+        first = false;
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] = 0.f;
       }
-      if (in) {
+    }
+    if (lane == 0) state[warp] = flags;
+  } else if (lane == 0) {
+    state[warp] = 0;
+  }
+  __syncthreads();
+  if (n <= 0 || !in) return;
+  // what begins in this run and goes on, and, by the first warp, what came in from the piece before
+  const int own = state[warp];
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] += x[k].get(e);
-      }
+  for (int turn = 0; turn < 2; ++turn) {
+    const bool incoming = turn == 0;
+    if (incoming ? warp != 0 || !(own & kFront) : !(own & kBack) || ((own & kOne) && (own & kFront))) continue;
+    const bool from_tail = !incoming && !(own & kOne);
+    float sum[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] = from_tail ? tail[warp][e][lane] : head[warp][e][lane];
+    bool open = incoming ? (own & kOne) && (own & kBack) : true;
+    for (int v = warp + 1; v < kSumWarps && open; ++v) {
+      const int st = state[v];
+      if (!(st & kFront)) break;  // nothing there: the piece ends before, and `open` stays
+#pragma unroll
+      for (int e = 0; e < E; ++e) sum[e] += head[v][e][lane];
+      open = (st & kOne) && (st & kBack);
+    }
+    if (open || incoming) {
+      float* to = s.parts + (static_cast<size_t>(piece) * 2 + (incoming ? 0 : 1)) * a.D + c;
+#pragma unroll
+      for (int e = 0; e < E; ++e) to[e] = sum[e];
+    } else {
+      G* at = dw + static_cast<size_t>(tail_id[warp]) * a.D + c;
+      Pack<G, E> old;
+      if (a.accumulate) old = old_of<G, E>(at);
+      finish<G, E>(at, sum, a, old);
     }
   }
-  close(true);
 }
 
-// A warp for each run whose last id goes on in the next one and begins in it: it adds up that id's parts.
+// A block for each piece whose last id goes on in the next one and begins in it: it adds up that id's parts, eight shares of them by
+// its warps, and the shares in order.
 template <typename G, int E>
 __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(SumArgs a, Scratch s, G* __restrict__ dw) {
-  const int lane = threadIdx.x % 32;
-  const long long unit = static_cast<long long>(blockIdx.x) * kSumWarps + threadIdx.x / 32;
-  const int run = static_cast<int>(unit / a.parts), c = static_cast<int>(unit % a.parts) * 32 + lane;
-  const int real = *s.real, i0 = run * kRun, next = i0 + kRun;
+  __shared__ float share[kSumWarps][E][32];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, piece = blockIdx.x / a.parts;
+  const int c = (blockIdx.x % a.parts * 32 + lane) * E;
+  const int real = *s.real, i0 = piece * kPiece, next = i0 + kPiece;
   if (next >= real) return;
   const unsigned id = __ldg(&s.a[next - 1].x);
-  if (__ldg(&s.a[next].x) != id) return;               // it ends here
-  const bool all = __ldg(&s.a[i0].x) == id;            // the run is all of that id
-  if (all && i0 > 0 && __ldg(&s.a[i0 - 1].x) == id) return;  // it began before
-  // the runs that it covers: up to the last one that begins with it
-  int lo = run + 1, hi = (real - 1) / kRun;
+  if (__ldg(&s.a[next].x) != id) return;              // it ends here
+  if (i0 > 0 && __ldg(&s.a[i0 - 1].x) == id) return;  // it began before
+  int lo = piece + 1, hi = (real - 1) / kPiece;       // the last piece that begins with it
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
-    if (__ldg(&s.a[mid * kRun].x) == id)
+    if (__ldg(&s.a[static_cast<size_t>(mid) * kPiece].x) == id)
       lo = mid;
     else
       hi = mid - 1;
   }
-  if (c * E >= a.D) return;
-  float sum[E];
-  const float* first = s.parts + (static_cast<size_t>(run) * 2 + (all ? 0 : 1)) * a.D + c * E;
+  const bool in = c < a.D;
+  // its parts: the second one of the piece where it begins, the first ones of those after
+  const int count = lo - piece + 1, each = (count + kSumWarps - 1) / kSumWarps, k0 = warp * each, k1 = min(count, k0 + each);
+  float sum[E] = {};
+  if (in)
+#pragma unroll 4
+    for (int k = k0; k < k1; ++k) {
+      const float* p = s.parts + (static_cast<size_t>(piece + k) * 2 + (k == 0 ? 1 : 0)) * a.D + c;
 #pragma unroll
-  for (int e = 0; e < E; ++e) sum[e] = first[e];
-#pragma unroll 8
-  for (int r = run + 1; r <= lo; ++r) {
-    const float* p = s.parts + static_cast<size_t>(r) * 2 * a.D + c * E;
+      for (int e = 0; e < E; ++e) sum[e] += __ldg(p + e);
+    }
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] += __ldg(p + e);
+  for (int e = 0; e < E; ++e) share[warp][e][lane] = sum[e];
+  __syncthreads();
+  if (warp != 0 || !in) return;
+  G* at = dw + static_cast<size_t>(id) * a.D + c;
+  Pack<G, E> old;
+  if (a.accumulate) old = old_of<G, E>(at);
+  for (int w = 1; w < kSumWarps; ++w) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] += share[w][e][lane];
   }
-  finish<G, E>(dw + static_cast<size_t>(id) * a.D + c * E, sum, a.scale, a.accumulate);
+  finish<G, E>(at, sum, a, old);
 }
 
 // Elements of an access: the most that divide a row and fill sixteen bytes at the wider type.
@@ -365,11 +438,10 @@ int fwd(const EmbedArgs& a, const T* weight, T* out, int num_sms, const DevCtl& 
 template <typename T, typename G, int E>
 int sums(SumArgs p, const Scratch& s, const T* dy, G* dw, cudaStream_t st) {
   p.parts = (p.D / E + 31) / 32;
-  const long long units = static_cast<long long>(runs_of(p.N)) * p.parts;
-  const unsigned grid = static_cast<unsigned>((units + kSumWarps - 1) / kSumWarps);
+  const unsigned grid = static_cast<unsigned>(pieces_of(p.N)) * p.parts;
   embed_sum_kernel<T, G, E><<<grid, 32 * kSumWarps, 0, st>>>(p, s, dy, dw);
   if (cudaGetLastError() != cudaSuccess) return -1;
-  if (p.N <= kRun) return 1;
+  if (p.N <= kPiece) return 1;
   embed_join_kernel<G, E><<<grid, 32 * kSumWarps, 0, st>>>(p, s, dw);
   return cudaGetLastError() == cudaSuccess ? 2 : -1;
 }
@@ -398,7 +470,7 @@ int embed_fwd(const EmbedArgs& a, const void* weight, void* out, bool bf16, int 
 }
 
 size_t embed_bwd_workspace_bytes(int N, int, int D) {
-  return 256 + 2 * align256(static_cast<size_t>(N) * sizeof(uint2)) + static_cast<size_t>(runs_of(N)) * 2 * D * sizeof(float);
+  return 256 + 2 * align256(static_cast<size_t>(N) * sizeof(uint2)) + static_cast<size_t>(pieces_of(N)) * 2 * D * sizeof(float);
 }
 
 int embed_bwd(const EmbedArgs& a, const void* dy, void* dweight, bool accumulate, bool bf16, bool grad_bf16, void* workspace, int num_sms,
