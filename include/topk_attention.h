@@ -407,7 +407,7 @@ int topk_embedding_fwd(const void* ids, int id_bits, const void* weight, void* o
  *   dy         : [N, D] of `dtype`.  dweight: [rows, D] of grad_dtype (TOPK_F32 or TOPK_BF16).
  *   accumulate : 0: every row of dweight is written, zeros where no id points.  1: the sums are added to what dweight
  *                holds (tied weights, several batches), rounded once; rows without an id are left alone.
- *   Scratch: topk_embedding_bwd_workspace_bytes(): 16 bytes for each id and two rows of D floats for every 256 ids.
+ *   Scratch: topk_embedding_bwd_workspace_bytes(): 16 bytes for each id and two rows of D floats for every 128 ids.
  */
 int topk_embedding_bwd(const void* dy, const void* ids, int id_bits, void* dweight, int N, int rows, int D, float scale,
                        int accumulate, int dtype, int grad_dtype, void* stream);

@@ -96,6 +96,9 @@ constexpr int kSortBlocks = 8;  // of the cluster: the portable size
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;  // two digits for tables of up to 262,143 rows
 static_assert(kDigits == kSortThreads, "a digit for each thread");
 
+constexpr int kSmall = 1024;  // tokens that one block sorts by comparing them
+static_assert(kSmall <= 2 * kSortThreads, "two tokens a thread");
+
 struct Scratch {
   uint2* a;     // (id, token), sorted
   uint2* b;
@@ -103,7 +106,7 @@ struct Scratch {
   int* real;    // tokens with an id in the table
 };
 
-constexpr int kRun = 32, kSumWarps = 8, kPiece = kRun * kSumWarps;  // sorted tokens that a warp and a block add up
+constexpr int kRun = 16, kSumWarps = 8, kPiece = kRun * kSumWarps;  // sorted tokens that a warp and a block add up
 int pieces_of(int N) { return (N + kPiece - 1) / kPiece; }
 
 struct SortShared {
@@ -114,8 +117,9 @@ struct SortShared {
 };
 
 // One digit of the cluster's sort: tokens [n0, n1) of `from` (or the ids themselves) into `to`.
+// real: where the tokens with an id below `none` are counted, or null.
 template <typename Get>
-__device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, uint2* to, int n0, int n1, int shift) {
+__device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, uint2* to, int n0, int n1, int shift, unsigned none, int* real) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, blocks = cluster.num_blocks(), rank = cluster.block_rank();
   for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&sh.count[0][0])[i] = 0;
   __syncthreads();
@@ -128,6 +132,7 @@ __device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, 
     for (int k = 0; k < AHEAD; ++k)
       if (i0 + 32 * k + lane < w1) x[k] = get(i0 + 32 * k + lane);
   };
+  int counted = 0;
   for (int i0 = w0; i0 < w1; i0 += 32 * AHEAD) {
     fetch(i0);
 #pragma unroll
@@ -136,6 +141,7 @@ __device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, 
         const bool in = i0 + 32 * k + lane < w1;
         const unsigned digit = in ? x[k].x >> shift & (kDigits - 1) : kDigits;
         const unsigned same = __match_any_sync(0xffffffffu, digit);
+        if (real) counted += __popc(__ballot_sync(0xffffffffu, in && x[k].x < none));
         if (in && (same & ((1u << lane) - 1u)) == 0) sh.count[warp][digit] += __popc(same);  // the first of its kind
         __syncwarp();
       }
@@ -155,6 +161,7 @@ __device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, 
     sh.total[d] = sum;
   }
   cluster.sync();
+  if (real && lane == 0 && counted) atomicAdd(real, counted);
   // where a digit begins: all smaller digits' tokens, and the earlier blocks' of its own
   unsigned mine = 0, all = 0, got[kSortBlocks];
 #pragma unroll
@@ -200,7 +207,7 @@ __device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, 
 }
 
 // The first cluster sorts; the other blocks write zeros (into dw where it is to be written, [bytes16] of 16 bytes and a tail).
-__global__ void __launch_bounds__(kSortThreads)
+__global__ void __launch_bounds__(kSortThreads, 1)
     embed_sort_kernel(EmbedArgs a, Scratch s, int passes, int sorters, uint4* zero, long long bytes16, int tail_bytes, DevCtl ctl) {
   __shared__ SortShared sh;
   cg::cluster_group cluster = cg::this_cluster();
@@ -215,17 +222,36 @@ __global__ void __launch_bounds__(kSortThreads)
   const int each = (a.N + sorters - 1) / sorters, n0 = min(a.N, rank * each), n1 = min(a.N, n0 + each);
   const unsigned none = static_cast<unsigned>(a.rows);  // the id of tokens without one: behind all others
   if (rank == 0 && threadIdx.x == 0) *s.real = 0;
-  cluster.sync();
-  int real = 0;
-  bool wrong = false;
-  for (int i = n0 + threadIdx.x; i < n1; i += kSortThreads) {
+  const auto token = [&](int i) {
     const long long id = id_at(a.ids, a.ids64, i);
-    wrong |= id >= a.rows;
-    real += id >= 0 && id < a.rows;
+    if (id >= a.rows) atomicOr(ctl.error, kDevErrRange);
+    return make_uint2(id >= 0 && id < a.rows ? static_cast<unsigned>(id) : none, static_cast<unsigned>(i));
+  };
+  if (a.N <= kSmall) {
+    // a few tokens: one block sorts (id, token) as numbers in shared memory
+    unsigned long long* keys = reinterpret_cast<unsigned long long*>(&sh);
+    int pow2 = 2;
+    while (pow2 < a.N) pow2 *= 2;
+    int real = 0;
+    for (int i = threadIdx.x; i < pow2; i += kSortThreads) {
+      const uint2 t = i < a.N ? token(i) : make_uint2(~0u, ~0u);
+      keys[i] = static_cast<unsigned long long>(t.x) << 32 | t.y;
+      real += t.x < none;
+    }
+    real = __syncthreads_count(real & 1) + 2 * __syncthreads_count(real & 2);
+    for (int size = 2; size <= pow2; size *= 2)
+      for (int step = size / 2; step; step /= 2) {
+        for (int i = threadIdx.x; i < pow2 / 2; i += kSortThreads) {
+          const int lo = (i / step) * 2 * step + i % step, hi = lo + step;
+          const unsigned long long x = keys[lo], y = keys[hi];
+          if ((x > y) == ((lo & size) == 0)) keys[lo] = y, keys[hi] = x;
+        }
+        __syncthreads();
+      }
+    for (int i = threadIdx.x; i < a.N; i += kSortThreads) s.a[i] = make_uint2(static_cast<unsigned>(keys[i] >> 32), static_cast<unsigned>(keys[i]));
+    if (threadIdx.x == 0) *s.real = real;
+    return;
   }
-  if (wrong) atomicOr(ctl.error, kDevErrRange);
-  for (int o = 16; o; o /= 2) real += __shfl_xor_sync(0xffffffffu, real, o);
-  if (threadIdx.x % 32 == 0 && real) atomicAdd(s.real, real);
   uint2 *from = s.b, *to = s.a;
   if (passes % 2 == 0) {
     uint2* t = from;
@@ -233,15 +259,9 @@ __global__ void __launch_bounds__(kSortThreads)
   }
   for (int p = 0; p < passes; ++p) {
     if (p == 0)
-      sort_digit(
-          cluster, sh,
-          [&](int i) {
-            const long long id = id_at(a.ids, a.ids64, i);
-            return make_uint2(id >= 0 && id < a.rows ? static_cast<unsigned>(id) : none, static_cast<unsigned>(i));
-          },
-          to, n0, n1, 0);
+      sort_digit(cluster, sh, token, to, n0, n1, 0, none, s.real);
     else
-      sort_digit(cluster, sh, [&](int i) { return __ldcg(from + i); }, to, n0, n1, p * kDigitBits);
+      sort_digit(cluster, sh, [&](int i) { return __ldcg(from + i); }, to, n0, n1, p * kDigitBits, none, nullptr);
     uint2* t = from;
     from = to, to = t;
   }
@@ -251,15 +271,14 @@ __global__ void __launch_bounds__(kSortThreads)
 struct SumArgs {
   int N, rows, D, parts;  // parts: of a row's columns
   float scale;
-  bool accumulate;
 };
 
 // An id's finished sum of E columns, added to `old` where there is something.
-template <typename G, int E>
+template <typename G, int E, bool ACC>
 __device__ __forceinline__ void finish(G* at, const float (&sum)[E], const SumArgs& a, const Pack<G, E>& old) {
   Pack<G, E> now;
 #pragma unroll
-  for (int e = 0; e < E; ++e) now.set(e, a.accumulate ? fmaf(sum[e], a.scale, old.get(e)) : sum[e] * a.scale);
+  for (int e = 0; e < E; ++e) now.set(e, ACC ? fmaf(sum[e], a.scale, old.get(e)) : sum[e] * a.scale);
   *reinterpret_cast<typename Pack<G, E>::Raw*>(at) = now.raw;
 }
 template <typename G, int E>
@@ -268,7 +287,7 @@ __device__ __forceinline__ Pack<G, E> old_of(const G* at) {
 }
 
 // A block: a piece of eight runs, 32 E columns; a warp for each run.
-template <typename T, typename G, int E>
+template <typename T, typename G, int E, bool ACC>
 __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(SumArgs a, Scratch s, const T* __restrict__ dy, G* __restrict__ dw) {
   constexpr int FLIGHT = 8;
   // the sums of a run's first and last id, where the run's edges cut them (head alone where the run is all of one id)
@@ -279,6 +298,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(SumArgs a, Sc
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, piece = blockIdx.x / a.parts;
   const int c = (blockIdx.x % a.parts * 32 + lane) * E;
   const bool in = c < a.D;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int real = *s.real, i0 = piece * kPiece + warp * kRun, n = min(kRun, real - i0);
   if (piece * kPiece >= real) return;
   if (n > 0) {
@@ -296,7 +316,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(SumArgs a, Sc
         const unsigned next = __shfl_sync(0xffffffffu, mine.x, (k0 + k + 1) & 31);
         if (k0 + k >= n || !in) continue;
         x[k] = load_pack<T, E>(dy + static_cast<size_t>(token) * a.D + c);
-        if (a.accumulate && (k0 + k + 1 == n || next != id)) old[k] = old_of<G, E>(dw + static_cast<size_t>(id) * a.D + c);
+        if (ACC && (k0 + k + 1 == n || next != id)) old[k] = old_of<G, E>(dw + static_cast<size_t>(id) * a.D + c);
       }
 #pragma unroll
       for (int k = 0; k < FLIGHT; ++k) {
@@ -318,7 +338,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(SumArgs a, Sc
           flags |= (front ? kFront : 0) | (back ? kBack : 0);
           if (back && lane == 0) tail_id[warp] = id;
         } else if (in) {
-          finish<G, E>(dw + static_cast<size_t>(id) * a.D + c, sum, a, old[k]);
+          finish<G, E, ACC>(dw + static_cast<size_t>(id) * a.D + c, sum, a, old[k]);
         }
         if (first && last) flags |= kOne;
         first = false;
@@ -357,19 +377,20 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(SumArgs a, Sc
     } else {
       G* at = dw + static_cast<size_t>(tail_id[warp]) * a.D + c;
       Pack<G, E> old;
-      if (a.accumulate) old = old_of<G, E>(at);
-      finish<G, E>(at, sum, a, old);
+      if (ACC) old = old_of<G, E>(at);
+      finish<G, E, ACC>(at, sum, a, old);
     }
   }
 }
 
 // A block for each piece whose last id goes on in the next one and begins in it: it adds up that id's parts, eight shares of them by
 // its warps, and the shares in order.
-template <typename G, int E>
+template <typename G, int E, bool ACC>
 __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(SumArgs a, Scratch s, G* __restrict__ dw) {
   __shared__ float share[kSumWarps][E][32];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, piece = blockIdx.x / a.parts;
   const int c = (blockIdx.x % a.parts * 32 + lane) * E;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int real = *s.real, i0 = piece * kPiece, next = i0 + kPiece;
   if (next >= real) return;
   const unsigned id = __ldg(&s.a[next - 1].x);
@@ -400,12 +421,12 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(SumArgs a, S
   if (warp != 0 || !in) return;
   G* at = dw + static_cast<size_t>(id) * a.D + c;
   Pack<G, E> old;
-  if (a.accumulate) old = old_of<G, E>(at);
+  if (ACC) old = old_of<G, E>(at);
   for (int w = 1; w < kSumWarps; ++w) {
 #pragma unroll
     for (int e = 0; e < E; ++e) sum[e] += share[w][e][lane];
   }
-  finish<G, E>(at, sum, a, old);
+  finish<G, E, ACC>(at, sum, a, old);
 }
 
 // Elements of an access: the most that divide a row and fill sixteen bytes at the wider type.
@@ -435,29 +456,43 @@ int fwd(const EmbedArgs& a, const T* weight, T* out, int num_sms, const DevCtl& 
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 
-template <typename T, typename G, int E>
+// Launches a kernel whose blocks may begin while the one before ends (they wait for its memory themselves).
+template <typename Kernel, typename... Args>
+bool launch_early(Kernel kernel, unsigned grid, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3(grid), config.blockDim = dim3(32 * kSumWarps), config.stream = st;
+  cudaLaunchAttribute early = {};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  config.attrs = &early, config.numAttrs = 1;
+  return cudaLaunchKernelEx(&config, kernel, args...) == cudaSuccess;
+}
+
+template <typename T, typename G, int E, bool ACC>
 int sums(SumArgs p, const Scratch& s, const T* dy, G* dw, cudaStream_t st) {
   p.parts = (p.D / E + 31) / 32;
   const unsigned grid = static_cast<unsigned>(pieces_of(p.N)) * p.parts;
-  embed_sum_kernel<T, G, E><<<grid, 32 * kSumWarps, 0, st>>>(p, s, dy, dw);
-  if (cudaGetLastError() != cudaSuccess) return -1;
+  if (!launch_early(embed_sum_kernel<T, G, E, ACC>, grid, st, p, s, dy, dw)) return -1;
   if (p.N <= kPiece) return 1;
-  embed_join_kernel<G, E><<<grid, 32 * kSumWarps, 0, st>>>(p, s, dw);
-  return cudaGetLastError() == cudaSuccess ? 2 : -1;
+  return launch_early(embed_join_kernel<G, E, ACC>, grid, st, p, s, dw) ? 2 : -1;
 }
 
 template <typename T, typename G>
-int sums_of(const SumArgs& p, const Scratch& s, const void* dy, void* dw, cudaStream_t st) {
+int sums_of(const SumArgs& p, const Scratch& s, const void* dy, void* dw, bool accumulate, cudaStream_t st) {
   const T* x = static_cast<const T*>(dy);
   G* y = static_cast<G*>(dw);
-  switch (pack_of(p.D, sizeof(T) > sizeof(G) ? sizeof(T) : sizeof(G))) {
-    case 8:
-      if constexpr (sizeof(T) == 2 && sizeof(G) == 2) return sums<T, G, 8>(p, s, x, y, st);
-      return -1;
-    case 4: return sums<T, G, 4>(p, s, x, y, st);
-    case 2: return sums<T, G, 2>(p, s, x, y, st);
-    default: return sums<T, G, 1>(p, s, x, y, st);
-  }
+  const auto of = [&](auto acc) {
+    constexpr bool ACC = decltype(acc)::value;
+    switch (pack_of(p.D, sizeof(T) > sizeof(G) ? sizeof(T) : sizeof(G))) {
+      case 8:
+        if constexpr (sizeof(T) == 2 && sizeof(G) == 2) return sums<T, G, 8, ACC>(p, s, x, y, st);
+        return -1;
+      case 4: return sums<T, G, 4, ACC>(p, s, x, y, st);
+      case 2: return sums<T, G, 2, ACC>(p, s, x, y, st);
+      default: return sums<T, G, 1, ACC>(p, s, x, y, st);
+    }
+  };
+  return accumulate ? of(std::true_type{}) : of(std::false_type{});
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -498,9 +533,9 @@ int embed_bwd(const EmbedArgs& a, const void* dy, void* dweight, bool accumulate
   if (cudaLaunchKernelEx(&config, embed_sort_kernel, a, s, passes, sorters, static_cast<uint4*>(dweight), bytes / 16, static_cast<int>(bytes % 16), ctl) !=
       cudaSuccess)
     return -1;
-  const SumArgs p{a.N, a.rows, a.D, 1, a.scale, accumulate};
-  const int n = bf16 ? (grad_bf16 ? sums_of<__nv_bfloat16, __nv_bfloat16>(p, s, dy, dweight, st) : sums_of<__nv_bfloat16, float>(p, s, dy, dweight, st))
-                     : (grad_bf16 ? sums_of<float, __nv_bfloat16>(p, s, dy, dweight, st) : sums_of<float, float>(p, s, dy, dweight, st));
+  const SumArgs p{a.N, a.rows, a.D, 1, a.scale};
+  const int n = bf16 ? (grad_bf16 ? sums_of<__nv_bfloat16, __nv_bfloat16>(p, s, dy, dweight, accumulate, st) : sums_of<__nv_bfloat16, float>(p, s, dy, dweight, accumulate, st))
+                     : (grad_bf16 ? sums_of<float, __nv_bfloat16>(p, s, dy, dweight, accumulate, st) : sums_of<float, float>(p, s, dy, dweight, accumulate, st));
   return n < 0 ? -1 : 1 + n;
 }
 
