@@ -17,6 +17,8 @@
 // such parts for each CTA, and grouped_join_kernel joins the parts of a unit in order.
 #include <cuda_bf16.h>
 
+#include <atomic>
+
 #include "kernels.h"
 #include "pairs.cuh"
 
@@ -916,7 +918,13 @@ template <int D, bool TREE>
 int launch(const CUtensorMap& tmq, const CUtensorMap& tmk, const CUtensorMap& tmv, const Work& w, int grid, const DevCtl& ctl, cudaStream_t st) {
   using L = Layout<D, TREE>;
   const auto kernel = grouped_kernel<D, TREE>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::BYTES)) != cudaSuccess) return -1;
+  int device = 0;
+  static std::atomic<unsigned long long> ready{0};  // a bit for each device whose kernel may take the shared memory
+  if (cudaGetDevice(&device) != cudaSuccess) return -1;
+  if (device > 63 || !(ready.load(std::memory_order_acquire) >> device & 1ull)) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::BYTES)) != cudaSuccess) return -1;
+    if (device <= 63) ready.fetch_or(1ull << device, std::memory_order_release);
+  }
   kernel<<<grid, kThreads, L::BYTES, st>>>(tmq, tmk, tmv, w, ctl);
   if (cudaGetLastError() != cudaSuccess) return -1;
   if (grid == 1) return 1;

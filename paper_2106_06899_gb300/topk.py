@@ -548,19 +548,23 @@ def _whole(name, t, shape) -> int:
     return 32 if t.dtype == torch.int32 else 64
 
 
-def topk_embedding_fwd(ids, weight, out, scale: float = 1.0, stream=None) -> None:
-    """out [*ids.shape, D] = scale weight[ids]: ids int32 or int64 (a negative one is padding and gives zeros), weight
-    [rows, D] and out fp32 or bf16."""
+def _embedding_args(ids, weight):
+    """(tokens, bits of an id, rows, D, dtype code) of a lookup."""
     if weight.dim() != 2 or not weight.is_contiguous():
         raise ValueError("weight must be a contiguous [rows, D] tensor")
     rows, D = weight.shape
     N = ids.numel()
     _fits(N, rows, D)
-    bits = _whole("ids", ids, ids.shape)
+    return N, _whole("ids", ids, ids.shape), rows, D, _dtype_code(weight)
+
+
+def topk_embedding_fwd(ids, weight, out, scale: float = 1.0, stream=None) -> None:
+    """out [*ids.shape, D] = scale weight[ids]: ids int32 or int64 (a negative one is padding and gives zeros), weight
+    [rows, D] and out fp32 or bf16."""
+    N, bits, rows, D, code = _embedding_args(ids, weight)
     _written("out", out, (*ids.shape, D), weight.dtype)
-    code = _dtype_code(weight)
     _on_gpu("ids, weight and out", weight, ids, out)
-    rc = lib().topk_embedding_fwd(_ptr(ids), bits, _ptr(weight), _ptr(out), N, rows, D, scale, code, _stream(stream))
+    rc = lib().topk_embedding_fwd(ids.data_ptr(), bits, weight.data_ptr(), out.data_ptr(), N, rows, D, scale, code, _stream(stream))
     _check(rc, "topk_embedding_fwd")
     _changed(out)
 
@@ -599,18 +603,22 @@ def _rows_of(name, t):
     return N, V, stride
 
 
+def _logprobs_args(logits, targets):
+    """(N, V, row stride, bits of a target, dtype code)."""
+    N, V, stride = _rows_of("logits", logits)
+    return N, V, stride, 32 if targets is None else _whole("targets", targets, (N,)), _dtype_code(logits)
+
+
 def topk_token_logprobs_fwd(logits, targets=None, logp=None, entropy=None, lse=None, top_logp=None, top_ids=None, scale: float = 1.0,
                             stream=None) -> None:
     """Of each row of logits [N, V] (fp32 or bf16; rows may be strided) times scale: logp [N] of the targets ([N], int32 or int64,
     negative: none), entropy [N], lse [N], and the largest tokens' top_logp and top_ids (int32) [N, top]; None where not wanted."""
-    N, V, stride = _rows_of("logits", logits)
+    N, V, stride, bits, code = _logprobs_args(logits, targets)
     top = 0 if top_ids is None else top_ids.shape[1]
-    bits = 32 if targets is None else _whole("targets", targets, (N,))
     for name, t in (("logp", logp), ("entropy", entropy), ("lse", lse)):
         _written(name, t, (N,), torch.float32)
     _written("top_logp", top_logp, (N, top), torch.float32)
     _written("top_ids", top_ids, (N, top), torch.int32)
-    code = _dtype_code(logits)
     _on_gpu("logits, targets and outputs", logits, targets, logp, entropy, lse, top_logp, top_ids)
     rc = lib().topk_token_logprobs_fwd(_ptr(logits), stride, _ptr(targets), bits, scale, top, _ptr(logp), _ptr(entropy), _ptr(lse),
                                        _ptr(top_logp), _ptr(top_ids), N, V, code, _stream(stream))
@@ -648,9 +656,11 @@ def _heads_bf16(dims, **tensors) -> None:
     for name, t in tensors.items():
         if t.dtype != torch.bfloat16:
             raise TypeError(f"{name} must be bfloat16")
-        if t.dim() != dims or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        shape = t.shape
+        if len(shape) != dims or (t.stride(-1) != 1 and shape[-1] > 1):
             raise ValueError(f"{name} must be a {dims}-dimensional tensor with contiguous rows")
-        _fits(*t.shape)
+        if max(shape) >= 1 << 31:
+            _fits(*shape)
 
 
 def _starts(name, t) -> None:
@@ -663,9 +673,8 @@ def topk_prompt_attn_fwd(q, k, v, out, q_starts, k_starts=None, causal: bool = T
     rows q_starts[b] to q_starts[b + 1] - 1 ([B + 1] int32), its keys by k_starts likewise (None: q_starts); out [Tq,Hq,d], whose
     rows of no sequence are left alone, or zeros with clear_rest."""
     _heads_bf16(3, q=q, k=k, v=v)
-    Tq, Hq, d = q.shape
-    Tk, Hkv = k.shape[:2]
-    if k.shape[2] != d or v.shape != k.shape:
+    (Tq, Hq, d), (Tk, Hkv, dk) = q.shape, k.shape
+    if dk != d or v.shape != k.shape:
         raise ValueError("shape mismatch between q, k, v")
     _written("out", out, (Tq, Hq, d), torch.bfloat16)
     _starts("q_starts", q_starts)
@@ -861,9 +870,13 @@ def linear_bwd(dy, x, w, preact=None, act: str = "none", bias: bool = False, nee
 
 def embedding(ids, weight, scale: float = 1.0, stream=None):
     """scale weight[ids], [*ids.shape, D]; a negative id is padding: zeros."""
-    (out,) = _allocate(stream, lambda: (weight.new_empty((*ids.shape, weight.shape[-1])),))
-    if ids.numel():
-        topk_embedding_fwd(ids, weight, out, scale, stream)
+    # a few tokens take 2 us on the GPU: what was made here is not checked again
+    N, bits, rows, D, code = _embedding_args(ids, weight)
+    _on_gpu("ids and weight", weight, ids)
+    (out,) = _allocate(stream, lambda: (torch.empty((*ids.shape, D), dtype=weight.dtype, device=weight.device),))
+    if N:
+        rc = lib().topk_embedding_fwd(ids.data_ptr(), bits, weight.data_ptr(), out.data_ptr(), N, rows, D, scale, code, _stream(stream))
+        _check(rc, "topk_embedding_fwd")
     return out
 
 
@@ -895,15 +908,22 @@ class TokenLogProbs(NamedTuple):
 def token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, stream=None) -> TokenLogProbs:
     """Log probabilities, in fp32, under softmax(scale logits) for logits [N, V]: of the targets ([N]; negative: none, 0), the
     entropy, the log of the sum, and the `top` likeliest tokens (ties to the lower id; a masked token, -inf, is none: id -1)."""
-    N = logits.shape[0]
-    ids, best, sums = _allocate(stream, lambda: (
-        torch.empty(N, top, dtype=torch.int32, device=logits.device) if top else None,
-        torch.empty(N, top, dtype=torch.float32, device=logits.device) if top else None,
-        torch.empty(2 if targets is None else 3, N, dtype=torch.float32, device=logits.device)))
-    entropy, lse, logp = (*sums, None)[:3]
-    if N:
-        topk_token_logprobs_fwd(logits, targets, logp, entropy, lse, best, ids, scale, stream)
-    return TokenLogProbs(logp, entropy, lse, best, ids)
+    N, V, stride, bits, code = _logprobs_args(logits, targets)
+    _on_gpu("logits and targets", logits, targets)
+    device = logits.device
+
+    def outputs():
+        f32 = torch.float32
+        return (None if targets is None else torch.empty(N, dtype=f32, device=device), torch.empty(N, dtype=f32, device=device),
+                torch.empty(N, dtype=f32, device=device), torch.empty((N, top), dtype=f32, device=device) if top else None,
+                torch.empty((N, top), dtype=torch.int32, device=device) if top else None)
+
+    out = logp, entropy, lse, best, ids = _allocate(stream, outputs)
+    if N:  # what was made here is not checked again
+        rc = lib().topk_token_logprobs_fwd(logits.data_ptr(), stride, _ptr(targets), bits, scale, top, _ptr(logp), entropy.data_ptr(),
+                                           lse.data_ptr(), _ptr(best), _ptr(ids), N, V, code, _stream(stream))
+        _check(rc, "topk_token_logprobs_fwd")
+    return TokenLogProbs(*out)
 
 
 def token_logprobs_bwd(logits, lse, targets=None, dlogp=None, entropy=None, dentropy=None, top_ids=None, dtop=None, scale: float = 1.0,
