@@ -12,7 +12,10 @@ they are the model around the method, not part of it.  The temperature of Eq. 1 
 With fused=True (bf16) those, but for the LayerNorms, are the library's operators too: the projections with
 their activation and residual (topk_linear_fwd / _bwd), and between the q/k/v projection and the attention
 the norms of queries and keys with a rotation by position (topk_qk_norm_rope_fwd / _bwd).  The fused
-decoder also generates, a token a step, against key/value caches (Decoder.step).
+decoder also generates, a token a step, against key/value caches (Decoder.step), after it has read packed prompts into
+them (Decoder.prefill), or several drafted tokens a step (Decoder.step_tree).  With vocab=V it works on token ids: an
+embedding before the first layer (topk_embedding_fwd / _bwd), the same weights behind the last norm, and
+log probabilities with their gradient (topk_token_logprobs_fwd / _bwd).
 
 The library's gradients have no gradients of their own: a second differentiation through one of these functions is
 an error.
@@ -143,6 +146,45 @@ class QKNormRopeFunction(torch.autograd.Function):
         return dqkv, dqw.to(q_weight.dtype), dkw.to(k_weight.dtype), None, None
 
 
+class EmbeddingFunction(torch.autograd.Function):
+    """scale weight[ids]; ids below 0 are padding."""
+
+    @staticmethod
+    def forward(ctx, ids, weight, scale: float):
+        ctx.save_for_backward(ids)
+        ctx.rows, ctx.dtype, ctx.scale = weight.shape[0], weight.dtype, scale
+        return T.embedding(ids, weight, scale=scale)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        (ids,) = ctx.saved_tensors
+        return None, T.embedding_bwd(dy.contiguous(), ids, ctx.rows, scale=ctx.scale, grad_dtype=ctx.dtype), None
+
+
+class TokenLogProbsFunction(torch.autograd.Function):
+    """T.token_logprobs of logits [N, V]; logp, entropy and top_logp have gradients, lse and top_ids none."""
+
+    @staticmethod
+    def forward(ctx, logits, targets, top: int, scale: float):
+        r = T.token_logprobs(logits, targets, top=top, scale=scale)
+        ctx.save_for_backward(logits, targets, r.lse, r.entropy, r.top_ids)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(*(t for t in (r.lse, r.top_ids) if t is not None))
+        return tuple(r)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dlogp, dentropy, _lse, dtop, _ids):
+        logits, targets, lse, entropy, ids = ctx.saved_tensors
+        if dlogp is None and dentropy is None and dtop is None:
+            return None, None, None, None
+        dlogp, dentropy, dtop = (None if g is None else g.contiguous() for g in (dlogp, dentropy, dtop))
+        return T.token_logprobs_bwd(logits, lse, targets=targets, dlogp=dlogp, entropy=entropy, dentropy=dentropy, top_ids=ids, dtop=dtop,
+                                    scale=ctx.scale), None, None, None
+
+
 class DecoderLayer(torch.nn.Module):
     def __init__(self, d_model: int, heads: int, d_ff: int, topk: int | None, ffn_topk: int | None,
                  dtype=torch.bfloat16, device="cuda", fused: bool = False):
@@ -192,20 +234,47 @@ class DecoderLayer(torch.nn.Module):
             a = RotaryAttentionFunction.apply(qkv, self.q_norm, self.k_norm, *tables, min(self.topk, L))
         return self._fused_tail(a.transpose(1, 2).reshape(B * L, D), x).view(B, L, D)
 
+    def _cached(self, x, cache, start, positions, tables):
+        """Queries [B, H, T, d] of x [B, T, D], whose keys and values go into the caches at rows start[b] on."""
+        B, T_, D = x.shape
+        qkv = T.linear(self.ln1(x).view(B * T_, D), self.qkv.weight).view(B, T_, 3 * self.h, self.dh)
+        return T.qk_norm_rope(qkv[:, :, :self.h], qkv[:, :, self.h:2 * self.h], qkv[:, :, 2 * self.h:], *tables, cache=cache, cache_start=start,
+                              positions=positions, q_weight=self.q_norm, k_weight=self.k_norm, q_scale=self.dh ** -0.5)[0]
+
     def step(self, x, cache, start, positions, tables):
         """One token for each of B sequences, x [B, D]: keys and values go into the caches [B, H, cap, d] at rows
         start [B], and attention reads the rows up to them."""
         B, D = x.shape
         keys, values = cache
-        qkv = T.linear(self.ln1(x), self.qkv.weight).view(B, 1, 3 * self.h, self.dh)
-        q, _, _ = T.qk_norm_rope(qkv[:, :, :self.h], qkv[:, :, self.h:2 * self.h], qkv[:, :, 2 * self.h:], *tables, cache=cache,
-                                 cache_start=start, positions=positions, q_weight=self.q_norm, k_weight=self.k_norm,
-                                 q_scale=self.dh ** -0.5)
+        q = self._cached(x.view(B, 1, D), cache, start, positions, tables)
         if self.topk is None:
             a = T.vanilla_attention(q, keys, values, kv_len=start + 1)
         else:
             a = T.attention(q, keys, values, min(self.topk, keys.shape[2]), kv_len=start + 1)
         return self._fused_tail(a.view(B, D), x)
+
+    def step_tree(self, x, cache, start, positions, tables, tree, mask):
+        """T drafted tokens of each of B sequences, x [B, T, D], behind the start[b] rows that the caches hold.  They read by tree,
+        or, with top-k attention, by mask [B, 1, T, cap]."""
+        B, T_, D = x.shape
+        q = self._cached(x, cache, start, positions, tables)
+        if self.topk is None:
+            a = T.tree_attention(q, *cache, start, tree=tree)
+        else:
+            a = T.attention(q, *cache, min(self.topk, mask.shape[3]), mask=mask)
+        return self._fused_tail(a.transpose(1, 2).reshape(B * T_, D), x.view(B * T_, D)).view(B, T_, D)
+
+    def prefill(self, x, cache, starts, token, positions, rows, tables):
+        """Packed prompts x [T, D] with plain attention; the keys and values of tokens token [T] go to rows positions of the caches of
+        sequences rows."""
+        n, D = x.shape
+        qkv = T.linear(self.ln1(x), self.qkv.weight).view(1, n, 3 * self.h, self.dh)
+        q, k, v = (t[0].transpose(0, 1) for t in T.qk_norm_rope(
+            qkv[:, :, :self.h], qkv[:, :, self.h:2 * self.h], qkv[:, :, 2 * self.h:], *tables, positions=positions.view(1, 1, n),
+            q_weight=self.q_norm, k_weight=self.k_norm, q_scale=self.dh ** -0.5))
+        for c, t in zip(cache, (k, v)):
+            c[rows, :, positions[token]] = t[token]
+        return self._fused_tail(T.prompt_attention(q, k, v, starts).view(n, D), x)
 
     def forward(self, x):
         B, L, D = x.shape
@@ -221,17 +290,23 @@ class DecoderLayer(torch.nn.Module):
 class Decoder(torch.nn.Module):
     """n_layers decoder layers over d_model features; topk / ffn_topk None selects the plain
     attention / the dense FF layer.  fused: the library's linear layers, and queries and keys normalised and
-    rotated by their positions, of which there are max_positions."""
+    rotated by their positions, of which there are max_positions.  vocab (fused; a multiple of 8): token ids in the place of
+    features, by an embedding that is also the output projection; ids below 0 are padding."""
 
     def __init__(self, n_layers=12, d_model=768, heads=12, d_ff=3072, topk: int | None = 64,
                  ffn_topk: int | None = None, dtype=torch.bfloat16, device="cuda", fused: bool = False,
-                 max_positions: int = 65536):
+                 max_positions: int = 65536, vocab: int | None = None):
         super().__init__()
+        if vocab is not None and (not fused or vocab % 8):
+            raise ValueError("a vocabulary needs a fused decoder and a multiple of 8")
         self.layers = torch.nn.ModuleList(
             DecoderLayer(d_model, heads, d_ff, topk, ffn_topk, dtype, device, fused) for _ in range(n_layers))
         self.norm = torch.nn.LayerNorm(d_model, dtype=dtype, device=device)
         self.fused = fused
         self.tables = T.rope_tables(max_positions, d_model // heads, device=device) if fused else None
+        self.vocab = vocab
+        if vocab is not None:
+            self.embedding = torch.nn.Parameter(torch.randn(vocab, d_model, dtype=dtype, device=device) * d_model ** -0.5)
 
     def _apply(self, fn, recurse=True):
         super()._apply(fn, recurse)
@@ -242,10 +317,31 @@ class Decoder(torch.nn.Module):
             self.tables = T.rope_tables(rows, 2 * half, device=device)
         return self
 
+    def _features(self, x):
+        """Features of token ids (int32 or int64, any shape), or x as it is."""
+        if self.vocab is None or x.is_floating_point():
+            return x
+        x, scale = x.contiguous(), self.embedding.shape[1] ** 0.5
+        if torch.is_grad_enabled() and self.embedding.requires_grad:
+            return EmbeddingFunction.apply(x, self.embedding, scale)
+        return T.embedding(x, self.embedding, scale=scale)
+
     def forward(self, x):
+        x = self._features(x)
         for layer in self.layers:
             x = layer.forward_fused(x, self.tables) if self.fused else layer(x)
         return self.norm(x)
+
+    def logprobs(self, features, targets=None, top: int = 0, scale: float = 1.0) -> T.TokenLogProbs:
+        """What features [.., d_model] (of forward, step, ..) say of the next tokens: T.token_logprobs of their logits, one row for
+        each of them, with targets [..] or None.  Differentiable where gradients are on."""
+        if self.vocab is None:
+            raise ValueError("logprobs() needs a vocabulary")
+        logits = linear(features.reshape(-1, features.shape[-1]), self.embedding)
+        targets = None if targets is None else targets.reshape(-1)
+        if torch.is_grad_enabled() and logits.requires_grad:
+            return T.TokenLogProbs(*TokenLogProbsFunction.apply(logits, targets, top, scale))
+        return T.token_logprobs(logits, targets, top=top, scale=scale)
 
     def new_cache(self, batch: int, capacity: int):
         """Key/value caches of every layer, [batch, heads, capacity, d] each, for step()."""
@@ -255,11 +351,64 @@ class Decoder(torch.nn.Module):
 
     @torch.no_grad()
     def step(self, x, caches, start):
-        """The next token of each of B sequences (fused only): x [B, d_model] at positions start [B] (int32), the
+        """The next token of each of B sequences (fused only): x [B, d_model] (or ids [B]) at positions start [B] (int32), the
         caches (new_cache) holding the tokens before; returns [B, d_model] and leaves the token in the caches."""
         if not self.fused:
             raise ValueError("step() needs a fused decoder")
+        x = self._features(x)
         positions = start.view(1, -1, 1)
         for layer, cache in zip(self.layers, caches):
             x = layer.step(x, cache, start, positions, self.tables)
         return self.norm(x)
+
+    @torch.no_grad()
+    def prefill(self, x, starts, caches):
+        """Reads packed prompts (fused, plain attention) into empty caches: x [T, d_model] (or ids [T]), sequence b's in rows
+        starts[b] to starts[b + 1] - 1 ([B + 1] int32, from 0 to T); returns [T, d_model]."""
+        if not self.fused or any(layer.topk is not None for layer in self.layers):
+            raise ValueError("prefill() needs a fused decoder with plain attention (topk=None)")
+        x = self._features(x)
+        n, cap, ends = x.shape[0], caches[0][0].shape[2], starts.long()
+        if n > cap and int((ends[1:] - ends[:-1]).max()) > cap:  # the host waits for the lengths only where they could be too long
+            raise ValueError("the caches have no room for the longest prompt")
+        # rows of no sequence write what the nearest token of one does
+        token = torch.minimum(torch.maximum(torch.arange(n, device=x.device), ends[0]), (ends[-1] - 1).clamp_min(0)).clamp(0, n - 1)
+        rows = torch.searchsorted(ends[1:], token, right=True).clamp_max(ends.shape[0] - 2)
+        at = (token - ends[rows]).clamp(0, cap - 1)
+        positions = torch.zeros(n, dtype=torch.int64, device=x.device).index_put_((token,), at)
+        for layer, cache in zip(self.layers, caches):
+            x = layer.prefill(x, cache, starts, token, positions.int(), rows, self.tables)
+        return self.norm(x)
+
+    @torch.no_grad()
+    def step_tree(self, x, caches, start, tree=None):
+        """T drafted tokens of each of B sequences at once (fused only): x [B, T, d_model] (or ids [B, T]) behind the start [B]
+        (int32) tokens that the caches hold.  tree [B, T] (T.tree_mask): which drafted tokens each one reads, its ancestors and itself;
+        None: a chain.  Returns [B, T, d_model] and leaves the tokens in rows start[b] on; keep() makes a path of them the sequence's."""
+        if not self.fused:
+            raise ValueError("step_tree() needs a fused decoder")
+        x = self._features(x)
+        B, n, _ = x.shape
+        i = torch.arange(n, device=x.device)
+        reads = (i <= i[:, None]).expand(B, n, n) if tree is None else (tree.expand(B, n)[..., None] >> i & 1).bool()
+        positions = (start[:, None] + reads.sum(-1) - 1).int()[None].contiguous()
+        mask = None
+        if any(layer.topk is not None for layer in self.layers):
+            j = torch.arange(caches[0][0].shape[2], device=x.device) - start[:, None].long()  # from the first drafted row on
+            drafted = reads.gather(2, j.clamp(0, n - 1)[:, None].expand(B, n, j.shape[1])) & ((j >= 0) & (j < n))[:, None]
+            mask = ((j < 0)[:, None] | drafted)[:, None]
+        for layer, cache in zip(self.layers, caches):
+            x = layer.step_tree(x, cache, start, positions, self.tables, tree, mask)
+        return self.norm(x)
+
+    @torch.no_grad()
+    def keep(self, caches, start, path):
+        """Moves the drafted tokens path [B, n] (indices into step_tree's, a token and its descendants in order) to rows start[b] to
+        start[b] + n - 1 of the caches; an index that repeats fills up a shorter path.  Rows outside the caches are cut to them."""
+        B, n = path.shape
+        b = torch.arange(B, device=path.device)[:, None]
+        last = caches[0][0].shape[2] - 1
+        to, of = ((start.long()[:, None] + i).clamp(0, last) for i in (torch.arange(n, device=path.device), path.long()))
+        for cache in caches:
+            for c in cache:
+                c[b, :, to] = c[b, :, of]
