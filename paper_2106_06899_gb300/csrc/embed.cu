@@ -15,6 +15,7 @@
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "kernels.h"
@@ -92,18 +93,16 @@ __global__ void __launch_bounds__(kFwdThreads) embed_fwd_kernel(EmbedArgs a, con
 
 // ------------------------------------------------------------ sorting the tokens
 constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
-constexpr int kSortBlocks = 8;  // of the cluster: the portable size
+constexpr int kSortBlocks = 16;  // of the cluster at most
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;  // two digits for tables of up to 262,143 rows
 static_assert(kDigits == kSortThreads, "a digit for each thread");
 
 constexpr int kSmall = 1024;  // tokens that one block sorts by comparing them
-static_assert(kSmall <= 2 * kSortThreads, "two tokens a thread");
 
 struct Scratch {
-  uint2* a;     // (id, token), sorted
+  uint2* a;     // (id, token), sorted; tokens without an id in the table have that of the row behind it
   uint2* b;
   float* parts; // [pieces][2][D]
-  int* real;    // tokens with an id in the table
 };
 
 constexpr int kRun = 16, kSumWarps = 8, kPiece = kRun * kSumWarps;  // sorted tokens that a warp and a block add up
@@ -117,9 +116,8 @@ struct SortShared {
 };
 
 // One digit of the cluster's sort: tokens [n0, n1) of `from` (or the ids themselves) into `to`.
-// real: where the tokens with an id below `none` are counted, or null.
 template <typename Get>
-__device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, uint2* to, int n0, int n1, int shift, unsigned none, int* real) {
+__device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, uint2* to, int n0, int n1, int shift) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, blocks = cluster.num_blocks(), rank = cluster.block_rank();
   for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&sh.count[0][0])[i] = 0;
   __syncthreads();
@@ -132,7 +130,6 @@ __device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, 
     for (int k = 0; k < AHEAD; ++k)
       if (i0 + 32 * k + lane < w1) x[k] = get(i0 + 32 * k + lane);
   };
-  int counted = 0;
   for (int i0 = w0; i0 < w1; i0 += 32 * AHEAD) {
     fetch(i0);
 #pragma unroll
@@ -141,7 +138,6 @@ __device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, 
         const bool in = i0 + 32 * k + lane < w1;
         const unsigned digit = in ? x[k].x >> shift & (kDigits - 1) : kDigits;
         const unsigned same = __match_any_sync(0xffffffffu, digit);
-        if (real) counted += __popc(__ballot_sync(0xffffffffu, in && x[k].x < none));
         if (in && (same & ((1u << lane) - 1u)) == 0) sh.count[warp][digit] += __popc(same);  // the first of its kind
         __syncwarp();
       }
@@ -161,7 +157,6 @@ __device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, 
     sh.total[d] = sum;
   }
   cluster.sync();
-  if (real && lane == 0 && counted) atomicAdd(real, counted);
   // where a digit begins: all smaller digits' tokens, and the earlier blocks' of its own
   unsigned mine = 0, all = 0, got[kSortBlocks];
 #pragma unroll
@@ -221,7 +216,6 @@ __global__ void __launch_bounds__(kSortThreads, 1)
   const int rank = blockIdx.x;
   const int each = (a.N + sorters - 1) / sorters, n0 = min(a.N, rank * each), n1 = min(a.N, n0 + each);
   const unsigned none = static_cast<unsigned>(a.rows);  // the id of tokens without one: behind all others
-  if (rank == 0 && threadIdx.x == 0) *s.real = 0;
   const auto token = [&](int i) {
     const long long id = id_at(a.ids, a.ids64, i);
     if (id >= a.rows) atomicOr(ctl.error, kDevErrRange);
@@ -232,13 +226,11 @@ __global__ void __launch_bounds__(kSortThreads, 1)
     unsigned long long* keys = reinterpret_cast<unsigned long long*>(&sh);
     int pow2 = 2;
     while (pow2 < a.N) pow2 *= 2;
-    int real = 0;
     for (int i = threadIdx.x; i < pow2; i += kSortThreads) {
       const uint2 t = i < a.N ? token(i) : make_uint2(~0u, ~0u);
       keys[i] = static_cast<unsigned long long>(t.x) << 32 | t.y;
-      real += t.x < none;
     }
-    real = __syncthreads_count(real & 1) + 2 * __syncthreads_count(real & 2);
+    __syncthreads();
     for (int size = 2; size <= pow2; size *= 2)
       for (int step = size / 2; step; step /= 2) {
         for (int i = threadIdx.x; i < pow2 / 2; i += kSortThreads) {
@@ -249,7 +241,6 @@ __global__ void __launch_bounds__(kSortThreads, 1)
         __syncthreads();
       }
     for (int i = threadIdx.x; i < a.N; i += kSortThreads) s.a[i] = make_uint2(static_cast<unsigned>(keys[i] >> 32), static_cast<unsigned>(keys[i]));
-    if (threadIdx.x == 0) *s.real = real;
     return;
   }
   uint2 *from = s.b, *to = s.a;
@@ -259,9 +250,9 @@ __global__ void __launch_bounds__(kSortThreads, 1)
   }
   for (int p = 0; p < passes; ++p) {
     if (p == 0)
-      sort_digit(cluster, sh, token, to, n0, n1, 0, none, s.real);
+      sort_digit(cluster, sh, token, to, n0, n1, 0);
     else
-      sort_digit(cluster, sh, [&](int i) { return __ldcg(from + i); }, to, n0, n1, p * kDigitBits, none, nullptr);
+      sort_digit(cluster, sh, [&](int i) { return __ldcg(from + i); }, to, n0, n1, p * kDigitBits);
     uint2* t = from;
     from = to, to = t;
   }
@@ -289,7 +280,7 @@ __device__ __forceinline__ Pack<G, E> old_of(const G* at) {
 // A block: a piece of eight runs, 32 E columns; a warp for each run.
 template <typename T, typename G, int E, bool ACC>
 __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(SumArgs a, Scratch s, const T* __restrict__ dy, G* __restrict__ dw) {
-  constexpr int FLIGHT = 8;
+  constexpr int FLIGHT = ACC ? 8 : 16;
   // the sums of a run's first and last id, where the run's edges cut them (head alone where the run is all of one id)
   __shared__ float head[kSumWarps][E][32], tail[kSumWarps][E][32];
   __shared__ unsigned tail_id[kSumWarps];
@@ -299,11 +290,11 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(SumArgs a, Sc
   const int c = (blockIdx.x % a.parts * 32 + lane) * E;
   const bool in = c < a.D;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int real = *s.real, i0 = piece * kPiece + warp * kRun, n = min(kRun, real - i0);
-  if (piece * kPiece >= real) return;
+  const int i0 = piece * kPiece + warp * kRun, end = min(kRun, a.N - i0);
+  const uint2 mine = lane < end ? __ldcg(s.a + i0 + lane) : make_uint2(~0u, 0u);
+  const unsigned before = i0 > 0 && end > 0 ? __ldcg(&s.a[i0 - 1].x) : ~0u, after = i0 + kRun < a.N ? __ldcg(&s.a[i0 + kRun].x) : ~0u;
+  const int n = __popc(__ballot_sync(0xffffffffu, mine.x < static_cast<unsigned>(a.rows)));  // those with an id come first
   if (n > 0) {
-    const uint2 mine = lane < n ? __ldg(s.a + i0 + lane) : make_uint2(~0u, 0u);
-    const unsigned before = i0 > 0 ? __ldg(&s.a[i0 - 1].x) : ~0u, after = i0 + n < real ? __ldg(&s.a[i0 + n].x) : ~0u;
     float sum[E] = {};
     bool first = true;
     int flags = 0;
@@ -322,7 +313,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(SumArgs a, Sc
       for (int k = 0; k < FLIGHT; ++k) {
         if (k0 + k >= n) continue;
         const unsigned id = __shfl_sync(0xffffffffu, mine.x, k0 + k);
-        const unsigned next = k0 + k + 1 < n ? __shfl_sync(0xffffffffu, mine.x, (k0 + k + 1) & 31) : after;
+        const unsigned next = k0 + k + 1 < n ? __shfl_sync(0xffffffffu, mine.x, (k0 + k + 1) & 31) : after;  // `after` of a whole run
         const bool last = k0 + k + 1 == n;
         if (in) {
 #pragma unroll
@@ -391,15 +382,14 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(SumArgs a, S
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, piece = blockIdx.x / a.parts;
   const int c = (blockIdx.x % a.parts * 32 + lane) * E;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int real = *s.real, i0 = piece * kPiece, next = i0 + kPiece;
-  if (next >= real) return;
-  const unsigned id = __ldg(&s.a[next - 1].x);
-  if (__ldg(&s.a[next].x) != id) return;              // it ends here
-  if (i0 > 0 && __ldg(&s.a[i0 - 1].x) == id) return;  // it began before
-  int lo = piece + 1, hi = (real - 1) / kPiece;       // the last piece that begins with it
+  const int i0 = piece * kPiece, next = i0 + kPiece;
+  if (next >= a.N) return;
+  const unsigned id = __ldcg(&s.a[next - 1].x), then = __ldcg(&s.a[next].x), before = i0 > 0 ? __ldcg(&s.a[i0 - 1].x) : ~0u;
+  if (id >= static_cast<unsigned>(a.rows) || then != id || before == id) return;  // it ends here, or began before
+  int lo = piece + 1, hi = (a.N - 1) / kPiece;                                     // the last piece that begins with it
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
-    if (__ldg(&s.a[static_cast<size_t>(mid) * kPiece].x) == id)
+    if (__ldcg(&s.a[static_cast<size_t>(mid) * kPiece].x) == id)
       lo = mid;
     else
       hi = mid - 1;
@@ -505,25 +495,32 @@ int embed_fwd(const EmbedArgs& a, const void* weight, void* out, bool bf16, int 
 }
 
 size_t embed_bwd_workspace_bytes(int N, int, int D) {
-  return 256 + 2 * align256(static_cast<size_t>(N) * sizeof(uint2)) + static_cast<size_t>(pieces_of(N)) * 2 * D * sizeof(float);
+  return 2 * align256(static_cast<size_t>(N) * sizeof(uint2)) + static_cast<size_t>(pieces_of(N)) * 2 * D * sizeof(float);
 }
 
 int embed_bwd(const EmbedArgs& a, const void* dy, void* dweight, bool accumulate, bool bf16, bool grad_bf16, void* workspace, int num_sms,
               const DevCtl& ctl, cudaStream_t st) {
   uint8_t* at = static_cast<uint8_t*>(workspace);
   Scratch s;
-  s.real = reinterpret_cast<int*>(at);
-  s.a = reinterpret_cast<uint2*>(at + 256);
-  s.b = reinterpret_cast<uint2*>(at + 256 + align256(static_cast<size_t>(a.N) * sizeof(uint2)));
-  s.parts = reinterpret_cast<float*>(at + 256 + 2 * align256(static_cast<size_t>(a.N) * sizeof(uint2)));
+  s.a = reinterpret_cast<uint2*>(at);
+  s.b = reinterpret_cast<uint2*>(at + align256(static_cast<size_t>(a.N) * sizeof(uint2)));
+  s.parts = reinterpret_cast<float*>(at + 2 * align256(static_cast<size_t>(a.N) * sizeof(uint2)));
   int passes = 1;
   while (passes * kDigitBits < 31 && a.rows >> (passes * kDigitBits)) ++passes;  // ids up to `rows` itself
   const long long bytes = accumulate ? 0 : static_cast<long long>(a.rows) * a.D * (grad_bf16 ? 2 : 4);
   // a sorter for every thousand tokens; the others fill the GPU where there are zeros to write
-  int sorters = 1;
+  int sorters = 1, device = 0;
   while (sorters < kSortBlocks && a.N > 1024 * sorters) sorters *= 2;
+  if (sorters > 8) {  // more than the portable size of a cluster
+    static std::atomic<unsigned long long> ready{0};
+    if (cudaGetDevice(&device) != cudaSuccess) return -1;
+    if (device > 63 || !(ready.load(std::memory_order_acquire) >> device & 1ull)) {
+      if (cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return -1;
+      if (device <= 63) ready.fetch_or(1ull << device, std::memory_order_release);
+    }
+  }
   const long long zeroers = bytes ? (bytes / 16 + 4 * kSortThreads) / (4 * kSortThreads) : 0, most = num_sms - sorters;
-  const int grid = sorters + static_cast<int>((zeroers < most ? zeroers : most) + sorters - 1) / sorters * sorters;
+  const int grid = sorters + static_cast<int>((zeroers < most ? zeroers + sorters - 1 : most) / sorters * sorters);
   cudaLaunchConfig_t config = {};
   config.gridDim = dim3(grid), config.blockDim = dim3(kSortThreads), config.stream = st;
   cudaLaunchAttribute attr = {};
