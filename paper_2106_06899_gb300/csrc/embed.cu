@@ -279,8 +279,8 @@ __device__ __forceinline__ Pack<G, E> old_of(const G* at) {
 
 // A block: a piece of eight runs, 32 E columns; a warp for each run.
 template <typename T, typename G, int E, bool ACC>
-__global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(SumArgs a, Scratch s, const T* __restrict__ dy, G* __restrict__ dw) {
-  constexpr int FLIGHT = ACC ? 8 : 16;
+__global__ void __launch_bounds__(32 * kSumWarps, ACC ? 2 : 4) embed_sum_kernel(SumArgs a, Scratch s, const T* __restrict__ dy, G* __restrict__ dw) {
+  constexpr int FLIGHT = 8;
   // the sums of a run's first and last id, where the run's edges cut them (head alone where the run is all of one id)
   __shared__ float head[kSumWarps][E][32], tail[kSumWarps][E][32];
   __shared__ unsigned tail_id[kSumWarps];
