@@ -56,6 +56,8 @@ struct Layout {
 template <int D>
 constexpr size_t kPartFloats = 256 * (D + 2);
 
+constexpr int kMostParts = 160;  // of a unit: one from each CTA, of which there are no more than SMs (152)
+
 // Where a CTA's run of steps begins, of how many steps and CTAs with work.
 struct Place {
   int b, h, block, kt;
@@ -119,9 +121,16 @@ __device__ __forceinline__ int block_tiles(const Work& w, const Seq& s, int bloc
   return key_tiles<TREE>(w, s, min((block + 1) * 2 * w.tokens, s.Lq) - 1);
 }
 
-// sum over i < n of floor((a i + b) / m), by the steps of Euclid's algorithm for (a, m)
-__device__ __forceinline__ long long floor_sum(unsigned n, unsigned m, unsigned a, unsigned b) {
-  long long sum = 0;
+// sum over i < n of floor((a i + b) / BN), by the steps of Euclid's algorithm for (a, BN)
+__device__ __forceinline__ long long floor_sum(unsigned n, unsigned a, unsigned b) {
+  // the first step, whose divisor is known
+  long long sum = static_cast<long long>(a / BN) * (static_cast<long long>(n) * (n - 1) / 2) + static_cast<long long>(b / BN) * n;
+  a %= BN, b %= BN;
+  const unsigned y = a * n + b;
+  if (y < BN) return sum;
+  n = y / BN, b = y % BN;
+  unsigned m = a;
+  a = BN;
   while (n) {
     sum += static_cast<long long>(a / m) * (static_cast<long long>(n) * (n - 1) / 2) + static_cast<long long>(b / m) * n;
     a %= m, b %= m;
@@ -143,13 +152,18 @@ __device__ __forceinline__ long long tiles_before(const Work& w, const Seq& s, i
   // block i < blocks - 1 reads (i + 1) step + Lk - Lq keys
   const int step = 2 * w.tokens, more = s.Lk - s.Lq;
   const int none = more < 0 ? min(block, -more / step) : 0;  // blocks that read nothing
-  return none + floor_sum(block - none, BN, step, (none + 1) * step + more + BN - 1);
+  if (block == none) return none;
+  return none + floor_sum(block - none, step, (none + 1) * step + more + BN - 1);
 }
 
-// The run of key tiles that CTA i of `ctas` begins with.
-__device__ __forceinline__ long long run_start(long long total, int ctas, int i) {
-  return total / ctas * i + total % ctas * i / ctas;
+// x / y; most are small, and a division of 64 bits takes hundreds of cycles
+__device__ __forceinline__ long long quotient(long long x, long long y) {
+  if (x >> 32 == 0 && y >> 32 == 0) return static_cast<unsigned>(x) / static_cast<unsigned>(y);
+  return x / y;
 }
+
+// The step that the run of CTA i of `ctas` begins with.  What memory holds makes fewer than 2^52 steps.
+__device__ __forceinline__ long long run_start(long long total, int ctas, int i) { return quotient(total * i, ctas); }
 
 // Where the step number run_start(total, .., i) is; computed by a whole warp.
 template <bool TREE>
@@ -157,11 +171,14 @@ __device__ Place locate(const Work& w, int i, int grid, unsigned* error) {
   const int lane = threadIdx.x & 31;
   Place p{};
   bool wrong = false;
+  Seq s{};
+  long long mine = 0;  // of the last sequence looked at: with up to 32 of them the lane's own
   for (int b = lane; b < w.B; b += 32) {
     bool bad;
-    const Seq s = seq_of<TREE>(w, b, &bad);
+    s = seq_of<TREE>(w, b, &bad);
     wrong |= bad;
-    p.total += tiles_before<TREE>(w, s, s.blocks) * w.Hkv;
+    mine = tiles_before<TREE>(w, s, s.blocks) * w.Hkv;
+    p.total += mine;
   }
   if (error && wrong) atomicOr(error, kDevErrRange);
   for (int o = 16; o; o >>= 1) p.total += __shfl_xor_sync(0xffffffffu, p.total, o);
@@ -169,11 +186,12 @@ __device__ Place locate(const Work& w, int i, int grid, unsigned* error) {
   if (i >= p.ctas) return p;
   long long left = run_start(p.total, p.ctas, i);
   for (int b0 = 0; b0 < w.B; b0 += 32) {
-    long long mine = 0;
-    Seq s{};
-    if (b0 + lane < w.B) {
-      s = seq_of<TREE>(w, b0 + lane);
-      mine = tiles_before<TREE>(w, s, s.blocks) * w.Hkv;
+    if (w.B > 32) {
+      mine = 0;
+      if (b0 + lane < w.B) {
+        s = seq_of<TREE>(w, b0 + lane);
+        mine = tiles_before<TREE>(w, s, s.blocks) * w.Hkv;
+      }
     }
     long long upto = mine;
     for (int o = 1; o < 32; o <<= 1) {
@@ -186,8 +204,8 @@ __device__ Place locate(const Work& w, int i, int grid, unsigned* error) {
       int h = 0, block = 0, kt = 0;
       if (lane == k) {
         left -= upto - mine;
-        const long long head = mine / w.Hkv;
-        h = static_cast<int>(left / head);
+        const long long head = quotient(mine, w.Hkv);
+        h = static_cast<int>(quotient(left, head));
         left -= h * head;
         int lo = 0, hi = s.blocks - 1;  // the last block with tiles_before <= left
         while (lo < hi) {
@@ -821,7 +839,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 // a thread for each row.
 template <int D, bool TREE>
 __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant__ Work w) {
-  constexpr int kMostParts = 256;
   __shared__ float weight[kMostParts][32];
   __shared__ float4 share[256];
   __shared__ float shared[8][32];
@@ -837,17 +854,23 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
   const int t0 = (2 * p.block + x) * w.tokens;
   const int rows = min(32, min(w.tokens, s.Lq - t0) * w.group - row0);
   if (rows <= 0) return;
-  int end = i + 1;  // CTAs i - 1 .. end - 1 have parts
-  while (end < p.ctas && run_start(p.total, p.ctas, end) < last) ++end;
+  // CTAs i - 1 .. end - 1 have parts: run_start(end) is the first that is not below `last`
+  const int end = min(p.ctas, static_cast<int>(quotient(last * p.ctas + p.total - 1, p.total)));
   const int parts = end - i + 1;
   const auto part = [&](int k) { return w.parts + (2 * static_cast<size_t>(i - 1 + k) + (k == 0 ? 1 : 0)) * kPartFloats<D>; };
 
+  // a row's maxima, then its sums, every eighth part's by a thread, four on their way at once
   const int row = threadIdx.x % 32, group = threadIdx.x / 32;
   float m = -INFINITY;
-  for (int k = group; k < parts; k += 8) {
-    const float mk = row < rows ? part(k)[256 * D + at0 + row] : -INFINITY;
-    weight[k][row] = mk;
-    m = fmaxf(m, mk);
+  for (int k0 = group; k0 < parts; k0 += 32) {
+    float mk[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) mk[t] = k0 + 8 * t < parts && row < rows ? __ldcg(part(k0 + 8 * t) + 256 * D + at0 + row) : -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      if (k0 + 8 * t < parts) weight[k0 + 8 * t][row] = mk[t];
+      m = fmaxf(m, mk[t]);
+    }
   }
   shared[group][row] = m;
   __syncthreads();
@@ -856,11 +879,17 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
   const float base = m == -INFINITY ? 0.f : m;
   __syncthreads();
   float z = 0.f;
-  for (int k = group; k < parts; k += 8) {
-    const float zk = row < rows ? part(k)[256 * D + 256 + at0 + row] : 0.f;
-    const float f = zk == 0.f ? 0.f : exp2_fast((weight[k][row] - base) * kLog2e);  // a part without a key has no O
-    weight[k][row] = f;
-    z += zk == 0.f ? 0.f : zk * f;
+  for (int k0 = group; k0 < parts; k0 += 32) {
+    float zk[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) zk[t] = k0 + 8 * t < parts && row < rows ? __ldcg(part(k0 + 8 * t) + 256 * D + 256 + at0 + row) : 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      if (k0 + 8 * t >= parts) continue;
+      const float f = zk[t] == 0.f ? 0.f : exp2_fast((weight[k0 + 8 * t][row] - base) * kLog2e);  // a part without a key has no O
+      weight[k0 + 8 * t][row] = f;
+      z += zk[t] == 0.f ? 0.f : zk[t] * f;
+    }
   }
   shared[group][row] = z;
   __syncthreads();
@@ -873,12 +902,19 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
     const int r = j % wide, c = j / wide % 16, lane = j / items;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r < rows)
-#pragma unroll 4
-      for (int k = lane; k < parts; k += lanes) {
-        const float f = weight[k][r];
-        if (f == 0.f) continue;
-        const float4 v = reinterpret_cast<const float4*>(part(k))[(c0 / 4 + c) * 256 + at0 + r];
-        o.x += v.x * f, o.y += v.y * f, o.z += v.z * f, o.w += v.w * f;
+      for (int k0 = lane; k0 < parts; k0 += 4 * lanes) {
+        float4 v[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int k = k0 + t * lanes;
+          if (k < parts && weight[k][r] != 0.f) v[t] = __ldcg(reinterpret_cast<const float4*>(part(k)) + (c0 / 4 + c) * 256 + at0 + r);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int k = k0 + t * lanes;
+          const float f = k < parts ? weight[k][r] : 0.f;
+          if (f != 0.f) o.x += v[t].x * f, o.y += v[t].y * f, o.z += v[t].z * f, o.w += v[t].w * f;
+        }
       }
     if (lanes > 1) {
       share[threadIdx.x] = o;
@@ -945,7 +981,7 @@ size_t grouped_workspace_bytes(int d, int num_sms) {
 }
 
 int prompt_attn(const topk_prompt_args& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
-  if (!encode_tiled_fn() || num_sms > 256) return -1;  // the join's parts in shared memory
+  if (!encode_tiled_fn() || num_sms > kMostParts) return -1;
   Work w = {};
   w.q_starts = a.q_starts, w.k_starts = a.k_starts ? a.k_starts : a.q_starts;
   w.out = static_cast<__nv_bfloat16*>(a.out), w.parts = static_cast<float*>(workspace);
@@ -961,7 +997,7 @@ int prompt_attn(const topk_prompt_args& a, void* workspace, int num_sms, const D
 }
 
 int tree_attn(const topk_tree_args& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
-  if (!encode_tiled_fn() || num_sms > 256) return -1;
+  if (!encode_tiled_fn() || num_sms > kMostParts) return -1;
   Work w = {};
   w.kv_len = a.kv_len, w.words = a.tree, w.word_stride = a.tree_stride;
   w.out = static_cast<__nv_bfloat16*>(a.out), w.parts = static_cast<float*>(workspace);
