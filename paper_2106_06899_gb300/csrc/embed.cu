@@ -204,7 +204,7 @@ __device__ void sort_digit(cg::cluster_group& cluster, SortShared& sh, Get get, 
 // The first cluster sorts; the other blocks write zeros (into dw where it is to be written, [bytes16] of 16 bytes and a tail).
 __global__ void __launch_bounds__(kSortThreads, 1)
     embed_sort_kernel(EmbedArgs a, Scratch s, int passes, int sorters, uint4* zero, long long bytes16, int tail_bytes, DevCtl ctl) {
-  __shared__ SortShared sh;
+  __shared__ alignas(16) SortShared sh;
   cg::cluster_group cluster = cg::this_cluster();
   if (static_cast<int>(blockIdx.x) >= sorters) {
     const long long at = static_cast<long long>(blockIdx.x - sorters) * kSortThreads + threadIdx.x,
@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(SumArgs a, S
     for (int k = k0; k < k1; ++k) {
       const float* p = s.parts + (static_cast<size_t>(piece + k) * 2 + (k == 0 ? 1 : 0)) * a.D + c;
 #pragma unroll
-      for (int e = 0; e < E; ++e) sum[e] += __ldg(p + e);
+      for (int e = 0; e < E; ++e) sum[e] += __ldcg(p + e);  // written while this kernel waited
     }
 #pragma unroll
   for (int e = 0; e < E; ++e) share[warp][e][lane] = sum[e];
