@@ -22,6 +22,13 @@
  *                     top-k attention"): gradients of q, k, v (x, W1, W2)
  *                     from dout, the kept indices and their scores, with the
  *                     activation recomputed from the cached scores.
+ *   topk_vanilla_attn_fwd, topk_vanilla_ffn_fwd -- Eq. 1 and the dense layer, for comparison.
+ *   topk_qk_norm_rope_*, topk_linear_*, topk_adamw_step -- the operators between two attention calls of a decoder,
+ *                     and its optimizer.
+ *   topk_embedding_*, topk_token_logprobs_* -- its two ends: the lookup of token ids, and what logits say of
+ *                     the next tokens, each with its gradient.
+ *   topk_prompt_attn_fwd, topk_tree_attn_fwd -- Eq. 1 with grouped heads for serving: packed prompts of different lengths,
+ *                     and single or drafted tokens against key/value caches.
  * Query chunking (Sec. 2.2 "Query chunking") bounds scheduling only: results
  * never depend on `chunk`, and no [chunk x L_K] score matrix is ever stored
  * in device memory.
@@ -34,7 +41,7 @@
  * Conventions shared by every call
  *   - Tensor pointers are DEVICE pointers (except the *_host entry points),
  *     owned by the caller, contiguous, row-major, 16-byte aligned.
- *     (topk_qk_norm_rope_fwd takes strided q, k and v.)
+ *     (topk_qk_norm_rope_fwd and the calls on tokens and prompts take strided tensors where they say so.)
  *   - Shapes: q, out [B, H, Lq, d]; k, v [B, H, Lk, d];
  *             x [N, d_model]; W1, W2 [d_ff, d_model]; ffn out [N, d_model].
  *   - dtype: TOPK_F32 (fp32 in/out, fp32 FMA scores, never TF32) or
@@ -395,7 +402,7 @@ int topk_adamw_step(const topk_adamw_tensor* tensors, int count, int param_dtype
  * Embedding lookup: out[n] = scale weight[ids[n]], rounded once, to nearest.
  *   ids      : [N] int32 or int64 (id_bits 32 or 64).  A negative id is padding: its row of out is zero.  An id
  *              of `rows` or more gives zeros too and is reported as TOPK_ERR_RANGE by topk_check().
- *   weight   : [rows, D].  out: [N, D].  `dtype`, contiguous, 16-byte aligned; any D.
+ *   weight   : [rows, D].  out: [N, D].  `dtype`, contiguous, 16-byte aligned; any D.  out overlaps no input.
  */
 int topk_embedding_fwd(const void* ids, int id_bits, const void* weight, void* out, int N, int rows, int D, float scale,
                        int dtype, void* stream);
@@ -404,7 +411,7 @@ int topk_embedding_fwd(const void* ids, int id_bits, const void* weight, void* o
  * Backward: dweight[v] = scale (sum of dy[n] over the n with ids[n] = v), in fp32 and always added up in the same
  * order: two runs give the same bits.  Ids that are padding or out of range add to nothing (the latter are reported
  * as TOPK_ERR_RANGE).
- *   dy         : [N, D] of `dtype`.  dweight: [rows, D] of grad_dtype (TOPK_F32 or TOPK_BF16).
+ *   dy         : [N, D] of `dtype`.  dweight: [rows, D] of grad_dtype (TOPK_F32 or TOPK_BF16); it overlaps no input.
  *   accumulate : 0: every row of dweight is written, zeros where no id points.  1: the sums are added to what dweight
  *                holds (tied weights, several batches), rounded once; rows without an id are left alone.
  *   Scratch: topk_embedding_bwd_workspace_bytes(): 16 bytes for each id and two rows of D floats for every 128 ids.
@@ -439,7 +446,7 @@ int topk_token_logprobs_fwd(const void* logits, long long row_stride, const void
  *   dlogp   : [N] fp32 with targets, both or neither.  dentropy: [N] fp32 with entropy, both or neither.
  *   dtop    : [N, top] fp32 with top_ids [N, top], both or neither (an index outside [0, V) gets nothing).  At least
  *             one of dlogp, dentropy and dtop.
- *   dlogits : [N, V], rows dlogits_stride elements apart; logits itself is allowed (with its stride).
+ *   dlogits : [N, V], rows dlogits_stride elements apart; logits itself is allowed (with its stride), and no other overlap.
  * A row none of whose gradients differs from 0 is written as zeros, whatever its logits hold; so is one with nothing but masked
  * logits.
  */
@@ -459,11 +466,12 @@ int topk_token_logprobs_bwd(const void* logits, long long row_stride, const floa
  *              clamped and reported as TOPK_ERR_RANGE by topk_check().
  *   causal   : a sequence's queries are the last of its positions: with Lq queries and Lk keys, query i reads keys
  *              j <= i + Lk - Lq (Lk > Lq: a prompt that goes on from cached keys).  0: every key of the sequence.
- *   out      : [Tq, Hq, d] bf16, contiguous.  A query without a key gets zeros.  Rows of no sequence are left alone, or
+ *   out      : [Tq, Hq, d] bf16, contiguous, outside q, k and v.  A query without a key gets zeros.  Rows of no sequence are left alone, or
  *              with clear_rest = 1 written as zeros.
  *   d        : 64 or 128.  Hq a multiple of Hkv, Hq / Hkv at most 128.
- * Keys and values outside a sequence are not read into its results, whatever they hold.  Scores and sums in fp32; weights are
- * rounded to bf16 as the tensor cores' operand (not in the softmax's sum).
+ * Keys and values outside a sequence are not read into its results, whatever they hold.  A key of the sequence that a query's
+ * mask leaves out has weight 0: its value must be finite, as in any product (0 x infinity is NaN); its score need
+ * not be.  Scores and sums in fp32; weights are rounded to bf16 as the tensor cores' operand (not in the softmax's sum).
  *   Scratch: topk_prompt_attn_workspace_bytes(), a fixed amount for each SM.
  */
 typedef struct {
@@ -488,9 +496,10 @@ size_t topk_prompt_attn_workspace_bytes(int d);
  *                  as TOPK_ERR_RANGE by topk_check(); rows from cap on do not exist.
  *   tree         : [B, T] int64, device, or NULL: token i reads drafted tokens 0 to i (a chain).
  *   tree_stride  : words from one sequence's to the next (0: one tree for all).
- *   out          : [B, Hq, T, d] bf16, contiguous.  A token that reads nothing gets zeros.
+ *   out          : [B, Hq, T, d] bf16, contiguous, outside q, keys and values.  A token that reads nothing gets zeros.
  *   T            : 1 to 64.  d, Hq and Hkv as above.
- * Rows of the cache that a sequence does not have are not read into its results, whatever they hold.
+ * Rows of the cache that a sequence does not have are not read into its results, whatever they hold; drafted values that a
+ * token does not read must be finite (as in topk_prompt_attn_fwd).
  *   Scratch: topk_prompt_attn_workspace_bytes().
  */
 typedef struct {

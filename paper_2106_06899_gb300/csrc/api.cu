@@ -758,6 +758,14 @@ int validate_strides(std::initializer_list<std::pair<int, long long>> dims) {
   return TOPK_OK;
 }
 
+// Whether rows of d bf16, strided along up to three axes, reach into [out, out + elements).
+bool reaches(const void* p, std::initializer_list<std::pair<int, long long>> dims, int d, const void* out, size_t elements) {
+  unsigned long long last = d;
+  for (const auto& [n, stride] : dims) last += n > 1 ? static_cast<unsigned long long>(n - 1) * stride : 0;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), o = reinterpret_cast<uintptr_t>(out);
+  return a < o + 2 * elements && o < a + 2 * last;
+}
+
 int validate_heads(int Hq, int Hkv, int d) {
   if (Hq <= 0 || Hkv <= 0 || d <= 0 || Hq % Hkv) return TOPK_ERR_INVALID_ARG;
   return (d != 64 && d != 128) || Hq / Hkv > 128 || Hq > 65536 ? TOPK_ERR_UNSUPPORTED : TOPK_OK;
@@ -790,6 +798,11 @@ int topk_prompt_attn_fwd(const topk_prompt_args* args, void* stream) {
   if (a.B > (1 << 20) || a.Tq > (1 << 28) || a.Tk > (1 << 28)) return TOPK_ERR_UNSUPPORTED;
   if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.v) || !aligned16(a.out) || !aligned4(a.q_starts) || !aligned4(a.k_starts))
     return TOPK_ERR_UNSUPPORTED;
+  const size_t elements = static_cast<size_t>(a.Tq) * a.Hq * a.d;
+  if (reaches(a.q, {{a.Tq, a.q_stride[0]}, {a.Hq, a.q_stride[1]}}, a.d, a.out, elements) ||
+      reaches(a.k, {{a.Tk, a.k_stride[0]}, {a.Hkv, a.k_stride[1]}}, a.d, a.out, elements) ||
+      reaches(a.v, {{a.Tk, a.v_stride[0]}, {a.Hkv, a.v_stride[1]}}, a.d, a.out, elements))
+    return TOPK_ERR_INVALID_ARG;  // blocks read them while others write
   return run_grouped(args, nullptr, a.d, stream);
 }
 
@@ -812,6 +825,11 @@ int topk_tree_attn_fwd(const topk_tree_args* args, void* stream) {
   if (!aligned16(a.q) || !aligned16(a.keys) || !aligned16(a.values) || !aligned16(a.out) || !aligned4(a.kv_len) ||
       (reinterpret_cast<uintptr_t>(a.tree) & 7u))
     return TOPK_ERR_UNSUPPORTED;
+  const size_t elements = static_cast<size_t>(a.B) * a.Hq * a.T * a.d;
+  if (reaches(a.q, {{a.B, a.q_stride[0]}, {a.Hq, a.q_stride[1]}, {a.T, a.q_stride[2]}}, a.d, a.out, elements) ||
+      reaches(a.keys, {{a.B, a.key_stride[0]}, {a.Hkv, a.key_stride[1]}, {a.cap, a.key_stride[2]}}, a.d, a.out, elements) ||
+      reaches(a.values, {{a.B, a.value_stride[0]}, {a.Hkv, a.value_stride[1]}, {a.cap, a.value_stride[2]}}, a.d, a.out, elements))
+    return TOPK_ERR_INVALID_ARG;
   return run_grouped(nullptr, args, a.d, stream);
 }
 

@@ -137,6 +137,22 @@ def test_tree_arguments(lib, kw, code):
     assert lib.topk_tree_attn_fwd(_tree(**kw), None) == code
 
 
+# of 8 rows of 4 heads of 64: q takes 4,096 bytes, k and v with two heads 2,048
+@pytest.mark.parametrize("kw", [dict(out=1 << 16), dict(out=(1 << 16) + 4080), dict(out=(1 << 16) - 4080), dict(out=(2 << 16) + 2032), dict(out=(3 << 16) - 16)], ids=str)
+def test_outputs_inside_the_inputs(lib, kw):
+    assert lib.topk_prompt_attn_fwd(_prompt(**{**dict(q=1 << 16, k=2 << 16, v=3 << 16), **kw}), None) == -1
+    tree = dict(B=1, T=8, cap=8, q_stride=(0, 64, 256), key_stride=(0, 64, 128), value_stride=(0, 64, 128))
+    assert lib.topk_tree_attn_fwd(_tree(**{**tree, **dict(q=1 << 16, keys=2 << 16, values=3 << 16), **kw}), None) == -1
+
+
+def test_outputs_beside_the_inputs(lib):
+    # every argument is taken: what is missing here is a device (on one that has it, these addresses are never read)
+    if torch.cuda.is_available():
+        pytest.skip("made-up addresses")
+    for out in ((1 << 16) + 4096, (1 << 16) - 4096, (2 << 16) + 2048):
+        assert lib.topk_prompt_attn_fwd(_prompt(q=1 << 16, k=2 << 16, v=3 << 16, out=out), None) == -6
+
+
 def test_null_records(lib):
     assert lib.topk_prompt_attn_fwd(None, None) == -1
     assert lib.topk_tree_attn_fwd(None, None) == -1
