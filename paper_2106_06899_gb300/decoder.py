@@ -367,10 +367,12 @@ class Decoder(torch.nn.Module):
         starts[b] to starts[b + 1] - 1 ([B + 1] int32, from 0 to T); returns [T, d_model]."""
         if not self.fused or any(layer.topk is not None for layer in self.layers):
             raise ValueError("prefill() needs a fused decoder with plain attention (topk=None)")
-        x = self._features(x)
         n, cap, ends = x.shape[0], caches[0][0].shape[2], starts.long()
+        if not 2 <= starts.shape[0] <= caches[0][0].shape[0] + 1:
+            raise ValueError("starts must have from one to the caches' number of sequences, and an end")
         if n > cap and int((ends[1:] - ends[:-1]).max()) > cap:  # the host waits for the lengths only where they could be too long
             raise ValueError("the caches have no room for the longest prompt")
+        x = self._features(x)
         # rows of no sequence write what the nearest token of one does
         token = torch.minimum(torch.maximum(torch.arange(n, device=x.device), ends[0]), (ends[-1] - 1).clamp_min(0)).clamp(0, n - 1)
         rows = torch.searchsorted(ends[1:], token, right=True).clamp_max(ends.shape[0] - 2)
@@ -406,6 +408,8 @@ class Decoder(torch.nn.Module):
         """Moves the drafted tokens path [B, n] (indices into step_tree's, a token and its descendants in order) to rows start[b] to
         start[b] + n - 1 of the caches; an index that repeats fills up a shorter path.  Rows outside the caches are cut to them."""
         B, n = path.shape
+        if B != start.shape[0] or B > caches[0][0].shape[0]:
+            raise ValueError("path must have a row for each of start's sequences, which the caches hold")
         b = torch.arange(B, device=path.device)[:, None]
         last = caches[0][0].shape[2] - 1
         to, of = ((start.long()[:, None] + i).clamp(0, last) for i in (torch.arange(n, device=path.device), path.long()))

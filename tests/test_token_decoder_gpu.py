@@ -187,3 +187,16 @@ def test_refusals():
         m.prefill(torch.zeros(4, dtype=torch.int64, device="cuda"), torch.tensor([0, 4], dtype=torch.int32, device="cuda"), m.new_cache(1, 8))
     with pytest.raises(ValueError):
         Decoder(1, 256, 4, 512, fused=True).logprobs(torch.zeros(1, 256, device="cuda", dtype=BF))
+
+
+def test_more_sequences_than_the_caches_hold():
+    m = _model()
+    ids, caches = torch.zeros(6, dtype=torch.int64, device="cuda"), m.new_cache(2, 8)
+    starts = torch.tensor([0, 2, 4, 6], dtype=torch.int32, device="cuda")
+    for bad in (starts, starts[:1], starts[:0]):
+        with pytest.raises(ValueError):
+            m.prefill(ids, bad, caches)
+    for sequences, rows in ((3, 3), (2, 1)):
+        with pytest.raises(ValueError):
+            m.keep(caches, torch.zeros(sequences, dtype=torch.int32, device="cuda"), torch.zeros((rows, 1), dtype=torch.int64, device="cuda"))
+    assert not any(t.any() for pair in caches for t in pair)
