@@ -5,9 +5,11 @@
 // T of 2^d d give lse = scale r + ln S and the entropy ln S - ln 2 T / S.  A thread keeps its own reference and raises it
 // only where an element exceeds it by more than kRaise; references are brought together at the end.
 // Alternatives: after a block's first tile the top-th largest of 64 to 256 groups' maxima is a value that at least `top` elements
-// reach, and hardly more do (1.1 to 1.4 times as many, for each tile); what reaches it goes to a buffer in
-// shared memory, where the candidates are ranked at the end.  A row that overflows the buffer (values that rise along the
-// row, or thousands of equal ones) is read a second time with a threshold that is raised whenever the buffer fills.
+// reach, and hardly more do (1.1 to 1.4 times as many, for each tile).  The pass notes which vectors reach it; these few are
+// looked at once more, an element a thread, and what reaches it is ranked (taken out of the vector as it passes, by the
+// lane that holds it, a candidate holds up its whole warp: 110 us in place of 100).  A row with more candidates
+// than the buffers hold (values that rise along the row, or thousands of equal ones) is read a second time with a threshold that is
+// raised whenever the buffer fills.
 //
 // A block takes a row, or a cluster of up to eight blocks a share of it each where there are few rows (a decoding step): the
 // first block then collects the others' sums and alternatives from their shared memory.
@@ -203,12 +205,13 @@ __device__ void sort_keys(unsigned long long* k, int n) {
 struct Shared {
   alignas(16) unsigned long long kept[kKept];
   unsigned long long best[kMaxAlternatives];
+  int hits[kKept];  // vectors with a candidate
   float groups[kThreads];
   Sums sums[kThreads / 32];
   Sums total;
   unsigned long long threshold;
   float bar;
-  int count, have;  // candidates, and the best among them
+  int vectors, count, have;  // with candidates, candidates, and the best among them
 };
 
 // The `top` best candidates in order; all threads.
@@ -267,8 +270,11 @@ __device__ __noinline__ void rescan(Shared& sh, const T* x, int e0, int e1, int 
   }
 }
 
-// 4,099 rows of 50,001 bf16 logits with 8 alternatives: see the table of measured cases; what bounds it is memory, then the issue of
-// about six instructions an element.
+// 4,099 rows of 50,001 bf16 logits with 8 alternatives: 100 us, 4.1 TB/s.  Without alternatives a warp issues 10.6 instructions an
+// element (2^x alone takes the special units 44 us) and about 3,500 a row, whose ends, sums and threshold are the rest; a
+// decoding step, 4 rows of 131,072 with 20 alternatives, takes 10 us, which is the latency of the same steps.  Products of two elements
+// at a time (100 us), five or six blocks an SM with half the loads in flight (97, but 13 for the decoding step) and three
+// (110) were measured.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kThreads, 4)
     logprob_fwd_kernel(LogprobArgs a, float* logp, float* entropy, float* lse, float* top_logp, int32_t* top_ids, DevCtl ctl) {
@@ -298,12 +304,12 @@ __global__ void __launch_bounds__(kThreads, 4)
   }
   float bar = -INFINITY;
   const auto offer = [&](float v, int j) {
-    if (v >= bar && v > -INFINITY) {
+    if (v >= bar) {
       const int at = atomicAdd(&sh.count, 1);
       if (at < kKept) sh.kept[at] = key_of(v, j);
     }
   };
-  if (TOP && threadIdx.x == 0) sh.count = 0;
+  if (TOP && threadIdx.x == 0) sh.count = sh.vectors = 0;
   Vec<T> ahead[UNROLL];
   const auto fetch = [&](int v) {
 #pragma unroll
@@ -343,32 +349,27 @@ __global__ void __launch_bounds__(kThreads, 4)
           if (before == a.top - 1) sh.bar = g;
         }
         __syncthreads();
-        bar = sh.bar;
+        bar = fmaxf(sh.bar, -3.402823466e38f);  // -inf is no candidate
         if (edge >= 0) offer(edge_x, edge);
       }
 #pragma unroll
       for (int i = 0; i < UNROLL; ++i) {
-        if (most[i] < bar || most[i] == -INFINITY) continue;
-        float e[N];
-        u[i].get(e);
-        const int at = v + i * kThreads + threadIdx.x;
-        uint32_t hits = 0;
-#pragma unroll
-        for (int k = 0; k < N; ++k) hits |= e[k] >= bar ? 1u << k : 0u;
-        while (hits) {  // one turn for nearly every warp
-          const int k = __ffs(hits) - 1;
-          hits &= hits - 1;
-          float ek = e[0];
-#pragma unroll
-          for (int q = 1; q < N; ++q) ek = q == k ? e[q] : ek;
-          offer(ek, lead + at * N + k);
+        if (most[i] >= bar) {
+          const int at = atomicAdd(&sh.vectors, 1);
+          if (at < kKept) sh.hits[at] = v + i * kThreads + threadIdx.x;
         }
       }
     }
   }
   if constexpr (TOP) {
     __syncthreads();
-    if (sh.count > kKept) rescan(sh, x, lead + v0 * N, lead + v1 * N, rank_here == 0 ? lead : 0, rank_here == 0 ? tail : a.V, a.V, a.top);
+    // the few vectors that reach the bar once more, an element a thread
+    for (int i = threadIdx.x, end = min(sh.vectors, kKept) * N; i < end; i += kThreads) {
+      const int j = sh.hits[i / N] * N + i % N;
+      offer(to_f(body[j]), lead + j);
+    }
+    __syncthreads();
+    if (max(sh.count, sh.vectors) > kKept) rescan(sh, x, lead + v0 * N, lead + v1 * N, rank_here == 0 ? lead : 0, rank_here == 0 ? tail : a.V, a.V, a.top);
     rank(sh, a.top);
   }
 
