@@ -839,9 +839,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 // a thread for each row.
 template <int D, bool TREE>
 __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant__ Work w) {
-  __shared__ float weight[kMostParts][32];
+  __shared__ float tops[kMostParts][32];  // a part's maximum, -inf where it has no key
   __shared__ float4 share[256];
-  __shared__ float shared[8][32];
+  __shared__ float2 shared[8][32];  // the maximum and the sum over every eighth part
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int i = blockIdx.x + 1;
   const Place p = w.places[i];
@@ -859,39 +859,30 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
   const int parts = end - i + 1;
   const auto part = [&](int k) { return w.parts + (2 * static_cast<size_t>(i - 1 + k) + (k == 0 ? 1 : 0)) * kPartFloats<D>; };
 
-  // a row's maxima, then its sums, every eighth part's by a thread, four on their way at once
+  // a row's maxima and sums, every eighth part's by a thread, four on their way at once
   const int row = threadIdx.x % 32, group = threadIdx.x / 32;
-  float m = -INFINITY;
+  float2 mine = make_float2(-INFINITY, 0.f);
   for (int k0 = group; k0 < parts; k0 += 32) {
-    float mk[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) mk[t] = k0 + 8 * t < parts && row < rows ? __ldcg(part(k0 + 8 * t) + 256 * D + at0 + row) : -INFINITY;
+    float mk[4], zk[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      if (k0 + 8 * t < parts) weight[k0 + 8 * t][row] = mk[t];
+      const bool in = k0 + 8 * t < parts && row < rows;
+      const float* p = part(k0 + 8 * t) + 256 * D + at0 + row;
+      mk[t] = in ? __ldcg(p) : -INFINITY, zk[t] = in ? __ldcg(p + 256) : 0.f;
+    }
+    float m = mine.x;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      if (k0 + 8 * t < parts) tops[k0 + 8 * t][row] = zk[t] == 0.f ? -INFINITY : mk[t];
       m = fmaxf(m, mk[t]);
     }
+    const float base = m == -INFINITY ? 0.f : m;
+    float z = mine.y == 0.f ? 0.f : mine.y * exp2_fast((mine.x - base) * kLog2e);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) z += zk[t] == 0.f ? 0.f : zk[t] * exp2_fast((mk[t] - base) * kLog2e);
+    mine = make_float2(m, z);
   }
-  shared[group][row] = m;
-  __syncthreads();
-#pragma unroll
-  for (int g = 0; g < 8; ++g) m = fmaxf(m, shared[g][row]);
-  const float base = m == -INFINITY ? 0.f : m;
-  __syncthreads();
-  float z = 0.f;
-  for (int k0 = group; k0 < parts; k0 += 32) {
-    float zk[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) zk[t] = k0 + 8 * t < parts && row < rows ? __ldcg(part(k0 + 8 * t) + 256 * D + 256 + at0 + row) : 0.f;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      if (k0 + 8 * t >= parts) continue;
-      const float f = zk[t] == 0.f ? 0.f : exp2_fast((weight[k0 + 8 * t][row] - base) * kLog2e);  // a part without a key has no O
-      weight[k0 + 8 * t][row] = f;
-      z += zk[t] == 0.f ? 0.f : zk[t] * f;
-    }
-  }
-  shared[group][row] = z;
+  shared[group][row] = mine;
   __syncthreads();
 
   // 16 columns of four for each row; the rest of the block's threads take other parts
@@ -900,6 +891,10 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
   const int items = 16 * wide, lanes = items >= 256 ? 1 : 256 / items;  // lanes: over the parts
   for (int j = threadIdx.x; j < items * lanes; j += 256) {
     const int r = j % wide, c = j / wide % 16, lane = j / items;
+    float m = -INFINITY;
+#pragma unroll
+    for (int g = 0; g < 8; ++g) m = fmaxf(m, shared[g][r].x);
+    const float base = m == -INFINITY ? 0.f : m;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r < rows)
       for (int k0 = lane; k0 < parts; k0 += 4 * lanes) {
@@ -907,13 +902,14 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const int k = k0 + t * lanes;
-          if (k < parts && weight[k][r] != 0.f) v[t] = __ldcg(reinterpret_cast<const float4*>(part(k)) + (c0 / 4 + c) * 256 + at0 + r);
+          if (k < parts && tops[k][r] > -INFINITY) v[t] = __ldcg(reinterpret_cast<const float4*>(part(k)) + (c0 / 4 + c) * 256 + at0 + r);
         }
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const int k = k0 + t * lanes;
-          const float f = k < parts ? weight[k][r] : 0.f;
-          if (f != 0.f) o.x += v[t].x * f, o.y += v[t].y * f, o.z += v[t].z * f, o.w += v[t].w * f;
+          if (k >= parts || tops[k][r] == -INFINITY) continue;
+          const float f = exp2_fast((tops[k][r] - base) * kLog2e);
+          o.x += v[t].x * f, o.y += v[t].y * f, o.z += v[t].z * f, o.w += v[t].w * f;
         }
       }
     if (lanes > 1) {
@@ -927,7 +923,7 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
     if (lane == 0 && r < rows) {
       float sum = 0.f;
 #pragma unroll
-      for (int g = 0; g < 8; ++g) sum += shared[g][r];
+      for (int g = 0; g < 8; ++g) sum += shared[g][r].y == 0.f ? 0.f : shared[g][r].y * exp2_fast((shared[g][r].x - base) * kLog2e);
       const float f = sum == 0.f ? 0.f : 1.f / sum;
       const int token = t0 + (row0 + r) / w.group, head = p.h * w.group + (row0 + r) % w.group;
       __nv_bfloat16* out =
