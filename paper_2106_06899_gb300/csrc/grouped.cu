@@ -3,11 +3,13 @@
 //
 // A unit of work is a key head of a sequence with the rows of two 128-row tiles: a row is one query head of one
 // token, and a tile takes as many tokens as its 128 rows hold of the group's heads, so that a group's heads share
-// every key tile that is staged.  Per 128 keys and tile
+// every key tile that is staged.  Per 64 keys and tile
 //   S = Q K^T      tcgen05.mma, fp32 in TMEM;
 //   P = 2^(S - m)  four warps, a row each thread, written over S as the bf16 operand that the next product
 //                  reads from TMEM;
 //   O += P V       tcgen05.mma, V as it lies in memory (its keys are the sum: the instruction transposes).
+// Over caches, which memory bounds, P is two bf16, the rounded weight and the rest, with a product each: the result is rounded once,
+// where one bf16 is a second rounding of the same size.
 // While the warps of one tile are at its exponentials, the tensor pipe works for the other.  A row's running maximum
 // m is raised only when a tile's exceeds it by more than kRaise; O and the sum are scaled then.
 //
@@ -572,8 +574,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc_fence_after();
           const uint64_t vd = ring_v + at.slot * (L::TILE >> 4);
 #pragma unroll
-          for (int k = 0; k < BN / 16; ++k)
-            mma_bf16_ts(tmem + L::O_COL + x * D, tmem + buf * BN + k * 8, vd + ((k * 2048) >> 4), IDESC_O, first && k == 0 ? 0u : 1u);
+          for (int k = 0; k < (TREE ? 2 : 1) * (BN / 16); ++k)  // with caches the weights' rests too
+            mma_bf16_ts(tmem + L::O_COL + x * D, tmem + buf * BN + k * 8, vd + ((k % (BN / 16) * 2048) >> 4), IDESC_O, first && k == 0 ? 0u : 1u);
           mma_commit(&pv_done[buf]);
           mma_commit(&empty[at.slot]);
           if (split ? kt + 2 >= seg.kt1 : kt + 1 == end) mma_commit(&o_full[x]);
@@ -687,15 +689,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           F2 sum[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
 #pragma unroll
           for (int c = 0; c < BN / 32; ++c) {
-            uint32_t p[16];
+            uint32_t p[16], rest[TREE ? 16 : 1];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               const F2 d = fma2(f2(s[32 * c + 2 * e], s[32 * c + 2 * e + 1]), scale, minus);
               const float a = exp2_fast(lo(d)), b = exp2_fast(hi(d));
               p[e] = pack2(a, b);
+              if constexpr (TREE) rest[e] = pack2(a - __uint_as_float(p[e] << 16), b - __uint_as_float(p[e] & 0xffff0000u));
               sum[e & 1] = add2(sum[e & 1], f2(a, b));
             }
             tmem_st16(s_addr + buf * BN + 16 * c, p);
+            if constexpr (TREE) tmem_st16(s_addr + buf * BN + BN / 2 + 16 * c, rest);
           }
           const F2 both = add2(sum[0], sum[1]);
           z += lo(both) + hi(both);

@@ -35,7 +35,7 @@ def _reads(parents):
     return ok.cuda()
 
 
-def _verify(got, q, keys, values, lens, reads, cap):
+def _verify(got, q, keys, values, lens, reads, cap, weight=2.0 ** -8):
     B, Hq, n, d = q.shape
     group = Hq // keys.shape[1]
     for b, m in enumerate(lens):
@@ -43,7 +43,7 @@ def _verify(got, q, keys, values, lens, reads, cap):
         ok = torch.ones(n, total, dtype=torch.bool, device="cuda")
         ok[:, max(m, 0):] = reads[b][:, :max(0, total - max(m, 0))]
         for h in range(0, Hq, max(1, Hq // 5)):
-            want, tol = attend(q[b, h], keys[b, h // group, :total], values[b, h // group, :total], ok)
+            want, tol = attend(q[b, h], keys[b, h // group, :total], values[b, h // group, :total], ok, weight)
             err = (got[b, h].to(F64) - want).abs()
             assert bool((err <= tol).all()), (b, h, float((err / tol).max()))
 
@@ -51,6 +51,19 @@ def _verify(got, q, keys, values, lens, reads, cap):
 CASES = [(1, 1, 1, 1, 8, [0]), (1, 12, 12, 1, 300, [299]), (4, 12, 12, 1, 4096, [0, 1, 2048, 4095]), (3, 8, 2, 5, 700, [0, 127, 695]), (2, 32, 8, 16, 2000, [1984, 130]),
          (2, 4, 4, 64, 1000, [64, 936]), (1, 16, 1, 33, 500, [128]), (2, 40, 8, 7, 400, [121, 3]), (1, 64, 1, 64, 300, [200]), (1, 128, 1, 2, 260, [126]),
          (2, 9, 3, 31, 12000, [11900, 7]), (6, 2, 1, 3, 129, [126, 125, 0, 1, 60, 64]), (40, 4, 2, 2, 150, [3 * i for i in range(40)])]
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,n,cap,lens", [CASES[i] for i in (1, 2, 4, 5, 8, 10)], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("sharp", [0.02, 1.0, 4.0])
+def test_weights_are_not_rounded_to_bf16(B, Hq, Hkv, n, cap, lens, d, sharp):
+    # scores that hardly differ, so that weights lie side by side in a binade, and rows of few keys
+    q, keys, values = _inputs(B, Hq, Hkv, n, cap, d, seed=cap + 1)
+    q = (q.float() * sharp).to(BF)
+    got = T.tree_attention(q, keys, values, torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    chain = torch.ones(n, n, dtype=torch.bool, device="cuda").tril().expand(B, n, n)
+    _verify(got, q, keys, values, lens, chain, cap, weight=2.0 ** -16)
+    T.topk_check()
 
 
 @pytest.mark.parametrize("B,Hq,Hkv,n,cap,lens", CASES, ids=str)
