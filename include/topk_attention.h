@@ -471,7 +471,9 @@ int topk_token_logprobs_bwd(const void* logits, long long row_stride, const floa
  *   d        : 64 or 128.  Hq a multiple of Hkv, Hq / Hkv at most 128.
  * Keys and values outside a sequence are not read into its results, whatever they hold.  A key of the sequence that a query's
  * mask leaves out has weight 0: its value must be finite, as in any product (0 x infinity is NaN); its score need
- * not be.  Scores and sums in fp32; weights are rounded to bf16 as the tensor cores' operand (not in the softmax's sum).
+ * not be.  Scores and sums in fp32; the tensor cores' operands
+ * are the weights rounded to bf16 (not in the softmax's sum), or for up to 9,728 rows of heads (Tq Hq, on 152 SMs) as
+ * two bf16, within 2^-16.
  *   Scratch: topk_prompt_attn_workspace_bytes(), a fixed amount for each SM.
  */
 typedef struct {

@@ -27,14 +27,14 @@ def _edges(lens):
     return torch.tensor([0] + torch.tensor(lens).cumsum(0).tolist(), dtype=torch.int32, device="cuda")
 
 
-def _verify(got, q, k, v, lq, lk, causal, heads=None):
+def _verify(got, q, k, v, lq, lk, causal, heads=None, weight=2.0 ** -8):
     group = q.shape[1] // k.shape[1]
     at = bt = 0
     for n, m in zip(lq, lk):
         i, j = torch.arange(n, device="cuda"), torch.arange(m, device="cuda")
         ok = (j <= i[:, None] + m - n) if causal else torch.ones(n, m, dtype=torch.bool, device="cuda")
         for h in heads or range(q.shape[1]):
-            want, tol = attend(q[at:at + n, h], k[bt:bt + m, h // group], v[bt:bt + m, h // group], ok)
+            want, tol = attend(q[at:at + n, h], k[bt:bt + m, h // group], v[bt:bt + m, h // group], ok, weight)
             err = (got[at:at + n, h].to(F64) - want).abs()
             assert bool((err <= tol).all()), (n, m, h, float((err / tol).max()))
         at, bt = at + n, bt + m
@@ -53,6 +53,29 @@ def test_prompts(lens, Hq, Hkv, d, causal):
     got = T.prompt_attention(q, k, v, _edges(lens), causal=causal)
     T.topk_check()
     _verify(got, q, k, v, lens, lens, causal, heads=range(0, Hq, max(1, Hq // 6)))
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv", CASES[:11] + CASES[12:13] + CASES[14:], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_padded_to_more_rows(lens, Hq, Hkv, d, causal):
+    # the same prompts before so many rows of no sequence that weights are one bf16 each
+    q, k, v = _inputs(lens, lens, Hq, Hkv, d, seed=sum(lens), rest=76 * 152 // Hq)
+    got = T.prompt_attention(q, k, v, _edges(lens), causal=causal)
+    T.topk_check()
+    assert not got[sum(lens):].any()
+    _verify(got, q, k, v, lens, lens, causal, heads=range(0, Hq, max(1, Hq // 6)))
+
+
+@pytest.mark.parametrize("lq,lk,Hq,Hkv", [([1], [4000], 4, 1), ([200], [200], 12, 12), ([40, 3, 0, 61], [40, 1003, 5, 61], 16, 4)], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("sharp", [0.02, 1.0, 4.0])
+def test_weights_of_few_rows_are_not_rounded_to_bf16(lq, lk, Hq, Hkv, d, sharp):
+    # scores that hardly differ, so that weights lie side by side in a binade, and rows of few keys
+    q, k, v = _inputs(lq, lk, Hq, Hkv, d, seed=sum(lk), scale=1.5 * sharp)
+    got = T.prompt_attention(q, k, v, _edges(lq), _edges(lk))
+    T.topk_check()
+    _verify(got, q, k, v, lq, lk, True, weight=2.0 ** -16)
 
 
 @pytest.mark.parametrize("d", [64, 128])
