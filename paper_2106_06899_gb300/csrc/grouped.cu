@@ -843,7 +843,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 // a thread for each row.
 template <int D, bool TREE>
 __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant__ Work w) {
-  __shared__ float tops[kMostParts][32];  // a part's maximum, -inf where it has no key
+  __shared__ float weight[kMostParts][32];  // a part's maximum, -inf where it has no key; then what its O counts for
+  __shared__ long long to[32];              // where the rows go in out
   __shared__ float4 share[256];
   __shared__ float2 shared[8][32];  // the maximum and the sum over every eighth part
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -877,7 +878,7 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
     float m = mine.x;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      if (k0 + 8 * t < parts) tops[k0 + 8 * t][row] = zk[t] == 0.f ? -INFINITY : mk[t];
+      if (k0 + 8 * t < parts) weight[k0 + 8 * t][row] = zk[t] == 0.f ? -INFINITY : mk[t];
       m = fmaxf(m, mk[t]);
     }
     const float base = m == -INFINITY ? 0.f : m;
@@ -888,17 +889,29 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
   }
   shared[group][row] = mine;
   __syncthreads();
+  {
+    const int lists = min(8, parts);
+    float m = -INFINITY, z = 0.f;
+    for (int g = 0; g < lists; ++g) m = fmaxf(m, shared[g][row].x);
+    const float base = m == -INFINITY ? 0.f : m;
+    for (int g = 0; g < lists; ++g) z += shared[g][row].y == 0.f ? 0.f : shared[g][row].y * exp2_fast((shared[g][row].x - base) * kLog2e);
+    const float f = z == 0.f ? 0.f : 1.f / z;
+    for (int k = group; k < parts; k += 8) {
+      const float top = weight[k][row];
+      weight[k][row] = top == -INFINITY && z == z ? 0.f : exp2_fast((top - base) * kLog2e) * f;
+    }
+    if (group == 0) {
+      const int token = t0 + (row0 + row) / w.group, head = p.h * w.group + (row0 + row) % w.group;
+      to[row] = (TREE ? (static_cast<long long>(p.b) * w.Hq + head) * w.T + token : static_cast<long long>(s.q0 + token) * w.Hq + head) * D + c0;
+    }
+  }
+  __syncthreads();
 
   // 16 columns of four for each row; the rest of the block's threads take other parts
-  int wide = 1;
-  while (wide < rows) wide *= 2;
-  const int items = 16 * wide, lanes = items >= 256 ? 1 : 256 / items;  // lanes: over the parts
+  const int bits = 32 - __clz(rows - 1), wide = 1 << bits;  // rows <= wide <= 32
+  const int items = 16 * wide, lanes = max(1, 16 >> bits);  // lanes: over the parts
   for (int j = threadIdx.x; j < items * lanes; j += 256) {
-    const int r = j % wide, c = j / wide % 16, lane = j / items;
-    float m = -INFINITY;
-#pragma unroll
-    for (int g = 0; g < 8; ++g) m = fmaxf(m, shared[g][r].x);
-    const float base = m == -INFINITY ? 0.f : m;
+    const int r = j & (wide - 1), c = j >> bits & 15, lane = j >> (bits + 4);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r < rows)
       for (int k0 = lane; k0 < parts; k0 += 4 * lanes) {
@@ -906,14 +919,13 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const int k = k0 + t * lanes;
-          if (k < parts && tops[k][r] > -INFINITY) v[t] = __ldcg(reinterpret_cast<const float4*>(part(k)) + (c0 / 4 + c) * 256 + at0 + r);
+          if (k < parts && weight[k][r] != 0.f) v[t] = __ldcg(reinterpret_cast<const float4*>(part(k)) + (c0 / 4 + c) * 256 + at0 + r);
         }
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const int k = k0 + t * lanes;
-          if (k >= parts || tops[k][r] == -INFINITY) continue;
-          const float f = exp2_fast((tops[k][r] - base) * kLog2e);
-          o.x += v[t].x * f, o.y += v[t].y * f, o.z += v[t].z * f, o.w += v[t].w * f;
+          const float f = k < parts ? weight[k][r] : 0.f;
+          if (f != 0.f) o.x += v[t].x * f, o.y += v[t].y * f, o.z += v[t].z * f, o.w += v[t].w * f;
         }
       }
     if (lanes > 1) {
@@ -924,16 +936,7 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
         o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
       }
     }
-    if (lane == 0 && r < rows) {
-      float sum = 0.f;
-#pragma unroll
-      for (int g = 0; g < 8; ++g) sum += shared[g][r].y == 0.f ? 0.f : shared[g][r].y * exp2_fast((shared[g][r].x - base) * kLog2e);
-      const float f = sum == 0.f ? 0.f : 1.f / sum;
-      const int token = t0 + (row0 + r) / w.group, head = p.h * w.group + (row0 + r) % w.group;
-      __nv_bfloat16* out =
-          w.out + (TREE ? (static_cast<size_t>(p.b) * w.Hq + head) * w.T + token : static_cast<size_t>(s.q0 + token) * w.Hq + head) * D + c0 + 4 * c;
-      *reinterpret_cast<uint2*>(out) = make_uint2(pack2(o.x * f, o.y * f), pack2(o.z * f, o.w * f));
-    }
+    if (lane == 0 && r < rows) *reinterpret_cast<uint2*>(w.out + to[r] + 4 * c) = make_uint2(pack2(o.x, o.y), pack2(o.z, o.w));
   }
 }
 
