@@ -838,11 +838,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Joins a unit's parts.  Block (i, y) looks at the place where CTA i + 1's run begins: where that is the first such place
-// inside its unit, it adds up the unit's parts, for 64 of the columns and 32 of the rows.  A few rows of many parts (one token over
-// a long cache) are shared out over the parts, and the shares added in order: 152 parts of 6 rows take 6 us, 120 with
-// a thread for each row.
+// inside its unit, it adds up the unit's parts, for 4 2^fours of the columns and 32 of the rows.  Few rows of many parts (one token over
+// a long cache) are shared out over the parts, and the shares added in order.  The time is that of a few loads behind one
+// another: 18 us for 151 units of 256 rows and 2 or 3 parts, 6 for single tokens of 4 sequences.
 template <int D, bool TREE>
-__global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant__ Work w) {
+__global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant__ Work w, int fours) {
   __shared__ float weight[kMostParts][32];  // a part's maximum, -inf where it has no key; then what its O counts for
   __shared__ long long to[32];              // where the rows go in out
   __shared__ float4 share[256];
@@ -855,7 +855,7 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
   const long long first = run_start(p.total, p.ctas, i) - p.kt, last = first + block_tiles<TREE>(w, s, p.block);
   if (run_start(p.total, p.ctas, i - 1) > first) return;
   // rows of this block: at most 32 of tile x
-  const int c0 = blockIdx.y % (D / 64) * 64, at0 = blockIdx.y / (D / 64) * 32, x = at0 / BM, row0 = at0 % BM;
+  const int slices = D / 4 >> fours, c0 = blockIdx.y % slices << (fours + 2), at0 = blockIdx.y / slices * 32, x = at0 / BM, row0 = at0 % BM;
   const int t0 = (2 * p.block + x) * w.tokens;
   const int rows = min(32, min(w.tokens, s.Lq - t0) * w.group - row0);
   if (rows <= 0) return;
@@ -907,11 +907,11 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
   }
   __syncthreads();
 
-  // 16 columns of four for each row; the rest of the block's threads take other parts
+  // 2^fours columns of four for each row; the rest of the block's threads take other parts
   const int bits = 32 - __clz(rows - 1), wide = 1 << bits;  // rows <= wide <= 32
-  const int items = 16 * wide, lanes = max(1, 16 >> bits);  // lanes: over the parts
+  const int items = wide << fours, lanes = max(1, 256 / items);  // lanes: over the parts
   for (int j = threadIdx.x; j < items * lanes; j += 256) {
-    const int r = j & (wide - 1), c = j >> bits & 15, lane = j >> (bits + 4);
+    const int r = j & (wide - 1), c = j >> bits & ((1 << fours) - 1), lane = j >> (bits + fours);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r < rows)
       for (int k0 = lane; k0 < parts; k0 += 4 * lanes) {
@@ -953,7 +953,7 @@ bool make_map(CUtensorMap* map, const void* base, uint64_t n0, uint64_t n1, long
 }
 
 template <int D, bool TREE, bool REST>
-int launch(const CUtensorMap& tmq, const CUtensorMap& tmk, const CUtensorMap& tmv, const Work& w, int grid, const DevCtl& ctl, cudaStream_t st) {
+int launch(const CUtensorMap& tmq, const CUtensorMap& tmk, const CUtensorMap& tmv, const Work& w, int grid, int fours, const DevCtl& ctl, cudaStream_t st) {
   using L = Layout<D, TREE>;
   const auto kernel = grouped_kernel<D, TREE, REST>;
   int device = 0;
@@ -969,12 +969,12 @@ int launch(const CUtensorMap& tmq, const CUtensorMap& tmk, const CUtensorMap& tm
   cudaLaunchConfig_t config = {};
   // rows that a unit can have: the second tile's begin at 128
   const int rows = TREE && w.T <= w.tokens ? w.T * w.group : 2 * BM;
-  config.gridDim = dim3(grid - 1, D / 64 * ((rows + 31) / 32)), config.blockDim = dim3(256), config.stream = st;
+  config.gridDim = dim3(grid - 1, (D / 4 >> fours) * ((rows + 31) / 32)), config.blockDim = dim3(256), config.stream = st;
   cudaLaunchAttribute early = {};
   early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   early.val.programmaticStreamSerializationAllowed = 1;
   config.attrs = &early, config.numAttrs = 1;
-  return cudaLaunchKernelEx(&config, grouped_join_kernel<D, TREE>, w) == cudaSuccess ? 2 : -1;
+  return cudaLaunchKernelEx(&config, grouped_join_kernel<D, TREE>, w, fours) == cudaSuccess ? 2 : -1;
 }
 
 }  // namespace
@@ -999,8 +999,8 @@ int prompt_attn(const topk_prompt_args& a, void* workspace, int num_sms, const D
   // The weights' rests double the products with the values: 2 % more time for 128 tokens of 32 heads (16.7 us), 7 % for 1,024, where the result's
   // error falls from 2.1e-3 to 1.6e-3, its own rounding; 21 % for 16,384 tokens.  So prompts of few rows have them.
   const bool few = static_cast<long long>(a.Tq) * a.Hq <= BM / 2 * num_sms;
-  if (a.d == 64) return few ? launch<64, false, true>(q, k, v, w, num_sms, ctl, st) : launch<64, false, false>(q, k, v, w, num_sms, ctl, st);
-  return few ? launch<128, false, true>(q, k, v, w, num_sms, ctl, st) : launch<128, false, false>(q, k, v, w, num_sms, ctl, st);
+  if (a.d == 64) return few ? launch<64, false, true>(q, k, v, w, num_sms, 4, ctl, st) : launch<64, false, false>(q, k, v, w, num_sms, 4, ctl, st);
+  return few ? launch<128, false, true>(q, k, v, w, num_sms, 4, ctl, st) : launch<128, false, false>(q, k, v, w, num_sms, 4, ctl, st);
 }
 
 int tree_attn(const topk_tree_args& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
@@ -1016,10 +1016,12 @@ int tree_attn(const topk_tree_args& a, void* workspace, int num_sms, const DevCt
       !make_map(&k, a.keys, a.d, a.cap, a.key_stride[2], a.Hkv, a.key_stride[1], a.B, a.key_stride[0], BN, 1) ||
       !make_map(&v, a.values, a.d, a.cap, a.value_stride[2], a.Hkv, a.value_stride[1], a.B, a.value_stride[0], BN, 1))
     return -1;
-  // key tiles of all units at most
-  const long long most = static_cast<long long>(a.B) * a.Hkv * ((a.T + 2 * w.tokens - 1) / (2 * w.tokens)) * ((a.cap + BN - 1) / BN);
+  const long long units = static_cast<long long>(a.B) * a.Hkv * ((a.T + 2 * w.tokens - 1) / (2 * w.tokens)), most = units * ((a.cap + BN - 1) / BN);  // key tiles
   const int grid = static_cast<int>(most < num_sms ? most : num_sms);
-  return a.d == 64 ? launch<64, true, true>(q, k, v, w, grid, ctl, st) : launch<128, true, true>(q, k, v, w, grid, ctl, st);
+  // units of 16 parts and more are joined by blocks of 16 columns: 2 units of six rows over up to 55,568 keys
+  // take 22 us in place of 28; 48 units (single tokens of 4 sequences), of four parts, would take 27 in place of 25
+  const int fours = units * 16 <= grid ? 2 : 4;
+  return a.d == 64 ? launch<64, true, true>(q, k, v, w, grid, fours, ctl, st) : launch<128, true, true>(q, k, v, w, grid, fours, ctl, st);
 }
 
 }  // namespace topk
