@@ -19,6 +19,9 @@ log probabilities with their gradient (topk_token_logprobs_fwd / _bwd).
 
 The library's gradients have no gradients of their own: a second differentiation through one of these functions is
 an error.
+A training step may be captured into a CUDA graph while no earlier eager graph of the same parameters is alive (drop the
+losses of warm-up steps first, and run them on the capturing stream): PyTorch adds up a leaf's gradient on the stream where
+its first graph was made, which ends a capture on another one.
 """
 from __future__ import annotations
 
