@@ -33,6 +33,14 @@ constexpr int kThreads = 384;     // loads, scores, products of each tile with t
 constexpr float kRaise = 8.0f;    // natural-log units
 constexpr float kLog2e = 1.4426950408889634f;
 
+// Where a CTA's run of steps begins, of how many steps and CTAs with work.
+struct Place {
+  int b, h, block, kt;
+  long long total;
+  int ctas;
+  int q0, Lq, tiles;  // of the sequence, and of the unit: for the join
+};
+
 template <int D, bool TREE>
 struct Layout {
   static constexpr int R = D / 64;                 // blocks of 128 bytes of a row
@@ -45,9 +53,10 @@ struct Layout {
   static constexpr size_t OFF_STAGE = OFF_RING + static_cast<size_t>(S) * TILE;
   static constexpr size_t OFF_BAR = OFF_STAGE + 8 * STAGE;
   static constexpr int NBARS = 2 * S + 22;
-  static constexpr size_t OFF_EXCH = OFF_BAR + NBARS * 8 + 64;
+  static constexpr size_t OFF_EXCH = OFF_BAR + NBARS * 8 + 64;  // flags and the place between them
   static constexpr size_t BYTES = 1024 + OFF_EXCH + BM * 8;
   static_assert(BYTES <= 232448, "shared memory");
+  static_assert(2 * sizeof(int) + sizeof(Place) + sizeof(long long) <= 64, "between the barriers and the exchange");
   static_assert(S >= 8 && S % 2 == 0, "scores run at most three steps ahead of the products with the values; keys lie in the even slots");
   // TMEM columns: two score buffers of each tile, two outputs
   static constexpr uint32_t O_COL = 4 * BN;
@@ -59,13 +68,6 @@ template <int D>
 constexpr size_t kPartFloats = 256 * (D + 2);
 
 constexpr int kMostParts = 160;  // of a unit: one from each CTA, of which there are no more than SMs (152)
-
-// Where a CTA's run of steps begins, of how many steps and CTAs with work.
-struct Place {
-  int b, h, block, kt;
-  long long total;
-  int ctas;
-};
 
 struct Work {
   const int32_t* q_starts;   // prompts
@@ -203,7 +205,7 @@ __device__ Place locate(const Work& w, int i, int grid, unsigned* error) {
     const unsigned at = __ballot_sync(0xffffffffu, upto > left);
     if (at) {
       const int k = __ffs(at) - 1;
-      int h = 0, block = 0, kt = 0;
+      int h = 0, block = 0, kt = 0, tiles = 0;
       if (lane == k) {
         left -= upto - mine;
         const long long head = quotient(mine, w.Hkv);
@@ -219,11 +221,15 @@ __device__ Place locate(const Work& w, int i, int grid, unsigned* error) {
         }
         block = lo;
         kt = static_cast<int>(left - tiles_before<TREE>(w, s, lo));
+        tiles = block_tiles<TREE>(w, s, lo);
       }
       p.b = b0 + k;
       p.h = __shfl_sync(0xffffffffu, h, k);
       p.block = __shfl_sync(0xffffffffu, block, k);
       p.kt = __shfl_sync(0xffffffffu, kt, k);
+      p.q0 = __shfl_sync(0xffffffffu, s.q0, k);
+      p.Lq = __shfl_sync(0xffffffffu, s.Lq, k);
+      p.tiles = __shfl_sync(0xffffffffu, tiles, k);
       return p;
     }
     left -= __shfl_sync(0xffffffffu, upto, 31);
@@ -438,6 +444,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_mbar_init();
   }
   if (warp == 1) tmem_alloc(tmem_slot, L::COLS);
+  if (warp == 3 && lane < 3) tma_prefetch_desc(lane == 0 ? &tmq : lane == 1 ? &tmk : &tmv);
   if (warp == 2) {
     const Place p = locate<TREE>(w, blockIdx.x, gridDim.x, blockIdx.x == 0 ? ctl.error : nullptr);
     if (lane == 0) {
@@ -458,9 +465,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 0) {
     // ------------------------------------------------------------ loads
     if (elect_one()) {
-      tma_prefetch_desc(&tmq);
-      tma_prefetch_desc(&tmk);
-      tma_prefetch_desc(&tmv);
       Run<TREE> run(w, place, steps);
       Segment seg;
       uint32_t it = 0, segs = 0;  // ring tiles and units' queries loaded
@@ -851,13 +855,12 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
   const int i = blockIdx.x + 1;
   const Place p = w.places[i];
   if (i >= p.ctas || p.kt == 0) return;
-  const Seq s = seq_of<TREE>(w, p.b);
-  const long long first = run_start(p.total, p.ctas, i) - p.kt, last = first + block_tiles<TREE>(w, s, p.block);
+  const long long first = run_start(p.total, p.ctas, i) - p.kt, last = first + p.tiles;
   if (run_start(p.total, p.ctas, i - 1) > first) return;
   // rows of this block: at most 32 of tile x
   const int slices = D / 4 >> fours, c0 = blockIdx.y % slices << (fours + 2), at0 = blockIdx.y / slices * 32, x = at0 / BM, row0 = at0 % BM;
   const int t0 = (2 * p.block + x) * w.tokens;
-  const int rows = min(32, min(w.tokens, s.Lq - t0) * w.group - row0);
+  const int rows = min(32, min(w.tokens, p.Lq - t0) * w.group - row0);
   if (rows <= 0) return;
   // CTAs i - 1 .. end - 1 have parts: run_start(end) is the first that is not below `last`
   const int end = min(p.ctas, static_cast<int>(quotient(last * p.ctas + p.total - 1, p.total)));
@@ -902,7 +905,7 @@ __global__ void __launch_bounds__(256) grouped_join_kernel(const __grid_constant
     }
     if (group == 0) {
       const int token = t0 + (row0 + row) / w.group, head = p.h * w.group + (row0 + row) % w.group;
-      to[row] = (TREE ? (static_cast<long long>(p.b) * w.Hq + head) * w.T + token : static_cast<long long>(s.q0 + token) * w.Hq + head) * D + c0;
+      to[row] = (TREE ? (static_cast<long long>(p.b) * w.Hq + head) * w.T + token : static_cast<long long>(p.q0 + token) * w.Hq + head) * D + c0;
     }
   }
   __syncthreads();

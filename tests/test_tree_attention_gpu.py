@@ -77,6 +77,20 @@ def test_trees(B, Hq, Hkv, n, cap, lens, d):
     _verify(got, q, keys, values, lens, _reads(parents), cap)
 
 
+@pytest.mark.parametrize("Hq,Hkv,n", [(4, 1, 8), (32, 1, 1), (31, 1, 1), (33, 1, 1), (11, 1, 3), (2, 2, 32), (2, 2, 33), (3, 3, 31)], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+def test_few_rows(Hq, Hkv, n, d):
+    cap, lens = 1400, [0, 1, 63, 64, 65, 127, 128, -1, 1300, 1200, 190, 700]
+    q, keys, values = _inputs(len(lens), Hq, Hkv, n, cap, d, seed=n)
+    parents = _parents(len(lens), n, seed=Hq)
+    for b, m in enumerate(lens):
+        keys[b, :, max(0, m + n) if m >= 0 else 0:] = math.nan
+        values[b, :, max(0, m + n) if m >= 0 else 0:] = math.nan
+    got = T.tree_attention(q, keys, values, torch.tensor(lens, dtype=torch.int32, device="cuda"), tree=T.tree_mask(parents).cuda())
+    T.topk_check()
+    _verify(got, q, keys, values, lens, _reads(parents), cap, weight=2.0 ** -16)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_chain(d):
     # without a tree a token reads those before it: the last tokens of a causal sequence
