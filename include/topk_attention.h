@@ -502,7 +502,7 @@ size_t topk_prompt_attn_workspace_bytes(int d);
  *   T            : 1 to 64.  d, Hq and Hkv as above.
  * Rows of the cache that a sequence does not have are not read into its results, whatever they hold; drafted values that a
  * token does not read must be finite (as in topk_prompt_attn_fwd).  The weights are the tensor cores' operands as two bf16
- * each, within 2^-16.
+ * each, within 2^-16, for T Hq / Hkv of up to 128, and rounded to bf16 for more.
  *   Scratch: topk_prompt_attn_workspace_bytes().
  */
 typedef struct {

@@ -8,7 +8,7 @@
 //   P = 2^(S - m)  four warps, a row each thread, written over S as the bf16 operand that the next product
 //                  reads from TMEM;
 //   O += P V       tcgen05.mma, V as it lies in memory (its keys are the sum: the instruction transposes).
-// With REST (over caches, which memory bounds, and for short prompts) P is two bf16, the rounded weight and the rest, with a
+// With REST (over caches, where memory bounds the call, and for short prompts) P is two bf16, the rounded weight and the rest, with a
 // product each: the result is then rounded once, where a single bf16 is a second rounding of the same size.
 // While the warps of one tile are at its exponentials, the tensor pipe works for the other.  A row's running maximum
 // m is raised only when a tile's exceeds it by more than kRaise; O and the sum are scaled then.
@@ -1024,7 +1024,11 @@ int tree_attn(const topk_tree_args& a, void* workspace, int num_sms, const DevCt
   // units of 16 parts and more are joined by blocks of 16 columns: 2 units of six rows over up to 55,568 keys
   // take 22 us in place of 28; 48 units (single tokens of 4 sequences), of four parts, would take 27 in place of 25
   const int fours = units * 16 <= grid ? 2 : 4;
-  return a.d == 64 ? launch<64, true, true>(q, k, v, w, grid, fours, ctl, st) : launch<128, true, true>(q, k, v, w, grid, fours, ctl, st);
+  // Memory bounds units of one tile, with or without the weights' rests (32 tokens of 4 heads a key head, 16 sequences of 16,384 rows: 174 and
+  // 175 us); units of more rows the products (64 tokens: 261 us with, 208 without).
+  const bool rest = a.T * w.group <= BM;
+  if (a.d == 64) return rest ? launch<64, true, true>(q, k, v, w, grid, fours, ctl, st) : launch<64, true, false>(q, k, v, w, grid, fours, ctl, st);
+  return rest ? launch<128, true, true>(q, k, v, w, grid, fours, ctl, st) : launch<128, true, false>(q, k, v, w, grid, fours, ctl, st);
 }
 
 }  // namespace topk
