@@ -775,7 +775,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int head = seg.h * w.group + head_in;
         __nv_bfloat16* out = w.out + (TREE ? (static_cast<size_t>(seg.b) * w.Hq + head) * w.T + token : static_cast<size_t>(seg.seq.q0 + token) * w.Hq + head) * D;
         // Rows lie apart: a lane that stored its own row would make a warp's store touch 32 lines, which the load/store unit
-        // takes one a cycle (4,700 cycles a unit of 128 columns, now 1,000).  Prompts' rows go through shared memory, eight lanes to a row.
+        // takes one a cycle (4,700 cycles a unit of 128 columns, 3,600 this way).  Prompts' rows go through shared memory, eight lanes to a row.
         if (mine) {
 #pragma unroll 1
           for (int c = 0; c < D; c += TREE ? 32 : 64) {
