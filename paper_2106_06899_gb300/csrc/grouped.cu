@@ -8,8 +8,9 @@
 //   P = 2^(S - m)  four warps, a row each thread, written over S as the bf16 operand that the next product
 //                  reads from TMEM;
 //   O += P V       tcgen05.mma, V as it lies in memory (its keys are the sum: the instruction transposes).
-// With REST (over caches, where memory bounds the call, and for short prompts) P is two bf16, the rounded weight and the rest, with a
-// product each: the result is then rounded once, where a single bf16 is a second rounding of the same size.
+// P is two bf16, the rounded weight and the rest, with a product each: the result is then rounded once, where a single bf16 is a
+// second rounding of the same size (error against 64 bits 1.6e-3 in place of 2.1e-3).  This is so for every call, so that what a
+// sequence gets does not depend on how much it is packed with.
 // While the warps of one tile are at its exponentials, the tensor pipe works for the other.  A row's running maximum
 // m is raised only when a tile's exceeds it by more than kRaise; O and the sum are scaled then.
 //
@@ -404,7 +405,7 @@ __device__ __forceinline__ void key_bits(uint32_t (&bits)[BN / 32], int j0, int 
 }
 
 // ------------------------------------------------------------ the kernel
-template <int D, bool TREE, bool REST>
+template <int D, bool TREE>
 __global__ void __launch_bounds__(kThreads, 1)
     grouped_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv,
                    const __grid_constant__ Work w, DevCtl ctl) {
@@ -591,7 +592,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc_fence_after();
           const uint64_t vd = ring_v + at.slot * (L::TILE >> 4);
 #pragma unroll
-          for (int k = 0; k < (REST ? 2 : 1) * (BN / 16); ++k)  // the weights, and their rests
+          for (int k = 0; k < 2 * (BN / 16); ++k)  // the weights, and their rests
             mma_bf16_ts(tmem + L::O_COL + x * D, tmem + buf * BN + k * 8, vd + ((k % (BN / 16) * 2048) >> 4), IDESC_O, first && k == 0 ? 0u : 1u);
           mma_commit(&pv_done[buf]);
           mma_commit(&empty[at.slot]);
@@ -706,17 +707,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           F2 sum[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
 #pragma unroll
           for (int c = 0; c < BN / 32; ++c) {
-            uint32_t p[16], rest[REST ? 16 : 1];
+            uint32_t p[16], rest[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               const F2 d = fma2(f2(s[32 * c + 2 * e], s[32 * c + 2 * e + 1]), scale, minus);
               const float a = exp2_fast(lo(d)), b = exp2_fast(hi(d));
               p[e] = pack2(a, b);
-              if constexpr (REST) rest[e] = pack2(a - __uint_as_float(p[e] << 16), b - __uint_as_float(p[e] & 0xffff0000u));
+              rest[e] = pack2(a - __uint_as_float(p[e] << 16), b - __uint_as_float(p[e] & 0xffff0000u));
               sum[e & 1] = add2(sum[e & 1], f2(a, b));
             }
             tmem_st16(s_addr + buf * BN + 16 * c, p);
-            if constexpr (REST) tmem_st16(s_addr + buf * BN + BN / 2 + 16 * c, rest);
+            tmem_st16(s_addr + buf * BN + BN / 2 + 16 * c, rest);
           }
           const F2 both = add2(sum[0], sum[1]);
           z += lo(both) + hi(both);
@@ -968,10 +969,10 @@ bool make_map(CUtensorMap* map, const void* base, uint64_t n0, uint64_t n1, long
                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool TREE, bool REST>
+template <int D, bool TREE>
 int launch(const CUtensorMap& tmq, const CUtensorMap& tmk, const CUtensorMap& tmv, const Work& w, int grid, int fours, const DevCtl& ctl, cudaStream_t st) {
   using L = Layout<D, TREE>;
-  const auto kernel = grouped_kernel<D, TREE, REST>;
+  const auto kernel = grouped_kernel<D, TREE>;
   int device = 0;
   static std::atomic<unsigned long long> ready{0};  // a bit for each device whose kernel may take the shared memory
   if (cudaGetDevice(&device) != cudaSuccess) return -1;
@@ -1012,11 +1013,7 @@ int prompt_attn(const topk_prompt_args& a, void* workspace, int num_sms, const D
       !make_map(&k, a.k, a.d, a.Tk, a.k_stride[0], a.Hkv, a.k_stride[1], 1, 0, BN, 1) ||
       !make_map(&v, a.v, a.d, a.Tk, a.v_stride[0], a.Hkv, a.v_stride[1], 1, 0, BN, 1))
     return -1;
-  // The weights' rests double the products with the values: 2 % more time for 128 tokens of 32 heads (16.7 us), 7 % for 1,024, where the result's
-  // error falls from 2.1e-3 to 1.6e-3, its own rounding; 21 % for 16,384 tokens.  So prompts of few rows have them.
-  const bool few = static_cast<long long>(a.Tq) * a.Hq <= BM / 2 * num_sms;
-  if (a.d == 64) return few ? launch<64, false, true>(q, k, v, w, num_sms, 4, ctl, st) : launch<64, false, false>(q, k, v, w, num_sms, 4, ctl, st);
-  return few ? launch<128, false, true>(q, k, v, w, num_sms, 4, ctl, st) : launch<128, false, false>(q, k, v, w, num_sms, 4, ctl, st);
+  return a.d == 64 ? launch<64, false>(q, k, v, w, num_sms, 4, ctl, st) : launch<128, false>(q, k, v, w, num_sms, 4, ctl, st);
 }
 
 int tree_attn(const topk_tree_args& a, void* workspace, int num_sms, const DevCtl& ctl, cudaStream_t st) {
@@ -1037,11 +1034,7 @@ int tree_attn(const topk_tree_args& a, void* workspace, int num_sms, const DevCt
   // units of 16 parts and more are joined by blocks of 16 columns: 2 units of six rows over up to 55,568 keys
   // take 22 us in place of 28; 48 units (single tokens of 4 sequences), of four parts, would take 27 in place of 25
   const int fours = units * 16 <= grid ? 2 : 4;
-  // Memory bounds units of one tile, with or without the weights' rests (32 tokens of 4 heads a key head, 16 sequences of 16,384 rows: 174 and
-  // 175 us); units of more rows the products (64 tokens: 261 us with, 208 without).
-  const bool rest = a.T * w.group <= BM;
-  if (a.d == 64) return rest ? launch<64, true, true>(q, k, v, w, grid, fours, ctl, st) : launch<64, true, false>(q, k, v, w, grid, fours, ctl, st);
-  return rest ? launch<128, true, true>(q, k, v, w, grid, fours, ctl, st) : launch<128, true, false>(q, k, v, w, grid, fours, ctl, st);
+  return a.d == 64 ? launch<64, true>(q, k, v, w, grid, fours, ctl, st) : launch<128, true>(q, k, v, w, grid, fours, ctl, st);
 }
 
 }  // namespace topk
