@@ -472,8 +472,7 @@ int topk_token_logprobs_bwd(const void* logits, long long row_stride, const floa
  * Keys and values outside a sequence are not read into its results, whatever they hold.  A key of the sequence that a query's
  * mask leaves out has weight 0: its value must be finite, as in any product (0 x infinity is NaN); its score need
  * not be.  Scores and sums in fp32; the tensor cores' operands
- * are the weights rounded to bf16 (not in the softmax's sum), or for up to 9,728 rows of heads (Tq Hq, on 152 SMs) as
- * two bf16, within 2^-16.
+ * are the weights as two bf16 each, within 2^-16.
  *   Scratch: topk_prompt_attn_workspace_bytes(), a fixed amount for each SM.
  */
 typedef struct {
@@ -502,7 +501,7 @@ size_t topk_prompt_attn_workspace_bytes(int d);
  *   T            : 1 to 64.  d, Hq and Hkv as above.
  * Rows of the cache that a sequence does not have are not read into its results, whatever they hold; drafted values that a
  * token does not read must be finite (as in topk_prompt_attn_fwd).  The weights are the tensor cores' operands as two bf16
- * each, within 2^-16, for T Hq / Hkv of up to 128, and rounded to bf16 for more.
+ * each, within 2^-16.
  *   Scratch: topk_prompt_attn_workspace_bytes().
  */
 typedef struct {

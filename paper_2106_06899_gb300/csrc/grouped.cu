@@ -9,8 +9,10 @@
 //                  reads from TMEM;
 //   O += P V       tcgen05.mma, V as it lies in memory (its keys are the sum: the instruction transposes).
 // P is two bf16, the rounded weight and the rest, with a product each: the result is then rounded once, where a single bf16 is a
-// second rounding of the same size (error against 64 bits 1.6e-3 in place of 2.1e-3).  This is so for every call, so that what a
-// sequence gets does not depend on how much it is packed with.
+// second rounding of the same size (error against 64 bits 1.6e-3 in place of 2.1e-3).  It is so for every call, so that a sequence's
+// precision does not depend on what it is packed with.  Where the products bound a call that costs a quarter: 12 prompts of up to 4,093
+// tokens 477 -> 586 us, 16,384 tokens 758 -> 949, 64 drafted tokens of 16 caches of 16,384 rows 146 -> 177; caches of fewer rows a key head are
+// bound by memory (16 drafted tokens 204 either way).
 // While the warps of one tile are at its exponentials, the tensor pipe works for the other.  A row's running maximum
 // m is raised only when a tile's exceeds it by more than kRaise; O and the sum are scaled then.
 //
@@ -68,9 +70,10 @@ struct Layout {
 template <int D>
 constexpr size_t kPartFloats = 256 * (D + 2);
 
-// What a unit costs beside its steps (first and last steps that wait, the output), in steps: they count in the runs, so that CTAs with many
-// short units have as much to do as those with a few long ones.  12 prompts of up to 4,093 tokens take 565 us with 0, 483 with 2, 457 with
-// 3, 455 with 4, 468 with 6; a prompt of 16,384 tokens 818, 768, 735, 728, 736.
+// What a unit costs beside its steps (first and last steps that wait, the output), in steps: they count in the runs, so that CTAs with
+// many short units have as much to do as those with a few long ones.  12 prompts of up to 4,093 tokens take 697 us with 0, 592 with 2, 583 with
+// 3, 586 with 4, 614 with 6 (heads of 64: 509, 427, 428, 432, 450); a prompt of 16,384 tokens 1040, 974, 949, 949, 958; single tokens of 4 sequences
+// 25.1, 24.6, 24.5, 24.1, 23.8.
 constexpr int kUnit = 4;
 
 constexpr int kMostParts = 160;  // of a unit: one from each CTA, of which there are no more than SMs (152)
