@@ -155,7 +155,9 @@ struct Running {
         t = f == 0.f ? 0.f : f * fmaf(d, s, t), s *= f;
       }
       r = top;
-      floor = top - 300.f / c - fabsf(top) * 0.03125f;  // the last part outlasts its rounding
+      // as a bf16, as at_least takes it (a finite one that rounds to -inf there would leave -inf elements, and 0 x -inf, in the sums); the last
+      // part outlasts the rounding
+      floor = __bfloat162float(__float2bfloat16_rn(top - 300.f / c - fabsf(top) * 0.03125f));
     }
   }
   // the vector's elements, `most` the largest of them
@@ -442,7 +444,8 @@ __global__ void __launch_bounds__(kThreads, 4)
   const auto log_p = [&](float v) { return bad ? NAN : v == -INFINITY ? -INFINITY : fmaf(v - all.r, a.scale, -ln_s); };
   if (threadIdx.x == 0) {
     if (lse) lse[n] = bad ? NAN : none ? -INFINITY : fmaf(all.r, a.scale, ln_s);
-    if (entropy) entropy[n] = bad ? NAN : none ? 0.f : fmaxf(ln_s - kLn2 * all.t / all.s, 0.f);
+    const float h = ln_s - kLn2 * all.t / all.s;
+    if (entropy) entropy[n] = bad ? NAN : none || h < 0.f ? 0.f : h;  // a NaN stays one
     const long long target = target_at(a, n);
     if (target >= a.V) atomicOr(ctl.error, kDevErrRange);
     if (logp) logp[n] = target >= 0 && target < a.V ? log_p(to_f(x[target])) : 0.f;
