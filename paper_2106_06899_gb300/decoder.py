@@ -25,10 +25,25 @@ its first graph was made, which ends a capture on another one.
 """
 from __future__ import annotations
 
+import itertools
+
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import topk as T
+
+
+def _tangents(tensors) -> bool:
+    """Whether one of the tensors (or None) has a forward-mode tangent, which the library's calls would drop."""
+    if getattr(forward_ad, "_current_level", 0) < 0:  # outside of every dual level: 0.1 us in place of 0.3 for each tensor
+        return False
+    return any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
+
+
+def _derived(*tensors) -> bool:
+    """Whether a derivative by one of the tensors (or None) is wanted: a gradient, or a tangent, which the functions below refuse."""
+    return (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)) or _tangents(tensors)
 
 
 class TopKAttentionFunction(torch.autograd.Function):
@@ -93,8 +108,8 @@ class LinearFunction(torch.autograd.Function):
 
 
 def linear(x, w, act: str = "none", residual=None):
-    """LinearFunction where a gradient is wanted, else the library's call, which then keeps nothing."""
-    if torch.is_grad_enabled() and (x.requires_grad or w.requires_grad or (residual is not None and residual.requires_grad)):
+    """LinearFunction where a derivative is wanted, else the library's call, which then keeps nothing."""
+    if _derived(x, w, residual):
         return LinearFunction.apply(x, w, act, residual)
     return T.linear(x, w, act=act, residual=residual)
 
@@ -325,9 +340,15 @@ class Decoder(torch.nn.Module):
         if self.vocab is None or x.is_floating_point():
             return x
         x, scale = x.contiguous(), self.embedding.shape[1] ** 0.5
-        if torch.is_grad_enabled() and self.embedding.requires_grad:
+        if _derived(self.embedding):
             return EmbeddingFunction.apply(x, self.embedding, scale)
         return T.embedding(x, self.embedding, scale=scale)
+
+    def _served(self, x):
+        """_features for calls that have no derivatives."""
+        if _tangents(itertools.chain((x,), self.parameters())):
+            raise NotImplementedError("generation has no forward-mode derivative")
+        return self._features(x)
 
     def forward(self, x):
         x = self._features(x)
@@ -342,7 +363,7 @@ class Decoder(torch.nn.Module):
             raise ValueError("logprobs() needs a vocabulary")
         logits = linear(features.reshape(-1, features.shape[-1]), self.embedding)
         targets = None if targets is None else targets.reshape(-1)
-        if torch.is_grad_enabled() and logits.requires_grad:
+        if _derived(logits):
             return T.TokenLogProbs(*TokenLogProbsFunction.apply(logits, targets, top, scale))
         return T.token_logprobs(logits, targets, top=top, scale=scale)
 
@@ -358,7 +379,7 @@ class Decoder(torch.nn.Module):
         caches (new_cache) holding the tokens before; returns [B, d_model] and leaves the token in the caches."""
         if not self.fused:
             raise ValueError("step() needs a fused decoder")
-        x = self._features(x)
+        x = self._served(x)
         positions = start.view(1, -1, 1)
         for layer, cache in zip(self.layers, caches):
             x = layer.step(x, cache, start, positions, self.tables)
@@ -375,7 +396,7 @@ class Decoder(torch.nn.Module):
             raise ValueError("starts must have from one to the caches' number of sequences, and an end")
         if n > cap and int((ends[1:] - ends[:-1]).max()) > cap:  # the host waits for the lengths only where they could be too long
             raise ValueError("the caches have no room for the longest prompt")
-        x = self._features(x)
+        x = self._served(x)
         # rows of no sequence write what the nearest token of one does
         token = torch.minimum(torch.maximum(torch.arange(n, device=x.device), ends[0]), (ends[-1] - 1).clamp_min(0)).clamp(0, n - 1)
         rows = torch.searchsorted(ends[1:], token, right=True).clamp_max(ends.shape[0] - 2)
@@ -392,7 +413,7 @@ class Decoder(torch.nn.Module):
         None: a chain.  Returns [B, T, d_model] and leaves the tokens in rows start[b] on; keep() makes a path of them the sequence's."""
         if not self.fused:
             raise ValueError("step_tree() needs a fused decoder")
-        x = self._features(x)
+        x = self._served(x)
         B, n, _ = x.shape
         i = torch.arange(n, device=x.device)
         reads = (i <= i[:, None]).expand(B, n, n) if tree is None else (tree.expand(B, n)[..., None] >> i & 1).bool()
