@@ -203,6 +203,19 @@ class TokenLogProbsFunction(torch.autograd.Function):
                                     scale=ctx.scale), None, None, None
 
 
+class WithoutGradientFunction(torch.autograd.Function):
+    """x as it is, for a user who looks at it; in a loss of `of` it is an error, where a part of the gradient would be missing."""
+
+    @staticmethod
+    def forward(ctx, x, of, name: str):
+        ctx.name = name
+        return x.view_as(x)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError(f"{ctx.name} has no gradient: detach it, or leave it out of the loss")
+
+
 class DecoderLayer(torch.nn.Module):
     def __init__(self, d_model: int, heads: int, d_ff: int, topk: int | None, ffn_topk: int | None,
                  dtype=torch.bfloat16, device="cuda", fused: bool = False):
@@ -358,13 +371,14 @@ class Decoder(torch.nn.Module):
 
     def logprobs(self, features, targets=None, top: int = 0, scale: float = 1.0) -> T.TokenLogProbs:
         """What features [.., d_model] (of forward, step, ..) say of the next tokens: T.token_logprobs of their logits, one row for
-        each of them, with targets [..] or None.  Differentiable where gradients are on."""
+        each of them, with targets [..] or None.  Differentiable where gradients are on, but for lse, which a loss may hold only detached."""
         if self.vocab is None:
             raise ValueError("logprobs() needs a vocabulary")
         logits = linear(features.reshape(-1, features.shape[-1]), self.embedding)
         targets = None if targets is None else targets.reshape(-1)
         if _derived(logits):
-            return T.TokenLogProbs(*TokenLogProbsFunction.apply(logits, targets, top, scale))
+            r = T.TokenLogProbs(*TokenLogProbsFunction.apply(logits, targets, top, scale))
+            return r._replace(lse=WithoutGradientFunction.apply(r.lse, logits, "lse"))
         return T.token_logprobs(logits, targets, top=top, scale=scale)
 
     def new_cache(self, batch: int, capacity: int):

@@ -119,3 +119,27 @@ def test_tangents_are_refused_by_generation(model):
 
             with pytest.raises(NotImplementedError, match="forward-mode"):
                 torch.func.functional_call(Call(), {"m.norm.weight": _tangent(model.norm.weight)}, args)
+
+
+def test_a_loss_with_the_sums_logarithm_is_refused(model):
+    # its gradient is not made: an error in place of a gradient without that term
+    ids = torch.arange(6).view(2, 3)
+    r = model.logprobs(model(ids)[:, :-1], ids[:, 1:])
+    with pytest.raises(RuntimeError, match="lse"):
+        (-r.logp.mean() + 1e-4 * r.lse.square().mean()).backward()
+    with pytest.raises(RuntimeError, match="lse"):
+        model.logprobs(model(ids)).lse.sum().backward()
+    for p in model.parameters():
+        p.grad = None
+    r = model.logprobs(model(ids)[:, :-1], ids[:, 1:])
+    assert torch.equal(r.lse, torch.logsumexp(model(ids)[:, :-1].reshape(-1, D) @ model.embedding.t(), 1))
+    loss = -r.logp.mean() - 0.1 * r.entropy.mean() + 0 * r.lse.detach().mean()  # as a number it may be used
+    loss.backward()
+    got = model.embedding.grad.clone()
+    model.embedding.grad = None
+    h = torch.nn.functional.layer_norm(model.embedding[ids] * D ** 0.5, (D,), model.norm.weight, model.norm.bias)
+    logp = torch.log_softmax(h[:, :-1].reshape(-1, D) @ model.embedding.t(), 1)
+    (-logp.gather(1, ids[:, 1:].reshape(-1, 1)).mean() + 0.1 * (logp.exp() * logp).sum(1).mean()).backward()
+    assert torch.allclose(got, model.embedding.grad, rtol=1e-4, atol=1e-5)
+    with torch.no_grad():
+        assert not model.logprobs(model(ids)).lse.requires_grad
