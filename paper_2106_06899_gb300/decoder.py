@@ -361,7 +361,7 @@ class Decoder(torch.nn.Module):
         """_features for calls that have no derivatives."""
         if _tangents(itertools.chain((x,), self.parameters())):
             raise NotImplementedError("generation has no forward-mode derivative")
-        return self._features(x)
+        return self._features(x).contiguous()
 
     def forward(self, x):
         x = self._features(x)
@@ -374,8 +374,9 @@ class Decoder(torch.nn.Module):
         each of them, with targets [..] or None.  Differentiable where gradients are on, but for lse, which a loss may hold only detached."""
         if self.vocab is None:
             raise ValueError("logprobs() needs a vocabulary")
-        logits = linear(features.reshape(-1, features.shape[-1]), self.embedding)
-        targets = None if targets is None else targets.reshape(-1)
+        # reshape leaves views such as the last tokens' features[:, -1] as they are
+        logits = linear(features.reshape(-1, features.shape[-1]).contiguous(), self.embedding)
+        targets = None if targets is None else targets.reshape(-1).contiguous()
         if _derived(logits):
             r = T.TokenLogProbs(*TokenLogProbsFunction.apply(logits, targets, top, scale))
             return r._replace(lse=WithoutGradientFunction.apply(r.lse, logits, "lse"))

@@ -143,3 +143,17 @@ def test_a_loss_with_the_sums_logarithm_is_refused(model):
     assert torch.allclose(got, model.embedding.grad, rtol=1e-4, atol=1e-5)
     with torch.no_grad():
         assert not model.logprobs(model(ids)).lse.requires_grad
+
+
+def test_views_of_features_and_targets(model):
+    # the last token of each sequence, and a column of a batch's ids
+    ids = torch.arange(12).view(3, 4)
+    features = model(ids)
+    for grad in (True, False):
+        with torch.set_grad_enabled(grad):
+            r = model.logprobs(features[:, -1], ids[:, 2], top=2)
+            want = model.logprobs(features[:, -1].contiguous(), ids[:, 2].contiguous(), top=2)
+            assert all(torch.equal(a, b) for a, b in zip(r, want))
+            # features by columns, and one row for all
+            assert torch.equal(model.logprobs(features[:, -1].t().contiguous().t()).lse, want.lse)
+            assert model.logprobs(features[0, 0].expand(3, D)).lse.shape == (3,)
