@@ -548,7 +548,8 @@ int embed_bwd(const EmbedArgs& a, const void* dy, void* dweight, bool accumulate
     if (most <= 0) return -1;
     sorters = sorters < most ? sorters : most;
   }
-  const long long zeroers = bytes ? (bytes / 16 + 4 * kSortThreads) / (4 * kSortThreads) : 0, most = num_sms - sorters;
+  // one cluster of them at least, however few SMs there are: they wait for nothing
+  const long long zeroers = bytes ? (bytes / 16 + 4 * kSortThreads) / (4 * kSortThreads) : 0, most = num_sms - sorters > sorters ? num_sms - sorters : sorters;
   const int grid = sorters + static_cast<int>((zeroers < most ? zeroers + sorters - 1 : most) / sorters * sorters);
   cudaLaunchConfig_t config = {};
   config.gridDim = dim3(grid), config.blockDim = dim3(kSortThreads), config.stream = st;
