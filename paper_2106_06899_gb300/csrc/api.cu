@@ -80,11 +80,22 @@ struct HostPipe {
 };
 HostPipe g_pipe[kMaxDevices];
 
+// While it lives this thread may create pools and streams although a stream is being captured, which makes none of them part of the graph.
+class WhileCapturing {
+ public:
+  WhileCapturing() { cudaThreadExchangeStreamCaptureMode(&mode_); }
+  ~WhileCapturing() { cudaThreadExchangeStreamCaptureMode(&mode_); }
+
+ private:
+  cudaStreamCaptureMode mode_ = cudaStreamCaptureModeRelaxed;
+};
+
 HostPipe* host_pipe() {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return nullptr;
   HostPipe& s = g_pipe[dev];
   std::call_once(s.once, [&s, dev]() {
+    const WhileCapturing first_call;
     cudaMemPoolProps props;
     std::memset(&props, 0, sizeof props);
     props.allocType = cudaMemAllocationTypePinned;
