@@ -18,7 +18,7 @@ embedding before the first layer (topk_embedding_fwd / _bwd), the same weights b
 log probabilities with their gradient (topk_token_logprobs_fwd / _bwd).
 
 The library's gradients have no gradients of their own: a second differentiation through one of these functions is
-an error.
+an error, and so is a forward-mode one.
 A training step may be captured into a CUDA graph while no earlier eager graph of the same parameters is alive (drop the
 losses of warm-up steps first, and run them on the capturing stream): PyTorch adds up a leaf's gradient on the stream where
 its first graph was made, which ends a capture on another one.
